@@ -79,7 +79,8 @@ typedef enum {
     NFAD_E_SCRATCH = 7,  /* scratch_bytes is smaller than the comparator needs        */
     NFAD_E_LAYOUT = 8,   /* layout is not an nfad_layout                              */
     NFAD_E_TOO_LARGE = 9, /* the tensors need more than the library's built-in scratch */
-    NFAD_E_PROGRAM = 10  /* malformed FAD sequence (see nfad_seq_forward)              */
+    NFAD_E_PROGRAM = 10, /* malformed FAD sequence (see nfad_seq_forward)              */
+    NFAD_E_VALUE = 11    /* a size or number is outside the range its entry point states */
 } nfad_status;
 
 /* How the tensor needed by backward is kept between the passes (Section II-C). */
@@ -337,6 +338,60 @@ NFAD_API int nfad_bias_act_backward(int kind, int dtype, const void* grad_out, c
                                     nfad_stream_t stream);
 /* Bytes of scratch nfad_bias_act_backward needs on the current device; 0 on a bad dtype or when none is needed. */
 NFAD_API size_t nfad_bias_act_backward_scratch_bytes(int dtype, size_t rows, size_t cols);
+
+/*
+ * ---- Around the activation: the rest of a feed-forward block ------------------------------
+ *
+ * The norms before and after a block.  With u the block's output and r the residual stream, both [rows, cols]:
+ *   a = N_post(u) post_gain + post_bias
+ *   s = residual_scale r + gate a          the stream's new value
+ *   h = N_pre(s) pre_gain + pre_bias       the next block's input, formed from s before s is rounded
+ * N is NFAD_NORM_NONE (a = u; for `pre`: no h), NFAD_NORM_RMS: x / sqrt(mean(x^2) + eps), or NFAD_NORM_LAYER:
+ * (x - mean) / sqrt(var + eps), per row.  Sums and statistics are fp32 for every storage type; every result is rounded
+ * once.  gate is [gate_rows, cols]: each of its rows governs rows / gate_rows consecutive rows (1: one gate for each
+ * channel; the number of sequences: one for each sequence).  Parameters have the tensors' dtype; each may be NULL (gain
+ * 1, bias 0, gate 1), and then gate_rows is ignored.  gate_rows must divide rows and eps must be > 0 and finite (NFAD_E_VALUE).
+ * A row that holds a NaN or an infinity spoils its own results only.
+ */
+typedef enum { NFAD_NORM_NONE = 0, NFAD_NORM_RMS = 1, NFAD_NORM_LAYER = 2 } nfad_norm;
+
+typedef struct {
+    int post, pre;                                   /* nfad_norm each (NFAD_E_KIND otherwise)  */
+    const void *post_gain, *post_bias;               /* [cols] or NULL; unused when post is NONE */
+    const void *gate;                                /* [gate_rows, cols] or NULL               */
+    size_t gate_rows;
+    const void *pre_gain, *pre_bias;                 /* [cols] or NULL; unused when pre is NONE  */
+    float residual_scale, eps;
+} nfad_block_norm;
+
+/* fp32 results of nfad_block_norm_backward, each of its parameter's shape; NULL: not wanted. */
+typedef struct { float *post_gain, *post_bias, *gate, *pre_gain, *pre_bias; } nfad_block_norm_grads;
+
+/*
+ *   u [in]; r [in] or NULL (s = gate a);  s_out [out] the stream, or NULL when only h is wanted;  h [out]: NULL exactly
+ *   when pre is NONE;  stats [out] rows x 4 floats, 16-byte aligned: mean and 1/sqrt of u, then of s (0 where there is no
+ *   norm or no mean) for nfad_block_norm_backward, or NULL in a pass that will not be differentiated.
+ * s_out and h may each equal u or r (not both the same tensor).  The 128-bit path needs cols to be a multiple of the
+ * packet (8 elements, 4 for fp32), 16-byte aligned tensors and at most 2048 packets in a row; otherwise a slower kernel takes
+ * every element by itself.  cols must be below 2^31 (NFAD_E_TOO_LARGE).
+ */
+NFAD_API int nfad_block_norm_forward(const nfad_block_norm* norm, int dtype, const void* u, const void* r, void* s_out, void* h,
+                                     float* stats, size_t rows, size_t cols, nfad_stream_t stream);
+
+/*
+ * Backward.  grad_h [in] (NULL exactly when pre is NONE): the gradient of h;  grad_s [in] or NULL (zero): what reaches s
+ * from elsewhere on the stream;  u, s, stats: the forward's (u may be NULL when neither post nor gate is there, s when pre
+ * is NONE);  grad_u [out];  grad_r [out] or NULL.  With pre NONE grad_s is required.  The parameters' gradients are summed in fp32
+ * in a fixed order: the same bits every time.  A gradient asked for a parameter that its norm does not have (post_* with
+ * post NONE, pre_* with pre NONE, gate without a gate) gives NFAD_E_VALUE.
+ * grad_u and grad_r may each equal one of grad_h, grad_s, u and s.  scratch: device memory, 16-byte aligned, of at least
+ * nfad_block_norm_backward_scratch_bytes() bytes (asked with the device current that will run the call).
+ */
+NFAD_API int nfad_block_norm_backward(const nfad_block_norm* norm, int dtype, const void* grad_h, const void* grad_s, const void* u,
+                                      const void* s, const float* stats, void* grad_u, void* grad_r,
+                                      const nfad_block_norm_grads* grads, void* scratch, size_t scratch_bytes, size_t rows,
+                                      size_t cols, nfad_stream_t stream);
+NFAD_API size_t nfad_block_norm_backward_scratch_bytes(int dtype, size_t rows, size_t cols);
 
 /*
  * The whole pass for tensors that live in HOST memory (no counterpart in the paper: a service entry

@@ -13,3 +13,7 @@ from .binding import (  # noqa: F401
     nfad_ew_op, nfad_host_step, nfad_host_step_workspace_bytes, nfad_probe_stream, nfad_saved_bytes_per_element, nfad_seq_backward, nfad_seq_forward,
     nfad_status_string, nfad_version,
 )
+from .block import (  # noqa: F401
+    NORMS, BlockNorm, nfad_block_norm_backward, nfad_block_norm_backward_scratch, nfad_block_norm_backward_scratch_bytes,
+    nfad_block_norm_forward,
+)

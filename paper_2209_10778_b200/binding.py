@@ -34,6 +34,7 @@ EXPORTS = (
     "nfad_act_forward_strict",
     "nfad_host_step", "nfad_host_step_workspace_bytes",
     "nfad_seq_set_executor", "nfad_seq_last_executor", "nfad_seq_compile_log", "nfad_seq_compiled_source",
+    "nfad_block_norm_forward", "nfad_block_norm_backward", "nfad_block_norm_backward_scratch_bytes",
 )
 OPCODES = {"add": 0, "mul": 1, "scale": 2, "add_const": 3, "exp": 4, "log1p": 5, "tanh": 6, "erf": 7, "softplus": 8,
            "sigmoid": 9, "half_one_plus_tanh": 10, "half_one_plus_erf": 11, "out": 12}
@@ -42,6 +43,20 @@ OPCODES = {"add": 0, "mul": 1, "scale": 2, "add_const": 3, "exp": 4, "log1p": 5,
 class SeqOp(ctypes.Structure):
     """One instruction of a FAD sequence: `nfad_seq_op` of the C interface."""
     _fields_ = [("op", ctypes.c_int), ("a", ctypes.c_int), ("b", ctypes.c_int), ("dst", ctypes.c_int), ("c", ctypes.c_float)]
+
+
+class BlockNormDesc(ctypes.Structure):
+    """`nfad_block_norm` of the C interface."""
+    _fields_ = [("post", ctypes.c_int), ("pre", ctypes.c_int), ("post_gain", ctypes.c_void_p), ("post_bias", ctypes.c_void_p),
+                ("gate", ctypes.c_void_p), ("gate_rows", ctypes.c_size_t), ("pre_gain", ctypes.c_void_p),
+                ("pre_bias", ctypes.c_void_p), ("residual_scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class BlockNormGrads(ctypes.Structure):
+    """`nfad_block_norm_grads` of the C interface."""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("post_gain", "post_bias", "gate", "pre_gain", "pre_bias")]
+
+
 NOALLOC_SCRATCH_BYTES = 8388608
 
 _lib: Optional[ctypes.CDLL] = None
@@ -90,6 +105,13 @@ def load() -> ctypes.CDLL:
         lib.nfad_bias_act_backward.restype = ci
         lib.nfad_bias_act_backward_scratch_bytes.argtypes = [ci, sz, sz]
         lib.nfad_bias_act_backward_scratch_bytes.restype = sz
+        norm = ctypes.POINTER(BlockNormDesc)
+        lib.nfad_block_norm_forward.argtypes = [norm, ci, vp, vp, vp, vp, vp, sz, sz, vp]
+        lib.nfad_block_norm_forward.restype = ci
+        lib.nfad_block_norm_backward.argtypes = [norm, ci, vp, vp, vp, vp, vp, vp, vp, ctypes.POINTER(BlockNormGrads), vp, sz, sz, sz, vp]
+        lib.nfad_block_norm_backward.restype = ci
+        lib.nfad_block_norm_backward_scratch_bytes.argtypes = [ci, sz, sz]
+        lib.nfad_block_norm_backward_scratch_bytes.restype = sz
         lib.nfad_seq_set_executor.argtypes = [ci]
         lib.nfad_seq_set_executor.restype = ci
         lib.nfad_seq_last_executor.argtypes = []

@@ -3,7 +3,7 @@
     python -m paper_2209_10778_b200.build          # rebuild if sources are newer
     python -m paper_2209_10778_b200.build --force
 
-Seven translation units: the fp32-storage kernels are compiled with
+One object file for each translation unit: the fp32-storage kernels are compiled with
 floating-point contraction OFF (their compensated arithmetic depends on every
 fused multiply-add being written out), the 16-bit-storage kernels and the run-time
 sequences with it on, the bias-gradient kernels (explicitly rounded intrinsics only),
@@ -30,7 +30,9 @@ UNITS = [
     ("nfad_kernels_16.cu", ["-fmad=true"]),
     ("nfad_kernels_seq.cu", ["-fmad=true"]),
     ("nfad_kernels_bias.cu", ["-fmad=false"]),
+    ("nfad_kernels_norm.cu", ["-fmad=true"]),
     ("nfad_api.cu", ["-fmad=false"]),
+    ("nfad_api_block.cu", ["-fmad=false"]),
     ("nfad_host.cu", ["-fmad=false"]),
     ("nfad_jit.cu", ["-fmad=false"]),
 ]

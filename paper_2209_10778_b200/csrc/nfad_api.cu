@@ -498,6 +498,7 @@ const char* nfad_status_string(int status)
     case NFAD_E_LAYOUT: return "unknown layout";
     case NFAD_E_TOO_LARGE: return "tensors larger than the library's built-in scratch";
     case NFAD_E_PROGRAM: return "malformed FAD sequence";
+    case NFAD_E_VALUE: return "a size or number is outside its range";
     default: return "unknown status";
     }
 }

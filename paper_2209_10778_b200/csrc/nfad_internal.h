@@ -65,4 +65,11 @@ cudaError_t launch_bias_backward(int dtype, const void* g, const void* d, void* 
                                  size_t rows, size_t cols, cudaStream_t st);
 cudaError_t bias_backward_scratch(int dtype, size_t rows, size_t cols, size_t* bytes);   // on the current device
 
+// The norms around a block (nfad_norm.cuh).
+struct NormForwardArgs;
+struct NormBackwardArgs;
+cudaError_t launch_norm_forward(int dtype, const NormForwardArgs& a, cudaStream_t st);
+cudaError_t launch_norm_backward(int dtype, const NormBackwardArgs& a, void* scratch, cudaStream_t st);
+cudaError_t norm_backward_scratch(int dtype, size_t rows, size_t cols, size_t* bytes);   // on the current device
+
 }  // namespace nfad

@@ -1,0 +1,729 @@
+// nfad_norm.cuh -- the norms before and after a block, fused with the block's gate and the residual scale.
+//
+//   a = N_post(u) g_post + b_post            u: the block's output
+//   s = alpha r + gate a                     r: the residual stream; s: its new value, stored rounded once
+//   h = N_pre(s) g_pre + b_pre               of the unrounded s: the next block's input
+//
+// N is nothing, x rho with rho = (mean x^2 + eps)^-1/2 (RMS), or (x - mu) rho with rho = (var + eps)^-1/2 (LAYER).
+// Unfused this is four passes (norm, gate, residual sum, norm) of 2 to 3 tensors each; here each row is read once,
+// held in registers across its two reductions, and s and h are written once: two tensors in, two out, which bounds it
+// by HBM traffic.  All arithmetic is fp32; the variance is taken about the mean in a second sweep over the registers.
+//
+// Backward, from dh and the stream's own gradient ds', the stored s, u and the four row statistics (^: normalised):
+//   d = dh g_pre;  ds = ds' + rho_s (d - mean d [LAYER] - s^ mean(d s^));      grad_r = alpha ds
+//   da = gate ds;  e = da g_post;  grad_u = rho_u (e - mean e [LAYER] - u^ mean(e u^))
+//   grad g_pre = sum dh s^, grad b_pre = sum dh, grad g_post = sum da u^, grad b_post = sum da over all rows;
+//   grad gate = sum ds a over the rows that a gate row governs.  All in fp32 and in a fixed order.
+// A CTA owns a run of consecutive rows and a thread the same columns of each, so the five column sums stay in
+// registers; each CTA writes its sums once and a second kernel adds the CTAs' in a fixed order.  The next row's packets
+// are in flight during the current row's two reductions.  Four tensors in, two out.
+#pragma once
+
+#include "nfad_internal.h"
+#include "nfad_norm_args.h"
+#include "nfad_stream.cuh"
+
+namespace nfad {
+
+// ---------------------------------------------------------------- sums over a row
+
+// N sums over the threads of a row: the lanes of a warp (kWarp) or the whole CTA.  `turn` alternates between two buffers,
+// so that one barrier per call is enough: a buffer is written again only after every thread has passed the next call's.
+template <int N, bool kWarp> struct RowSum {
+    float (*buf)[N][32];
+    int turn;
+    __device__ __forceinline__ void operator()(float (&v)[N])
+    {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+        if (kWarp || blockDim.x == 32) return;
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = (blockDim.x + 31) >> 5;
+        float (*b)[32] = buf[turn];
+        turn ^= 1;
+        if (lane == 0)
+#pragma unroll
+            for (int k = 0; k < N; ++k) b[k][warp] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] = lane < warps ? b[k][lane] : 0.0f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    }
+};
+
+// ---------------------------------------------------------------- forward
+
+template <class S> __device__ __forceinline__ void load_row_packet(const void* base, size_t row, uint32_t packets, uint32_t p, float (&v)[S::kVec])
+{
+    S::unpack(load_packet(static_cast<const uint4*>(base) + row * packets + p), v);
+}
+
+// parameters are read by every row: plain cached loads
+template <class S> __device__ __forceinline__ void load_parameter(const void* base, size_t row, uint32_t packets, uint32_t p, float (&v)[S::kVec])
+{
+    S::unpack(__ldg(static_cast<const uint4*>(base) + row * packets + p), v);
+}
+
+// mean and reciprocal deviation of the values a row's threads hold (I packets each, the valid ones)
+template <int V, int I, bool kWarp>
+__device__ __forceinline__ void row_statistics(const float (&v)[I][V], const bool (&on)[I], int kind, float inv_cols, float eps,
+                                               RowSum<1, kWarp>& sum, float* mean, float* rstd)
+{
+    *mean = 0.0f;
+    float t[1];
+    if (kind == kNormLayer) {
+        t[0] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) t[0] += v[i][e];           // packets past the row hold zeros
+        sum(t);
+        *mean = t[0] * inv_cols;
+    }
+    t[0] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+        if (on[i])
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float c = v[i][e] - *mean;
+                t[0] = fmaf(c, c, t[0]);
+            }
+    sum(t);
+    *rstd = 1.0f / sqrtf(fmaf(t[0], inv_cols, eps));
+}
+
+// One row per CTA, or per warp (kWarp); cols a multiple of the packet, every pointer on a 16-byte boundary.
+template <class S, int I, bool kWarp>
+__global__ void __launch_bounds__(1024) norm_forward_kernel(const __grid_constant__ NormForwardArgs a)
+{
+    constexpr int V = S::kVec;
+    __shared__ float buf[2][1][32];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const uint32_t lane = kWarp ? threadIdx.x & 31 : threadIdx.x, width = kWarp ? 32 : blockDim.x;
+    const size_t per_cta = kWarp ? blockDim.x >> 5 : 1;
+    RowSum<1, kWarp> sum{buf, 0};
+    for (size_t row = blockIdx.x * per_cta + (kWarp ? threadIdx.x >> 5 : 0); row < a.rows; row += gridDim.x * per_cta) {
+        float u[I][V], r[I][V];
+        bool on[I];
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const uint32_t p = lane + i * width;
+            on[i] = p < a.packets;
+#pragma unroll
+            for (int e = 0; e < V; ++e) u[i][e] = r[i][e] = 0.0f;
+            if (on[i]) {
+                load_row_packet<S>(a.u, row, a.packets, p, u[i]);
+                if (a.r) load_row_packet<S>(a.r, row, a.packets, p, r[i]);
+            }
+        }
+        float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (a.post != kNormNone) row_statistics<V, I, kWarp>(u, on, a.post, a.inv_cols, a.eps, sum, &st.x, &st.y);
+        const size_t gate_row = a.gate ? row / a.rows_per_gate : 0;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const uint32_t p = lane + i * width;
+            if (!on[i]) continue;
+            float w[V];
+            if (a.post != kNormNone) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) u[i][e] = (u[i][e] - st.x) * st.y;
+                if (a.post_gain) {
+                    load_parameter<S>(a.post_gain, 0, a.packets, p, w);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) u[i][e] *= w[e];
+                }
+                if (a.post_bias) {
+                    load_parameter<S>(a.post_bias, 0, a.packets, p, w);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) u[i][e] += w[e];
+                }
+            }
+            if (a.gate) {
+                load_parameter<S>(a.gate, gate_row, a.packets, p, w);
+#pragma unroll
+                for (int e = 0; e < V; ++e) u[i][e] *= w[e];
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) r[i][e] = a.r ? fmaf(a.alpha, r[i][e], u[i][e]) : u[i][e];
+            if (a.s) store_packet<true>(static_cast<uint4*>(a.s) + row * a.packets + p, S::pack(r[i]));
+        }
+        if (a.pre != kNormNone) {
+            row_statistics<V, I, kWarp>(r, on, a.pre, a.inv_cols, a.eps, sum, &st.z, &st.w);
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                const uint32_t p = lane + i * width;
+                if (!on[i]) continue;
+                float w[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) r[i][e] = (r[i][e] - st.z) * st.w;
+                if (a.pre_gain) {
+                    load_parameter<S>(a.pre_gain, 0, a.packets, p, w);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) r[i][e] *= w[e];
+                }
+                if (a.pre_bias) {
+                    load_parameter<S>(a.pre_bias, 0, a.packets, p, w);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) r[i][e] += w[e];
+                }
+                store_packet<true>(static_cast<uint4*>(a.h) + row * a.packets + p, S::pack(r[i]));
+            }
+        }
+        if (a.stats && lane == 0) a.stats[row] = st;
+    }
+}
+
+// Element access of the any-shape kernels.
+template <class S> __device__ __forceinline__ float at(const void* base, size_t i) { return S::load1(static_cast<const typename S::elem*>(base) + i); }
+template <class S> __device__ __forceinline__ void put(void* base, size_t i, float v) { S::store1(static_cast<typename S::elem*>(base) + i, v); }
+
+// Any cols, any element-aligned pointers, rows too long for registers: a CTA sweeps its row once per statistic (from
+// L1 or L2 after the first sweep) and once to write.  Every element is read before its place is written, by one thread.
+template <class S>
+__global__ void __launch_bounds__(kBlock) norm_forward_any_kernel(const __grid_constant__ NormForwardArgs a)
+{
+    __shared__ float buf[2][1][32];
+    RowSum<1, false> sum{buf, 0};
+    for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const size_t base = row * a.cols, gate = a.gate ? row / a.rows_per_gate * a.cols : 0;
+        float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        auto stream = [&](uint32_t c) {                              // s of one element, from u, r and u's statistics
+            float v = at<S>(a.u, base + c);
+            if (a.post != kNormNone) {
+                v = (v - st.x) * st.y;
+                if (a.post_gain) v *= at<S>(a.post_gain, c);
+                if (a.post_bias) v += at<S>(a.post_bias, c);
+            }
+            if (a.gate) v *= at<S>(a.gate, gate + c);
+            return a.r ? fmaf(a.alpha, at<S>(a.r, base + c), v) : v;
+        };
+        auto statistics = [&](auto value, int kind, float* mean, float* rstd) {
+            float t[1] = {0.0f}, m = 0.0f;
+            if (kind == kNormLayer) {
+                for (uint32_t c = threadIdx.x; c < a.cols; c += kBlock) t[0] += value(c);
+                sum(t);
+                m = t[0] * a.inv_cols;
+            }
+            t[0] = 0.0f;
+            for (uint32_t c = threadIdx.x; c < a.cols; c += kBlock) {
+                const float d = value(c) - m;
+                t[0] = fmaf(d, d, t[0]);
+            }
+            sum(t);
+            *mean = m;
+            *rstd = 1.0f / sqrtf(fmaf(t[0], a.inv_cols, a.eps));
+        };
+        if (a.post != kNormNone) {
+            float m, q;
+            statistics([&](uint32_t c) { return at<S>(a.u, base + c); }, a.post, &m, &q);
+            st.x = m; st.y = q;
+        }
+        if (a.pre != kNormNone) {
+            float m, q;
+            statistics(stream, a.pre, &m, &q);
+            st.z = m; st.w = q;
+        }
+        for (uint32_t c = threadIdx.x; c < a.cols; c += kBlock) {
+            const float v = stream(c);
+            if (a.pre != kNormNone) {
+                float n = (v - st.z) * st.w;
+                if (a.pre_gain) n *= at<S>(a.pre_gain, c);
+                if (a.pre_bias) n += at<S>(a.pre_bias, c);
+                if (a.s) put<S>(a.s, base + c, v);
+                put<S>(a.h, base + c, n);
+            } else if (a.s) {
+                put<S>(a.s, base + c, v);
+            }
+        }
+        if (a.stats && threadIdx.x == 0) a.stats[row] = st;
+    }
+}
+
+template <class S> inline bool norm_vector_ok(const void* const* p, int n, size_t cols)
+{
+    if (cols % S::kVec) return false;
+    for (int i = 0; i < n; ++i)
+        if (reinterpret_cast<uintptr_t>(p[i]) & 15u) return false;   // a null pointer passes
+    return true;
+}
+
+inline void norm_launch_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attr, size_t grid, unsigned block, cudaStream_t st)
+{
+    *cfg = cudaLaunchConfig_t{};
+    cfg->gridDim = dim3((unsigned)(grid < 0x7fffffffu ? grid : 0x7fffffffu));
+    cfg->blockDim = dim3(block);
+    cfg->stream = st;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg->attrs = attr;
+    cfg->numAttrs = 1;
+}
+
+template <class S>
+cudaError_t launch_norm_forward(const NormForwardArgs& in, cudaStream_t st)
+{
+    NormForwardArgs a = in;
+    if (a.rows == 0 || a.cols == 0) return cudaSuccess;
+    const void* p[9] = {a.u, a.r, a.post_gain, a.post_bias, a.gate, a.pre_gain, a.pre_bias, a.s, a.h};
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[1];
+    a.packets = a.cols / S::kVec;
+    // a row in registers: a warp of one to four packets per lane, or a CTA of one or two (up to 1024 threads)
+    if (!norm_vector_ok<S>(p, 9, a.cols) || a.packets > 2048) {
+        DeviceInfo di;
+        cudaError_t e = device_info(&di);
+        if (e != cudaSuccess) return e;
+        const size_t cap = size_t(di.sm_count) * 8;
+        norm_forward_any_kernel<S><<<(unsigned)(a.rows < cap ? a.rows : cap), kBlock, 0, st>>>(a);
+        return cudaPeekAtLastError();
+    }
+    if (a.packets <= 128) {
+        norm_launch_config(&cfg, attr, (a.rows + 3) / 4, 128, st);
+        if (a.packets <= 32) return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 1, true>, a);
+        if (a.packets <= 64) return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 2, true>, a);
+        return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 4, true>, a);
+    }
+    const unsigned block = ((a.packets + 1) / 2 + 31) / 32 * 32;
+    norm_launch_config(&cfg, attr, a.rows, block, st);
+    return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 2, false>, a);
+}
+
+// ---------------------------------------------------------------- backward
+
+// A chunk's sum of ds a for one gate row: straight to the result when the chunk holds all of that gate row's rows, else to
+// the chunk's slot 0 (the gate row that the chunk begins with) or 1 (a later one, which the chunk ends with).
+__device__ __forceinline__ float* gate_target(const NormBackwardArgs& a, size_t chunk, size_t r0, size_t r1, size_t gate_row)
+{
+    const size_t g0 = gate_row * a.rows_per_gate, g1 = g0 + a.rows_per_gate;
+    if (g0 >= r0 && g1 <= r1) return a.grad_gate + gate_row * a.cols;
+    return a.partial + (size_t(a.chunks) * kNormSums + chunk * 2 + (g0 <= r0 ? 0 : 1)) * a.cols;
+}
+
+template <class S> __device__ __forceinline__ uint4 raw_row_packet(const void* base, size_t row, uint32_t packets, uint32_t p)
+{
+    return load_packet(static_cast<const uint4*>(base) + row * packets + p);
+}
+
+template <class S> struct NormRaw { uint4 dh, s, gs, u; };
+
+template <class S> __device__ __forceinline__ void load_norm_raw(const NormBackwardArgs& a, size_t row, uint32_t p, bool on, NormRaw<S>* q)
+{
+    q->dh = q->s = q->gs = q->u = make_uint4(0, 0, 0, 0);
+    if (!on) return;
+    if (a.pre != kNormNone) {
+        q->dh = raw_row_packet<S>(a.grad_h, row, a.packets, p);
+        q->s = raw_row_packet<S>(a.s, row, a.packets, p);
+    }
+    if (a.grad_s) q->gs = raw_row_packet<S>(a.grad_s, row, a.packets, p);
+    if (a.u) q->u = raw_row_packet<S>(a.u, row, a.packets, p);
+}
+
+// I packets per thread; kBias: the two bias sums are kept too.  Aligned rows of up to 512 I packets.
+template <class S, int I, bool kGate, bool kBias>
+__global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constant__ NormBackwardArgs a)
+{
+    constexpr int V = S::kVec;
+    __shared__ float buf[2][2][32];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    RowSum<2, false> sum{buf, 0};
+    const size_t r0 = blockIdx.x * a.chunk_rows, r1 = r0 + a.chunk_rows < a.rows ? r0 + a.chunk_rows : a.rows;
+    float acc[kNormSums][I][V], accg[I][V];
+    bool on[I];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        on[i] = threadIdx.x + i * blockDim.x < a.packets;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+#pragma unroll
+            for (int k = 0; k < kNormSums; ++k) acc[k][i][e] = 0.0f;
+            accg[i][e] = 0.0f;
+        }
+    }
+    NormRaw<S> next[I];
+    float4 next_st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (r0 < r1) {
+#pragma unroll
+        for (int i = 0; i < I; ++i) load_norm_raw<S>(a, r0, threadIdx.x + i * blockDim.x, on[i], &next[i]);
+        next_st = a.stats[r0];
+    }
+    size_t gate_row = kGate ? r0 / a.rows_per_gate : 0, gate_end = (gate_row + 1) * a.rows_per_gate;
+    for (size_t row = r0; row < r1; ++row) {
+        float ds[I][V], hat[I][V], t[2] = {0.0f, 0.0f};
+        uint4 gs[I], ru[I];
+        const float4 st = next_st;
+        // d = dh g_pre and s^; their two sums
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            gs[i] = next[i].gs; ru[i] = next[i].u;
+            S::unpack(next[i].dh, ds[i]);
+            S::unpack(next[i].s, hat[i]);
+        }
+        if (row + 1 < r1) {
+#pragma unroll
+            for (int i = 0; i < I; ++i) load_norm_raw<S>(a, row + 1, threadIdx.x + i * blockDim.x, on[i], &next[i]);
+            next_st = a.stats[row + 1];
+        }
+        if (a.pre != kNormNone) {
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                if (!on[i]) continue;
+                float w[V];
+                if (a.pre_gain) load_parameter<S>(a.pre_gain, 0, a.packets, threadIdx.x + i * blockDim.x, w);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    hat[i][e] = (hat[i][e] - st.z) * st.w;
+                    acc[kSumPreGain][i][e] = fmaf(ds[i][e], hat[i][e], acc[kSumPreGain][i][e]);
+                    if (kBias) acc[kSumPreBias][i][e] += ds[i][e];
+                    if (a.pre_gain) ds[i][e] *= w[e];
+                    t[0] += ds[i][e];
+                    t[1] = fmaf(ds[i][e], hat[i][e], t[1]);
+                }
+            }
+            sum(t);
+            const float m = a.pre == kNormLayer ? t[0] * a.inv_cols : 0.0f, q = t[1] * a.inv_cols;
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                float v[V];
+                S::unpack(gs[i], v);
+#pragma unroll
+                for (int e = 0; e < V; ++e) ds[i][e] = fmaf(st.w, ds[i][e] - m - hat[i][e] * q, v[e]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < I; ++i) S::unpack(gs[i], ds[i]);
+        }
+        if (kGate && row == gate_end) {                              // the rows of one gate row are done: hand their sum over
+#pragma unroll
+            for (int i = 0; i < I; ++i) {
+                if (on[i] && a.grad_gate) {
+                    float* dst = gate_target(a, blockIdx.x, r0, r1, gate_row) + size_t(threadIdx.x + i * blockDim.x) * V;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) dst[e] = accg[i][e];
+                }
+#pragma unroll
+                for (int e = 0; e < V; ++e) accg[i][e] = 0.0f;
+            }
+            ++gate_row;
+            gate_end += a.rows_per_gate;
+        }
+        // grad_r; then da = gate ds, e = da g_post and u^, and their two sums
+        t[0] = t[1] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            if (!on[i]) continue;
+            const uint32_t p = threadIdx.x + i * blockDim.x;
+            float v[V], w[V];
+            if (a.grad_r) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = a.alpha * ds[i][e];
+                store_packet<true>(static_cast<uint4*>(a.grad_r) + row * a.packets + p, S::pack(v));
+            }
+            float gain[V];
+            if (a.post != kNormNone && a.post_gain) load_parameter<S>(a.post_gain, 0, a.packets, p, gain);
+            S::unpack(ru[i], hat[i]);
+            if (a.post != kNormNone) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) hat[i][e] = (hat[i][e] - st.x) * st.y;
+            }
+            if (kGate) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = hat[i][e];
+                if (a.post != kNormNone) {
+                    if (a.post_gain)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) v[e] *= gain[e];
+                    if (a.post_bias) {
+                        load_parameter<S>(a.post_bias, 0, a.packets, p, w);
+#pragma unroll
+                        for (int e = 0; e < V; ++e) v[e] += w[e];
+                    }
+                }
+                load_parameter<S>(a.gate, gate_row, a.packets, p, w);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    accg[i][e] = fmaf(ds[i][e], v[e], accg[i][e]);
+                    ds[i][e] *= w[e];
+                }
+            }
+            if (a.post != kNormNone) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    acc[kSumPostGain][i][e] = fmaf(ds[i][e], hat[i][e], acc[kSumPostGain][i][e]);
+                    if (kBias) acc[kSumPostBias][i][e] += ds[i][e];
+                    if (a.post_gain) ds[i][e] *= gain[e];
+                    t[0] += ds[i][e];
+                    t[1] = fmaf(ds[i][e], hat[i][e], t[1]);
+                }
+            }
+        }
+        if (a.post != kNormNone) {
+            sum(t);
+            const float m = a.post == kNormLayer ? t[0] * a.inv_cols : 0.0f, q = t[1] * a.inv_cols;
+#pragma unroll
+            for (int i = 0; i < I; ++i)
+#pragma unroll
+                for (int e = 0; e < V; ++e) ds[i][e] = st.y * (ds[i][e] - m - hat[i][e] * q);
+        }
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+            if (on[i]) store_packet<true>(static_cast<uint4*>(a.grad_u) + row * a.packets + threadIdx.x + i * blockDim.x, S::pack(ds[i]));
+    }
+    if (r0 >= r1) return;
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        if (!on[i]) continue;
+        const size_t col = size_t(threadIdx.x + i * blockDim.x) * V;
+#pragma unroll
+        for (int k = 0; k < kNormSums; ++k) {
+            if (!kBias && (k == kSumPreBias || k == kSumPostBias)) continue;
+            if (!a.sums[k]) continue;
+            float4* dst = reinterpret_cast<float4*>(a.partial + (size_t(blockIdx.x) * kNormSums + k) * a.cols + col);
+#pragma unroll
+            for (int e = 0; e < V; e += 4) dst[e / 4] = make_float4(acc[k][i][e], acc[k][i][e + 1], acc[k][i][e + 2], acc[k][i][e + 3]);
+        }
+        if (kGate && a.grad_gate) {
+            float* dst = gate_target(a, blockIdx.x, r0, r1, gate_row) + col;
+#pragma unroll
+            for (int e = 0; e < V; ++e) dst[e] = accg[i][e];
+        }
+    }
+}
+
+// Any shape, first kernel: the four row means that the gradients need, (mean d, mean d s^, mean e, mean e u^).
+template <class S> struct NormElement {
+    float d, shat, ds, uhat, a, da;
+};
+
+// everything of one element up to e = da g_post, from the row's statistics and (for ds) its first two means
+template <class S>
+__device__ __forceinline__ NormElement<S> norm_element(const NormBackwardArgs& a, size_t base, size_t gate, uint32_t c, float4 st, float m, float q)
+{
+    NormElement<S> x;
+    x.d = x.shat = 0.0f;
+    x.ds = a.grad_s ? at<S>(a.grad_s, base + c) : 0.0f;
+    if (a.pre != kNormNone) {
+        x.d = at<S>(a.grad_h, base + c);
+        x.shat = (at<S>(a.s, base + c) - st.z) * st.w;
+        const float d = a.pre_gain ? x.d * at<S>(a.pre_gain, c) : x.d;
+        x.ds = fmaf(st.w, d - m - x.shat * q, x.ds);
+    }
+    x.uhat = a.u ? at<S>(a.u, base + c) : 0.0f;
+    if (a.post != kNormNone) x.uhat = (x.uhat - st.x) * st.y;
+    x.a = x.uhat;
+    if (a.post != kNormNone) {
+        if (a.post_gain) x.a *= at<S>(a.post_gain, c);
+        if (a.post_bias) x.a += at<S>(a.post_bias, c);
+    }
+    x.da = a.gate ? x.ds * at<S>(a.gate, gate + c) : x.ds;
+    return x;
+}
+
+template <class S>
+__global__ void __launch_bounds__(kBlock) norm_backward_means_kernel(const __grid_constant__ NormBackwardArgs a)
+{
+    __shared__ float buf[2][2][32];
+    RowSum<2, false> sum{buf, 0};
+    for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const size_t base = row * a.cols, gate = a.gate ? row / a.rows_per_gate * a.cols : 0;
+        const float4 st = a.stats[row];
+        float t[2] = {0.0f, 0.0f};
+        float4 out = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (a.pre != kNormNone) {
+            for (uint32_t c = threadIdx.x; c < a.cols; c += kBlock) {
+                float d = at<S>(a.grad_h, base + c);
+                if (a.pre_gain) d *= at<S>(a.pre_gain, c);
+                t[0] += d;
+                t[1] = fmaf(d, (at<S>(a.s, base + c) - st.z) * st.w, t[1]);
+            }
+            sum(t);
+            out.x = a.pre == kNormLayer ? t[0] * a.inv_cols : 0.0f;
+            out.y = t[1] * a.inv_cols;
+        }
+        if (a.post != kNormNone) {
+            t[0] = t[1] = 0.0f;
+            for (uint32_t c = threadIdx.x; c < a.cols; c += kBlock) {
+                const NormElement<S> x = norm_element<S>(a, base, gate, c, st, out.x, out.y);
+                const float e = a.post_gain ? x.da * at<S>(a.post_gain, c) : x.da;
+                t[0] += e;
+                t[1] = fmaf(e, x.uhat, t[1]);
+            }
+            sum(t);
+            out.z = a.post == kNormLayer ? t[0] * a.inv_cols : 0.0f;
+            out.w = t[1] * a.inv_cols;
+        }
+        if (threadIdx.x == 0) a.row_means[row] = out;
+    }
+}
+
+// Any shape, second kernel: a thread owns one column of a chunk of rows, writes the two gradients and its column's sums.
+template <class S>
+__global__ void __launch_bounds__(kBlock) norm_backward_columns_kernel(const __grid_constant__ NormBackwardArgs a)
+{
+    const size_t col = size_t(blockIdx.x) * kBlock + threadIdx.x;
+    if (col >= a.cols) return;
+    const uint32_t c = uint32_t(col);
+    const size_t r0 = blockIdx.y * a.chunk_rows, r1 = r0 + a.chunk_rows < a.rows ? r0 + a.chunk_rows : a.rows;
+    if (r0 >= r1) return;
+    float acc[kNormSums] = {0.0f, 0.0f, 0.0f, 0.0f}, accg = 0.0f;
+    size_t gate_row = a.gate ? r0 / a.rows_per_gate : 0, gate_end = (gate_row + 1) * a.rows_per_gate;
+    for (size_t row = r0; row < r1; ++row) {
+        if (a.gate && row == gate_end) {
+            if (a.grad_gate) gate_target(a, blockIdx.y, r0, r1, gate_row)[c] = accg;
+            accg = 0.0f;
+            ++gate_row;
+            gate_end += a.rows_per_gate;
+        }
+        const float4 st = a.stats[row], mean = a.row_means[row];
+        const size_t base = row * a.cols;
+        const NormElement<S> x = norm_element<S>(a, base, gate_row * a.cols, c, st, mean.x, mean.y);
+        acc[kSumPreGain] = fmaf(x.d, x.shat, acc[kSumPreGain]);
+        acc[kSumPreBias] += x.d;
+        acc[kSumPostGain] = fmaf(x.da, x.uhat, acc[kSumPostGain]);
+        acc[kSumPostBias] += x.da;
+        accg = fmaf(x.ds, x.a, accg);
+        float du = x.da;
+        if (a.post != kNormNone) {
+            const float e = a.post_gain ? du * at<S>(a.post_gain, c) : du;
+            du = st.y * (e - mean.z - x.uhat * mean.w);
+        }
+        if (a.grad_r) put<S>(a.grad_r, base + c, a.alpha * x.ds);
+        put<S>(a.grad_u, base + c, du);
+    }
+#pragma unroll
+    for (int k = 0; k < kNormSums; ++k)
+        if (a.sums[k]) a.partial[(size_t(blockIdx.y) * kNormSums + k) * a.cols + c] = acc[k];
+    if (a.grad_gate) gate_target(a, blockIdx.y, r0, r1, gate_row)[c] = accg;
+}
+
+// Adds the chunks' sums: blockIdx.y < kNormSums one of the parameters', beyond that a gate row's.  32 columns times 32 runs
+// of consecutive chunks, each run summed in order by one thread, the runs' sums then in order: the same bits every time.
+static __global__ void __launch_bounds__(1024) norm_reduce_kernel(const __grid_constant__ NormBackwardArgs a)
+{
+    __shared__ float smem[32][32];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
+    const size_t col = size_t(blockIdx.x) * 32 + lane;
+    const size_t gate_rows = a.grad_gate ? a.rows / a.rows_per_gate : 0;
+    for (size_t job = blockIdx.y; job < kNormSums + gate_rows; job += gridDim.y) {
+        float* out = job < kNormSums ? a.sums[job] : a.grad_gate + (job - kNormSums) * a.cols;
+        size_t c0 = 0, c1 = a.chunks;
+        if (job >= kNormSums) {
+            const size_t g0 = (job - kNormSums) * a.rows_per_gate, g1 = g0 + a.rows_per_gate;
+            c0 = g0 / a.chunk_rows;
+            c1 = (g1 - 1) / a.chunk_rows + 1;
+            if (c1 - c0 == 1) continue;                              // written by its chunk
+        } else if (!out) {
+            continue;
+        }
+        const size_t per = (c1 - c0 + 31) / 32;
+        const size_t k0 = c0 + group * per, k1 = k0 + per < c1 ? k0 + per : c1;
+        float s = 0.0f;
+        if (col < a.cols)
+            for (size_t k = k0; k < k1; ++k) {
+                if (job < kNormSums) {
+                    s += a.partial[(k * kNormSums + job) * a.cols + col];
+                } else {
+                    const size_t g0 = (job - kNormSums) * a.rows_per_gate;
+                    s += a.partial[(size_t(a.chunks) * kNormSums + k * 2 + (g0 <= k * a.chunk_rows ? 0 : 1)) * a.cols + col];
+                }
+            }
+        smem[group][lane] = s;
+        __syncthreads();
+        if (group == 0 && col < a.cols) {
+            float t = smem[0][lane];
+#pragma unroll
+            for (int j = 1; j < 32; ++j) t += smem[j][lane];
+            out[col] = t;
+        }
+        __syncthreads();
+    }
+}
+
+// How the rows are cut: by shape, type and device alone, so that a call's scratch can be asked for beforehand.
+struct NormPlan { unsigned block; int packets_per_thread; size_t chunk_rows; uint32_t chunks; };
+
+template <class S> inline NormPlan norm_plan(size_t rows, size_t cols, int sm_count)
+{
+    NormPlan p;
+    const size_t packets = (cols + S::kVec - 1) / S::kVec;
+    p.packets_per_thread = packets <= 512 ? 1 : 2;
+    size_t block = ((packets + p.packets_per_thread - 1) / p.packets_per_thread + 31) / 32 * 32;
+    p.block = unsigned(block < 512 ? block : 512);
+    const size_t target = size_t(sm_count) * (512 / p.block);
+    size_t chunks = rows < target ? rows : target;
+    if (chunks == 0) chunks = 1;
+    p.chunk_rows = (rows + chunks - 1) / chunks;
+    if (p.chunk_rows == 0) p.chunk_rows = 1;
+    p.chunks = uint32_t((rows + p.chunk_rows - 1) / p.chunk_rows);
+    if (p.chunks == 0) p.chunks = 1;
+    return p;
+}
+
+template <class S> inline size_t norm_backward_scratch_bytes(size_t rows, size_t cols, int sm_count)
+{
+    const NormPlan p = norm_plan<S>(rows, cols, sm_count);
+    return rows * sizeof(float4) + size_t(p.chunks) * (kNormSums + 2) * cols * sizeof(float);
+}
+
+template <class S, int I>
+cudaError_t launch_norm_backward_rows(const cudaLaunchConfig_t& cfg, const NormBackwardArgs& a)
+{
+    const bool bias = a.sums[kSumPreBias] || a.sums[kSumPostBias];
+    if (a.gate) return bias ? cudaLaunchKernelEx(&cfg, norm_backward_kernel<S, I, true, true>, a)
+                            : cudaLaunchKernelEx(&cfg, norm_backward_kernel<S, I, true, false>, a);
+    return bias ? cudaLaunchKernelEx(&cfg, norm_backward_kernel<S, I, false, true>, a)
+                : cudaLaunchKernelEx(&cfg, norm_backward_kernel<S, I, false, false>, a);
+}
+
+template <class S>
+cudaError_t launch_norm_backward(const NormBackwardArgs& in, void* scratch, cudaStream_t st)
+{
+    NormBackwardArgs a = in;
+    DeviceInfo di;
+    cudaError_t e = device_info(&di);
+    if (e != cudaSuccess) return e;
+    if (a.cols == 0) return cudaSuccess;
+    if (a.rows == 0) {
+        for (int k = 0; k < kNormSums; ++k)
+            if (a.sums[k] && (e = cudaMemsetAsync(a.sums[k], 0, a.cols * sizeof(float), st)) != cudaSuccess) return e;
+        return cudaSuccess;
+    }
+    const NormPlan p = norm_plan<S>(a.rows, a.cols, di.sm_count);
+    a.row_means = static_cast<float4*>(scratch);
+    a.partial = reinterpret_cast<float*>(a.row_means + a.rows);
+    a.chunk_rows = p.chunk_rows;
+    a.chunks = p.chunks;
+    a.packets = a.cols / S::kVec;
+    const void* ptr[10] = {a.grad_h, a.grad_s, a.u, a.s, a.post_gain, a.post_bias, a.gate, a.pre_gain, a.grad_u, a.grad_r};
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[1];
+    // the row in registers, two packets a thread at most (more spill beside the column sums)
+    if (norm_vector_ok<S>(ptr, 10, a.cols) && a.packets <= 1024) {
+        norm_launch_config(&cfg, attr, p.chunks, p.block, st);
+        e = p.packets_per_thread == 1 ? launch_norm_backward_rows<S, 1>(cfg, a) : launch_norm_backward_rows<S, 2>(cfg, a);
+    } else {
+        const size_t cap = size_t(di.sm_count) * 8;
+        norm_backward_means_kernel<S><<<(unsigned)(a.rows < cap ? a.rows : cap), kBlock, 0, st>>>(a);
+        if ((e = cudaPeekAtLastError()) != cudaSuccess) return e;
+        norm_backward_columns_kernel<S><<<dim3((a.cols + kBlock - 1) / kBlock, p.chunks), kBlock, 0, st>>>(a);
+        e = cudaPeekAtLastError();
+    }
+    if (e != cudaSuccess) return e;
+    const size_t gate_rows = a.grad_gate && a.rows_per_gate > 1 ? a.rows / a.rows_per_gate : 0;
+    bool any = gate_rows > 0;
+    for (int k = 0; k < kNormSums; ++k) any = any || a.sums[k];
+    if (!any) return cudaSuccess;
+    const size_t jobs = kNormSums + gate_rows;
+    norm_launch_config(&cfg, attr, (a.cols + 31) / 32, 1024, st);
+    cfg.gridDim.y = (unsigned)(jobs < 65535 ? jobs : 65535);
+    return cudaLaunchKernelEx(&cfg, norm_reduce_kernel, a);
+}
+
+}  // namespace nfad

@@ -394,6 +394,70 @@ NFAD_API int nfad_block_norm_backward(const nfad_block_norm* norm, int dtype, co
 NFAD_API size_t nfad_block_norm_backward_scratch_bytes(int dtype, size_t rows, size_t cols);
 
 /*
+ * Matrix products grouped by expert, with the nested activation in their epilogue.
+ *
+ * x is [rows, in], its rows sorted by expert; w is [experts, out, in] (each expert's weight as a linear layer keeps it);
+ * offsets is a DEVICE array of experts + 1 ints: expert e has the rows from offsets[e] up to offsets[e + 1].  The runs may be
+ * ragged and empty.  Nothing is read back: the call does not synchronise, and a CUDA graph may be replayed with other
+ * offsets.  Offsets are held to [0, rows] and to ascending order on the device, so that no value of theirs reaches memory outside the
+ * tensors.  Rows before offsets[0] and from offsets[experts] on belong to no expert: they are not read and their results are 0.
+ * experts is at most NFAD_MAX_EXPERTS (NFAD_E_TOO_LARGE); one expert with offsets {0, rows} is an ordinary linear layer.
+ * dtype is NFAD_BF16 or NFAD_F16 (NFAD_E_DTYPE otherwise); products are exact and summed in fp32 by the tensor cores, and
+ * every result is rounded once.  in, out and rows must be below 2^31.  Tensors whose rows do not start on 16-byte
+ * boundaries (in or, for the backward products, out not a multiple of 8; an unaligned pointer) go through a slower gather.
+ *
+ * Forward: z = x w_e^T + bias_e;  kind NFAD_NO_ACT: y = z; otherwise y = f(z) and, when dfdx is not NULL, dfdx = f'(z): the
+ *   one tensor to keep for back-propagation (Section II-C approach 3); z never reaches memory.  bias [experts, out] or NULL.
+ *   y (and dfdx) [rows, out] must not overlap the inputs or each other.  With NFAD_NO_ACT dfdx must be NULL (NFAD_E_VALUE).
+ * Backward, first the multiplication of Eq. 4 on grouped rows: grad_z = round(grad_out dfdx) and grad_bias[e] = the column
+ *   sums of the unrounded products over expert e's rows (fp32, in a fixed order).  dfdx NULL: f' = 1, and grad_z may be NULL.
+ *   grad_z may equal grad_out or dfdx.  grad_bias [experts, out] or NULL.  scratch: nfad_expert_act_backward_scratch_bytes(), 16-byte
+ *   aligned; needed for grad_bias only.
+ * grad_x = grad_z w_e, times `dfdx_x` [rows, in] when that is not NULL: the f' of the layer in front, whose Eq. 4 is then done
+ *   here.  grad_x may equal dfdx_x.
+ * grad_w[e] = grad_z_e^T x_e, [experts, out, in], rounded to dtype; an expert without rows gets zeros.
+ */
+#define NFAD_NO_ACT (-1)
+#define NFAD_MAX_EXPERTS 1024
+NFAD_API int nfad_expert_linear(int kind, int dtype, const void* x, const void* w, const void* bias, const int* offsets, void* y, void* dfdx,
+                                size_t rows, size_t in, size_t out, size_t experts, nfad_stream_t stream);
+NFAD_API int nfad_expert_act_backward(int dtype, const void* grad_out, const void* dfdx, const int* offsets, void* grad_z, float* grad_bias,
+                                      void* scratch, size_t scratch_bytes, size_t rows, size_t out, size_t experts, nfad_stream_t stream);
+NFAD_API size_t nfad_expert_act_backward_scratch_bytes(size_t rows, size_t out);
+NFAD_API int nfad_expert_linear_backward_input(int dtype, const void* grad_z, const void* w, const int* offsets, const void* dfdx_x, void* grad_x,
+                                               size_t rows, size_t in, size_t out, size_t experts, nfad_stream_t stream);
+NFAD_API int nfad_expert_linear_backward_weight(int dtype, const void* grad_z, const void* x, const int* offsets, void* grad_w, size_t rows,
+                                                size_t in, size_t out, size_t experts, nfad_stream_t stream);
+
+/*
+ * Linear layer in 8-bit integers, with a scale for each token (row of x) and for each output channel (row of w).
+ *
+ * nfad_i8_quantize_rows: scale[r] = amax / 127, q = rint(x (127 / amax)) in [-127, 127], amax the row's largest magnitude.
+ *   Rows with amax below 2^-120 get scale 0 and q 0; rows that hold an infinity or a NaN get scale NaN and q 0.  x of any
+ *   dtype [rows, cols]; q signed bytes; scale fp32.  Serves weights [out, in] (once) and activations alike.
+ * nfad_i8_linear: y[r, o] = f(x_scale[r] w_scale[o] sum_i xq[r, i] wq[o, i] + bias[o]); the sum exact in 32-bit integers, the
+ *   rest fp32, rounded once to dtype (NFAD_BF16 or NFAD_F16).  kind NFAD_NO_ACT: no activation; value only.  Bytes may
+ *   be -128.  in is at most NFAD_I8_MAX_IN, beyond which 32 bits could overflow (NFAD_E_TOO_LARGE).  bias [out] of dtype, or NULL.
+ * nfad_i8_linear_dynamic: the same from x itself [rows, in] of dtype, quantised by rows on the way.  scratch: device memory, 16-byte
+ *   aligned, of nfad_i8_linear_dynamic_scratch_bytes() bytes, contents irrelevant before and after.
+ * Rows of xq and wq that do not start on 16-byte boundaries (in not a multiple of 16) go through a slower gather.
+ */
+#define NFAD_I8_MAX_IN 131071
+NFAD_API int nfad_i8_quantize_rows(int dtype, const void* x, signed char* q, float* scale, size_t rows, size_t cols, nfad_stream_t stream);
+NFAD_API int nfad_i8_linear(int kind, int dtype, const signed char* xq, const float* x_scale, const signed char* wq, const float* w_scale,
+                            const void* bias, void* y, size_t rows, size_t in, size_t out, nfad_stream_t stream);
+NFAD_API int nfad_i8_linear_dynamic(int kind, int dtype, const void* x, const signed char* wq, const float* w_scale, const void* bias, void* y,
+                                    void* scratch, size_t scratch_bytes, size_t rows, size_t in, size_t out, nfad_stream_t stream);
+NFAD_API size_t nfad_i8_linear_dynamic_scratch_bytes(size_t rows, size_t in);
+
+/*
+ * How many CTAs of the products above have given up waiting for their own copies or products since the library was loaded
+ * on the current device (0 in a healthy process; a launch that gave up leaves its results undefined instead of hanging the
+ * device), or a negative nfad_status.  Synchronises the device: a diagnostic, not for a hot path.
+ */
+NFAD_API int nfad_product_faults(void);
+
+/*
  * The whole pass for tensors that live in HOST memory (no counterpart in the paper: a service entry
  * point for callers whose activations are kept off the device, and the end-to-end form of the pass
  * that the benchmark times).  Forward and backward of one batch:

@@ -16,4 +16,8 @@ from .binding import (  # noqa: F401
 from .block import (  # noqa: F401
     NORMS, BlockNorm, nfad_block_norm_backward, nfad_block_norm_backward_scratch, nfad_block_norm_backward_scratch_bytes,
     nfad_block_norm_forward,
+    nfad_expert_act_backward, nfad_expert_act_backward_scratch, nfad_expert_act_backward_scratch_bytes, nfad_expert_linear,
+    nfad_expert_linear_backward_input, nfad_expert_linear_backward_weight,
+    nfad_i8_linear, nfad_i8_linear_dynamic, nfad_i8_linear_dynamic_scratch, nfad_i8_linear_dynamic_scratch_bytes,
+    nfad_i8_quantize_rows, nfad_product_faults,
 )

@@ -126,3 +126,162 @@ def nfad_block_norm_backward(norm: BlockNorm, grad_h: Optional[torch.Tensor], gr
                                                _raw(stats, "stats", torch.float32, (rows, 4), grad_u.device), pg,
                                                _like(grad_r, "grad_r", grad_u), ctypes.byref(out), sp, sb, rows, cols,
                                                _stream(grad_u)), "nfad_block_norm_backward")
+
+
+# ---------------------------------------------------------------- products grouped by expert
+
+def _act(kind) -> int:
+    return NO_ACT if kind is None else _kind(kind)
+
+
+def _matrix(t: torch.Tensor, name: str, dims: int = 2) -> int:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.dim() != dims or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of {dims} dimensions")
+    if t.dtype not in _TORCH_TO_CODE:
+        raise TypeError(f"{name}: unsupported dtype {t.dtype}")
+    return t.data_ptr()
+
+
+def _offsets(offsets: torch.Tensor, device) -> int:
+    if not isinstance(offsets, torch.Tensor) or offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() == 0:
+        raise TypeError("offsets must be an int32 tensor of experts + 1 values")
+    if offsets.device != device or not offsets.is_contiguous():
+        raise ValueError("offsets must be contiguous and on the tensors' device")
+    return offsets.data_ptr()
+
+
+def nfad_expert_linear(kind, x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor], offsets: torch.Tensor, y: torch.Tensor,
+                       dfdx: Optional[torch.Tensor] = None) -> None:
+    """y = f(x w_e^T + bias_e), dfdx = f' of it: x [rows, in] sorted by expert, w [experts, out, in], bias [experts, out],
+    offsets [experts + 1] int32.  kind None: no activation (and no dfdx)."""
+    px, pw = _matrix(x, "x"), _matrix(w, "w", 3)
+    (rows, n_in), (experts, n_out, w_in) = x.shape, w.shape
+    if w_in != n_in or w.dtype != x.dtype or w.device != x.device:
+        raise ValueError("w must be [experts, out, in] of x's dtype and device")
+    if offsets.numel() != experts + 1:
+        raise ValueError("offsets must hold experts + 1 values")
+    shape = (rows, n_out)
+    pb = _raw(bias, "bias", x.dtype, (experts, n_out), x.device)
+    py, pd = _raw(y, "y", x.dtype, shape, x.device), _raw(dfdx, "dfdx", x.dtype, shape, x.device)
+    with _on_device(x.device):
+        _check(load().nfad_expert_linear(_act(kind), _TORCH_TO_CODE[x.dtype], px, pw, pb, _offsets(offsets, x.device), py, pd, rows, n_in, n_out,
+                                         experts, _stream(x)), "nfad_expert_linear")
+
+
+def nfad_expert_act_backward_scratch_bytes(rows: int, out: int, device=None) -> int:
+    with torch.cuda.device(device if device is not None else torch.cuda.current_device()):
+        return int(load().nfad_expert_act_backward_scratch_bytes(rows, out))
+
+
+def nfad_expert_act_backward_scratch(grad_out: torch.Tensor, experts: int = 0) -> torch.Tensor:
+    """A scratch tensor for nfad_expert_act_backward on tensors like grad_out (the number of experts does not change its size)."""
+    n = nfad_expert_act_backward_scratch_bytes(grad_out.shape[0], grad_out.shape[1], grad_out.device)
+    return torch.empty(max(n, 16), dtype=torch.uint8, device=grad_out.device)
+
+
+def nfad_expert_act_backward(grad_out: torch.Tensor, dfdx: Optional[torch.Tensor], offsets: torch.Tensor, grad_z: Optional[torch.Tensor],
+                             grad_bias: Optional[torch.Tensor], scratch: Optional[torch.Tensor]) -> None:
+    """grad_z = grad_out dfdx; grad_bias (fp32 [experts, out]) = each expert's column sums of the unrounded products."""
+    pg = _matrix(grad_out, "grad_out")
+    rows, n_out = grad_out.shape
+    experts = offsets.numel() - 1
+    pd = _raw(dfdx, "dfdx", grad_out.dtype, grad_out.shape, grad_out.device)
+    pz = _raw(grad_z, "grad_z", grad_out.dtype, grad_out.shape, grad_out.device)
+    pb = _raw(grad_bias, "grad_bias", torch.float32, (experts, n_out), grad_out.device)
+    sp, sb = _scratch(scratch)
+    with _on_device(grad_out.device):
+        _check(load().nfad_expert_act_backward(_TORCH_TO_CODE[grad_out.dtype], pg, pd, _offsets(offsets, grad_out.device), pz, pb, sp, sb, rows,
+                                               n_out, experts, _stream(grad_out)), "nfad_expert_act_backward")
+
+
+def nfad_expert_linear_backward_input(grad_z: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, dfdx_x: Optional[torch.Tensor],
+                                      grad_x: torch.Tensor) -> None:
+    """grad_x = (grad_z w_e) dfdx_x: the gradient of the layer's input, times the f' of the activation in front when given."""
+    pg, pw = _matrix(grad_z, "grad_z"), _matrix(w, "w", 3)
+    (rows, n_out), (experts, w_out, n_in) = grad_z.shape, w.shape
+    if w_out != n_out or w.dtype != grad_z.dtype or w.device != grad_z.device:
+        raise ValueError("w must be [experts, out, in] of grad_z's dtype and device")
+    if offsets.numel() != experts + 1:
+        raise ValueError("offsets must hold experts + 1 values")
+    shape = (rows, n_in)
+    pd = _raw(dfdx_x, "dfdx_x", grad_z.dtype, shape, grad_z.device)
+    px = _raw(grad_x, "grad_x", grad_z.dtype, shape, grad_z.device)
+    with _on_device(grad_z.device):
+        _check(load().nfad_expert_linear_backward_input(_TORCH_TO_CODE[grad_z.dtype], pg, pw, _offsets(offsets, grad_z.device), pd, px, rows, n_in,
+                                                        n_out, experts, _stream(grad_z)), "nfad_expert_linear_backward_input")
+
+
+def nfad_expert_linear_backward_weight(grad_z: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor, grad_w: torch.Tensor) -> None:
+    """grad_w[e] = grad_z_e^T x_e, [experts, out, in]."""
+    pg, px = _matrix(grad_z, "grad_z"), _matrix(x, "x")
+    (rows, n_out), n_in, experts = grad_z.shape, x.shape[1], offsets.numel() - 1
+    if x.shape[0] != rows or x.dtype != grad_z.dtype or x.device != grad_z.device:
+        raise ValueError("x must have grad_z's rows, dtype and device")
+    pw = _raw(grad_w, "grad_w", grad_z.dtype, (experts, n_out, n_in), grad_z.device)
+    with _on_device(grad_z.device):
+        _check(load().nfad_expert_linear_backward_weight(_TORCH_TO_CODE[grad_z.dtype], pg, px, _offsets(offsets, grad_z.device), pw, rows, n_in,
+                                                         n_out, experts, _stream(grad_z)), "nfad_expert_linear_backward_weight")
+
+
+# ---------------------------------------------------------------- the linear layer in 8-bit integers
+
+def nfad_i8_quantize_rows(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor) -> None:
+    """q (int8) and scale (fp32 [rows]) of x [rows, cols]: x = scale q up to half a step of the row's own scale."""
+    px = _matrix(x, "x")
+    pq, ps = _raw(q, "q", torch.int8, x.shape, x.device), _raw(scale, "scale", torch.float32, x.shape[:1], x.device)
+    with _on_device(x.device):
+        _check(load().nfad_i8_quantize_rows(_TORCH_TO_CODE[x.dtype], px, pq, ps, x.shape[0], x.shape[1], _stream(x)), "nfad_i8_quantize_rows")
+
+
+def _i8_weight(wq: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor], y: torch.Tensor, n_in: int):
+    if not isinstance(wq, torch.Tensor) or wq.dim() != 2 or wq.shape[1] != n_in:
+        raise ValueError("wq must be [out, in]")
+    n_out = wq.shape[0]
+    return (n_out, _raw(wq, "wq", torch.int8, (n_out, n_in), y.device), _raw(w_scale, "w_scale", torch.float32, (n_out,), y.device),
+            _raw(bias, "bias", y.dtype, (n_out,), y.device))
+
+
+def nfad_i8_linear(kind, xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor],
+                   y: torch.Tensor) -> None:
+    """y = f(x_scale w_scale (xq wq^T) + bias): xq [rows, in] and wq [out, in] int8, scales fp32, bias and y 16-bit."""
+    py = _matrix(y, "y")
+    rows, n_in = xq.shape
+    n_out, pw, pws, pb = _i8_weight(wq, w_scale, bias, y, n_in)
+    if y.shape != (rows, n_out):
+        raise ValueError("y must be [rows, out]")
+    px, pxs = _raw(xq, "xq", torch.int8, (rows, n_in), y.device), _raw(x_scale, "x_scale", torch.float32, (rows,), y.device)
+    with _on_device(y.device):
+        _check(load().nfad_i8_linear(_act(kind), _TORCH_TO_CODE[y.dtype], px, pxs, pw, pws, pb, py, rows, n_in, n_out, _stream(y)), "nfad_i8_linear")
+
+
+def nfad_i8_linear_dynamic_scratch_bytes(rows: int, n_in: int) -> int:
+    return int(load().nfad_i8_linear_dynamic_scratch_bytes(rows, n_in))
+
+
+def nfad_i8_linear_dynamic_scratch(x: torch.Tensor) -> torch.Tensor:
+    """A scratch tensor for nfad_i8_linear_dynamic on inputs like x."""
+    return torch.empty(max(nfad_i8_linear_dynamic_scratch_bytes(*x.shape), 16), dtype=torch.uint8, device=x.device)
+
+
+def nfad_i8_linear_dynamic(kind, x: torch.Tensor, wq: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor], y: torch.Tensor,
+                           scratch: torch.Tensor) -> None:
+    """nfad_i8_linear from the 16-bit x [rows, in], each row quantised on the way."""
+    px, py = _matrix(x, "x"), _matrix(y, "y")
+    rows, n_in = x.shape
+    n_out, pw, pws, pb = _i8_weight(wq, w_scale, bias, y, n_in)
+    if y.shape != (rows, n_out) or y.dtype != x.dtype or y.device != x.device:
+        raise ValueError("y must be [rows, out] of x's dtype and device")
+    sp, sb = _scratch(scratch)
+    with _on_device(x.device):
+        _check(load().nfad_i8_linear_dynamic(_act(kind), _TORCH_TO_CODE[x.dtype], px, pw, pws, pb, py, sp, sb, rows, n_in, n_out, _stream(x)),
+               "nfad_i8_linear_dynamic")
+
+
+def nfad_product_faults() -> int:
+    """How many CTAs of the products have given up waiting since the library was loaded (0 in a healthy process).  Synchronises."""
+    n = int(load().nfad_product_faults())
+    if n < 0:
+        _check(-n, "nfad_product_faults")
+    return n

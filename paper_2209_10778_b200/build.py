@@ -31,6 +31,11 @@ UNITS = [
     ("nfad_kernels_seq.cu", ["-fmad=true"]),
     ("nfad_kernels_bias.cu", ["-fmad=false"]),
     ("nfad_kernels_norm.cu", ["-fmad=true"]),
+    ("nfad_kernels_prod_forward.cu", ["-fmad=true"]),
+    ("nfad_kernels_prod_input.cu", ["-fmad=true"]),
+    ("nfad_kernels_prod_weight.cu", ["-fmad=true"]),
+    ("nfad_kernels_prod_bytes.cu", ["-fmad=true"]),
+    ("nfad_kernels_expert.cu", ["-fmad=true"]),
     ("nfad_api.cu", ["-fmad=false"]),
     ("nfad_api_block.cu", ["-fmad=false"]),
     ("nfad_host.cu", ["-fmad=false"]),

@@ -8,6 +8,7 @@
 #include "../../include/nfad.h"
 #include "nfad_internal.h"
 #include "nfad_norm_args.h"
+#include "nfad_product_args.h"
 
 namespace {
 
@@ -57,6 +58,18 @@ int finish(cudaError_t e)
     if (e == cudaSuccess) return NFAD_OK;
     nfad::note_cuda_error(e);
     return NFAD_E_CUDA;
+}
+
+// a product's sizes: every one below 2^31, and each tensor's bytes countable
+int check_product(int kind, int dtype, size_t rows, size_t in, size_t out, size_t experts)
+{
+    if (kind < nfad::kNoAct || kind > 3) return NFAD_E_KIND;
+    if (dtype != NFAD_BF16 && dtype != NFAD_F16) return NFAD_E_DTYPE;
+    const size_t most = (size_t(1) << 31) - 256;                      // tile indices past the end stay below 2^31
+    if (rows > most || in > most || out > most || experts > NFAD_MAX_EXPERTS) return NFAD_E_TOO_LARGE;
+    if (out && in > (size_t(1) << 39) / out) return NFAD_E_TOO_LARGE; // bytes of one expert's weights: a tensor copy's largest stride
+    if (experts == 0 && rows) return NFAD_E_VALUE;
+    return NFAD_OK;
 }
 
 int check_norm(const nfad_block_norm* norm, int dtype, size_t rows, size_t cols, size_t* n)
@@ -155,6 +168,162 @@ int nfad_block_norm_backward(const nfad_block_norm* norm, int dtype, const void*
         if (e != cudaSuccess) return finish(e);
     }
     return finish(nfad::launch_norm_backward(dtype, a, scratch, static_cast<cudaStream_t>(stream)));
+}
+
+int nfad_expert_linear(int kind, int dtype, const void* x, const void* w, const void* bias, const int* offsets, void* y, void* dfdx, size_t rows,
+                       size_t in, size_t out, size_t experts, nfad_stream_t stream)
+{
+    int rc = check_product(kind, dtype, rows, in, out, experts);
+    if (rc) return rc;
+    if (kind == NFAD_NO_ACT && dfdx) return NFAD_E_VALUE;
+    if (rows == 0 || out == 0) return NFAD_OK;
+    if ((in && (!x || !w)) || !offsets || !y) return NFAD_E_NULL;
+    const Span sx{x, rows * in * 2, 2}, sw{w, experts * out * in * 2, 2}, sb{bias, experts * out * 2, 2}, so{offsets, (experts + 1) * 4, 4};
+    const Span oy{y, rows * out * 2, 2}, od{dfdx, rows * out * 2, 2};
+    if ((rc = aligned({sx, sw, sb, so, oy, od}))) return rc;
+    if ((rc = aliasing({oy, od}, {}, {sx, sw, sb, so}))) return rc;
+    nfad::ProdArgs g = {};
+    g.a = x; g.b = w; g.bias = bias; g.offsets = offsets; g.out = y; g.slope = dfdx;
+    g.rows = rows; g.in = uint32_t(in); g.outs = uint32_t(out); g.experts = uint32_t(experts); g.act = kind;
+    return finish(nfad::launch_product_forward(dtype, g, static_cast<cudaStream_t>(stream)));
+}
+
+size_t nfad_expert_act_backward_scratch_bytes(size_t rows, size_t out)
+{
+    size_t n = 0, bytes = 0;
+    if (element_count(rows, out, &n) || n == 0) return 0;
+    return finish(nfad::expert_act_backward_scratch(rows, out, &bytes)) ? 0 : bytes;
+}
+
+int nfad_expert_act_backward(int dtype, const void* grad_out, const void* dfdx, const int* offsets, void* grad_z, float* grad_bias, void* scratch,
+                             size_t scratch_bytes, size_t rows, size_t out, size_t experts, nfad_stream_t stream)
+{
+    int rc = check_product(nfad::kNoAct, dtype, rows, 0, out, experts);
+    if (rc) return rc;
+    if (out == 0 || experts == 0) return NFAD_OK;
+    const size_t bytes = rows * out * 2;
+    if (!offsets || (bytes && (!grad_out || (dfdx && !grad_z)))) return NFAD_E_NULL;
+    size_t need = 0;
+    if (grad_bias && bytes) {
+        if ((rc = finish(nfad::expert_act_backward_scratch(rows, out, &need)))) return rc;
+        if (!scratch) return NFAD_E_NULL;
+        if (scratch_bytes < need) return NFAD_E_SCRATCH;
+    }
+    const Span sg{grad_out, bytes, 2}, sd{dfdx, bytes, 2}, so{offsets, (experts + 1) * 4, 4};
+    const Span oz{grad_z, bytes, 2}, ob{grad_bias, experts * out * 4, 4}, sc{need ? scratch : nullptr, need, 16};
+    if ((rc = aligned({sg, sd, so, oz, ob, sc}))) return rc;
+    if ((rc = aliasing({oz}, {sg, sd}, {so, ob, sc}))) return rc;
+    if ((rc = aliasing({ob, sc}, {}, {sg, sd, so}))) return rc;
+    return finish(nfad::launch_expert_act_backward(dtype, grad_out, dfdx, offsets, grad_z, grad_bias, scratch, rows, uint32_t(out),
+                                                   uint32_t(experts), static_cast<cudaStream_t>(stream)));
+}
+
+int nfad_expert_linear_backward_input(int dtype, const void* grad_z, const void* w, const int* offsets, const void* dfdx_x, void* grad_x, size_t rows,
+                                      size_t in, size_t out, size_t experts, nfad_stream_t stream)
+{
+    int rc = check_product(nfad::kNoAct, dtype, rows, in, out, experts);
+    if (rc) return rc;
+    if (rows == 0 || in == 0) return NFAD_OK;
+    if ((out && (!grad_z || !w)) || !offsets || !grad_x) return NFAD_E_NULL;
+    const Span sg{grad_z, rows * out * 2, 2}, sw{w, experts * out * in * 2, 2}, so{offsets, (experts + 1) * 4, 4}, sd{dfdx_x, rows * in * 2, 2};
+    const Span ox{grad_x, rows * in * 2, 2};
+    if ((rc = aligned({sg, sw, so, sd, ox}))) return rc;
+    if ((rc = aliasing({ox}, {sd}, {sg, sw, so}))) return rc;
+    nfad::ProdArgs g = {};
+    g.a = grad_z; g.b = w; g.prev = dfdx_x; g.offsets = offsets; g.out = grad_x;
+    g.rows = rows; g.in = uint32_t(in); g.outs = uint32_t(out); g.experts = uint32_t(experts); g.act = nfad::kNoAct;
+    return finish(nfad::launch_product_input(dtype, g, static_cast<cudaStream_t>(stream)));
+}
+
+int nfad_expert_linear_backward_weight(int dtype, const void* grad_z, const void* x, const int* offsets, void* grad_w, size_t rows, size_t in,
+                                       size_t out, size_t experts, nfad_stream_t stream)
+{
+    int rc = check_product(nfad::kNoAct, dtype, rows, in, out, experts);
+    if (rc) return rc;
+    if (in == 0 || out == 0 || experts == 0) return NFAD_OK;
+    if ((rows && (!grad_z || !x)) || !offsets || !grad_w) return NFAD_E_NULL;
+    const Span sg{grad_z, rows * out * 2, 2}, sx{x, rows * in * 2, 2}, so{offsets, (experts + 1) * 4, 4}, ow{grad_w, experts * out * in * 2, 2};
+    if ((rc = aligned({sg, sx, so, ow}))) return rc;
+    if ((rc = aliasing({ow}, {}, {sg, sx, so}))) return rc;
+    nfad::ProdArgs g = {};
+    g.a = grad_z; g.b = x; g.offsets = offsets; g.out = grad_w;
+    g.rows = rows; g.in = uint32_t(in); g.outs = uint32_t(out); g.experts = uint32_t(experts); g.act = nfad::kNoAct;
+    return finish(nfad::launch_product_weight(dtype, g, static_cast<cudaStream_t>(stream)));
+}
+
+int nfad_i8_quantize_rows(int dtype, const void* x, signed char* q, float* scale, size_t rows, size_t cols, nfad_stream_t stream)
+{
+    if (dtype < 0 || dtype > 2) return NFAD_E_DTYPE;
+    size_t n = 0;
+    int rc = element_count(rows, cols, &n);
+    if (rc) return rc;
+    if (rows == 0) return NFAD_OK;
+    if (rows >= (size_t(1) << 31)) return NFAD_E_TOO_LARGE;
+    if ((n && (!x || !q)) || !scale) return NFAD_E_NULL;
+    const size_t es = elem_size(dtype);
+    const Span sx{x, n * es, es}, oq{q, n, 1}, os{scale, rows * 4, 4};
+    if ((rc = aligned({sx, oq, os}))) return rc;
+    if ((rc = aliasing({oq, os}, {}, {sx}))) return rc;
+    return finish(nfad::launch_quantize_rows(dtype, x, q, scale, rows, uint32_t(cols), static_cast<cudaStream_t>(stream)));
+}
+
+int nfad_i8_linear(int kind, int dtype, const signed char* xq, const float* x_scale, const signed char* wq, const float* w_scale, const void* bias,
+                   void* y, size_t rows, size_t in, size_t out, nfad_stream_t stream)
+{
+    int rc = check_product(kind, dtype, rows, in, out, 1);
+    if (rc) return rc;
+    if (in > NFAD_I8_MAX_IN) return NFAD_E_TOO_LARGE;
+    if (rows == 0 || out == 0) return NFAD_OK;
+    if ((in && (!xq || !wq)) || !x_scale || !w_scale || !y) return NFAD_E_NULL;
+    const Span sx{xq, rows * in, 1}, sxs{x_scale, rows * 4, 4}, sw{wq, out * in, 1}, sws{w_scale, out * 4, 4}, sb{bias, out * 2, 2};
+    const Span oy{y, rows * out * 2, 2};
+    if ((rc = aligned({sx, sxs, sw, sws, sb, oy}))) return rc;
+    if ((rc = aliasing({oy}, {}, {sx, sxs, sw, sws, sb}))) return rc;
+    nfad::ProdArgs g = {};
+    g.a = xq; g.b = wq; g.bias = bias; g.a_scale = x_scale; g.b_scale = w_scale; g.out = y;
+    g.rows = rows; g.in = uint32_t(in); g.outs = uint32_t(out); g.experts = 1; g.act = kind;
+    return finish(nfad::launch_product_bytes(dtype, g, static_cast<cudaStream_t>(stream)));
+}
+
+size_t nfad_i8_linear_dynamic_scratch_bytes(size_t rows, size_t in)
+{
+    if (in > NFAD_I8_MAX_IN || rows >= (size_t(1) << 31)) return 0;
+    return ((rows * in + 15) & ~size_t(15)) + rows * sizeof(float);   // the integers, then the scales
+}
+
+int nfad_i8_linear_dynamic(int kind, int dtype, const void* x, const signed char* wq, const float* w_scale, const void* bias, void* y, void* scratch,
+                           size_t scratch_bytes, size_t rows, size_t in, size_t out, nfad_stream_t stream)
+{
+    int rc = check_product(kind, dtype, rows, in, out, 1);
+    if (rc) return rc;
+    if (in > NFAD_I8_MAX_IN) return NFAD_E_TOO_LARGE;
+    if (rows == 0 || out == 0) return NFAD_OK;
+    if ((in && (!x || !wq)) || !w_scale || !y || !scratch) return NFAD_E_NULL;
+    const size_t need = nfad_i8_linear_dynamic_scratch_bytes(rows, in);
+    const Span sx{x, rows * in * 2, 2}, sw{wq, out * in, 1}, sws{w_scale, out * 4, 4}, sb{bias, out * 2, 2};
+    const Span oy{y, rows * out * 2, 2}, sc{scratch, need, 16};
+    if ((rc = aligned({sx, sw, sws, sb, oy, sc}))) return rc;
+    if (scratch_bytes < need) return NFAD_E_SCRATCH;
+    if ((rc = aliasing({oy, sc}, {}, {sx, sw, sws, sb}))) return rc;
+    signed char* q = static_cast<signed char*>(scratch);
+    float* scale = reinterpret_cast<float*>(q + ((rows * in + 15) & ~size_t(15)));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if ((rc = finish(nfad::launch_quantize_rows(dtype, x, q, scale, rows, uint32_t(in), st)))) return rc;
+    nfad::ProdArgs g = {};
+    g.a = q; g.b = wq; g.bias = bias; g.a_scale = scale; g.b_scale = w_scale; g.out = y;
+    g.rows = rows; g.in = uint32_t(in); g.outs = uint32_t(out); g.experts = 1; g.act = kind;
+    return finish(nfad::launch_product_bytes(dtype, g, st));
+}
+
+int nfad_product_faults(void)
+{
+    unsigned total = 0;
+    for (auto count : {nfad::product_faults_forward, nfad::product_faults_input, nfad::product_faults_weight, nfad::product_faults_bytes}) {
+        unsigned n = 0;
+        if (int rc = finish(count(&n))) return -rc;
+        total += n;
+    }
+    return int(total & 0x7fffffff);
 }
 
 }  // extern "C"

@@ -5,6 +5,7 @@
 
 #include <cuda_runtime.h>
 #include <stddef.h>
+#include <stdint.h>
 
 #include <string>
 
@@ -71,5 +72,20 @@ struct NormBackwardArgs;
 cudaError_t launch_norm_forward(int dtype, const NormForwardArgs& a, cudaStream_t st);
 cudaError_t launch_norm_backward(int dtype, const NormBackwardArgs& a, void* scratch, cudaStream_t st);
 cudaError_t norm_backward_scratch(int dtype, size_t rows, size_t cols, size_t* bytes);   // on the current device
+
+// Matrix products (nfad_product.cuh), what stands beside them (nfad_expert.cuh, nfad_bytes.cuh), and the CTAs that gave up waiting.
+struct ProdArgs;
+cudaError_t launch_product_forward(int dtype, const ProdArgs& g, cudaStream_t st);
+cudaError_t launch_product_input(int dtype, const ProdArgs& g, cudaStream_t st);
+cudaError_t launch_product_weight(int dtype, const ProdArgs& g, cudaStream_t st);
+cudaError_t launch_product_bytes(int dtype, const ProdArgs& g, cudaStream_t st);
+cudaError_t product_faults_forward(unsigned* n);
+cudaError_t product_faults_input(unsigned* n);
+cudaError_t product_faults_weight(unsigned* n);
+cudaError_t product_faults_bytes(unsigned* n);
+cudaError_t launch_expert_act_backward(int dtype, const void* g, const void* d, const int* offsets, void* gz, float* grad_bias, void* scratch,
+                                       size_t rows, uint32_t cols, uint32_t experts, cudaStream_t st);
+cudaError_t expert_act_backward_scratch(size_t rows, size_t cols, size_t* bytes);        // on the current device
+cudaError_t launch_quantize_rows(int dtype, const void* x, signed char* q, float* scale, size_t rows, uint32_t cols, cudaStream_t st);
 
 }  // namespace nfad

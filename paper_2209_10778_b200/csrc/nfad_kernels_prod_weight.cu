@@ -1,0 +1,8 @@
+#include "nfad_product_launch.cuh"
+
+namespace nfad {
+
+cudaError_t launch_product_weight(int dtype, const ProdArgs& g, cudaStream_t st) { return launch_product_op<kProdWeight>(dtype, g, st); }
+cudaError_t product_faults_weight(unsigned* n) { return product_faults_here(n); }
+
+}  // namespace nfad

@@ -1,0 +1,481 @@
+// nfad_product.cuh -- matrix products grouped by expert, and the 8-bit product, on the fifth-generation tensor cores, with
+// the nested activation in the epilogue: z = x W_e^T + b_e lives only in tensor memory; y = f(z) and f'(z) leave the kernel.
+//
+// One CTA per SM stays for the whole launch and walks over result tiles of 128 x BN.  Its warps have roles:
+//   copy      (one thread) tensor copies of the operands' 128-byte wide boxes into a ring of stages;
+//   products  (one thread) 128 x BN x 64 (128 bytes of the reduction) per stage into one of two accumulators;
+//   results   (eight warps) read the other accumulator, apply the epilogue, store.
+// So copies, products and epilogues of neighbouring tiles overlap.  Which rows a tile has comes from the offsets on the
+// device: every CTA builds the table of row ranges in shared memory and finds its tiles in it, with no word from the host.
+// A tile's last rows may belong to the next expert (forward, input gradient): they are computed and not stored, as rows do
+// not mix.  In the weight gradient rows are the reduction, so rows past the expert's end are cleared in shared memory
+// (both operands: 0 times a NaN of the neighbour would be one).
+//
+// Operands that no tensor copy can take (rows that do not start on 16-byte boundaries) are gathered by four further warps
+// with plain loads into the same swizzled stages (kGather); everything behind the stages is shared.
+//
+// What bounds it: the tensor cores for long inputs (2 rows in out operations, 32 KB + 16 KB of operands for each 128 x 256 x
+// 64 step); the weights' bytes when an expert has few rows.  BN is chosen by how many tiles there are (see product_width).
+#pragma once
+
+#include "nfad_internal.h"
+#include "nfad_ops.cuh"
+#include "nfad_product_args.h"
+#include "nfad_storage.cuh"
+#include "nfad_stream.cuh"
+#include "nfad_tcgen.cuh"
+
+namespace nfad {
+
+constexpr int kTileRows = 128;
+constexpr int kStepBytes = 128;                    // of the reduction, per stage
+constexpr int kResultWarps = 8;
+constexpr int kGatherWarps = 4;
+constexpr int kFirstResultWarp = 4;                // a warp reads the 32 tensor-memory lanes of its index modulo 4
+constexpr int kRingBytes = 196608;
+constexpr int kMaxStages = 9;
+constexpr long long kWaitDrain = 2000000000ll;     // cycles that a CTA which gave up waits for its own work in flight
+
+template <int OP> struct ProdKind {
+    static constexpr bool kBytes = OP == kProdBytes;
+    static constexpr bool kTurnA = OP == kProdWeight;                     // operand A runs along its rows' dimension in memory
+    static constexpr bool kTurnB = OP == kProdWeight || OP == kProdInput;
+    static constexpr int kElem = kBytes ? 1 : 2;
+    static constexpr int kStep = kStepBytes / kElem;                      // reduction steps per stage: 64, 128 for bytes
+};
+template <class S> struct IsBF16 { static constexpr bool value = false; };
+template <> struct IsBF16<StoreBF16> { static constexpr bool value = true; };
+
+template <int BN> struct ProdTile {
+    static constexpr int kStage = (kTileRows + BN) * kStepBytes;
+    static constexpr int kStages = kRingBytes / kStage < kMaxStages ? kRingBytes / kStage : kMaxStages;
+};
+
+struct ProdShared {
+    uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drained;
+    uint32_t tmem, gave_up;
+    int start[kMaxExperts + 1];                     // first row of each expert
+    int tiles[kMaxExperts + 1];                     // row tiles before each expert
+};
+constexpr int kProdSmem = 1024 + kRingBytes + int(sizeof(ProdShared));
+
+// CTAs one of whose waits ran out; one counter for each translation unit that includes this file
+static __device__ unsigned g_product_faults;
+
+struct ProdTileAt {
+    uint32_t expert;
+    int a0, b0;                                     // first index of the tile along A's and B's own dimension (A: a row or an output)
+    int a_end;                                      // end of A's valid indices
+    int r0, r_end;                                  // kProdWeight: the reduction's rows; else [0, reduction)
+};
+
+// Tile t.  Within an expert, bands of kBand tiles along A's dimension, B's tile changing slowest inside a band: the CTAs that run
+// at one time then share a few tiles of each operand through L2.
+constexpr int kBand = 16;
+template <int OP, int BN> __device__ __forceinline__ ProdTileAt tile_at(const ProdArgs& g, const ProdShared& s, long long t, int b_tiles)
+{
+    ProdTileAt q;
+    int a_tiles;
+    long long local;
+    if (OP == kProdWeight) {
+        a_tiles = int((g.outs + kTileRows - 1) / kTileRows);
+        const long long per = (long long)a_tiles * b_tiles;
+        q.expert = uint32_t(t / per);
+        local = t - q.expert * per;
+    } else {
+        uint32_t lo = 0, hi = g.experts;            // the last expert whose first tile is not past t
+        while (hi - lo > 1) {
+            const uint32_t mid = (lo + hi) / 2;
+            if ((long long)s.tiles[mid] * b_tiles <= t) lo = mid;
+            else hi = mid;
+        }
+        q.expert = lo;
+        a_tiles = s.tiles[lo + 1] - s.tiles[lo];
+        local = t - (long long)s.tiles[lo] * b_tiles;
+    }
+    const long long band = local / ((long long)kBand * b_tiles);
+    const int in_band = int(local - band * kBand * b_tiles);
+    const int height = min(kBand, a_tiles - int(band) * kBand);
+    const int at = int(band) * kBand + in_band % height, bt = in_band / height;
+    const int r0 = s.start[q.expert], r1 = s.start[q.expert + 1];
+    q.b0 = bt * BN;
+    if (OP == kProdWeight) {
+        q.a0 = at * kTileRows;
+        q.a_end = int(g.outs);
+        q.r0 = r0;
+        q.r_end = r1;
+    } else {
+        q.a0 = r0 + at * kTileRows;
+        q.a_end = r1;
+        q.r0 = 0;
+        q.r_end = int(OP == kProdInput ? g.outs : g.in);
+    }
+    return q;
+}
+
+// ---------------------------------------------------------------- gathering without tensor copies
+
+// `rows` runs of 128 bytes, swizzled as a tensor copy would leave them; elements outside [row, row_end) x [c, c_end) are zero
+template <int ES> __device__ __forceinline__ void gather_box(unsigned char* dst, const unsigned char* src, size_t pitch, int rows, int row, int row_end,
+                                                             int c, int c_end, int thread)
+{
+    constexpr int PER = 16 / ES;
+    for (int i = thread; i < rows * 8; i += kGatherWarps * 32) {
+        const int r = i >> 3, chunk = i & 7;
+        const int col = c + chunk * PER;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row + r < row_end && col < c_end) {
+            const unsigned char* p = src + size_t(row + r) * pitch + size_t(col) * ES;
+            if (col + PER <= c_end && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
+                v = __ldg(reinterpret_cast<const uint4*>(p));
+            } else {
+                uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int e = 0; e < PER; ++e)
+                    if (col + e < c_end) {
+                        if (ES == 2) w[e >> 1] |= uint32_t(__ldg(reinterpret_cast<const unsigned short*>(p) + e)) << (16 * (e & 1));
+                        else w[e >> 2] |= uint32_t(__ldg(p + e)) << (8 * (e & 3));
+                    }
+                v = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+        *reinterpret_cast<uint4*>(dst + r * 128 + ((chunk ^ (r & 7)) << 4)) = v;
+    }
+}
+
+// ---------------------------------------------------------------- epilogue
+
+// eight values at a time: z -> y (and f' when it is asked for)
+template <class K> __device__ __forceinline__ void act8(float (&z)[8], float (&d)[8], bool slope)
+{
+    if (slope) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            const ActOut2 o = evaluate(K{}, Fast2{}, make_float2(z[e], z[e + 1]));
+            z[e] = o.y.x; z[e + 1] = o.y.y;
+            d[e] = o.dydx.x; d[e + 1] = o.dydx.y;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            const float2 y = evaluate_value(K{}, Fast2{}, make_float2(z[e], z[e + 1]));
+            z[e] = y.x; z[e + 1] = y.y;
+        }
+    }
+}
+
+__device__ __forceinline__ void act8(int kind, float (&z)[8], float (&d)[8], bool slope)
+{
+    switch (kind) {
+    case kGeluErf:  act8<GeluErf>(z, d, slope); break;
+    case kGeluTanh: act8<GeluTanh>(z, d, slope); break;
+    case kSwish:    act8<Swish>(z, d, slope); break;
+    case kMish:     act8<Mish>(z, d, slope); break;
+    default:
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] = 1.0f;
+    }
+}
+
+// eight neighbours of a [*, width] tensor from column c on; past the width: 0 (unaligned rows: one by one)
+template <class S> __device__ __forceinline__ void load8(const void* base, size_t row, uint32_t width, uint32_t c, bool vec, float (&v)[8])
+{
+    const typename S::elem* p = static_cast<const typename S::elem*>(base) + row * width + c;
+    if (vec) {
+        S::unpack(*reinterpret_cast<const uint4*>(p), v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = c + e < width ? S::load1(p + e) : 0.0f;
+    }
+}
+template <class S> __device__ __forceinline__ void store8(void* base, size_t row, uint32_t width, uint32_t c, bool vec, const float (&v)[8])
+{
+    typename S::elem* p = static_cast<typename S::elem*>(base) + row * width + c;
+    if (vec) {
+        *reinterpret_cast<uint4*>(p) = S::pack(v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (c + e < width) S::store1(p + e, v[e]);
+    }
+}
+
+// rows that belong to no expert: zeros
+template <class S> __device__ __forceinline__ void clear_rows(const ProdArgs& g, int first, int end, uint32_t width, int thread)
+{
+    const size_t n0 = size_t(first) * width, n1 = size_t(end) * width;
+    for (size_t i = n0 + size_t(blockIdx.x) * (kResultWarps * 32) + thread; i < n1; i += size_t(gridDim.x) * (kResultWarps * 32)) {
+        S::store1(static_cast<typename S::elem*>(g.out) + i, 0.0f);
+        if (g.slope) S::store1(static_cast<typename S::elem*>(g.slope) + i, 0.0f);
+    }
+}
+
+// ---------------------------------------------------------------- the kernel
+
+template <int OP, int BN, class S, bool kGather>
+__global__ void __launch_bounds__((kFirstResultWarp + kResultWarps + (kGather ? kGatherWarps : 0)) * 32, 1)
+product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b)
+{
+    using Kind = ProdKind<OP>;
+    using Tile = ProdTile<BN>;
+    constexpr int kStages = Tile::kStages, kStep = Kind::kStep;
+    constexpr uint32_t kTmem = 2 * BN < 32 ? 32 : 2 * BN;
+    extern __shared__ unsigned char raw[];
+    unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    ProdShared& s = *reinterpret_cast<ProdShared*>(ring + kRingBytes);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t ring_at = tc::shared_address(ring);
+    auto full = [&](int i) { return tc::shared_address(&s.full[i]); };
+    auto empty = [&](int i) { return tc::shared_address(&s.empty[i]); };
+    auto acc_full = [&](int i) { return tc::shared_address(&s.acc_full[i]); };
+    auto acc_empty = [&](int i) { return tc::shared_address(&s.acc_empty[i]); };
+    volatile uint32_t* gave_up = &s.gave_up;
+
+    if (threadIdx.x == 0) {
+        s.gave_up = 0;
+        for (int i = 0; i < kStages; ++i) {
+            tc::barrier_init(full(i), kGather ? kGatherWarps * 32 : 1);
+            tc::barrier_init(empty(i), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            tc::barrier_init(acc_full(i), 1);
+            tc::barrier_init(acc_empty(i), kResultWarps);
+        }
+        tc::barrier_init(tc::shared_address(&s.drained), 1);
+        tc::barrier_init_done();
+        if (!kGather) {
+            tc::prefetch_map(&map_a);
+            tc::prefetch_map(&map_b);
+        }
+    }
+    if (warp == 2) tc::tmem_alloc(tc::shared_address(&s.tmem), kTmem);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    // the experts' row ranges, held inside [0, rows] whatever the offsets say, and the row tiles before each
+    if (warp == 3) {
+        int before = 0, last = 0;
+        for (uint32_t e0 = 0; e0 <= g.experts; e0 += 32) {
+            const uint32_t e = e0 + lane;
+            int first = e < g.experts ? 0 : int(g.rows);
+            if (g.offsets && e <= g.experts) first = min(max(__ldg(g.offsets + e), 0), int(g.rows));
+            // ranges that run backwards are empty: an expert begins no earlier than the largest offset before it
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, first, o);
+                if (lane >= o) first = max(first, v);
+            }
+            first = max(first, last);
+            int prev = __shfl_up_sync(0xffffffffu, first, 1);
+            if (lane == 0) prev = e0 ? last : first;
+            int n = (first - prev + kTileRows - 1) / kTileRows;          // of the expert before this one
+            if (e > g.experts) n = 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xffffffffu, n, o);
+                if (lane >= o) n += v;
+            }
+            n += before;
+            if (e <= g.experts) {
+                s.start[e] = first;
+                s.tiles[e] = n;
+            }
+            before = __shfl_sync(0xffffffffu, n, 31);
+            last = __shfl_sync(0xffffffffu, first, 31);
+        }
+    }
+    tc::fence_before_sync();
+    __syncthreads();
+    tc::fence_after_sync();
+    const uint32_t tmem = s.tmem;
+    const uint32_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs;       // of a result's row
+    const int b_tiles = int((width + BN - 1) / BN);
+    const long long total = OP == kProdWeight ? (long long)g.experts * ((g.outs + kTileRows - 1) / kTileRows) * b_tiles
+                                              : (long long)s.tiles[g.experts] * b_tiles;
+
+    const bool copies = kGather ? warp >= kFirstResultWarp + kResultWarps : warp == 0;
+    if (copies) {
+        // ------------------------------------------------ operands into the ring
+        uint32_t stage = 0, phase = 0;
+        int in_flight = 0;
+        bool ok = true;
+        if (kGather || lane == 0)
+            for (long long t = blockIdx.x; t < total && ok; t += gridDim.x) {
+                const ProdTileAt q = tile_at<OP, BN>(g, s, t, b_tiles);
+                const int a_rows = min(kTileRows, q.a_end - q.a0);
+                const int boxes = (a_rows + 31) / 32;                     // of A, when it is not turned
+                for (int r = q.r0; r < q.r_end; r += kStep) {
+                    if (!(ok = tc::barrier_wait(empty(stage), phase ^ 1, gave_up))) break;
+                    const uint32_t at_a = ring_at + stage * Tile::kStage, at_b = at_a + kTileRows * kStepBytes;
+                    if (!kGather) {
+                        constexpr uint32_t kB = BN * kStepBytes;
+                        tc::barrier_expect(full(stage), kB + (Kind::kTurnA ? kTileRows * kStepBytes : uint32_t(boxes) * 32 * kStepBytes));
+                        if (Kind::kTurnA) {
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) tc::load_box(at_a + j * 64 * 128, &map_a, full(stage), q.a0 + j * 64, r);
+                        } else {
+                            for (int j = 0; j < boxes; ++j) tc::load_box(at_a + j * 32 * 128, &map_a, full(stage), r, q.a0 + j * 32);
+                        }
+                        if (OP == kProdWeight) {
+#pragma unroll
+                            for (int j = 0; j < BN / 64; ++j) tc::load_box(at_b + j * 64 * 128, &map_b, full(stage), q.b0 + j * 64, r);
+                        } else if (Kind::kTurnB) {
+#pragma unroll
+                            for (int j = 0; j < BN / 64; ++j) tc::load_box(at_b + j * 64 * 128, &map_b, full(stage), q.b0 + j * 64, r, int(q.expert));
+                        } else {
+                            tc::load_box(at_b, &map_b, full(stage), r, q.b0, int(q.expert));
+                        }
+                        if (++in_flight > kStages) in_flight = kStages;
+                    } else {
+                        constexpr int ES = Kind::kElem;
+                        unsigned char *da = ring + stage * Tile::kStage, *db = da + kTileRows * kStepBytes;
+                        const int thread = threadIdx.x - (kFirstResultWarp + kResultWarps) * 32;
+                        const unsigned char *pa = static_cast<const unsigned char*>(g.a), *pb = static_cast<const unsigned char*>(g.b);
+                        if (Kind::kTurnA) {
+                            for (int j = 0; j < 2; ++j)
+                                gather_box<ES>(da + j * 64 * 128, pa, size_t(g.outs) * ES, kStep, r, q.r_end, q.a0 + j * 64, int(g.outs), thread);
+                        } else {
+                            const uint32_t w = OP == kProdInput ? g.outs : g.in;
+                            gather_box<ES>(da, pa, size_t(w) * ES, kTileRows, q.a0, q.a_end, r, int(w), thread);
+                        }
+                        if (Kind::kTurnB) {
+                            const unsigned char* p = OP == kProdInput ? pb + size_t(q.expert) * g.outs * g.in * ES : pb;
+                            for (int j = 0; j < BN / 64; ++j)
+                                gather_box<ES>(db + j * 64 * 128, p, size_t(g.in) * ES, kStep, r, q.r_end, q.b0 + j * 64, int(g.in), thread);
+                        } else {
+                            gather_box<ES>(db, pb + size_t(q.expert) * g.outs * g.in * ES, size_t(g.in) * ES, BN, q.b0, int(g.outs), r, int(g.in), thread);
+                        }
+                        tc::writes_to_async();
+                        tc::barrier_arrive(full(stage));
+                    }
+                    if (++stage == kStages) { stage = 0; phase ^= 1; }
+                }
+            }
+        // after a wait that ran out: the copies in flight land before the CTA's memory goes away
+        if (!ok && !kGather && lane == 0)
+            for (int i = 0; i < in_flight; ++i) {
+                const uint32_t at = (stage + kStages - 1 - i) % kStages, ph = at < stage ? phase : phase ^ 1;
+                const long long t0 = clock64();
+                while (!tc::barrier_try(full(at), ph) && clock64() - t0 < kWaitDrain) {}
+            }
+    } else if (warp == 1) {
+        // ------------------------------------------------ products
+        uint32_t stage = 0, phase = 0, turn = 0, turn_phase = 0;
+        bool ok = true;
+        for (long long t = blockIdx.x; t < total && ok; t += gridDim.x) {
+            const ProdTileAt q = tile_at<OP, BN>(g, s, t, b_tiles);
+            if (!(ok = tc::barrier_wait(acc_empty(turn), turn_phase ^ 1, gave_up))) break;
+            tc::fence_after_sync();
+            // the result's last columns need a narrower product only (a multiple of 16)
+            const uint32_t n = min(uint32_t(BN), (width - q.b0 + 15) / 16 * 16);
+            const uint32_t what = tc::instruction(Kind::kBytes ? tc::kNumberS8 : IsBF16<S>::value ? tc::kNumberBF16 : tc::kNumberF16,
+                                                  Kind::kTurnA, Kind::kTurnB, kTileRows, n);
+            for (int r = q.r0; r < q.r_end; r += kStep) {
+                if (!(ok = tc::barrier_wait(full(stage), phase, gave_up))) break;
+                tc::fence_after_sync();
+                const uint32_t at_a = ring_at + stage * Tile::kStage, at_b = at_a + kTileRows * kStepBytes;
+                if (OP == kProdWeight && !kGather && r + kStep > q.r_end) {
+                    // rows past the expert's end: the next expert's, cleared in every 128-byte run of both operands
+                    const int keep = q.r_end - r;
+                    unsigned char* at = ring + stage * Tile::kStage;
+                    for (int j = 0; j < 2 + BN / 64; ++j)
+                        for (int i = keep * 8 + lane; i < kStep * 8; i += 32) *reinterpret_cast<uint4*>(at + j * 64 * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+                    tc::writes_to_async();
+                    __syncwarp();
+                }
+                if (lane == 0) {
+#pragma unroll
+                    for (int k = 0; k < kStepBytes / 32; ++k) {
+                        // 32 bytes of the reduction: along the 128-byte rows, or 16 reduction steps of 128 bytes further
+                        const uint64_t da = Kind::kTurnA ? tc::operand(at_a + k * 2048, 64 * 128, 1024) : tc::operand(at_a + k * 32, 16, 1024);
+                        const uint64_t db = Kind::kTurnB ? tc::operand(at_b + k * 2048, 64 * 128, 1024) : tc::operand(at_b + k * 32, 16, 1024);
+                        tc::product<Kind::kBytes>(tmem + turn * BN, da, db, what, r > q.r0 || k > 0);
+                    }
+                    tc::products_to(empty(stage));
+                }
+                __syncwarp();
+                if (++stage == kStages) { stage = 0; phase ^= 1; }
+            }
+            if (lane == 0 && ok) tc::products_to(acc_full(turn));
+            __syncwarp();
+            turn ^= 1;
+            if (turn == 0) turn_phase ^= 1;
+        }
+        if (!ok && lane == 0) {
+            tc::products_to(tc::shared_address(&s.drained));
+            const long long t0 = clock64();
+            while (!tc::barrier_try(tc::shared_address(&s.drained), 0) && clock64() - t0 < kWaitDrain) {}
+        }
+    } else if (warp >= kFirstResultWarp && warp < kFirstResultWarp + kResultWarps) {
+        // ------------------------------------------------ results
+        const int lanes = (warp & 3) * 32, half = (warp - kFirstResultWarp) >> 2;
+        if (OP != kProdWeight && g.offsets) {
+            clear_rows<S>(g, 0, s.start[0], width, threadIdx.x - kFirstResultWarp * 32);
+            clear_rows<S>(g, s.start[g.experts], int(g.rows), width, threadIdx.x - kFirstResultWarp * 32);
+        }
+        // whole 16-byte packets: rows start on packets and no packet crosses a row's end
+        const bool vec = width % 8 == 0 && ((reinterpret_cast<uintptr_t>(g.out) | reinterpret_cast<uintptr_t>(g.slope) | reinterpret_cast<uintptr_t>(g.bias) |
+                                             reinterpret_cast<uintptr_t>(g.prev)) & 15u) == 0;
+        uint32_t turn = 0, turn_phase = 0;
+        for (long long t = blockIdx.x; t < total; t += gridDim.x) {
+            const ProdTileAt q = tile_at<OP, BN>(g, s, t, b_tiles);
+            if (!tc::barrier_wait(acc_full(turn), turn_phase, gave_up)) break;
+            tc::fence_after_sync();
+            const int row = q.a0 + lanes + lane;
+            const bool mine = row < q.a_end, none = q.r0 >= q.r_end;
+            const size_t out_row = OP == kProdWeight ? size_t(q.expert) * g.outs + row : size_t(row);
+            const float scale = Kind::kBytes && mine ? g.a_scale[row] : 0.0f;
+            constexpr int kChunks = BN / 32;
+            for (int c = half; c < kChunks; c += 2) {
+                if (uint32_t(q.b0 + c * 32) >= width) break;
+                uint32_t v[32];
+                tc::tmem_load32(tmem + (uint32_t(lanes) << 16) + turn * BN + c * 32, v);
+                tc::tmem_load_wait();
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    const uint32_t col = q.b0 + c * 32 + p * 8;
+                    if (!mine || col >= width) continue;
+                    float z[8], d[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        z[e] = Kind::kBytes ? float(int(v[p * 8 + e])) : __uint_as_float(v[p * 8 + e]);
+                        if (none) z[e] = 0.0f;
+                    }
+                    if (Kind::kBytes) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z[e] *= scale * (col + e < width ? __ldg(g.b_scale + col + e) : 0.0f);
+                    }
+                    if (OP == kProdForward || OP == kProdBytes) {
+                        if (g.bias) {
+                            float b[8];
+                            load8<S>(g.bias, q.expert, width, col, vec, b);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) z[e] += b[e];
+                        }
+                        act8(g.act, z, d, g.slope != nullptr);
+                        if (g.slope) store8<S>(g.slope, out_row, width, col, vec, d);
+                    } else if (OP == kProdInput) {
+                        if (g.prev) {
+                            float f[8];
+                            load8<S>(g.prev, out_row, width, col, vec, f);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) z[e] *= f[e];
+                        }
+                    }
+                    store8<S>(g.out, out_row, width, col, vec, z);
+                }
+            }
+            tc::fence_before_sync();
+            __syncwarp();
+            if (lane == 0) tc::barrier_arrive(acc_empty(turn));
+            turn ^= 1;
+            if (turn == 0) turn_phase ^= 1;
+        }
+    }
+    tc::fence_before_sync();
+    __syncthreads();
+    if (warp == 2) tc::tmem_free(tmem, kTmem);
+    if (threadIdx.x == 0 && s.gave_up) atomicAdd(&g_product_faults, 1u);
+}
+
+}  // namespace nfad

@@ -1,0 +1,129 @@
+// nfad_product_launch.cuh -- tensor maps, tile widths and launches of the matrix products.
+#pragma once
+
+#include <atomic>
+#include <mutex>
+
+#include "nfad_product.cuh"
+
+namespace nfad {
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+inline cudaError_t encode_function(EncodeTiled* out)
+{
+    static std::mutex lock;
+    static EncodeTiled found = nullptr;
+    std::lock_guard<std::mutex> hold(lock);
+    if (!found) {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r);
+        if (e != cudaSuccess) return e;
+        if (r != cudaDriverEntryPointSuccess || !p) return cudaErrorNotSupported;
+        found = reinterpret_cast<EncodeTiled>(p);
+    }
+    *out = found;
+    return cudaSuccess;
+}
+
+// [d2, d1, d0] contiguous elements in boxes of b1 rows of 128 bytes; d2 == 0: two dimensions.  What lies outside reads as zero.
+inline cudaError_t make_map(CUtensorMap* m, int number, const void* p, uint64_t d0, uint64_t d1, uint64_t d2, uint32_t b1)
+{
+    EncodeTiled encode;
+    cudaError_t e = encode_function(&encode);
+    if (e != cudaSuccess) return e;
+    const uint32_t es = number == tc::kNumberS8 ? 1 : 2;
+    const CUtensorMapDataType type = number == tc::kNumberS8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                     : number == tc::kNumberBF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    const cuuint64_t dims[3] = {d0, d1, d2}, strides[2] = {d0 * es, d0 * d1 * es};
+    const cuuint32_t box[3] = {128 / es, b1, 1}, step[3] = {1, 1, 1};
+    const CUresult r = encode(m, type, d2 ? 3 : 2, const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <int OP, int BN, class S, bool kGather>
+cudaError_t launch_product_tile(const ProdArgs& g, int sms, cudaStream_t st)
+{
+    using Kind = ProdKind<OP>;
+    auto kernel = product_kernel<OP, BN, S, kGather>;
+    static std::atomic<bool> ready[64] = {};         // the shared-memory opt-in of this kernel, by device (setting it twice is harmless)
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64 || !ready[dev]) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kProdSmem);
+        if (e != cudaSuccess) return e;
+        if (dev >= 0 && dev < 64) ready[dev] = true;
+    }
+    CUtensorMap map_a = {}, map_b = {};
+    if (!kGather) {
+        const int number = Kind::kBytes ? tc::kNumberS8 : IsBF16<S>::value ? tc::kNumberBF16 : tc::kNumberF16;
+        const uint64_t pitch_a = OP == kProdInput || OP == kProdWeight ? g.outs : g.in;
+        e = make_map(&map_a, number, g.a, pitch_a, g.rows, 0, Kind::kTurnA ? 64 : 32);
+        if (e != cudaSuccess) return e;
+        e = OP == kProdWeight ? make_map(&map_b, number, g.b, g.in, g.rows, 0, 64) : make_map(&map_b, number, g.b, g.in, g.outs, g.experts, Kind::kTurnB ? 64 : BN);
+        if (e != cudaSuccess) return e;
+    }
+    const size_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs, b_tiles = (width + BN - 1) / BN;
+    const size_t a_tiles = OP == kProdWeight ? size_t(g.experts) * ((g.outs + kTileRows - 1) / kTileRows)
+                                             : (g.rows + kTileRows - 1) / kTileRows + (g.offsets ? g.experts : 0);
+    size_t grid = a_tiles * b_tiles;                 // at most this many tiles
+    if (grid > size_t(sms)) grid = sms;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(grid));
+    cfg.blockDim = dim3((kFirstResultWarp + kResultWarps + (kGather ? kGatherWarps : 0)) * 32);
+    cfg.dynamicSmemBytes = kProdSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, g, map_a, map_b);
+}
+
+// Columns of a tile: the widest of 256, 128 and 64 that still gives every SM a tile, by the tiles that the rows make when they
+// spread evenly over the experts.  A wide tile reads operands from shared memory the fewest times per product; many narrow ones keep
+// every SM's loads in flight when there are few rows and the weights' bytes are what takes the time.
+template <int OP> int product_width(const ProdArgs& g, int sms)
+{
+    const size_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs;
+    const size_t live = g.rows < g.experts ? g.rows : g.experts;
+    const size_t a_tiles = OP == kProdWeight ? size_t(g.experts) * ((g.outs + kTileRows - 1) / kTileRows)
+                                             : live * ((g.rows + live * kTileRows - 1) / (live * kTileRows));
+    for (int bn = 256; bn > 64; bn /= 2)
+        if (a_tiles * ((width + bn - 1) / bn) >= size_t(sms)) return bn;
+    return 64;
+}
+
+template <int OP, class S> cudaError_t launch_product_store(const ProdArgs& g, cudaStream_t st)
+{
+    using Kind = ProdKind<OP>;
+    DeviceInfo di;
+    cudaError_t e = device_info(&di);
+    if (e != cudaSuccess) return e;
+    const size_t reduction = OP == kProdInput ? g.outs : OP == kProdWeight ? g.rows : g.in;
+    const uintptr_t low = reinterpret_cast<uintptr_t>(g.a) | reinterpret_cast<uintptr_t>(g.b) | uintptr_t(g.in) * Kind::kElem |
+                          (Kind::kTurnB ? uintptr_t(g.outs) * Kind::kElem : 0);
+    // a tensor copy needs rows that begin on 16-byte boundaries (and something to copy)
+    if (low % 16 || reduction == 0) return launch_product_tile<OP, 128, S, true>(g, di.sm_count, st);
+    switch (product_width<OP>(g, di.sm_count)) {
+    case 256: return launch_product_tile<OP, 256, S, false>(g, di.sm_count, st);
+    case 128: return launch_product_tile<OP, 128, S, false>(g, di.sm_count, st);
+    default:  return launch_product_tile<OP, 64, S, false>(g, di.sm_count, st);
+    }
+}
+
+template <int OP> cudaError_t launch_product_op(int dtype, const ProdArgs& g, cudaStream_t st)
+{
+    if (dtype == kBF16) return launch_product_store<OP, StoreBF16>(g, st);
+    if (dtype == kF16) return launch_product_store<OP, StoreF16>(g, st);
+    return cudaErrorInvalidValue;
+}
+
+inline cudaError_t product_faults_here(unsigned* n) { return cudaMemcpyFromSymbol(n, g_product_faults, sizeof *n); }
+
+}  // namespace nfad

@@ -133,3 +133,47 @@ def block_norm_backward(p, dh, gs, u, s, stats):
         da, dam = through(da * g, dam * g.abs(), xhat, xm, ru, p["post"])
     out["u"] = (da, dam)
     return out
+
+
+# ---------------------------------------------------------------- activations
+
+def act(z, kind):
+    """f and f' in 64 bits, the derivative from the formulas of the gates."""
+    z = z.double()
+    if kind is None:
+        return z, torch.ones_like(z)
+    if kind == "gelu_erf":
+        h, dh = 0.5 * torch.special.erfc(-z / np.sqrt(2.0)), torch.exp(-z * z / 2) / np.sqrt(2 * np.pi)
+    elif kind == "gelu_tanh":
+        v = 2 * np.sqrt(2 / np.pi) * (z + 0.044715 * z ** 3)
+        h = torch.sigmoid(v)
+        dh = h * torch.sigmoid(-v) * 2 * np.sqrt(2 / np.pi) * (1 + 3 * 0.044715 * z * z)
+    elif kind == "swish":
+        h = torch.sigmoid(z)
+        dh = h * torch.sigmoid(-z)
+    else:
+        h = torch.tanh(torch.nn.functional.softplus(z))
+        dh = (1 - h) * (1 + h) * torch.sigmoid(z)
+    return z * h, h + z * dh
+
+
+#: largest |f'| and |f''| of the four activations are below these
+SLOPE, CURVATURE = 1.2, 1.1
+
+
+def check_act(y, d, z, z_err, kind, what):
+    """y = f(z), d = f'(z) for a z that the kernel forms with an error of at most z_err.  The 16-bit chains give y within one
+    spacing (not half of one) and f' within one spacing plus a sixteenth of the spacing of its terms, |h| + |z h'| < 1.25."""
+    want, slope = act(z, kind)
+    if kind is None:
+        check(y, want, z_err, what + " y")
+        return
+    check(y, want, SLOPE * z_err + half_ulp(want, y.dtype), what + " y")
+    if d is not None:
+        check(d, slope, CURVATURE * z_err + half_ulp(slope, d.dtype) + half_ulp(torch.full_like(slope, 1.25), d.dtype) / 8, what + " f'")
+
+
+def dot_error(mag, terms):
+    """Of a tensor-core sum of `terms` products whose magnitudes add up to mag: each step of 16 terms adds to the fp32
+    accumulator with at most 2^-23 (truncation included) of what has been added so far."""
+    return 2.0 ** -23 * (terms / 16 + 4) * mag

@@ -46,18 +46,23 @@ template <int OP> struct ProdKind {
 template <class S> struct IsBF16 { static constexpr bool value = false; };
 template <> struct IsBF16<StoreBF16> { static constexpr bool value = true; };
 
-template <int BN> struct ProdTile {
-    static constexpr int kStage = (kTileRows + BN) * kStepBytes;
+// kPair: two CTAs share a tile of twice the rows; each holds its own 128 rows of A and half of B's columns
+template <int BN, bool kPair> struct ProdTile {
+    static constexpr int kRows = kTileRows * (kPair ? 2 : 1);
+    static constexpr int kOwnColumns = kPair ? BN / 2 : BN;
+    static constexpr int kBoxRows = BN > 64 ? 128 : 32;              // rows of A that one copy brings
+    static constexpr int kStage = (kTileRows + kOwnColumns) * kStepBytes;
     static constexpr int kStages = kRingBytes / kStage < kMaxStages ? kRingBytes / kStage : kMaxStages;
 };
 
 struct ProdShared {
-    uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drained;
+    uint64_t full[kMaxStages], empty[kMaxStages], landed[kMaxStages], acc_full[2], acc_empty[2], drained;
     uint32_t tmem, gave_up;
     int start[kMaxExperts + 1];                     // first row of each expert
     int tiles[kMaxExperts + 1];                     // row tiles before each expert
 };
-constexpr int kProdSmem = 1024 + kRingBytes + int(sizeof(ProdShared));
+constexpr int kStageBytes = 32 * 64;              // a result warp's 32 rows of 32 16-bit results
+constexpr int kProdSmem = 1024 + kRingBytes + kResultWarps * kStageBytes + int(sizeof(ProdShared));
 
 // CTAs one of whose waits ran out; one counter for each translation unit that includes this file
 static __device__ unsigned g_product_faults;
@@ -72,13 +77,14 @@ struct ProdTileAt {
 // Tile t.  Within an expert, bands of kBand tiles along A's dimension, B's tile changing slowest inside a band: the CTAs that run
 // at one time then share a few tiles of each operand through L2.
 constexpr int kBand = 16;
-template <int OP, int BN> __device__ __forceinline__ ProdTileAt tile_at(const ProdArgs& g, const ProdShared& s, long long t, int b_tiles)
+template <int OP, int BN, bool kPair> __device__ __forceinline__ ProdTileAt tile_at(const ProdArgs& g, const ProdShared& s, long long t, int b_tiles)
 {
+    constexpr int kRows = ProdTile<BN, kPair>::kRows;
     ProdTileAt q;
     int a_tiles;
     long long local;
     if (OP == kProdWeight) {
-        a_tiles = int((g.outs + kTileRows - 1) / kTileRows);
+        a_tiles = int((g.outs + kRows - 1) / kRows);
         const long long per = (long long)a_tiles * b_tiles;
         q.expert = uint32_t(t / per);
         local = t - q.expert * per;
@@ -100,12 +106,12 @@ template <int OP, int BN> __device__ __forceinline__ ProdTileAt tile_at(const Pr
     const int r0 = s.start[q.expert], r1 = s.start[q.expert + 1];
     q.b0 = bt * BN;
     if (OP == kProdWeight) {
-        q.a0 = at * kTileRows;
+        q.a0 = at * kRows;
         q.a_end = int(g.outs);
         q.r0 = r0;
         q.r_end = r1;
     } else {
-        q.a0 = r0 + at * kTileRows;
+        q.a0 = r0 + at * kRows;
         q.a_end = r1;
         q.r0 = 0;
         q.r_end = int(OP == kProdInput ? g.outs : g.in);
@@ -181,24 +187,65 @@ __device__ __forceinline__ void act8(int kind, float (&z)[8], float (&d)[8], boo
 template <class S> __device__ __forceinline__ void load8(const void* base, size_t row, uint32_t width, uint32_t c, bool vec, float (&v)[8])
 {
     const typename S::elem* p = static_cast<const typename S::elem*>(base) + row * width + c;
-    if (vec) {
+    if (vec && c < width) {
         S::unpack(*reinterpret_cast<const uint4*>(p), v);
     } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = c + e < width ? S::load1(p + e) : 0.0f;
     }
 }
-template <class S> __device__ __forceinline__ void store8(void* base, size_t row, uint32_t width, uint32_t c, bool vec, const float (&v)[8])
+template <class S> __device__ __forceinline__ void store8(void* base, size_t row, uint32_t width, uint32_t c, const float (&v)[8])
 {
     typename S::elem* p = static_cast<typename S::elem*>(base) + row * width + c;
-    if (vec) {
-        *reinterpret_cast<uint4*>(p) = S::pack(v);
-    } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (c + e < width) S::store1(p + e, v[e]);
-    }
+    for (int e = 0; e < 8; ++e)
+        if (c + e < width) S::store1(p + e, v[e]);
 }
+
+// A lane holds a row's 32 results (four packets); memory wants whole lines.  Packets go through the warp's 2 KB of shared
+// memory, four to a row, their places rotated so that neither side meets bank conflicts: a lane writes its row's and reads
+// back packet lane % 4 of rows lane / 4 + 0, 8, 16, 24, so that each access covers 64 bytes of eight rows (written straight from
+// the rows, each touches 32 lines and the stores alone took 5 us a tile).
+__device__ __forceinline__ int staged_at(int row, int packet) { return row * 4 + (packet ^ (row >> 1 & 3)); }
+struct RowPackets {
+    size_t row0, row_end;                           // of the warp's first row; rows from row_end on are not touched
+    uint32_t width, col;                            // of the first packet
+    int lane;
+    uint4* stage;
+    template <class F> __device__ __forceinline__ void each(F f) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = i * 8 + (lane >> 2), c = lane & 3;
+            f(i, staged_at(r, c), row0 + r < row_end && col + c * 8 < width, (row0 + r) * width + col + c * 8);
+        }
+    }
+    template <class S> __device__ __forceinline__ void store(void* base, const uint4 (&v)[4]) const
+    {
+#pragma unroll
+        for (int p = 0; p < 4; ++p) stage[staged_at(lane, p)] = v[p];
+        __syncwarp();
+        each([&](int, int at, bool on, size_t i) {
+            if (on) *reinterpret_cast<uint4*>(static_cast<typename S::elem*>(base) + i) = stage[at];
+        });
+        __syncwarp();
+    }
+    template <class S> __device__ __forceinline__ void fetch(const void* base, uint4 (&v)[4]) const
+    {
+        each([&](int k, int, bool on, size_t i) {
+            v[k] = on ? *reinterpret_cast<const uint4*>(static_cast<const typename S::elem*>(base) + i) : make_uint4(0, 0, 0, 0);
+        });
+    }
+    // what fetch brought, turned into this lane's own row
+    __device__ __forceinline__ void to_rows(uint4 (&v)[4]) const
+    {
+        each([&](int k, int at, bool, size_t) { stage[at] = v[k]; });
+        __syncwarp();
+#pragma unroll
+        for (int p = 0; p < 4; ++p) v[p] = stage[staged_at(lane, p)];
+        __syncwarp();
+    }
+};
 
 // rows that belong to no expert: zeros
 template <class S> __device__ __forceinline__ void clear_rows(const ProdArgs& g, int first, int end, uint32_t width, int thread)
@@ -212,34 +259,40 @@ template <class S> __device__ __forceinline__ void clear_rows(const ProdArgs& g,
 
 // ---------------------------------------------------------------- the kernel
 
-template <int OP, int BN, class S, bool kGather>
+template <int OP, int BN, class S, bool kGather, bool kPair>
 __global__ void __launch_bounds__((kFirstResultWarp + kResultWarps + (kGather ? kGatherWarps : 0)) * 32, 1)
 product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b)
 {
     using Kind = ProdKind<OP>;
-    using Tile = ProdTile<BN>;
-    constexpr int kStages = Tile::kStages, kStep = Kind::kStep;
-    constexpr uint32_t kTmem = 2 * BN < 32 ? 32 : 2 * BN;
+    using Tile = ProdTile<BN, kPair>;
+    constexpr int kStages = Tile::kStages, kStep = Kind::kStep, kOwn = Tile::kOwnColumns;
+    constexpr uint32_t kTmem = 2 * BN;
+    constexpr int kBoxRows = Tile::kBoxRows;
     extern __shared__ unsigned char raw[];
     unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
-    ProdShared& s = *reinterpret_cast<ProdShared*>(ring + kRingBytes);
+    ProdShared& s = *reinterpret_cast<ProdShared*>(ring + kRingBytes + kResultWarps * kStageBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = kPair ? tc::rank_in_pair() : 0;
+    const long long unit = kPair ? blockIdx.x >> 1 : blockIdx.x, units = kPair ? gridDim.x >> 1 : gridDim.x;
     const uint32_t ring_at = tc::shared_address(ring);
     auto full = [&](int i) { return tc::shared_address(&s.full[i]); };
     auto empty = [&](int i) { return tc::shared_address(&s.empty[i]); };
     auto acc_full = [&](int i) { return tc::shared_address(&s.acc_full[i]); };
     auto acc_empty = [&](int i) { return tc::shared_address(&s.acc_empty[i]); };
+    auto landed = [&](int i) { return tc::shared_address(&s.landed[i]); };
     volatile uint32_t* gave_up = &s.gave_up;
 
     if (threadIdx.x == 0) {
         s.gave_up = 0;
         for (int i = 0; i < kStages; ++i) {
-            tc::barrier_init(full(i), kGather ? kGatherWarps * 32 : 1);
+            // per stage: both copying warps of each CTA (or every gathering thread); the products' one commit
+            tc::barrier_init(full(i), kGather ? kGatherWarps * 32 : kPair ? 4 : 2);
             tc::barrier_init(empty(i), 1);
+            tc::barrier_init(landed(i), 2);
         }
         for (int i = 0; i < 2; ++i) {
             tc::barrier_init(acc_full(i), 1);
-            tc::barrier_init(acc_empty(i), kResultWarps);
+            tc::barrier_init(acc_empty(i), kResultWarps * (kPair ? 2 : 1));
         }
         tc::barrier_init(tc::shared_address(&s.drained), 1);
         tc::barrier_init_done();
@@ -248,7 +301,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
             tc::prefetch_map(&map_b);
         }
     }
-    if (warp == 2) tc::tmem_alloc(tc::shared_address(&s.tmem), kTmem);
+    if (warp == 2) tc::tmem_alloc<kPair>(tc::shared_address(&s.tmem), kTmem);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
@@ -268,7 +321,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
             first = max(first, last);
             int prev = __shfl_up_sync(0xffffffffu, first, 1);
             if (lane == 0) prev = e0 ? last : first;
-            int n = (first - prev + kTileRows - 1) / kTileRows;          // of the expert before this one
+            int n = (first - prev + Tile::kRows - 1) / Tile::kRows;      // of the expert before this one
             if (e > g.experts) n = 0;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -286,125 +339,177 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
     }
     tc::fence_before_sync();
     __syncthreads();
+    if (kPair) tc::pair_sync();                      // the other CTA's barriers exist
     tc::fence_after_sync();
     const uint32_t tmem = s.tmem;
     const uint32_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs;       // of a result's row
     const int b_tiles = int((width + BN - 1) / BN);
-    const long long total = OP == kProdWeight ? (long long)g.experts * ((g.outs + kTileRows - 1) / kTileRows) * b_tiles
+    const long long total = OP == kProdWeight ? (long long)g.experts * ((g.outs + Tile::kRows - 1) / Tile::kRows) * b_tiles
                                               : (long long)s.tiles[g.experts] * b_tiles;
+    // the last tile along a result's row is a narrower product (a multiple of 16 columns, of 32 for a pair, which halves it)
+    auto columns = [&](const ProdTileAt& q) {
+        const uint32_t unit_n = kPair ? 32 : 16, left = (width - q.b0 + unit_n - 1) / unit_n * unit_n;
+        return left < uint32_t(BN) ? left : uint32_t(BN);
+    };
+    // a step of the weight gradient that holds rows past the expert's end (gathered operands come without them)
+    auto ragged = [&](const ProdTileAt& q, int r) { return OP == kProdWeight && !kGather && r + kStep > q.r_end; };
+    // clears those rows in every 128-byte run of this CTA's two operands
+    auto clear_ragged = [&](const ProdTileAt& q, int r, uint32_t stage) {
+        const int keep = q.r_end - r;
+        unsigned char* at = ring + stage * Tile::kStage;
+        for (int j = 0; j < 2 + kOwn / 64; ++j)
+            for (int i = keep * 8 + lane; i < kStep * 8; i += 32) *reinterpret_cast<uint4*>(at + j * 64 * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+        tc::writes_to_async();
+        if (kPair) tc::pair_fence();
+        __syncwarp();
+    };
 
-    const bool copies = kGather ? warp >= kFirstResultWarp + kResultWarps : warp == 0;
-    if (copies) {
-        // ------------------------------------------------ operands into the ring
+    if (!kGather && (warp == 0 || warp == 3)) {
+        // ------------------------------------------------ tensor copies into the ring: one thread for A, one for B (issuing a
+        // copy takes a thread longer than a pair's product step of 512 cycles leaves for four of them)
         uint32_t stage = 0, phase = 0;
-        int in_flight = 0;
-        bool ok = true;
-        if (kGather || lane == 0)
-            for (long long t = blockIdx.x; t < total && ok; t += gridDim.x) {
-                const ProdTileAt q = tile_at<OP, BN>(g, s, t, b_tiles);
-                const int a_rows = min(kTileRows, q.a_end - q.a0);
-                const int boxes = (a_rows + 31) / 32;                     // of A, when it is not turned
+        const bool for_a = warp == 0;
+        if (lane == 0)
+            for (long long t = unit; t < total; t += units) {
+                const ProdTileAt q = tile_at<OP, BN, kPair>(g, s, t, b_tiles);
+                const int a0 = q.a0 + int(rank) * kTileRows, b0 = q.b0 + (rank ? int(columns(q)) / 2 : 0);
+                const int a_rows = max(0, min(kTileRows, q.a_end - a0));
+                const int boxes = (a_rows + kBoxRows - 1) / kBoxRows;     // of A, when it is not turned
+                const uint32_t bytes = !for_a ? kOwn * kStepBytes : Kind::kTurnA ? kTileRows * kStepBytes : uint32_t(boxes) * kBoxRows * kStepBytes;
+                bool ok = true;
                 for (int r = q.r0; r < q.r_end; r += kStep) {
                     if (!(ok = tc::barrier_wait(empty(stage), phase ^ 1, gave_up))) break;
                     const uint32_t at_a = ring_at + stage * Tile::kStage, at_b = at_a + kTileRows * kStepBytes;
-                    if (!kGather) {
-                        constexpr uint32_t kB = BN * kStepBytes;
-                        tc::barrier_expect(full(stage), kB + (Kind::kTurnA ? kTileRows * kStepBytes : uint32_t(boxes) * 32 * kStepBytes));
-                        if (Kind::kTurnA) {
-#pragma unroll
-                            for (int j = 0; j < 2; ++j) tc::load_box(at_a + j * 64 * 128, &map_a, full(stage), q.a0 + j * 64, r);
-                        } else {
-                            for (int j = 0; j < boxes; ++j) tc::load_box(at_a + j * 32 * 128, &map_a, full(stage), r, q.a0 + j * 32);
-                        }
-                        if (OP == kProdWeight) {
-#pragma unroll
-                            for (int j = 0; j < BN / 64; ++j) tc::load_box(at_b + j * 64 * 128, &map_b, full(stage), q.b0 + j * 64, r);
-                        } else if (Kind::kTurnB) {
-#pragma unroll
-                            for (int j = 0; j < BN / 64; ++j) tc::load_box(at_b + j * 64 * 128, &map_b, full(stage), q.b0 + j * 64, r, int(q.expert));
-                        } else {
-                            tc::load_box(at_b, &map_b, full(stage), r, q.b0, int(q.expert));
-                        }
-                        if (++in_flight > kStages) in_flight = kStages;
+                    // a ragged step is announced by the warp that clears it, once it has landed
+                    uint32_t bar;
+                    if (ragged(q, r)) {
+                        bar = landed(stage);
+                        tc::barrier_expect(bar, bytes);
+                    } else if (kPair) {
+                        bar = tc::first_of_pair(full(stage));
+                        tc::barrier_expect_first(bar, bytes);
                     } else {
-                        constexpr int ES = Kind::kElem;
-                        unsigned char *da = ring + stage * Tile::kStage, *db = da + kTileRows * kStepBytes;
-                        const int thread = threadIdx.x - (kFirstResultWarp + kResultWarps) * 32;
-                        const unsigned char *pa = static_cast<const unsigned char*>(g.a), *pb = static_cast<const unsigned char*>(g.b);
+                        bar = full(stage);
+                        tc::barrier_expect(bar, bytes);
+                    }
+                    if (for_a) {
                         if (Kind::kTurnA) {
-                            for (int j = 0; j < 2; ++j)
-                                gather_box<ES>(da + j * 64 * 128, pa, size_t(g.outs) * ES, kStep, r, q.r_end, q.a0 + j * 64, int(g.outs), thread);
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) tc::load_box<kPair>(at_a + j * 64 * 128, &map_a, bar, a0 + j * 64, r);
                         } else {
-                            const uint32_t w = OP == kProdInput ? g.outs : g.in;
-                            gather_box<ES>(da, pa, size_t(w) * ES, kTileRows, q.a0, q.a_end, r, int(w), thread);
+                            for (int j = 0; j < boxes; ++j) tc::load_box<kPair>(at_a + j * kBoxRows * 128, &map_a, bar, r, a0 + j * kBoxRows);
                         }
-                        if (Kind::kTurnB) {
-                            const unsigned char* p = OP == kProdInput ? pb + size_t(q.expert) * g.outs * g.in * ES : pb;
-                            for (int j = 0; j < BN / 64; ++j)
-                                gather_box<ES>(db + j * 64 * 128, p, size_t(g.in) * ES, kStep, r, q.r_end, q.b0 + j * 64, int(g.in), thread);
-                        } else {
-                            gather_box<ES>(db, pb + size_t(q.expert) * g.outs * g.in * ES, size_t(g.in) * ES, BN, q.b0, int(g.outs), r, int(g.in), thread);
-                        }
-                        tc::writes_to_async();
-                        tc::barrier_arrive(full(stage));
+                    } else if (OP == kProdWeight) {
+#pragma unroll
+                        for (int j = 0; j < kOwn / 64; ++j) tc::load_box<kPair>(at_b + j * 64 * 128, &map_b, bar, b0 + j * 64, r);
+                    } else if (Kind::kTurnB) {
+#pragma unroll
+                        for (int j = 0; j < kOwn / 64; ++j) tc::load_box<kPair>(at_b + j * 64 * 128, &map_b, bar, b0 + j * 64, r, int(q.expert));
+                    } else {
+                        tc::load_box<kPair>(at_b, &map_b, bar, r, b0, int(q.expert));
                     }
                     if (++stage == kStages) { stage = 0; phase ^= 1; }
                 }
+                if (!ok) {
+                    // a wait ran out: the copies in flight land before the CTA's memory goes away
+                    const long long t0 = clock64();
+                    while (clock64() - t0 < kWaitDrain) {}
+                    break;
+                }
             }
-        // after a wait that ran out: the copies in flight land before the CTA's memory goes away
-        if (!ok && !kGather && lane == 0)
-            for (int i = 0; i < in_flight; ++i) {
-                const uint32_t at = (stage + kStages - 1 - i) % kStages, ph = at < stage ? phase : phase ^ 1;
-                const long long t0 = clock64();
-                while (!tc::barrier_try(full(at), ph) && clock64() - t0 < kWaitDrain) {}
-            }
-    } else if (warp == 1) {
-        // ------------------------------------------------ products
-        uint32_t stage = 0, phase = 0, turn = 0, turn_phase = 0;
+    } else if (kGather && warp >= kFirstResultWarp + kResultWarps) {
+        // ------------------------------------------------ the same by plain loads
+        uint32_t stage = 0, phase = 0;
         bool ok = true;
-        for (long long t = blockIdx.x; t < total && ok; t += gridDim.x) {
-            const ProdTileAt q = tile_at<OP, BN>(g, s, t, b_tiles);
+        for (long long t = unit; t < total && ok; t += units) {
+            const ProdTileAt q = tile_at<OP, BN, kPair>(g, s, t, b_tiles);
+            for (int r = q.r0; r < q.r_end; r += kStep) {
+                if (!(ok = tc::barrier_wait(empty(stage), phase ^ 1, gave_up))) break;
+                constexpr int ES = Kind::kElem;
+                unsigned char *da = ring + stage * Tile::kStage, *db = da + kTileRows * kStepBytes;
+                const int thread = threadIdx.x - (kFirstResultWarp + kResultWarps) * 32;
+                const unsigned char *pa = static_cast<const unsigned char*>(g.a), *pb = static_cast<const unsigned char*>(g.b);
+                if (Kind::kTurnA) {
+                    for (int j = 0; j < 2; ++j)
+                        gather_box<ES>(da + j * 64 * 128, pa, size_t(g.outs) * ES, kStep, r, q.r_end, q.a0 + j * 64, int(g.outs), thread);
+                } else {
+                    const uint32_t w = OP == kProdInput ? g.outs : g.in;
+                    gather_box<ES>(da, pa, size_t(w) * ES, kTileRows, q.a0, q.a_end, r, int(w), thread);
+                }
+                if (Kind::kTurnB) {
+                    const unsigned char* p = OP == kProdInput ? pb + size_t(q.expert) * g.outs * g.in * ES : pb;
+                    for (int j = 0; j < BN / 64; ++j)
+                        gather_box<ES>(db + j * 64 * 128, p, size_t(g.in) * ES, kStep, r, q.r_end, q.b0 + j * 64, int(g.in), thread);
+                } else {
+                    gather_box<ES>(db, pb + size_t(q.expert) * g.outs * g.in * ES, size_t(g.in) * ES, BN, q.b0, int(g.outs), r, int(g.in), thread);
+                }
+                tc::writes_to_async();
+                tc::barrier_arrive(full(stage));
+                if (++stage == kStages) { stage = 0; phase ^= 1; }
+            }
+        }
+    } else if (warp == 1 && rank == 0) {
+        // ------------------------------------------------ products
+        uint32_t stage = 0, phase = 0, turn = 0, turn_phase = 0, landed_phases = 0;              // landed_phases: a bit for each stage
+        bool ok = true;
+        for (long long t = unit; t < total && ok; t += units) {
+            const ProdTileAt q = tile_at<OP, BN, kPair>(g, s, t, b_tiles);
             if (!(ok = tc::barrier_wait(acc_empty(turn), turn_phase ^ 1, gave_up))) break;
             tc::fence_after_sync();
-            // the result's last columns need a narrower product only (a multiple of 16)
-            const uint32_t n = min(uint32_t(BN), (width - q.b0 + 15) / 16 * 16);
-            const uint32_t what = tc::instruction(Kind::kBytes ? tc::kNumberS8 : IsBF16<S>::value ? tc::kNumberBF16 : tc::kNumberF16,
-                                                  Kind::kTurnA, Kind::kTurnB, kTileRows, n);
+            const uint32_t what = tc::instruction(Kind::kBytes ? tc::kNumberS8 : IsBF16<S>::value ? tc::kNumberBF16 : tc::kNumberF16, Kind::kTurnA, Kind::kTurnB,
+                                                  Tile::kRows, columns(q));
             for (int r = q.r0; r < q.r_end; r += kStep) {
+                if (ragged(q, r)) {
+                    if (!(ok = tc::barrier_wait(landed(stage), landed_phases >> stage & 1, gave_up))) break;
+                    landed_phases ^= 1u << stage;
+                    clear_ragged(q, r, stage);
+                    if (lane < 2) tc::barrier_arrive(full(stage));       // in the copying threads' place
+                }
                 if (!(ok = tc::barrier_wait(full(stage), phase, gave_up))) break;
+                if (kPair && ragged(q, r)) {
+                    tc::pair_fence();
+                    tc::writes_to_async();
+                }
                 tc::fence_after_sync();
                 const uint32_t at_a = ring_at + stage * Tile::kStage, at_b = at_a + kTileRows * kStepBytes;
-                if (OP == kProdWeight && !kGather && r + kStep > q.r_end) {
-                    // rows past the expert's end: the next expert's, cleared in every 128-byte run of both operands
-                    const int keep = q.r_end - r;
-                    unsigned char* at = ring + stage * Tile::kStage;
-                    for (int j = 0; j < 2 + BN / 64; ++j)
-                        for (int i = keep * 8 + lane; i < kStep * 8; i += 32) *reinterpret_cast<uint4*>(at + j * 64 * 128 + i * 16) = make_uint4(0, 0, 0, 0);
-                    tc::writes_to_async();
-                    __syncwarp();
-                }
                 if (lane == 0) {
 #pragma unroll
                     for (int k = 0; k < kStepBytes / 32; ++k) {
                         // 32 bytes of the reduction: along the 128-byte rows, or 16 reduction steps of 128 bytes further
                         const uint64_t da = Kind::kTurnA ? tc::operand(at_a + k * 2048, 64 * 128, 1024) : tc::operand(at_a + k * 32, 16, 1024);
                         const uint64_t db = Kind::kTurnB ? tc::operand(at_b + k * 2048, 64 * 128, 1024) : tc::operand(at_b + k * 32, 16, 1024);
-                        tc::product<Kind::kBytes>(tmem + turn * BN, da, db, what, r > q.r0 || k > 0);
+                        tc::product<Kind::kBytes, kPair>(tmem + turn * BN, da, db, what, r > q.r0 || k > 0);
                     }
-                    tc::products_to(empty(stage));
+                    tc::products_to<kPair>(empty(stage));
                 }
                 __syncwarp();
                 if (++stage == kStages) { stage = 0; phase ^= 1; }
             }
-            if (lane == 0 && ok) tc::products_to(acc_full(turn));
+            if (lane == 0 && ok) tc::products_to<kPair>(acc_full(turn));
             __syncwarp();
             turn ^= 1;
             if (turn == 0) turn_phase ^= 1;
         }
         if (!ok && lane == 0) {
-            tc::products_to(tc::shared_address(&s.drained));
+            tc::products_to<kPair>(tc::shared_address(&s.drained));
             const long long t0 = clock64();
             while (!tc::barrier_try(tc::shared_address(&s.drained), 0) && clock64() - t0 < kWaitDrain) {}
+        }
+    } else if (warp == 1 && OP == kProdWeight) {
+        // ------------------------------------------------ the second CTA's ragged steps
+        uint32_t stage = 0, landed_phases = 0;
+        bool ok = true;
+        for (long long t = unit; t < total && ok; t += units) {
+            const ProdTileAt q = tile_at<OP, BN, kPair>(g, s, t, b_tiles);
+            for (int r = q.r0; r < q.r_end; r += kStep) {
+                if (ragged(q, r)) {
+                    if (!(ok = tc::barrier_wait(landed(stage), landed_phases >> stage & 1, gave_up))) break;
+                    landed_phases ^= 1u << stage;
+                    clear_ragged(q, r, stage);
+                    if (lane < 2) tc::barrier_arrive_first(tc::first_of_pair(full(stage)));
+                }
+                if (++stage == kStages) stage = 0;
+            }
         }
     } else if (warp >= kFirstResultWarp && warp < kFirstResultWarp + kResultWarps) {
         // ------------------------------------------------ results
@@ -416,25 +521,36 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
         // whole 16-byte packets: rows start on packets and no packet crosses a row's end
         const bool vec = width % 8 == 0 && ((reinterpret_cast<uintptr_t>(g.out) | reinterpret_cast<uintptr_t>(g.slope) | reinterpret_cast<uintptr_t>(g.bias) |
                                              reinterpret_cast<uintptr_t>(g.prev)) & 15u) == 0;
+        const bool vec_scale = Kind::kBytes && width % 8 == 0 && (reinterpret_cast<uintptr_t>(g.b_scale) & 15u) == 0;
         uint32_t turn = 0, turn_phase = 0;
-        for (long long t = blockIdx.x; t < total; t += gridDim.x) {
-            const ProdTileAt q = tile_at<OP, BN>(g, s, t, b_tiles);
+        for (long long t = unit; t < total; t += units) {
+            const ProdTileAt q = tile_at<OP, BN, kPair>(g, s, t, b_tiles);
             if (!tc::barrier_wait(acc_full(turn), turn_phase, gave_up)) break;
             tc::fence_after_sync();
-            const int row = q.a0 + lanes + lane;
+            const int row = q.a0 + int(rank) * kTileRows + lanes + lane;
             const bool mine = row < q.a_end, none = q.r0 >= q.r_end;
             const size_t out_row = OP == kProdWeight ? size_t(q.expert) * g.outs + row : size_t(row);
             const float scale = Kind::kBytes && mine ? g.a_scale[row] : 0.0f;
+            RowPackets rows;
+            rows.row0 = out_row - lane;
+            rows.row_end = rows.row0 + max(0, q.a_end - (row - lane));
+            rows.width = width;
+            rows.lane = lane;
+            rows.stage = reinterpret_cast<uint4*>(ring + kRingBytes + (warp - kFirstResultWarp) * kStageBytes);
             constexpr int kChunks = BN / 32;
             for (int c = half; c < kChunks; c += 2) {
-                if (uint32_t(q.b0 + c * 32) >= width) break;
+                const uint32_t col0 = q.b0 + c * 32;
+                if (col0 >= width || rows.row0 >= rows.row_end) break;     // past the result's columns; a warp without rows
+                rows.col = col0;
                 uint32_t v[32];
                 tc::tmem_load32(tmem + (uint32_t(lanes) << 16) + turn * BN + c * 32, v);
+                uint4 y[4], slope[4];
+                if (OP == kProdInput && g.prev && vec) rows.template fetch<S>(g.prev, slope);
                 tc::tmem_load_wait();
+                if (OP == kProdInput && g.prev && vec) rows.to_rows(slope);
 #pragma unroll
                 for (int p = 0; p < 4; ++p) {
-                    const uint32_t col = q.b0 + c * 32 + p * 8;
-                    if (!mine || col >= width) continue;
+                    const uint32_t col = col0 + p * 8;
                     float z[8], d[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -442,8 +558,16 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
                         if (none) z[e] = 0.0f;
                     }
                     if (Kind::kBytes) {
+                        float w[8];
+                        if (vec_scale && col < width) {
+                            const float4 lo = __ldg(reinterpret_cast<const float4*>(g.b_scale + col)), hi = __ldg(reinterpret_cast<const float4*>(g.b_scale + col) + 1);
+                            w[0] = lo.x; w[1] = lo.y; w[2] = lo.z; w[3] = lo.w; w[4] = hi.x; w[5] = hi.y; w[6] = hi.z; w[7] = hi.w;
+                        } else {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) z[e] *= scale * (col + e < width ? __ldg(g.b_scale + col + e) : 0.0f);
+                            for (int e = 0; e < 8; ++e) w[e] = col + e < width ? __ldg(g.b_scale + col + e) : 0.0f;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z[e] *= scale * w[e];
                     }
                     if (OP == kProdForward || OP == kProdBytes) {
                         if (g.bias) {
@@ -453,28 +577,41 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
                             for (int e = 0; e < 8; ++e) z[e] += b[e];
                         }
                         act8(g.act, z, d, g.slope != nullptr);
-                        if (g.slope) store8<S>(g.slope, out_row, width, col, vec, d);
+                        if (g.slope && vec) slope[p] = S::pack(d);
+                        if (g.slope && !vec && mine) store8<S>(g.slope, out_row, width, col, d);
                     } else if (OP == kProdInput) {
                         if (g.prev) {
                             float f[8];
-                            load8<S>(g.prev, out_row, width, col, vec, f);
+                            if (vec) S::unpack(slope[p], f);
+                            else if (mine) load8<S>(g.prev, out_row, width, col, false, f);
 #pragma unroll
                             for (int e = 0; e < 8; ++e) z[e] *= f[e];
                         }
                     }
-                    store8<S>(g.out, out_row, width, col, vec, z);
+                    if (vec) y[p] = S::pack(z);
+                    else if (mine) store8<S>(g.out, out_row, width, col, z);
+                }
+                if (vec) {
+                    rows.template store<S>(g.out, y);
+                    if ((OP == kProdForward) && g.slope) rows.template store<S>(g.slope, slope);
                 }
             }
             tc::fence_before_sync();
             __syncwarp();
-            if (lane == 0) tc::barrier_arrive(acc_empty(turn));
+            if (lane == 0) {
+                if (kPair) tc::barrier_arrive_first(tc::first_of_pair(acc_empty(turn)));
+                else tc::barrier_arrive(acc_empty(turn));
+            }
             turn ^= 1;
             if (turn == 0) turn_phase ^= 1;
         }
     }
+    __syncwarp();
     tc::fence_before_sync();
     __syncthreads();
-    if (warp == 2) tc::tmem_free(tmem, kTmem);
+    if (kPair) tc::pair_sync();                      // nothing of the pair arrives on this CTA's barriers or reads its memory any more
+    tc::fence_after_sync();
+    if (warp == 2) tc::tmem_free<kPair>(tmem, kTmem);
     if (threadIdx.x == 0 && s.gave_up) atomicAdd(&g_product_faults, 1u);
 }
 

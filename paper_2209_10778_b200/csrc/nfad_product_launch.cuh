@@ -44,11 +44,12 @@ inline cudaError_t make_map(CUtensorMap* m, int number, const void* p, uint64_t 
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <int OP, int BN, class S, bool kGather>
+template <int OP, int BN, class S, bool kGather, bool kPair = false>
 cudaError_t launch_product_tile(const ProdArgs& g, int sms, cudaStream_t st)
 {
     using Kind = ProdKind<OP>;
-    auto kernel = product_kernel<OP, BN, S, kGather>;
+    using Tile = ProdTile<BN, kPair>;
+    auto kernel = product_kernel<OP, BN, S, kGather, kPair>;
     static std::atomic<bool> ready[64] = {};         // the shared-memory opt-in of this kernel, by device (setting it twice is harmless)
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -62,26 +63,30 @@ cudaError_t launch_product_tile(const ProdArgs& g, int sms, cudaStream_t st)
     if (!kGather) {
         const int number = Kind::kBytes ? tc::kNumberS8 : IsBF16<S>::value ? tc::kNumberBF16 : tc::kNumberF16;
         const uint64_t pitch_a = OP == kProdInput || OP == kProdWeight ? g.outs : g.in;
-        e = make_map(&map_a, number, g.a, pitch_a, g.rows, 0, Kind::kTurnA ? 64 : 32);
+        e = make_map(&map_a, number, g.a, pitch_a, g.rows, 0, Kind::kTurnA ? 64 : Tile::kBoxRows);
         if (e != cudaSuccess) return e;
-        e = OP == kProdWeight ? make_map(&map_b, number, g.b, g.in, g.rows, 0, 64) : make_map(&map_b, number, g.b, g.in, g.outs, g.experts, Kind::kTurnB ? 64 : BN);
+        e = OP == kProdWeight ? make_map(&map_b, number, g.b, g.in, g.rows, 0, 64) : make_map(&map_b, number, g.b, g.in, g.outs, g.experts, Kind::kTurnB ? 64 : Tile::kOwnColumns);
         if (e != cudaSuccess) return e;
     }
     const size_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs, b_tiles = (width + BN - 1) / BN;
-    const size_t a_tiles = OP == kProdWeight ? size_t(g.experts) * ((g.outs + kTileRows - 1) / kTileRows)
-                                             : (g.rows + kTileRows - 1) / kTileRows + (g.offsets ? g.experts : 0);
+    const size_t a_tiles = OP == kProdWeight ? size_t(g.experts) * ((g.outs + Tile::kRows - 1) / Tile::kRows)
+                                             : (g.rows + Tile::kRows - 1) / Tile::kRows + (g.offsets ? g.experts : 0);
     size_t grid = a_tiles * b_tiles;                 // at most this many tiles
-    if (grid > size_t(sms)) grid = sms;
+    if (grid > size_t(sms / (kPair ? 2 : 1))) grid = sms / (kPair ? 2 : 1);
+    if (kPair) grid *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(grid));
     cfg.blockDim = dim3((kFirstResultWarp + kResultWarps + (kGather ? kGatherWarps : 0)) * 32);
     cfg.dynamicSmemBytes = kProdSmem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = kPair ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, g, map_a, map_b);
 }
 
@@ -99,6 +104,13 @@ template <int OP> int product_width(const ProdArgs& g, int sms)
     return 64;
 }
 
+// Whether pairs of CTAs share tiles of 256 x 256.
+template <int OP> bool product_pairs(const ProdArgs& g, int sms)
+{
+    const size_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs, a = OP == kProdWeight ? g.outs : g.rows / g.experts;
+    return a >= 512 && (OP == kProdWeight ? size_t(g.experts) * ((g.outs + 255) / 256) : g.rows / 256) * ((width + 255) / 256) >= size_t(sms / 2);
+}
+
 template <int OP, class S> cudaError_t launch_product_store(const ProdArgs& g, cudaStream_t st)
 {
     using Kind = ProdKind<OP>;
@@ -110,6 +122,7 @@ template <int OP, class S> cudaError_t launch_product_store(const ProdArgs& g, c
                           (Kind::kTurnB ? uintptr_t(g.outs) * Kind::kElem : 0);
     // a tensor copy needs rows that begin on 16-byte boundaries (and something to copy)
     if (low % 16 || reduction == 0) return launch_product_tile<OP, 128, S, true>(g, di.sm_count, st);
+    if (product_pairs<OP>(g, di.sm_count)) return launch_product_tile<OP, 256, S, false, true>(g, di.sm_count, st);
     switch (product_width<OP>(g, di.sm_count)) {
     case 256: return launch_product_tile<OP, 256, S, false>(g, di.sm_count, st);
     case 128: return launch_product_tile<OP, 128, S, false>(g, di.sm_count, st);

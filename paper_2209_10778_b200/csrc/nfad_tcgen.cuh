@@ -19,6 +19,33 @@ NFAD_TC uint32_t shared_address(const void* p) { return uint32_t(__cvta_generic_
 NFAD_TC void barrier_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 NFAD_TC void barrier_init_done() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
 NFAD_TC void barrier_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// the first CTA of the pair's own copy of a shared-memory address
+NFAD_TC uint32_t first_of_pair(uint32_t address)
+{
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(address));
+    return r;
+}
+NFAD_TC uint32_t rank_in_pair()
+{
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+NFAD_TC void pair_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// On a barrier of the first CTA (an address from first_of_pair).  No cluster-wide release: what these arrivals stand for are
+// asynchronous copies (the transaction count orders them) and tensor-memory reads (fenced on their own); a release at
+// cluster scope in every step halved the rate of the products.
+NFAD_TC void barrier_arrive_first(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+NFAD_TC void barrier_expect_first(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// orders plain writes of one CTA of the pair before an arrival that the other waits for
+NFAD_TC void pair_fence() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
 NFAD_TC void barrier_expect(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
@@ -54,27 +81,43 @@ NFAD_TC void writes_to_async() { asm volatile("fence.proxy.async.shared::cta;" :
 
 NFAD_TC void prefetch_map(const CUtensorMap* m) { asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory"); }
 
-NFAD_TC void load_box(uint32_t dst, const CUtensorMap* m, uint32_t bar, int c0, int c1)
+// kPair: `bar` may be a barrier of the first CTA of the pair
+template <bool kPair> NFAD_TC void load_box(uint32_t dst, const CUtensorMap* m, uint32_t bar, int c0, int c1)
 {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 ::"r"(dst), "l"(m), "r"(bar), "r"(c0), "r"(c1) : "memory");
+    if (kPair)
+        asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                     ::"r"(dst), "l"(m), "r"(bar), "r"(c0), "r"(c1) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                     ::"r"(dst), "l"(m), "r"(bar), "r"(c0), "r"(c1) : "memory");
 }
-NFAD_TC void load_box(uint32_t dst, const CUtensorMap* m, uint32_t bar, int c0, int c1, int c2)
+template <bool kPair> NFAD_TC void load_box(uint32_t dst, const CUtensorMap* m, uint32_t bar, int c0, int c1, int c2)
 {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-                 ::"r"(dst), "l"(m), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+    if (kPair)
+        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                     ::"r"(dst), "l"(m), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                     ::"r"(dst), "l"(m), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
 
 // ---------------------------------------------------------------- tensor memory and products
 
-NFAD_TC void tmem_alloc(uint32_t slot, uint32_t columns)
+// kPair: the pair allocates and frees together (one warp of each CTA)
+template <bool kPair> NFAD_TC void tmem_alloc(uint32_t slot, uint32_t columns)
 {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(columns) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (kPair) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
 }
-NFAD_TC void tmem_free(uint32_t at, uint32_t columns)
+template <bool kPair> NFAD_TC void tmem_free(uint32_t at, uint32_t columns)
 {
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
+    if (kPair) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
 }
 NFAD_TC void fence_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 NFAD_TC void fence_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -112,20 +155,27 @@ NFAD_TC uint32_t instruction(int number, bool a_turned, bool b_turned, uint32_t 
     return (acc << 4) | (in << 7) | (in << 10) | (uint32_t(a_turned) << 15) | (uint32_t(b_turned) << 16) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
 
-template <bool kBytes> NFAD_TC void product(uint32_t acc, uint64_t a, uint64_t b, uint32_t what, bool add)
+// kPair: one product of both CTAs, 128 rows of the result in each one's tensor memory; A's rows and B's columns are split
+// between their shared memories.  Issued by the first CTA.
+template <bool kBytes, bool kPair> NFAD_TC void product(uint32_t acc, uint64_t a, uint64_t b, uint32_t what, bool add)
 {
-    if (kBytes)
-        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n}"
-                     ::"r"(acc), "l"(a), "l"(b), "r"(what), "r"(uint32_t(add)) : "memory");
-    else
-        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                     ::"r"(acc), "l"(a), "l"(b), "r"(what), "r"(uint32_t(add)) : "memory");
+#define NFAD_PRODUCT(group, kind)                                                                                                    \
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::" group ".kind::" kind " [%0], %1, %2, %3, p;\n}" \
+                 ::"r"(acc), "l"(a), "l"(b), "r"(what), "r"(uint32_t(add)) : "memory")
+    if (kBytes && kPair) NFAD_PRODUCT("2", "i8");
+    else if (kBytes) NFAD_PRODUCT("1", "i8");
+    else if (kPair) NFAD_PRODUCT("2", "f16");
+    else NFAD_PRODUCT("1", "f16");
+#undef NFAD_PRODUCT
 }
 
-// the barrier gets one arrival when every product issued so far by this thread is done
-NFAD_TC void products_to(uint32_t bar)
+// the barrier (kPair: that of each CTA of the pair) gets one arrival when every product issued so far by this thread is done
+template <bool kPair> NFAD_TC void products_to(uint32_t bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    if (kPair)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((unsigned short)3) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 
 }  // namespace tc

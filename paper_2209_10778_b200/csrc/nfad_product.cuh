@@ -32,7 +32,7 @@ constexpr int kStepBytes = 128;                    // of the reduction, per stag
 constexpr int kResultWarps = 8;
 constexpr int kGatherWarps = 4;
 constexpr int kFirstResultWarp = 4;                // a warp reads the 32 tensor-memory lanes of its index modulo 4
-constexpr int kRingBytes = 196608;
+constexpr int kRingBytes = 163840;
 constexpr int kMaxStages = 9;
 constexpr long long kWaitDrain = 2000000000ll;     // cycles that a CTA which gave up waits for its own work in flight
 
@@ -61,7 +61,7 @@ struct ProdShared {
     int start[kMaxExperts + 1];                     // first row of each expert
     int tiles[kMaxExperts + 1];                     // row tiles before each expert
 };
-constexpr int kStageBytes = 32 * 64;              // a result warp's 32 rows of 32 16-bit results
+constexpr int kStageBytes = 32 * 128;             // a result warp's 32 rows of 128 bytes
 constexpr int kProdSmem = 1024 + kRingBytes + kResultWarps * kStageBytes + int(sizeof(ProdShared));
 
 // CTAs one of whose waits ran out; one counter for each translation unit that includes this file
@@ -74,50 +74,47 @@ struct ProdTileAt {
     int r0, r_end;                                  // kProdWeight: the reduction's rows; else [0, reduction)
 };
 
-// Tile t.  Within an expert, bands of kBand tiles along A's dimension, B's tile changing slowest inside a band: the CTAs that run
-// at one time then share a few tiles of each operand through L2.
-constexpr int kBand = 16;
-template <int OP, int BN, bool kPair> __device__ __forceinline__ ProdTileAt tile_at(const ProdArgs& g, const ProdShared& s, long long t, int b_tiles)
-{
-    constexpr int kRows = ProdTile<BN, kPair>::kRows;
-    ProdTileAt q;
-    int a_tiles;
-    long long local;
-    if (OP == kProdWeight) {
-        a_tiles = int((g.outs + kRows - 1) / kRows);
-        const long long per = (long long)a_tiles * b_tiles;
-        q.expert = uint32_t(t / per);
-        local = t - q.expert * per;
-    } else {
-        uint32_t lo = 0, hi = g.experts;            // the last expert whose first tile is not past t
-        while (hi - lo > 1) {
-            const uint32_t mid = (lo + hi) / 2;
-            if ((long long)s.tiles[mid] * b_tiles <= t) lo = mid;
-            else hi = mid;
+// Tile t, for one role's walk over its tiles (t ascending).  Within an expert, bands of kBand tiles along A's dimension, B's tile
+// changing slowest inside a band: the CTAs that run at one time then share a few tiles of each operand through L2.  32-bit
+// arithmetic throughout: tiles are counted below 2^31 (the launch sees to it), and every role does this once per tile.
+constexpr uint32_t kBand = 16;
+template <int OP, int BN, bool kPair> struct TileWalk {
+    uint32_t b_tiles, expert = 0;
+    __device__ __forceinline__ ProdTileAt at(const ProdArgs& g, const ProdShared& s, uint32_t t)
+    {
+        constexpr int kRows = ProdTile<BN, kPair>::kRows;
+        ProdTileAt q;
+        uint32_t a_tiles, local;
+        if (OP == kProdWeight) {
+            a_tiles = (g.outs + kRows - 1) / kRows;
+            expert = t / (a_tiles * b_tiles);
+            local = t - expert * a_tiles * b_tiles;
+        } else {
+            while (uint32_t(s.tiles[expert + 1]) * b_tiles <= t) ++expert;
+            a_tiles = s.tiles[expert + 1] - s.tiles[expert];
+            local = t - uint32_t(s.tiles[expert]) * b_tiles;
         }
-        q.expert = lo;
-        a_tiles = s.tiles[lo + 1] - s.tiles[lo];
-        local = t - (long long)s.tiles[lo] * b_tiles;
+        const uint32_t band = local / (kBand * b_tiles);
+        const uint32_t in_band = local - band * kBand * b_tiles;
+        const uint32_t height = min(kBand, a_tiles - band * kBand);
+        const uint32_t bt = in_band / height, at = band * kBand + in_band - bt * height;
+        const int r0 = s.start[expert], r1 = s.start[expert + 1];
+        q.expert = expert;
+        q.b0 = int(bt) * BN;
+        if (OP == kProdWeight) {
+            q.a0 = int(at) * kRows;
+            q.a_end = int(g.outs);
+            q.r0 = r0;
+            q.r_end = r1;
+        } else {
+            q.a0 = r0 + int(at) * kRows;
+            q.a_end = r1;
+            q.r0 = 0;
+            q.r_end = int(OP == kProdInput ? g.outs : g.in);
+        }
+        return q;
     }
-    const long long band = local / ((long long)kBand * b_tiles);
-    const int in_band = int(local - band * kBand * b_tiles);
-    const int height = min(kBand, a_tiles - int(band) * kBand);
-    const int at = int(band) * kBand + in_band % height, bt = in_band / height;
-    const int r0 = s.start[q.expert], r1 = s.start[q.expert + 1];
-    q.b0 = bt * BN;
-    if (OP == kProdWeight) {
-        q.a0 = at * kRows;
-        q.a_end = int(g.outs);
-        q.r0 = r0;
-        q.r_end = r1;
-    } else {
-        q.a0 = r0 + at * kRows;
-        q.a_end = r1;
-        q.r0 = 0;
-        q.r_end = int(OP == kProdInput ? g.outs : g.in);
-    }
-    return q;
-}
+};
 
 // ---------------------------------------------------------------- gathering without tensor copies
 
@@ -151,35 +148,30 @@ template <int ES> __device__ __forceinline__ void gather_box(unsigned char* dst,
 
 // ---------------------------------------------------------------- epilogue
 
-// eight values at a time: z -> y (and f' when it is asked for)
-template <class K> __device__ __forceinline__ void act8(float (&z)[8], float (&d)[8], bool slope)
+// a lane's 32 values: z -> y in place (and f' when it is asked for)
+template <class K, bool kSlope> __device__ __forceinline__ void act32(float (&z)[32], float (&d)[32])
 {
-    if (slope) {
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
+    for (int e = 0; e < 32; e += 2) {
+        if (kSlope) {
             const ActOut2 o = evaluate(K{}, Fast2{}, make_float2(z[e], z[e + 1]));
             z[e] = o.y.x; z[e + 1] = o.y.y;
             d[e] = o.dydx.x; d[e + 1] = o.dydx.y;
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {
+        } else {
             const float2 y = evaluate_value(K{}, Fast2{}, make_float2(z[e], z[e + 1]));
             z[e] = y.x; z[e + 1] = y.y;
         }
     }
 }
 
-__device__ __forceinline__ void act8(int kind, float (&z)[8], float (&d)[8], bool slope)
+template <bool kSlope> __device__ __forceinline__ void act32(int kind, float (&z)[32], float (&d)[32])
 {
     switch (kind) {
-    case kGeluErf:  act8<GeluErf>(z, d, slope); break;
-    case kGeluTanh: act8<GeluTanh>(z, d, slope); break;
-    case kSwish:    act8<Swish>(z, d, slope); break;
-    case kMish:     act8<Mish>(z, d, slope); break;
-    default:
-#pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] = 1.0f;
+    case kGeluErf:  act32<GeluErf, kSlope>(z, d); break;
+    case kGeluTanh: act32<GeluTanh, kSlope>(z, d); break;
+    case kSwish:    act32<Swish, kSlope>(z, d); break;
+    case kMish:     act32<Mish, kSlope>(z, d); break;
+    default: break;                                  // no activation (and then no slope is asked for)
     }
 }
 
@@ -194,7 +186,7 @@ template <class S> __device__ __forceinline__ void load8(const void* base, size_
         for (int e = 0; e < 8; ++e) v[e] = c + e < width ? S::load1(p + e) : 0.0f;
     }
 }
-template <class S> __device__ __forceinline__ void store8(void* base, size_t row, uint32_t width, uint32_t c, const float (&v)[8])
+template <class S> __device__ __forceinline__ void store8(void* base, size_t row, uint32_t width, uint32_t c, const float* v)
 {
     typename S::elem* p = static_cast<typename S::elem*>(base) + row * width + c;
 #pragma unroll
@@ -202,48 +194,56 @@ template <class S> __device__ __forceinline__ void store8(void* base, size_t row
         if (c + e < width) S::store1(p + e, v[e]);
 }
 
-// A lane holds a row's 32 results (four packets); memory wants whole lines.  Packets go through the warp's 2 KB of shared
-// memory, four to a row, their places rotated so that neither side meets bank conflicts: a lane writes its row's and reads
-// back packet lane % 4 of rows lane / 4 + 0, 8, 16, 24, so that each access covers 64 bytes of eight rows (written straight from
-// the rows, each touches 32 lines and the stores alone took 5 us a tile).
-__device__ __forceinline__ int staged_at(int row, int packet) { return row * 4 + (packet ^ (row >> 1 & 3)); }
-struct RowPackets {
-    size_t row0, row_end;                           // of the warp's first row; rows from row_end on are not touched
-    uint32_t width, col;                            // of the first packet
-    int lane;
-    uint4* stage;
-    template <class F> __device__ __forceinline__ void each(F f) const
-    {
+template <class S> __device__ __forceinline__ uint4 pack8(const float (&z)[32], int p)
+{
+    float o[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = i * 8 + (lane >> 2), c = lane & 3;
-            f(i, staged_at(r, c), row0 + r < row_end && col + c * 8 < width, (row0 + r) * width + col + c * 8);
+    for (int e = 0; e < 8; ++e) o[e] = z[p * 8 + e];
+    return S::pack(o);
+}
+
+// A lane holds results of its own row; memory wants whole lines.  So packets of eight go through the warp's 4 KB of shared
+// memory: 32 rows of eight packets, their places rotated so that neither side meets bank conflicts.  The eight packets are 64
+// neighbouring results (whole 128-byte lines on the way out), or 32 results and their 32 slopes, or 32 factors on the way in.
+// Written straight from the rows, every access touched 32 lines, and the stores alone took 5 us a tile.
+struct RowPackets {
+    int lane, rows;                                 // how many of the warp's 32 rows there are
+    uint32_t width;
+    size_t row0;                                    // the first one
+    uint4* stage;
+    static __device__ __forceinline__ int at(int row, int packet) { return row * 8 + (packet ^ (row & 7)); }
+    __device__ __forceinline__ void put(int packet, const uint4& v) const { stage[at(lane, packet)] = v; }
+    __device__ __forceinline__ uint4 get(int packet) const { return stage[at(lane, packet)]; }
+    // Calls f(i, place in the stage, address) for each packet of this lane that is inside: packet lane % kPackets, counted from
+    // column `col` and from the stage's packet `first`, of every 32 / kPackets-th row.
+    template <class E, int kPackets, class F> __device__ __forceinline__ void each(E* base, uint32_t col, int first, F f) const
+    {
+        const int r0 = lane / kPackets, c = lane % kPackets;
+        if (col + c * 8 >= width) return;
+        E* p = base + ((row0 + r0) * width + col + c * 8);
+        const size_t step = size_t(32 / kPackets) * width;
+#pragma unroll
+        for (int i = 0; i < kPackets; ++i, p += step) {
+            const int r = r0 + i * (32 / kPackets);
+            if (r < rows) f(i, at(r, first + c), p);
         }
     }
-    template <class S> __device__ __forceinline__ void store(void* base, const uint4 (&v)[4]) const
+    template <class S, int kPackets> __device__ __forceinline__ void store(void* base, uint32_t col, int first) const
+    {
+        each<typename S::elem, kPackets>(static_cast<typename S::elem*>(base), col, first,
+                                         [&](int, int place, typename S::elem* p) { *reinterpret_cast<uint4*>(p) = stage[place]; });
+    }
+    // four packets of each row, on their way in
+    template <class S> __device__ __forceinline__ void fetch(const void* base, uint32_t col, uint4 (&v)[4]) const
+    {
+        each<const typename S::elem, 4>(static_cast<const typename S::elem*>(base), col, 0,
+                                        [&](int i, int, const typename S::elem* p) { v[i] = *reinterpret_cast<const uint4*>(p); });
+    }
+    // what fetch brought, to the stage's packets from `first` on (values of packets outside are never used)
+    __device__ __forceinline__ void settle(const uint4 (&v)[4], int first) const
     {
 #pragma unroll
-        for (int p = 0; p < 4; ++p) stage[staged_at(lane, p)] = v[p];
-        __syncwarp();
-        each([&](int, int at, bool on, size_t i) {
-            if (on) *reinterpret_cast<uint4*>(static_cast<typename S::elem*>(base) + i) = stage[at];
-        });
-        __syncwarp();
-    }
-    template <class S> __device__ __forceinline__ void fetch(const void* base, uint4 (&v)[4]) const
-    {
-        each([&](int k, int, bool on, size_t i) {
-            v[k] = on ? *reinterpret_cast<const uint4*>(static_cast<const typename S::elem*>(base) + i) : make_uint4(0, 0, 0, 0);
-        });
-    }
-    // what fetch brought, turned into this lane's own row
-    __device__ __forceinline__ void to_rows(uint4 (&v)[4]) const
-    {
-        each([&](int k, int at, bool, size_t) { stage[at] = v[k]; });
-        __syncwarp();
-#pragma unroll
-        for (int p = 0; p < 4; ++p) v[p] = stage[staged_at(lane, p)];
-        __syncwarp();
+        for (int i = 0; i < 4; ++i) stage[at((lane >> 2) + i * 8, first + (lane & 3))] = v[i];
     }
 };
 
@@ -273,7 +273,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
     ProdShared& s = *reinterpret_cast<ProdShared*>(ring + kRingBytes + kResultWarps * kStageBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = kPair ? tc::rank_in_pair() : 0;
-    const long long unit = kPair ? blockIdx.x >> 1 : blockIdx.x, units = kPair ? gridDim.x >> 1 : gridDim.x;
+    const uint32_t unit = kPair ? blockIdx.x >> 1 : blockIdx.x, units = kPair ? gridDim.x >> 1 : gridDim.x;
     const uint32_t ring_at = tc::shared_address(ring);
     auto full = [&](int i) { return tc::shared_address(&s.full[i]); };
     auto empty = [&](int i) { return tc::shared_address(&s.empty[i]); };
@@ -343,9 +343,9 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
     tc::fence_after_sync();
     const uint32_t tmem = s.tmem;
     const uint32_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs;       // of a result's row
-    const int b_tiles = int((width + BN - 1) / BN);
-    const long long total = OP == kProdWeight ? (long long)g.experts * ((g.outs + Tile::kRows - 1) / Tile::kRows) * b_tiles
-                                              : (long long)s.tiles[g.experts] * b_tiles;
+    TileWalk<OP, BN, kPair> walk;
+    walk.b_tiles = (width + BN - 1) / BN;
+    const uint32_t total = (OP == kProdWeight ? g.experts * ((g.outs + Tile::kRows - 1) / Tile::kRows) : uint32_t(s.tiles[g.experts])) * walk.b_tiles;
     // the last tile along a result's row is a narrower product (a multiple of 16 columns, of 32 for a pair, which halves it)
     auto columns = [&](const ProdTileAt& q) {
         const uint32_t unit_n = kPair ? 32 : 16, left = (width - q.b0 + unit_n - 1) / unit_n * unit_n;
@@ -370,8 +370,8 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
         uint32_t stage = 0, phase = 0;
         const bool for_a = warp == 0;
         if (lane == 0)
-            for (long long t = unit; t < total; t += units) {
-                const ProdTileAt q = tile_at<OP, BN, kPair>(g, s, t, b_tiles);
+            for (uint32_t t = unit; t < total; t += units) {
+                const ProdTileAt q = walk.at(g, s, t);
                 const int a0 = q.a0 + int(rank) * kTileRows, b0 = q.b0 + (rank ? int(columns(q)) / 2 : 0);
                 const int a_rows = max(0, min(kTileRows, q.a_end - a0));
                 const int boxes = (a_rows + kBoxRows - 1) / kBoxRows;     // of A, when it is not turned
@@ -421,8 +421,8 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
         // ------------------------------------------------ the same by plain loads
         uint32_t stage = 0, phase = 0;
         bool ok = true;
-        for (long long t = unit; t < total && ok; t += units) {
-            const ProdTileAt q = tile_at<OP, BN, kPair>(g, s, t, b_tiles);
+        for (uint32_t t = unit; t < total && ok; t += units) {
+            const ProdTileAt q = walk.at(g, s, t);
             for (int r = q.r0; r < q.r_end; r += kStep) {
                 if (!(ok = tc::barrier_wait(empty(stage), phase ^ 1, gave_up))) break;
                 constexpr int ES = Kind::kElem;
@@ -452,8 +452,8 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
         // ------------------------------------------------ products
         uint32_t stage = 0, phase = 0, turn = 0, turn_phase = 0, landed_phases = 0;              // landed_phases: a bit for each stage
         bool ok = true;
-        for (long long t = unit; t < total && ok; t += units) {
-            const ProdTileAt q = tile_at<OP, BN, kPair>(g, s, t, b_tiles);
+        for (uint32_t t = unit; t < total && ok; t += units) {
+            const ProdTileAt q = walk.at(g, s, t);
             if (!(ok = tc::barrier_wait(acc_empty(turn), turn_phase ^ 1, gave_up))) break;
             tc::fence_after_sync();
             const uint32_t what = tc::instruction(Kind::kBytes ? tc::kNumberS8 : IsBF16<S>::value ? tc::kNumberBF16 : tc::kNumberF16, Kind::kTurnA, Kind::kTurnB,
@@ -499,8 +499,8 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
         // ------------------------------------------------ the second CTA's ragged steps
         uint32_t stage = 0, landed_phases = 0;
         bool ok = true;
-        for (long long t = unit; t < total && ok; t += units) {
-            const ProdTileAt q = tile_at<OP, BN, kPair>(g, s, t, b_tiles);
+        for (uint32_t t = unit; t < total && ok; t += units) {
+            const ProdTileAt q = walk.at(g, s, t);
             for (int r = q.r0; r < q.r_end; r += kStep) {
                 if (ragged(q, r)) {
                     if (!(ok = tc::barrier_wait(landed(stage), landed_phases >> stage & 1, gave_up))) break;
@@ -523,77 +523,108 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
                                              reinterpret_cast<uintptr_t>(g.prev)) & 15u) == 0;
         const bool vec_scale = Kind::kBytes && width % 8 == 0 && (reinterpret_cast<uintptr_t>(g.b_scale) & 15u) == 0;
         uint32_t turn = 0, turn_phase = 0;
-        for (long long t = unit; t < total; t += units) {
-            const ProdTileAt q = tile_at<OP, BN, kPair>(g, s, t, b_tiles);
-            if (!tc::barrier_wait(acc_full(turn), turn_phase, gave_up)) break;
-            tc::fence_after_sync();
+        for (uint32_t t = unit; t < total; t += units) {
+            const ProdTileAt q = walk.at(g, s, t);
             const int row = q.a0 + int(rank) * kTileRows + lanes + lane;
             const bool mine = row < q.a_end, none = q.r0 >= q.r_end;
             const size_t out_row = OP == kProdWeight ? size_t(q.expert) * g.outs + row : size_t(row);
             const float scale = Kind::kBytes && mine ? g.a_scale[row] : 0.0f;
             RowPackets rows;
-            rows.row0 = out_row - lane;
-            rows.row_end = rows.row0 + max(0, q.a_end - (row - lane));
-            rows.width = width;
             rows.lane = lane;
+            rows.rows = min(32, q.a_end - (row - lane));
+            rows.width = width;
+            rows.row0 = out_row - lane;
             rows.stage = reinterpret_cast<uint4*>(ring + kRingBytes + (warp - kFirstResultWarp) * kStageBytes);
-            constexpr int kChunks = BN / 32;
-            for (int c = half; c < kChunks; c += 2) {
+            // 32 columns at a time; without slopes two of them leave together; the factors of the next are fetched during the current
+            constexpr int kChunks = BN / 32, kOwnChunks = kChunks / 2;
+            constexpr bool kTwo = kOwnChunks > 1;
+            const bool slopes = OP == kProdForward && g.slope;
+            uint4 prev[4] = {};
+            if (OP == kProdInput && g.prev && vec) rows.template fetch<S>(g.prev, q.b0 + half * kOwnChunks * 32, prev);
+            if (!tc::barrier_wait(acc_full(turn), turn_phase, gave_up)) break;
+            tc::fence_after_sync();
+            for (int c = half * kOwnChunks; c < (half + 1) * kOwnChunks; ++c) {
                 const uint32_t col0 = q.b0 + c * 32;
-                if (col0 >= width || rows.row0 >= rows.row_end) break;     // past the result's columns; a warp without rows
-                rows.col = col0;
+                if (col0 >= width || rows.rows <= 0) break;     // past the result's columns; a warp without rows
+                const bool second = kTwo && !slopes && (c & 1);
                 uint32_t v[32];
                 tc::tmem_load32(tmem + (uint32_t(lanes) << 16) + turn * BN + c * 32, v);
-                uint4 y[4], slope[4];
-                if (OP == kProdInput && g.prev && vec) rows.template fetch<S>(g.prev, slope);
                 tc::tmem_load_wait();
-                if (OP == kProdInput && g.prev && vec) rows.to_rows(slope);
+                float z[32], d[32];
 #pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                    const uint32_t col = col0 + p * 8;
-                    float z[8], d[8];
+                for (int e = 0; e < 32; ++e) z[e] = Kind::kBytes ? float(int(v[e])) : __uint_as_float(v[e]);
+                if (none)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        z[e] = Kind::kBytes ? float(int(v[p * 8 + e])) : __uint_as_float(v[p * 8 + e]);
-                        if (none) z[e] = 0.0f;
-                    }
-                    if (Kind::kBytes) {
-                        float w[8];
-                        if (vec_scale && col < width) {
-                            const float4 lo = __ldg(reinterpret_cast<const float4*>(g.b_scale + col)), hi = __ldg(reinterpret_cast<const float4*>(g.b_scale + col) + 1);
-                            w[0] = lo.x; w[1] = lo.y; w[2] = lo.z; w[3] = lo.w; w[4] = hi.x; w[5] = hi.y; w[6] = hi.z; w[7] = hi.w;
+                    for (int e = 0; e < 32; ++e) z[e] = 0.0f;
+                if (Kind::kBytes) {
+#pragma unroll
+                    for (int p = 0; p < 8; ++p) {
+                        const uint32_t col = col0 + p * 4;
+                        float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        if (vec_scale) {
+                            if (col < width) w = __ldg(reinterpret_cast<const float4*>(g.b_scale + col));
                         } else {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) w[e] = col + e < width ? __ldg(g.b_scale + col + e) : 0.0f;
+                            if (col < width) w.x = __ldg(g.b_scale + col);
+                            if (col + 1 < width) w.y = __ldg(g.b_scale + col + 1);
+                            if (col + 2 < width) w.z = __ldg(g.b_scale + col + 2);
+                            if (col + 3 < width) w.w = __ldg(g.b_scale + col + 3);
                         }
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) z[e] *= scale * w[e];
+                        z[p * 4] *= scale * w.x; z[p * 4 + 1] *= scale * w.y; z[p * 4 + 2] *= scale * w.z; z[p * 4 + 3] *= scale * w.w;
                     }
-                    if (OP == kProdForward || OP == kProdBytes) {
-                        if (g.bias) {
-                            float b[8];
-                            load8<S>(g.bias, q.expert, width, col, vec, b);
+                }
+                if ((OP == kProdForward || OP == kProdBytes) && g.bias) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) z[e] += b[e];
-                        }
-                        act8(g.act, z, d, g.slope != nullptr);
-                        if (g.slope && vec) slope[p] = S::pack(d);
-                        if (g.slope && !vec && mine) store8<S>(g.slope, out_row, width, col, d);
-                    } else if (OP == kProdInput) {
-                        if (g.prev) {
-                            float f[8];
-                            if (vec) S::unpack(slope[p], f);
-                            else if (mine) load8<S>(g.prev, out_row, width, col, false, f);
+                    for (int p = 0; p < 4; ++p) {
+                        float b[8];
+                        load8<S>(g.bias, q.expert, width, col0 + p * 8, vec, b);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) z[e] *= f[e];
-                        }
+                        for (int e = 0; e < 8; ++e) z[p * 8 + e] += b[e];
                     }
-                    if (vec) y[p] = S::pack(z);
-                    else if (mine) store8<S>(g.out, out_row, width, col, z);
+                }
+                if (OP == kProdInput && g.prev) {
+                    const int first = second ? 4 : 0;                 // the places that this chunk's results will take
+                    if (vec) {
+                        rows.settle(prev, first);
+                        __syncwarp();
+                        if (c + 1 < (half + 1) * kOwnChunks) rows.template fetch<S>(g.prev, col0 + 32, prev);
+                    }
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        float f[8];
+                        if (vec) S::unpack(rows.get(first + p), f);
+                        else load8<S>(g.prev, mine ? out_row : rows.row0, width, col0 + p * 8, false, f);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z[p * 8 + e] *= f[e];
+                    }
+                    if (vec) __syncwarp();
+                }
+                if constexpr (OP == kProdForward) {
+                    if (slopes) act32<true>(g.act, z, d);
+                    else act32<false>(g.act, z, d);
+                } else if constexpr (OP == kProdBytes) {
+                    act32<false>(g.act, z, d);
                 }
                 if (vec) {
-                    rows.template store<S>(g.out, y);
-                    if ((OP == kProdForward) && g.slope) rows.template store<S>(g.slope, slope);
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        rows.put((second ? 4 : 0) + p, pack8<S>(z, p));
+                        if (OP == kProdForward && slopes) rows.put(4 + p, pack8<S>(d, p));
+                    }
+                    if (kTwo && !slopes && !second && c + 1 < (half + 1) * kOwnChunks && col0 + 32 < width) continue;   // the next 32 first
+                    __syncwarp();
+                    if (kTwo && second) {
+                        rows.template store<S, 8>(g.out, col0 - 32, 0);
+                    } else {
+                        rows.template store<S, 4>(g.out, col0, 0);
+                        if (OP == kProdForward && slopes) rows.template store<S, 4>(g.slope, col0, 4);
+                    }
+                    __syncwarp();
+                } else if (mine) {
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        store8<S>(g.out, out_row, width, col0 + p * 8, &z[p * 8]);
+                        if (OP == kProdForward && slopes) store8<S>(g.slope, out_row, width, col0 + p * 8, &d[p * 8]);
+                    }
                 }
             }
             tc::fence_before_sync();

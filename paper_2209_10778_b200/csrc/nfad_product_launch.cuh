@@ -72,6 +72,7 @@ cudaError_t launch_product_tile(const ProdArgs& g, int sms, cudaStream_t st)
     const size_t a_tiles = OP == kProdWeight ? size_t(g.experts) * ((g.outs + Tile::kRows - 1) / Tile::kRows)
                                              : (g.rows + Tile::kRows - 1) / Tile::kRows + (g.offsets ? g.experts : 0);
     size_t grid = a_tiles * b_tiles;                 // at most this many tiles
+    if (grid >= (size_t(1) << 31)) return cudaErrorInvalidValue;     // beyond what any device's memory holds
     if (grid > size_t(sms / (kPair ? 2 : 1))) grid = sms / (kPair ? 2 : 1);
     if (kPair) grid *= 2;
     cudaLaunchConfig_t cfg = {};

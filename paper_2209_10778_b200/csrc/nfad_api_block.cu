@@ -312,6 +312,7 @@ int nfad_i8_linear_dynamic(int kind, int dtype, const void* x, const signed char
     nfad::ProdArgs g = {};
     g.a = q; g.b = wq; g.bias = bias; g.a_scale = scale; g.b_scale = w_scale; g.out = y;
     g.rows = rows; g.in = uint32_t(in); g.outs = uint32_t(out); g.experts = 1; g.act = kind;
+    g.b_ready = 1;                                                    // the quantiser lets its successor start only after its own wait
     return finish(nfad::launch_product_bytes(dtype, g, st));
 }
 

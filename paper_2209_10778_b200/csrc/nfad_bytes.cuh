@@ -42,8 +42,10 @@ template <class S> __global__ void __launch_bounds__(kBlock) quantize_kernel(con
 {
     constexpr int V = S::kVec;
     __shared__ float part[2][kBlock / 32];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // in this order: the next kernel may start only when everything in front of this one is complete, so that it may read what
+    // neither of the two writes (the weights) before this one has ended
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     int turn = 0;
     for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
         const typename S::elem* x = static_cast<const typename S::elem*>(a.x) + row * a.cols;

@@ -51,70 +51,92 @@ __device__ __forceinline__ float* expert_target(const ExpertActArgs& a, size_t c
     return a.partial + (chunk * 2 + (g0 <= r0 ? 0 : 1)) * a.cols;
 }
 
-// kVec: whole 16-byte packets; else one column a thread
+// kVec: whole 16-byte packets; else one column a thread.  The rows go by fours, whatever experts they belong to, so that the
+// loads of a group are all in flight before the first is used and an expert's border costs a thread one look at the offsets.
+template <class S, bool kVec> struct ExpertPacket { uint4 v; };
+template <class S> struct ExpertPacket<S, false> { typename S::elem v; };
+
 template <class S, bool kVec>
-__global__ void __launch_bounds__(kBiasMaxBlock) expert_act_kernel(const __grid_constant__ ExpertActArgs a)
+__global__ void __launch_bounds__(kBiasMaxBlock, 4) expert_act_kernel(const __grid_constant__ ExpertActArgs a)
 {
     constexpr int V = kVec ? S::kVec : 1, U = kBiasRows;
     using E = typename S::elem;
+    using Packet = ExpertPacket<S, kVec>;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t cp = blockIdx.x * blockDim.x + threadIdx.x;
     if (cp >= a.row_packets) return;
     const size_t r0 = size_t(blockIdx.y) * a.chunk_rows, r1 = r0 + a.chunk_rows < a.rows ? r0 + a.chunk_rows : a.rows;
-    auto load = [&](const void* base, size_t row, float (&v)[V]) {
-        if constexpr (kVec) S::unpack(load_packet(static_cast<const uint4*>(base) + row * a.row_packets + cp), v);
-        else v[0] = S::load1(static_cast<const E*>(base) + row * a.cols + cp);
+    if (r0 >= r1) return;
+    auto load = [&](const void* base, size_t row) {
+        Packet p;
+        if constexpr (kVec) p.v = load_packet(static_cast<const uint4*>(base) + row * a.row_packets + cp);
+        else p.v = static_cast<const E*>(base)[row * a.cols + cp];
+        return p;
     };
-    auto store = [&](size_t row, const float (&v)[V]) {
-        if constexpr (kVec) store_packet<true>(static_cast<uint4*>(a.gz) + row * a.row_packets + cp, S::pack(v));
-        else S::store1(static_cast<E*>(a.gz) + row * a.cols + cp, v[0]);
+    auto widen = [&](const Packet& p, float (&v)[V]) {
+        if constexpr (kVec) S::unpack(p.v, v);
+        else v[0] = S::load1(&p.v);
     };
-    for (size_t row = r0; row < r1;) {
-        size_t end;
-        const uint32_t e = expert_of(a, row, &end);
-        if (end > r1) end = r1;
-        float acc[V];
+    float acc[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) acc[i] = 0.0f;
-        if (e >= a.experts) {                                        // nobody's rows
-            if (a.gz)
-                for (; row < end; ++row) store(row, acc);
-            row = end;
-            continue;
-        }
-        for (; row < end; row += U) {
-            float g[U][V], d[U][V];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (row + u < end) {
-                    load(a.g, row + u, g[u]);
-                    if (a.d) load(a.d, row + u, d[u]);
-                }
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (row + u < end) {
-                    if (a.d)
-#pragma unroll
-                        for (int i = 0; i < V; ++i) g[u][i] = __fmul_rn(g[u][i], d[u][i]);
-                    if (a.gz) store(row + u, g[u]);
-#pragma unroll
-                    for (int i = 0; i < V; ++i) acc[i] = __fadd_rn(acc[i], g[u][i]);
-                }
-        }
-        row = end;
-        if (a.grad_bias) {
+    for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+    uint32_t e = a.experts;
+    size_t end = r0;                                                  // of the run of rows that `row` is in
+    auto hand_over = [&]() {
+        if (a.grad_bias && e < a.experts) {
             float* dst = expert_target(a, blockIdx.y, r0, r1, e) + size_t(cp) * V;
 #pragma unroll
             for (int i = 0; i < V; ++i) dst[i] = acc[i];
         }
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+    };
+    for (size_t row = r0; row < r1; row += U) {
+        Packet g[U], d[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (row + u < r1) {
+                g[u] = load(a.g, row + u);
+                if (a.d) d[u] = load(a.d, row + u);
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (row + u >= r1) break;
+            if (row + u == end) {
+                if (row + u > r0) hand_over();
+                e = expert_of(a, row + u, &end);
+            }
+            float v[V];
+            if (e < a.experts) {
+                widen(g[u], v);
+                if (a.d) {
+                    float f[V];
+                    widen(d[u], f);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) v[i] = __fmul_rn(v[i], f[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] = __fadd_rn(acc[i], v[i]);
+            } else {                                                 // nobody's row, whatever it holds
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] = 0.0f;
+            }
+            if (a.gz) {
+                if constexpr (kVec) store_packet<true>(static_cast<uint4*>(a.gz) + (row + u) * a.row_packets + cp, S::pack(v));
+                else S::store1(static_cast<E*>(a.gz) + (row + u) * a.cols + cp, v[0]);
+            }
+        }
     }
+    hand_over();
 }
 
-// The experts whose rows lie in several chunks, and those without rows.
-static __global__ void __launch_bounds__(32 * kBiasGroups) expert_reduce_kernel(const __grid_constant__ ExpertActArgs a)
+// The experts whose rows lie in several chunks, and those without rows.  32 columns times kExpertGroups runs of consecutive
+// chunks to a CTA: small, as an expert has few chunks when there are many experts (32 runs: 14 us for 61 experts of 1416).
+constexpr int kExpertGroups = 8;
+static __global__ void __launch_bounds__(32 * kExpertGroups) expert_reduce_kernel(const __grid_constant__ ExpertActArgs a)
 {
-    __shared__ float smem[kBiasGroups][32];
+    __shared__ float smem[kExpertGroups][32];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
     const size_t col = size_t(blockIdx.x) * 32 + lane;
@@ -127,25 +149,45 @@ static __global__ void __launch_bounds__(32 * kBiasGroups) expert_reduce_kernel(
     }
     const size_t c0 = g0 / a.chunk_rows, c1 = (g1 - 1) / a.chunk_rows + 1;
     if (c1 - c0 == 1) return;                                        // written by its chunk
-    const size_t per = (c1 - c0 + kBiasGroups - 1) / kBiasGroups;
+    const size_t per = (c1 - c0 + kExpertGroups - 1) / kExpertGroups;
     const size_t k0 = c0 + group * per, k1 = k0 + per < c1 ? k0 + per : c1;
     float s = 0.0f;
     if (col < a.cols)
-        for (size_t k = k0; k < k1; ++k) s = __fadd_rn(s, a.partial[(k * 2 + (g0 <= k * a.chunk_rows ? 0 : 1)) * a.cols + col]);
+        for (size_t k = k0; k < k1; k += 8) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v[j] = k + j < k1 ? a.partial[((k + j) * 2 + (g0 <= (k + j) * a.chunk_rows ? 0 : 1)) * a.cols + col] : 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (k + j < k1) s = __fadd_rn(s, v[j]);
+        }
     smem[group][lane] = s;
     __syncthreads();
     if (group == 0 && col < a.cols) {
         float t = smem[0][lane];
 #pragma unroll
-        for (int j = 1; j < kBiasGroups; ++j) t = __fadd_rn(t, smem[j][lane]);
+        for (int j = 1; j < kExpertGroups; ++j) t = __fadd_rn(t, smem[j][lane]);
         out[col] = t;
     }
+}
+
+// Rows of a chunk, by shape and device alone: as many CTAs of 256 threads as are resident at a time (four to an SM), twice over, and
+// no fewer than eight rows to a chunk.
+inline uint32_t expert_chunk_rows(size_t rows, size_t cols, int sms)
+{
+    const size_t strips = (cols / 8 + kBiasMaxBlock - 1) / kBiasMaxBlock + (cols < 8);
+    const size_t chunks = (size_t(sms) * 8 + strips - 1) / strips;
+    size_t n = (rows + chunks - 1) / chunks;
+    n = (n + kBiasRows - 1) / kBiasRows * kBiasRows;
+    return uint32_t(n < 8 ? 8 : n);
 }
 
 inline size_t expert_act_scratch_bytes(size_t rows, size_t cols, int sms)
 {
     if (rows == 0 || cols == 0) return 0;
-    return size_t(bias_plan<8>(rows, cols, sms).chunks) * 2 * cols * sizeof(float);
+    const size_t n = expert_chunk_rows(rows, cols, sms);
+    return (rows + n - 1) / n * 2 * cols * sizeof(float);
 }
 
 template <class S> cudaError_t launch_expert_act(const ExpertActArgs& in, cudaStream_t st)
@@ -156,20 +198,19 @@ template <class S> cudaError_t launch_expert_act(const ExpertActArgs& in, cudaSt
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];
-    const BiasPlan p = bias_plan<8>(a.rows ? a.rows : 1, a.cols, di.sm_count);
-    a.chunk_rows = p.chunk_rows;
-    a.chunks = p.chunks;
+    a.chunk_rows = expert_chunk_rows(a.rows, a.cols, di.sm_count);
+    a.chunks = uint32_t((a.rows + a.chunk_rows - 1) / a.chunk_rows);
     if (a.rows) {
         const bool vec = a.cols % 8 == 0 && aligned16(a.g) && aligned16(a.d) && aligned16(a.gz);
         a.row_packets = vec ? a.cols / 8 : a.cols;
         const unsigned block = bias_block(a.row_packets);
         bias_launch_config(&cfg, attr, (a.row_packets + block - 1) / block, block, st, true);
-        cfg.gridDim.y = p.chunks;
+        cfg.gridDim.y = a.chunks;
         e = vec ? cudaLaunchKernelEx(&cfg, expert_act_kernel<S, true>, a) : cudaLaunchKernelEx(&cfg, expert_act_kernel<S, false>, a);
         if (e != cudaSuccess) return e;
     }
     if (!a.grad_bias) return cudaSuccess;
-    bias_launch_config(&cfg, attr, (a.cols + 31) / 32, 32 * kBiasGroups, st, true);
+    bias_launch_config(&cfg, attr, (a.cols + 31) / 32, 32 * kExpertGroups, st, true);
     cfg.gridDim.y = a.experts;
     return cudaLaunchKernelEx(&cfg, expert_reduce_kernel, a);
 }

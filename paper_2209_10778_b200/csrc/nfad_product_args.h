@@ -28,6 +28,7 @@ struct ProdArgs {
     size_t rows;
     uint32_t in, outs, experts;
     int act;                         // a Kind or kNoAct
+    int b_ready;                     // the kernel in front of this one does not write b, and began after whatever did
 };
 
 }  // namespace nfad

@@ -4,6 +4,7 @@
 #include <atomic>
 #include <mutex>
 
+#include "nfad_few_rows.cuh"
 #include "nfad_product.cuh"
 
 namespace nfad {
@@ -105,11 +106,15 @@ template <int OP> int product_width(const ProdArgs& g, int sms)
     return 64;
 }
 
-// Whether pairs of CTAs share tiles of 256 x 256.
+// Whether pairs of CTAs share tiles of 256 x 256: when every pair gets one, and the tile's second 128 rows are not empty as a
+// rule (forward, input gradient; 67 rows an expert: 56 us in pairs, 49 by single CTAs; 128 and more: pairs equal or faster, 450 against 550
+// us with 2048), and the reduction is long enough to pay for the pair's hand-shakes (weight gradient; 128 to 256 rows
+// an expert: 55 and 196 us in pairs, 47 and 187 by single CTAs; 1024 and more: 377 against 410 us).
 template <int OP> bool product_pairs(const ProdArgs& g, int sms)
 {
-    const size_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs, a = OP == kProdWeight ? g.outs : g.rows / g.experts;
-    return a >= 512 && (OP == kProdWeight ? size_t(g.experts) * ((g.outs + 255) / 256) : g.rows / 256) * ((width + 255) / 256) >= size_t(sms / 2);
+    const size_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs, mean = g.rows / g.experts;
+    const size_t a_tiles = OP == kProdWeight ? size_t(g.experts) * ((g.outs + 255) / 256) : (g.rows + 255) / 256;
+    return mean >= (OP == kProdWeight ? 512 : 128) && a_tiles * ((width + 255) / 256) >= size_t(sms / 2);
 }
 
 template <int OP, class S> cudaError_t launch_product_store(const ProdArgs& g, cudaStream_t st)
@@ -123,6 +128,8 @@ template <int OP, class S> cudaError_t launch_product_store(const ProdArgs& g, c
                           (Kind::kTurnB ? uintptr_t(g.outs) * Kind::kElem : 0);
     // a tensor copy needs rows that begin on 16-byte boundaries (and something to copy)
     if (low % 16 || reduction == 0) return launch_product_tile<OP, 128, S, true>(g, di.sm_count, st);
+    if constexpr (OP == kProdForward || OP == kProdBytes)
+        if (few_rows(g)) return launch_few_rows<Kind::kBytes, S>(g, di.sm_count, g.b_ready, st);
     if (product_pairs<OP>(g, di.sm_count)) return launch_product_tile<OP, 256, S, false, true>(g, di.sm_count, st);
     switch (product_width<OP>(g, di.sm_count)) {
     case 256: return launch_product_tile<OP, 256, S, false>(g, di.sm_count, st);

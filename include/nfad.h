@@ -451,11 +451,11 @@ NFAD_API int nfad_i8_linear_dynamic(int kind, int dtype, const void* x, const si
 NFAD_API size_t nfad_i8_linear_dynamic_scratch_bytes(size_t rows, size_t in);
 
 /*
- * How many CTAs of the products above have given up waiting for their own copies or products since the library was loaded
+ * How many CTAs of the kernels above have given up waiting for their own copies or products since the library was loaded
  * on the current device (0 in a healthy process; a launch that gave up leaves its results undefined instead of hanging the
  * device), or a negative nfad_status.  Synchronises the device: a diagnostic, not for a hot path.
  */
-NFAD_API int nfad_product_faults(void);
+NFAD_API int nfad_wait_faults(void);
 
 /*
  * The whole pass for tensors that live in HOST memory (no counterpart in the paper: a service entry

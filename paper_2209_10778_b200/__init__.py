@@ -19,5 +19,5 @@ from .block import (  # noqa: F401
     nfad_expert_act_backward, nfad_expert_act_backward_scratch, nfad_expert_act_backward_scratch_bytes, nfad_expert_linear,
     nfad_expert_linear_backward_input, nfad_expert_linear_backward_weight,
     nfad_i8_linear, nfad_i8_linear_dynamic, nfad_i8_linear_dynamic_scratch, nfad_i8_linear_dynamic_scratch_bytes,
-    nfad_i8_quantize_rows, nfad_product_faults,
+    nfad_i8_quantize_rows, nfad_wait_faults,
 )

@@ -38,7 +38,7 @@ EXPORTS = (
     "nfad_expert_linear", "nfad_expert_act_backward", "nfad_expert_act_backward_scratch_bytes",
     "nfad_expert_linear_backward_input", "nfad_expert_linear_backward_weight",
     "nfad_i8_quantize_rows", "nfad_i8_linear", "nfad_i8_linear_dynamic", "nfad_i8_linear_dynamic_scratch_bytes",
-    "nfad_product_faults",
+    "nfad_wait_faults",
 )
 OPCODES = {"add": 0, "mul": 1, "scale": 2, "add_const": 3, "exp": 4, "log1p": 5, "tanh": 6, "erf": 7, "softplus": 8,
            "sigmoid": 9, "half_one_plus_tanh": 10, "half_one_plus_erf": 11, "out": 12}
@@ -125,7 +125,7 @@ def load() -> ctypes.CDLL:
                 ("nfad_i8_quantize_rows", [ci, vp, vp, vp, sz, sz, vp], ci),
                 ("nfad_i8_linear", [ci, ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, vp], ci),
                 ("nfad_i8_linear_dynamic", [ci, ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, sz, vp], ci),
-                ("nfad_i8_linear_dynamic_scratch_bytes", [sz, sz], sz), ("nfad_product_faults", [], ci)):
+                ("nfad_i8_linear_dynamic_scratch_bytes", [sz, sz], sz), ("nfad_wait_faults", [], ci)):
             getattr(lib, name).argtypes, getattr(lib, name).restype = args, res
         lib.nfad_seq_set_executor.argtypes = [ci]
         lib.nfad_seq_set_executor.restype = ci

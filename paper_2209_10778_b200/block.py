@@ -279,9 +279,9 @@ def nfad_i8_linear_dynamic(kind, x: torch.Tensor, wq: torch.Tensor, w_scale: tor
                "nfad_i8_linear_dynamic")
 
 
-def nfad_product_faults() -> int:
+def nfad_wait_faults() -> int:
     """How many CTAs of the products have given up waiting since the library was loaded (0 in a healthy process).  Synchronises."""
-    n = int(load().nfad_product_faults())
+    n = int(load().nfad_wait_faults())
     if n < 0:
-        _check(-n, "nfad_product_faults")
+        _check(-n, "nfad_wait_faults")
     return n

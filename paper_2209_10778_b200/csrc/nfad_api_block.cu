@@ -316,10 +316,10 @@ int nfad_i8_linear_dynamic(int kind, int dtype, const void* x, const signed char
     return finish(nfad::launch_product_bytes(dtype, g, st));
 }
 
-int nfad_product_faults(void)
+int nfad_wait_faults(void)
 {
     unsigned total = 0;
-    for (auto count : {nfad::product_faults_forward, nfad::product_faults_input, nfad::product_faults_weight, nfad::product_faults_bytes}) {
+    for (auto count : {nfad::wait_faults_norm, nfad::product_faults_forward, nfad::product_faults_input, nfad::product_faults_weight, nfad::product_faults_bytes}) {
         unsigned n = 0;
         if (int rc = finish(count(&n))) return -rc;
         total += n;

@@ -79,6 +79,7 @@ cudaError_t launch_product_forward(int dtype, const ProdArgs& g, cudaStream_t st
 cudaError_t launch_product_input(int dtype, const ProdArgs& g, cudaStream_t st);
 cudaError_t launch_product_weight(int dtype, const ProdArgs& g, cudaStream_t st);
 cudaError_t launch_product_bytes(int dtype, const ProdArgs& g, cudaStream_t st);
+cudaError_t wait_faults_norm(unsigned* n);
 cudaError_t product_faults_forward(unsigned* n);
 cudaError_t product_faults_input(unsigned* n);
 cudaError_t product_faults_weight(unsigned* n);

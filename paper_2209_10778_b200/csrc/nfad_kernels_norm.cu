@@ -34,4 +34,6 @@ cudaError_t norm_backward_scratch(int dtype, size_t rows, size_t cols, size_t* b
     return cudaSuccess;
 }
 
+cudaError_t wait_faults_norm(unsigned* n) { return cudaMemcpyFromSymbol(n, g_norm_faults, sizeof *n); }
+
 }  // namespace nfad

@@ -34,7 +34,6 @@ constexpr int kGatherWarps = 4;
 constexpr int kFirstResultWarp = 4;                // a warp reads the 32 tensor-memory lanes of its index modulo 4
 constexpr int kRingBytes = 163840;
 constexpr int kMaxStages = 9;
-constexpr long long kWaitDrain = 2000000000ll;     // cycles that a CTA which gave up waits for its own work in flight
 
 template <int OP> struct ProdKind {
     static constexpr bool kBytes = OP == kProdBytes;
@@ -413,7 +412,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
                 if (!ok) {
                     // a wait ran out: the copies in flight land before the CTA's memory goes away
                     const long long t0 = clock64();
-                    while (clock64() - t0 < kWaitDrain) {}
+                    while (clock64() - t0 < tc::kWaitDrain) {}
                     break;
                 }
             }
@@ -493,7 +492,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
         if (!ok && lane == 0) {
             tc::products_to<kPair>(tc::shared_address(&s.drained));
             const long long t0 = clock64();
-            while (!tc::barrier_try(tc::shared_address(&s.drained), 0) && clock64() - t0 < kWaitDrain) {}
+            while (!tc::barrier_try(tc::shared_address(&s.drained), 0) && clock64() - t0 < tc::kWaitDrain) {}
         }
     } else if (warp == 1 && OP == kProdWeight) {
         // ------------------------------------------------ the second CTA's ragged steps

@@ -63,6 +63,7 @@ NFAD_TC bool barrier_try(uint32_t bar, uint32_t parity)
 // A wait that ends: when the barrier's phase completes (true), when another role of the CTA has given up, or after about ten
 // seconds of SM cycles (false; nothing that a correct launch waits for takes a hundredth of that).
 constexpr long long kWaitCycles = 20000000000ll;
+constexpr long long kWaitDrain = 2000000000ll;      // what a CTA that gave up leaves its own work in flight
 NFAD_TC bool barrier_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up)
 {
     if (barrier_try(bar, parity)) return true;
@@ -102,6 +103,12 @@ template <bool kPair> NFAD_TC void load_box(uint32_t dst, const CUtensorMap* m, 
     else
         asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                      ::"r"(dst), "l"(m), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+
+// `bytes` (a multiple of 16) between 16-byte boundaries, no tensor map
+NFAD_TC void load_run(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
 // ---------------------------------------------------------------- tensor memory and products

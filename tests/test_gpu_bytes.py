@@ -83,7 +83,7 @@ def test_linear(dtype, shape):
             nfad.nfad_i8_linear(kind, q.to(DEV), xs.to(DEV), wq.to(DEV), ws.to(DEV), None if b is None else b.to(DEV), y)
             torch.cuda.synchronize()
             _check(kind, q, xs, wq, ws, b, y)
-    assert nfad.nfad_product_faults() == 0
+    assert nfad.nfad_wait_faults() == 0
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])

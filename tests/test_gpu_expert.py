@@ -76,7 +76,7 @@ def test_forward(dtype, case):
         for bias in (b, None):
             _check_forward(kind, x, w, bias, o, *_forward(kind, x, w, bias, off))
             _check_forward(kind, x, w, bias, o, *_forward(kind, x, w, bias, off, slope=False))
-    assert nfad.nfad_product_faults() == 0
+    assert nfad.nfad_wait_faults() == 0
 
 
 def _act_backward(g, d, off, experts):
@@ -139,7 +139,7 @@ def test_backward(dtype, case):
     prev = W.uniform(x.numel(), dtype, 11, -0.2, 1.1).view(x.shape)
     for f in (None, prev):
         _check_backward(gz, x, w, o, f, *_backward(gz, x, w, off, f))
-    assert nfad.nfad_product_faults() == 0
+    assert nfad.nfad_wait_faults() == 0
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -150,7 +150,7 @@ def test_many_tiles(dtype):
         _check_forward("swish", x, w, b, o, *_forward("swish", x, w, b, off))
         gz = W.normal(x.shape[0] * n_out, dtype, 9, 1.0).view(x.shape[0], n_out)
         _check_backward(gz, x, w, o, None, *_backward(gz, x, w, off))
-    assert nfad.nfad_product_faults() == 0
+    assert nfad.nfad_wait_faults() == 0
 
 
 @pytest.mark.parametrize("dtype", DTYPES)

@@ -62,127 +62,204 @@ template <int N, bool kWarp> struct RowSum {
 
 // ---------------------------------------------------------------- forward
 
-template <class S> __device__ __forceinline__ void load_row_packet(const void* base, size_t row, uint32_t packets, uint32_t p, float (&v)[S::kVec])
-{
-    S::unpack(load_packet(static_cast<const uint4*>(base) + row * packets + p), v);
-}
-
 // parameters are read by every row: plain cached loads
 template <class S> __device__ __forceinline__ void load_parameter(const void* base, size_t row, uint32_t packets, uint32_t p, float (&v)[S::kVec])
 {
     S::unpack(__ldg(static_cast<const uint4*>(base) + row * packets + p), v);
 }
 
-// mean and reciprocal deviation of the values a row's threads hold (I packets each, the valid ones)
-template <int V, int I, bool kWarp>
-__device__ __forceinline__ void row_statistics(const float (&v)[I][V], const bool (&on)[I], int kind, float inv_cols, float eps,
-                                               RowSum<1, kWarp>& sum, float* mean, float* rstd)
+// 1 / sqrt(x): the hardware's approximation and one Newton step, within two units in the last place
+__device__ __forceinline__ float reciprocal_root(float x)
 {
-    *mean = 0.0f;
-    float t[1];
-    if (kind == kNormLayer) {
-        t[0] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < I; ++i)
-#pragma unroll
-            for (int e = 0; e < V; ++e) t[0] += v[i][e];           // packets past the row hold zeros
-        sum(t);
-        *mean = t[0] * inv_cols;
-    }
-    t[0] = 0.0f;
-#pragma unroll
-    for (int i = 0; i < I; ++i)
-        if (on[i])
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float c = v[i][e] - *mean;
-                t[0] = fmaf(c, c, t[0]);
-            }
-    sum(t);
-    *rstd = 1.0f / sqrtf(fmaf(t[0], inv_cols, eps));
+    const float y = rsqrtf(x);
+    return y * fmaf(-0.5f * x * y, y, 1.5f);
 }
 
-// One row per CTA, or per warp (kWarp); cols a multiple of the packet, every pointer on a 16-byte boundary.
-template <class S, int I, bool kWarp>
-__global__ void __launch_bounds__(1024) norm_forward_kernel(const __grid_constant__ NormForwardArgs a)
+// which gate row governs a row; divisions of 64 bits cost as much as a row's arithmetic, and are rarely needed
+__device__ __forceinline__ size_t gate_row_of(size_t row, size_t rows_per_gate)
+{
+    if (row < rows_per_gate) return 0;
+    if ((row | rows_per_gate) >> 32) return row / rows_per_gate;
+    return uint32_t(row) / uint32_t(rows_per_gate);
+}
+
+// Means and reciprocal deviations of kR rows whose threads hold kI packets each; packets past the row hold zeros.
+template <int V, int kR, int kI, bool kWarp, bool kMean>
+__device__ __forceinline__ void row_statistics(const float (&v)[kR][kI][V], const bool (&on)[kI], int kind, float inv_cols, float eps,
+                                               RowSum<kR, kWarp>& sum, float (&mean)[kR], float (&rstd)[kR])
+{
+    float t[kR];
+    if (kMean && kind == kNormLayer) {
+#pragma unroll
+        for (int k = 0; k < kR; ++k) {
+            t[k] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kI; ++i)
+#pragma unroll
+                for (int e = 0; e < V; ++e) t[k] += v[k][i][e];
+        }
+        sum(t);
+#pragma unroll
+        for (int k = 0; k < kR; ++k) mean[k] = t[k] * inv_cols;
+    }
+#pragma unroll
+    for (int k = 0; k < kR; ++k) {
+        t[k] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kI; ++i)
+            if (!kMean || on[i])
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float c = kMean ? v[k][i][e] - mean[k] : v[k][i][e];
+                    t[k] = fmaf(c, c, t[k]);
+                }
+    }
+    sum(t);
+#pragma unroll
+    for (int k = 0; k < kR; ++k) rstd[k] = reciprocal_root(fmaf(t[k], inv_cols, eps));
+}
+
+// kR consecutive rows per CTA, or per warp (kWarp), kI packets of each per thread; cols a multiple of the packet, every pointer on a
+// 16-byte boundary.  kMean: one of the norms is LAYER.  For 16-bit storage instructions are what is short (49 per element at
+// first, 4.1 TB/s on [16384, 4096] bf16 against 6.0 for fp32 storage, where they are half as many per byte): so two rows share
+// each parameter's load and widening and each barrier, the normalisation is one multiply-add, and no 64-bit division is left.
+template <class S, int kI, int kR, bool kWarp, bool kMean>
+__global__ void __launch_bounds__(kI == 1 || kWarp ? 512 : 1024) norm_forward_kernel(const __grid_constant__ NormForwardArgs a)
 {
     constexpr int V = S::kVec;
-    __shared__ float buf[2][1][32];
+    __shared__ float buf[2][kR][32];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t lane = kWarp ? threadIdx.x & 31 : threadIdx.x, width = kWarp ? 32 : blockDim.x;
     const size_t per_cta = kWarp ? blockDim.x >> 5 : 1;
-    RowSum<1, kWarp> sum{buf, 0};
-    for (size_t row = blockIdx.x * per_cta + (kWarp ? threadIdx.x >> 5 : 0); row < a.rows; row += gridDim.x * per_cta) {
-        float u[I][V], r[I][V];
-        bool on[I];
+    RowSum<kR, kWarp> sum{buf, 0};
+    for (size_t turn = blockIdx.x * per_cta + (kWarp ? threadIdx.x >> 5 : 0); turn * kR < a.rows; turn += gridDim.x * per_cta) {
+        const size_t row = turn * kR;
+        uint4 ru[kR][kI], rr[kR][kI];
+        bool on[kI], there[kR];
 #pragma unroll
-        for (int i = 0; i < I; ++i) {
+        for (int k = 0; k < kR; ++k) there[k] = k == 0 || row + k < a.rows;
+#pragma unroll
+        for (int i = 0; i < kI; ++i) {
             const uint32_t p = lane + i * width;
             on[i] = p < a.packets;
 #pragma unroll
-            for (int e = 0; e < V; ++e) u[i][e] = r[i][e] = 0.0f;
-            if (on[i]) {
-                load_row_packet<S>(a.u, row, a.packets, p, u[i]);
-                if (a.r) load_row_packet<S>(a.r, row, a.packets, p, r[i]);
+            for (int k = 0; k < kR; ++k) {
+                ru[k][i] = rr[k][i] = make_uint4(0, 0, 0, 0);
+                if (on[i] && there[k]) {
+                    ru[k][i] = load_packet(static_cast<const uint4*>(a.u) + (row + k) * a.packets + p);
+                    if (a.r) rr[k][i] = load_packet(static_cast<const uint4*>(a.r) + (row + k) * a.packets + p);
+                }
             }
         }
-        float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (a.post != kNormNone) row_statistics<V, I, kWarp>(u, on, a.post, a.inv_cols, a.eps, sum, &st.x, &st.y);
-        const size_t gate_row = a.gate ? row / a.rows_per_gate : 0;
+        float v[kR][kI][V], mean[kR], rstd[kR], mean2[kR], rstd2[kR];
 #pragma unroll
-        for (int i = 0; i < I; ++i) {
+        for (int k = 0; k < kR; ++k) {
+            mean[k] = rstd[k] = mean2[k] = rstd2[k] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kI; ++i) S::unpack(ru[k][i], v[k][i]);
+        }
+        if (a.post != kNormNone) row_statistics<V, kR, kI, kWarp, kMean>(v, on, a.post, a.inv_cols, a.eps, sum, mean, rstd);
+        size_t gate_row[kR];
+#pragma unroll
+        for (int k = 0; k < kR; ++k) gate_row[k] = a.gate ? gate_row_of(row + k, a.rows_per_gate) : 0;
+#pragma unroll
+        for (int i = 0; i < kI; ++i) {
             const uint32_t p = lane + i * width;
             if (!on[i]) continue;
             float w[V];
             if (a.post != kNormNone) {
 #pragma unroll
-                for (int e = 0; e < V; ++e) u[i][e] = (u[i][e] - st.x) * st.y;
+                for (int k = 0; k < kR; ++k)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[k][i][e] = kMean ? (v[k][i][e] - mean[k]) * rstd[k] : v[k][i][e] * rstd[k];
                 if (a.post_gain) {
                     load_parameter<S>(a.post_gain, 0, a.packets, p, w);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) u[i][e] *= w[e];
+                    for (int k = 0; k < kR; ++k)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) v[k][i][e] *= w[e];
                 }
                 if (a.post_bias) {
                     load_parameter<S>(a.post_bias, 0, a.packets, p, w);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) u[i][e] += w[e];
+                    for (int k = 0; k < kR; ++k)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) v[k][i][e] += w[e];
                 }
             }
             if (a.gate) {
-                load_parameter<S>(a.gate, gate_row, a.packets, p, w);
 #pragma unroll
-                for (int e = 0; e < V; ++e) u[i][e] *= w[e];
+                for (int k = 0; k < kR; ++k) {
+                    if (k > 0 && !there[k]) continue;
+                    if (k == 0 || gate_row[k] != gate_row[0]) load_parameter<S>(a.gate, gate_row[k], a.packets, p, w);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[k][i][e] *= w[e];
+                }
             }
 #pragma unroll
-            for (int e = 0; e < V; ++e) r[i][e] = a.r ? fmaf(a.alpha, r[i][e], u[i][e]) : u[i][e];
-            if (a.s) store_packet<true>(static_cast<uint4*>(a.s) + row * a.packets + p, S::pack(r[i]));
+            for (int k = 0; k < kR; ++k) {
+                if (a.r) {
+                    S::unpack(rr[k][i], w);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[k][i][e] = fmaf(a.alpha, w[e], v[k][i][e]);
+                }
+                if (a.s && there[k]) store_packet<true>(static_cast<uint4*>(a.s) + (row + k) * a.packets + p, S::pack(v[k][i]));
+            }
         }
         if (a.pre != kNormNone) {
-            row_statistics<V, I, kWarp>(r, on, a.pre, a.inv_cols, a.eps, sum, &st.z, &st.w);
+            row_statistics<V, kR, kI, kWarp, kMean>(v, on, a.pre, a.inv_cols, a.eps, sum, mean2, rstd2);
 #pragma unroll
-            for (int i = 0; i < I; ++i) {
+            for (int i = 0; i < kI; ++i) {
                 const uint32_t p = lane + i * width;
                 if (!on[i]) continue;
                 float w[V];
 #pragma unroll
-                for (int e = 0; e < V; ++e) r[i][e] = (r[i][e] - st.z) * st.w;
+                for (int k = 0; k < kR; ++k)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[k][i][e] = kMean ? (v[k][i][e] - mean2[k]) * rstd2[k] : v[k][i][e] * rstd2[k];
                 if (a.pre_gain) {
                     load_parameter<S>(a.pre_gain, 0, a.packets, p, w);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) r[i][e] *= w[e];
+                    for (int k = 0; k < kR; ++k)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) v[k][i][e] *= w[e];
                 }
                 if (a.pre_bias) {
                     load_parameter<S>(a.pre_bias, 0, a.packets, p, w);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) r[i][e] += w[e];
+                    for (int k = 0; k < kR; ++k)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) v[k][i][e] += w[e];
                 }
-                store_packet<true>(static_cast<uint4*>(a.h) + row * a.packets + p, S::pack(r[i]));
+#pragma unroll
+                for (int k = 0; k < kR; ++k)
+                    if (there[k]) store_packet<true>(static_cast<uint4*>(a.h) + (row + k) * a.packets + p, S::pack(v[k][i]));
             }
         }
-        if (a.stats && lane == 0) a.stats[row] = st;
+        if (a.stats && lane == 0)
+#pragma unroll
+            for (int k = 0; k < kR; ++k)
+                if (there[k]) a.stats[row + k] = make_float4(mean[k], rstd[k], mean2[k], rstd2[k]);
     }
 }
+
+inline void norm_launch_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attr, size_t grid, unsigned block, cudaStream_t st)
+{
+    *cfg = cudaLaunchConfig_t{};
+    cfg->gridDim = dim3((unsigned)(grid < 0x7fffffffu ? grid : 0x7fffffffu));
+    cfg->blockDim = dim3(block);
+    cfg->stream = st;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg->attrs = attr;
+    cfg->numAttrs = 1;
+}
+
+constexpr int kNormMaxStages = 8;
+constexpr int kNormRingBytes = 200 * 1024;          // of an SM's shared memory, over its resident CTAs
+
+static __device__ unsigned g_norm_faults;           // CTAs whose wait ran out
 
 // Element access of the any-shape kernels.
 template <class S> __device__ __forceinline__ float at(const void* base, size_t i) { return S::load1(static_cast<const typename S::elem*>(base) + i); }
@@ -196,7 +273,7 @@ __global__ void __launch_bounds__(kBlock) norm_forward_any_kernel(const __grid_c
     __shared__ float buf[2][1][32];
     RowSum<1, false> sum{buf, 0};
     for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const size_t base = row * a.cols, gate = a.gate ? row / a.rows_per_gate * a.cols : 0;
+        const size_t base = row * a.cols, gate = a.gate ? gate_row_of(row, a.rows_per_gate) * a.cols : 0;
         float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         auto stream = [&](uint32_t c) {                              // s of one element, from u, r and u's statistics
             float v = at<S>(a.u, base + c);
@@ -222,7 +299,7 @@ __global__ void __launch_bounds__(kBlock) norm_forward_any_kernel(const __grid_c
             }
             sum(t);
             *mean = m;
-            *rstd = 1.0f / sqrtf(fmaf(t[0], a.inv_cols, a.eps));
+            *rstd = reciprocal_root(fmaf(t[0], a.inv_cols, a.eps));
         };
         if (a.post != kNormNone) {
             float m, q;
@@ -258,16 +335,23 @@ template <class S> inline bool norm_vector_ok(const void* const* p, int n, size_
     return true;
 }
 
-inline void norm_launch_config(cudaLaunchConfig_t* cfg, cudaLaunchAttribute* attr, size_t grid, unsigned block, cudaStream_t st)
+template <class S, bool kMean> cudaError_t launch_norm_forward_rows(const NormForwardArgs& a, cudaStream_t st)
 {
-    *cfg = cudaLaunchConfig_t{};
-    cfg->gridDim = dim3((unsigned)(grid < 0x7fffffffu ? grid : 0x7fffffffu));
-    cfg->blockDim = dim3(block);
-    cfg->stream = st;
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg->attrs = attr;
-    cfg->numAttrs = 1;
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[1];
+    if (a.packets <= 128) {                          // a warp per row (two when a lane has one packet of each), four warps
+        const size_t rows = a.packets <= 32 ? 8 : 4;
+        norm_launch_config(&cfg, attr, (a.rows + rows - 1) / rows, 128, st);
+        if (a.packets <= 32) return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 1, 2, true, kMean>, a);
+        if (a.packets <= 64) return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 2, 1, true, kMean>, a);
+        return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 4, 1, true, kMean>, a);
+    }
+    if (a.packets <= 512) {
+        norm_launch_config(&cfg, attr, (a.rows + 1) / 2, (a.packets + 31) / 32 * 32, st);
+        return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 1, 2, false, kMean>, a);
+    }
+    norm_launch_config(&cfg, attr, a.rows, ((a.packets + 1) / 2 + 31) / 32 * 32, st);
+    return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 2, 1, false, kMean>, a);
 }
 
 template <class S>
@@ -276,8 +360,6 @@ cudaError_t launch_norm_forward(const NormForwardArgs& in, cudaStream_t st)
     NormForwardArgs a = in;
     if (a.rows == 0 || a.cols == 0) return cudaSuccess;
     const void* p[9] = {a.u, a.r, a.post_gain, a.post_bias, a.gate, a.pre_gain, a.pre_bias, a.s, a.h};
-    cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute attr[1];
     a.packets = a.cols / S::kVec;
     // a row in registers: a warp of one to four packets per lane, or a CTA of one or two (up to 1024 threads)
     if (!norm_vector_ok<S>(p, 9, a.cols) || a.packets > 2048) {
@@ -288,15 +370,7 @@ cudaError_t launch_norm_forward(const NormForwardArgs& in, cudaStream_t st)
         norm_forward_any_kernel<S><<<(unsigned)(a.rows < cap ? a.rows : cap), kBlock, 0, st>>>(a);
         return cudaPeekAtLastError();
     }
-    if (a.packets <= 128) {
-        norm_launch_config(&cfg, attr, (a.rows + 3) / 4, 128, st);
-        if (a.packets <= 32) return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 1, true>, a);
-        if (a.packets <= 64) return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 2, true>, a);
-        return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 4, true>, a);
-    }
-    const unsigned block = ((a.packets + 1) / 2 + 31) / 32 * 32;
-    norm_launch_config(&cfg, attr, a.rows, block, st);
-    return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 2, false>, a);
+    return a.post == kNormLayer || a.pre == kNormLayer ? launch_norm_forward_rows<S, true>(a, st) : launch_norm_forward_rows<S, false>(a, st);
 }
 
 // ---------------------------------------------------------------- backward
@@ -318,11 +392,6 @@ __device__ __forceinline__ float* gate_target(const NormBackwardArgs& a, size_t 
 //   grad gate = g_post P + b_post Q, grad g_post += gate P, grad b_post += gate Q.
 // Measured on [32768, 4096] bf16, RMS norms and a gate (1.6 GB): next row prefetched into registers 418 us, this ring 355 us, these
 // sums 290 us.
-constexpr int kNormMaxStages = 8;
-constexpr int kNormRingBytes = 200 * 1024;          // of an SM's shared memory, over its resident CTAs
-
-static __device__ unsigned g_norm_faults;           // CTAs whose wait ran out
-
 // kI packets per thread, kR rows at a time; kGate: there is a gate; kFull: means and bias sums are kept too (without: RMS norms
 // and no bias sums).  Aligned rows of up to 512 kI packets.  Dynamic shared memory: `stages` rows of the tensors that are there.
 template <class S, int kI, int kR, bool kGate, bool kFull>
@@ -616,7 +685,7 @@ __global__ void __launch_bounds__(kBlock) norm_backward_means_kernel(const __gri
     __shared__ float buf[2][2][32];
     RowSum<2, false> sum{buf, 0};
     for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const size_t base = row * a.cols, gate = a.gate ? row / a.rows_per_gate * a.cols : 0;
+        const size_t base = row * a.cols, gate = a.gate ? gate_row_of(row, a.rows_per_gate) * a.cols : 0;
         const float4 st = a.stats[row];
         float t[2] = {0.0f, 0.0f};
         float4 out = make_float4(0.0f, 0.0f, 0.0f, 0.0f);

@@ -19,6 +19,7 @@
 // are in flight during the current row's two reductions.  Four tensors in, two out.
 #pragma once
 
+#include "nfad_hw.cuh"
 #include "nfad_internal.h"
 #include "nfad_norm_args.h"
 #include "nfad_stream.cuh"
@@ -261,6 +262,177 @@ constexpr int kNormRingBytes = 200 * 1024;          // of an SM's shared memory,
 
 static __device__ unsigned g_norm_faults;           // CTAs whose wait ran out
 
+// Many rows: a CTA stays and takes kR consecutive rows at a time, through a ring in shared memory that bulk copies of whole rows
+// fill several rows ahead, so that reads are in flight while a row waits for its reductions.  A thread owns the same columns of
+// every row: gain times gate is formed once (per gate row).  RMS norms without biases only: with means and biases the registers
+// leave one CTA to an SM, and its barriers show (150 against 141 us for a LayerNorm pair on [16384, 4096] bf16).
+// Measured on bf16 RMS pairs with a gate against a CTA per two rows: [16384, 4096] 93 (113) us, [8192, 8192] 94 (112), [4096, 6144]
+// 46.5 (50.6), [32768, 2048] 100 (102), and on fp32 [8192, 4096] 98 (87).
+template <class S, int kI, int kR>
+__global__ void __launch_bounds__(512, kI == 1 ? 2 : 1) norm_forward_ring_kernel(const __grid_constant__ NormForwardArgs a, int stages)
+{
+    constexpr int V = S::kVec;
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ float buf[2][kR][32];
+    __shared__ uint64_t full[kNormMaxStages];
+    __shared__ uint32_t gave_up_;
+    volatile uint32_t* gave_up = &gave_up_;
+    const uint32_t row_bytes = a.packets * 16, stage_bytes = a.r ? 2 * row_bytes : row_bytes;
+    const bool post = a.post != kNormNone, pre = a.pre != kNormNone;
+    if (threadIdx.x == 0) {
+        gave_up_ = 0;
+        for (int i = 0; i < stages; ++i) tc::barrier_init(tc::shared_address(&full[i]), 1);
+        tc::barrier_init_done();
+    }
+    __syncthreads();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    RowSum<kR, false> sum{buf, 0};
+    const size_t r0 = blockIdx.x * a.chunk_rows, r1 = r0 + a.chunk_rows < a.rows ? r0 + a.chunk_rows : a.rows;
+    if (r0 >= r1) return;
+    auto request = [&](size_t row, int stage) {                       // by one thread
+        const uint32_t bar = tc::shared_address(&full[stage]), dst = tc::shared_address(ring) + stage * stage_bytes;
+        tc::barrier_expect(bar, stage_bytes);
+        tc::load_run(dst, static_cast<const unsigned char*>(a.u) + row * row_bytes, row_bytes, bar);
+        if (a.r) tc::load_run(dst + row_bytes, static_cast<const unsigned char*>(a.r) + row * row_bytes, row_bytes, bar);
+    };
+    if (threadIdx.x == 0)
+        for (int i = 0; i < stages && r0 + i < r1; ++i) request(r0 + i, i);
+    uint32_t column[kI];
+    bool on[kI];
+    uint4 pre_gain[kI];
+    float gain[kI][V];                               // times the gate
+    size_t gate_row = a.gate ? r0 / a.rows_per_gate : 0, gate_end = a.gate ? (gate_row + 1) * a.rows_per_gate : a.rows;
+    auto parameter = [&](const void* base, size_t row, int i, float none, float (&v)[V]) {
+        if (base && on[i]) {
+            S::unpack(__ldg(static_cast<const uint4*>(base) + row * a.packets + column[i]), v);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = on[i] ? none : 0.0f;  // columns past the row: nothing
+        }
+    };
+    auto set_gate = [&]() {
+#pragma unroll
+        for (int i = 0; i < kI; ++i) {
+            float w[V];
+            parameter(post ? a.post_gain : nullptr, 0, i, 1.0f, gain[i]);
+            if (!a.gate) continue;
+            parameter(a.gate, gate_row, i, 1.0f, w);
+#pragma unroll
+            for (int e = 0; e < V; ++e) gain[i][e] *= w[e];
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < kI; ++i) {
+        column[i] = threadIdx.x + i * blockDim.x;
+        on[i] = column[i] < a.packets;
+        pre_gain[i] = on[i] && a.pre_gain ? __ldg(static_cast<const uint4*>(a.pre_gain) + column[i]) : make_uint4(0, 0, 0, 0);
+    }
+    set_gate();
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (size_t row = r0; row < r1 && ok; row += kR) {
+        float v[kR][kI][V], mean[kR], rstd[kR], rstd2[kR];            // mean stays 0
+        const bool two = kR == 1 || row + 1 < r1;
+        const unsigned char* at[kR];
+#pragma unroll
+        for (int k = 0; k < kR; ++k) {                               // stages are a multiple of kR: no wrap inside
+            if (k == 0 || two) tc::barrier_wait(tc::shared_address(&full[stage + k]), phase, gave_up);
+            at[k] = ring + (stage + k) * stage_bytes;
+            mean[k] = rstd2[k] = 0.0f;
+            rstd[k] = post ? 0.0f : 1.0f;
+        }
+        // A thread whose wait ran out carries on to this row's last barrier, behind which all learn of it together.
+        // Columns past the row and rows past the chunk read as zeros, and are not stored.
+        auto in_ring = [&](int k, uint32_t tensor_at, int i) {
+            return on[i] && (k == 0 || two) ? *reinterpret_cast<const uint4*>(at[k] + tensor_at + column[i] * 16) : make_uint4(0, 0, 0, 0);
+        };
+#pragma unroll
+        for (int k = 0; k < kR; ++k)
+#pragma unroll
+            for (int i = 0; i < kI; ++i) S::unpack(in_ring(k, 0, i), v[k][i]);
+        if (post) row_statistics<V, kR, kI, false, false>(v, on, a.post, a.inv_cols, a.eps, sum, mean, rstd);
+#pragma unroll
+        for (int k = 0; k < kR; ++k) {
+            if (k > 0 && !two) break;
+            if (row + k == gate_end) {
+                ++gate_row;
+                gate_end += a.rows_per_gate;
+                set_gate();
+            }
+#pragma unroll
+            for (int i = 0; i < kI; ++i) {
+                float w[V];
+                S::unpack(a.r ? in_ring(k, row_bytes, i) : make_uint4(0, 0, 0, 0), w);
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[k][i][e] = fmaf(v[k][i][e] * rstd[k], gain[i][e], a.alpha * w[e]);
+                if (a.s && on[i]) store_packet<true>(static_cast<uint4*>(a.s) + (row + k) * a.packets + column[i], S::pack(v[k][i]));
+            }
+        }
+        if (pre) row_statistics<V, kR, kI, false, false>(v, on, a.pre, a.inv_cols, a.eps, sum, mean, rstd2);
+        else __syncthreads();
+        if (blockDim.x == 32) __syncwarp();
+        ok = *gave_up == 0;
+        // every thread has read the rows: their places in the ring are free
+        if (threadIdx.x == 0 && ok) {
+#pragma unroll
+            for (int k = 0; k < kR; ++k)
+                if (row + k + stages < r1) request(row + k + stages, stage + k);
+        }
+        stage += kR;
+        if (stage >= stages) { stage = 0; phase ^= 1; }
+        if (pre) {
+#pragma unroll
+            for (int i = 0; i < kI; ++i) {
+                if (!on[i]) continue;
+                float w[V];
+                S::unpack(pre_gain[i], w);
+#pragma unroll
+                for (int k = 0; k < kR; ++k) {
+                    if (k > 0 && !two) break;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        v[k][i][e] *= rstd2[k];
+                        if (a.pre_gain) v[k][i][e] *= w[e];
+                    }
+                    store_packet<true>(static_cast<uint4*>(a.h) + (row + k) * a.packets + column[i], S::pack(v[k][i]));
+                }
+            }
+        }
+        if (a.stats && threadIdx.x < kR && (threadIdx.x == 0 || two)) {
+            const bool last = kR > 1 && threadIdx.x == 1;
+            a.stats[row + threadIdx.x] = make_float4(0.0f, post ? (last ? rstd[kR - 1] : rstd[0]) : 0.0f, 0.0f, last ? rstd2[kR - 1] : rstd2[0]);
+        }
+    }
+    if (!ok) {
+        // copies in flight land before the CTA's memory goes away
+        const long long t0 = clock64();
+        while (clock64() - t0 < tc::kWaitDrain) {}
+    }
+    if (threadIdx.x == 0 && gave_up_) atomicAdd(&g_norm_faults, 1u);
+}
+
+template <class S, int kI, int kR> cudaError_t launch_norm_forward_ring(const NormForwardArgs& in, unsigned block, int sms, cudaStream_t st)
+{
+    NormForwardArgs a = in;
+    auto kernel = norm_forward_ring_kernel<S, kI, kR>;
+    const unsigned per_sm = (kI == 1 ? 1024 : 512) / block;
+    const size_t row = size_t(a.packets) * 16 * (a.r ? 2 : 1);
+    size_t stages = kNormRingBytes / per_sm / row;
+    if (stages > kNormMaxStages) stages = kNormMaxStages;
+    stages -= stages % kR;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(stages * row));
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[1];
+    const size_t most = size_t(sms) * per_sm;
+    a.chunk_rows = (a.rows + most - 1) / most;
+    norm_launch_config(&cfg, attr, (a.rows + a.chunk_rows - 1) / a.chunk_rows, block, st);
+    cfg.dynamicSmemBytes = stages * row;
+    return cudaLaunchKernelEx(&cfg, kernel, a, int(stages));
+}
+
 // Element access of the any-shape kernels.
 template <class S> __device__ __forceinline__ float at(const void* base, size_t i) { return S::load1(static_cast<const typename S::elem*>(base) + i); }
 template <class S> __device__ __forceinline__ void put(void* base, size_t i, float v) { S::store1(static_cast<typename S::elem*>(base) + i, v); }
@@ -370,7 +542,16 @@ cudaError_t launch_norm_forward(const NormForwardArgs& in, cudaStream_t st)
         norm_forward_any_kernel<S><<<(unsigned)(a.rows < cap ? a.rows : cap), kBlock, 0, st>>>(a);
         return cudaPeekAtLastError();
     }
-    return a.post == kNormLayer || a.pre == kNormLayer ? launch_norm_forward_rows<S, true>(a, st) : launch_norm_forward_rows<S, false>(a, st);
+    const bool mean = a.post == kNormLayer || a.pre == kNormLayer;
+    // long rows, many of them, 16-bit storage (fp32 storage is not short of instructions), no means and no biases
+    if (S::kVec == 8 && !mean && !a.post_bias && !a.pre_bias && a.packets >= 384 && a.packets <= 1024 && a.rows >= 2048) {
+        DeviceInfo di;
+        cudaError_t e = device_info(&di);
+        if (e != cudaSuccess) return e;
+        if (a.packets <= 512) return launch_norm_forward_ring<S, 1, 2>(a, (a.packets + 31) / 32 * 32, di.sm_count, st);
+        return launch_norm_forward_ring<S, 2, 1>(a, ((a.packets + 1) / 2 + 31) / 32 * 32, di.sm_count, st);
+    }
+    return mean ? launch_norm_forward_rows<S, true>(a, st) : launch_norm_forward_rows<S, false>(a, st);
 }
 
 // ---------------------------------------------------------------- backward
@@ -382,6 +563,36 @@ __device__ __forceinline__ float* gate_target(const NormBackwardArgs& a, size_t 
     const size_t g0 = gate_row * a.rows_per_gate, g1 = g0 + a.rows_per_gate;
     if (g0 >= r0 && g1 <= r1) return a.grad_gate + gate_row * a.cols;
     return a.partial + (size_t(a.chunks) * kNormSums + chunk * 2 + (g0 <= r0 ? 0 : 1)) * a.cols;
+}
+
+// Two neighbours at a time: Blackwell multiplies and adds two fp32 values in one instruction.  Worth 3 % here, where most of the work
+// is multiply-adds (290 -> 282 us for [32768, 4096] bf16); the forward kernels lose by it (113 -> 120 us), as their pairs have to be
+// brought together first.
+template <class S> __device__ __forceinline__ void widen(const uint4& p, float2 (&v)[S::kVec / 2])
+{
+    float w[S::kVec];
+    S::unpack(p, w);
+#pragma unroll
+    for (int e = 0; e < S::kVec / 2; ++e) v[e] = make_float2(w[2 * e], w[2 * e + 1]);
+}
+template <class S> __device__ __forceinline__ uint4 narrow(const float2 (&v)[S::kVec / 2])
+{
+    float w[S::kVec];
+#pragma unroll
+    for (int e = 0; e < S::kVec / 2; ++e) { w[2 * e] = v[e].x; w[2 * e + 1] = v[e].y; }
+    return S::pack(w);
+}
+__device__ __forceinline__ float2 twice(float a) { return make_float2(a, a); }
+using hw::add2;
+using hw::fma2;
+using hw::mul2;
+
+// (x - mean) rstd
+template <bool kMean, int P> __device__ __forceinline__ void normalise(float2 (&v)[P], float mean, float rstd)
+{
+    const float2 m = twice(-mean), r = twice(rstd);
+#pragma unroll
+    for (int e = 0; e < P; ++e) v[e] = mul2(kMean ? add2(v[e], m) : v[e], r);
 }
 
 // Rows travel through a ring in shared memory: bulk copies of whole rows (and of their statistics), several rows ahead, so that
@@ -397,7 +608,7 @@ __device__ __forceinline__ float* gate_target(const NormBackwardArgs& a, size_t 
 template <class S, int kI, int kR, bool kGate, bool kFull>
 __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constant__ NormBackwardArgs a, int stages)
 {
-    constexpr int V = S::kVec, kSums = kFull ? 2 : 1;
+    constexpr int P = S::kVec / 2, kSums = kFull ? 2 : 1;
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ float buf[2][kSums * kR][32];
     __shared__ uint64_t full[kNormMaxStages];
@@ -436,32 +647,32 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
     uint32_t column[kI];
     bool on[kI];
     uint4 pre_gain[kI];
-    float both[kI][V];                               // gate g_post
-    float acc_pre[kI][V], acc_pre_bias[kFull ? kI : 1][V], acc_p[kI][V], acc_q[kFull ? kI : 1][V];
-    float acc_post[kGate ? kI : 1][V], acc_post_bias[kGate && kFull ? kI : 1][V];
+    float2 both[kI][P];                              // gate g_post
+    float2 acc_pre[kI][P], acc_pre_bias[kFull ? kI : 1][P], acc_p[kI][P], acc_q[kFull ? kI : 1][P];
+    float2 acc_post[kGate ? kI : 1][P], acc_post_bias[kGate && kFull ? kI : 1][P];
     size_t gate_row = kGate ? r0 / a.rows_per_gate : 0, gate_end = (gate_row + 1) * a.rows_per_gate;
     // a parameter's packet of this thread's columns; `none` when there is no such parameter
-    auto parameter = [&](const void* base, size_t row, int i, float none, float (&v)[V]) {
+    auto parameter = [&](const void* base, size_t row, int i, float none, float2 (&v)[P]) {
         if (base && on[i]) {
-            S::unpack(__ldg(static_cast<const uint4*>(base) + row * a.packets + column[i]), v);
+            widen<S>(__ldg(static_cast<const uint4*>(base) + row * a.packets + column[i]), v);
         } else {
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = none;
+            for (int e = 0; e < P; ++e) v[e] = twice(none);
         }
     };
     auto set_both = [&]() {
 #pragma unroll
         for (int i = 0; i < kI; ++i) {
-            float w[V];
+            float2 w[P];
             parameter(post ? a.post_gain : nullptr, 0, i, 1.0f, both[i]);
             if (kGate) {
                 parameter(a.gate, gate_row, i, 1.0f, w);
 #pragma unroll
-                for (int e = 0; e < V; ++e) both[i][e] *= w[e];
+                for (int e = 0; e < P; ++e) both[i][e] = mul2(both[i][e], w[e]);
             }
             if (!on[i])                              // a mean taken from a column past the row would leave something there
 #pragma unroll
-                for (int e = 0; e < V; ++e) both[i][e] = 0.0f;
+                for (int e = 0; e < P; ++e) both[i][e] = twice(0.0f);
         }
     };
 #pragma unroll
@@ -470,11 +681,11 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
         on[i] = column[i] < a.packets;
         pre_gain[i] = on[i] && a.pre_gain ? __ldg(static_cast<const uint4*>(a.pre_gain) + column[i]) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            acc_pre[i][e] = acc_p[i][e] = 0.0f;
-            if (kFull) acc_pre_bias[i][e] = acc_q[i][e] = 0.0f;
-            if (kGate) acc_post[i][e] = 0.0f;
-            if (kGate && kFull) acc_post_bias[i][e] = 0.0f;
+        for (int e = 0; e < P; ++e) {
+            acc_pre[i][e] = acc_p[i][e] = twice(0.0f);
+            if (kFull) acc_pre_bias[i][e] = acc_q[i][e] = twice(0.0f);
+            if (kGate) acc_post[i][e] = twice(0.0f);
+            if (kGate && kFull) acc_post_bias[i][e] = twice(0.0f);
         }
     }
     set_both();
@@ -482,19 +693,19 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
     auto hand_over_gate = [&]() {
 #pragma unroll
         for (int i = 0; i < kI; ++i) {
-            float gate[V], gain[V], bias[V];
+            float2 gate[P], gain[P], bias[P];
             parameter(a.gate, gate_row, i, 0.0f, gate);
             parameter(post ? a.post_gain : nullptr, 0, i, 1.0f, gain);
             parameter(post ? a.post_bias : nullptr, 0, i, 0.0f, bias);
-            float* dst = on[i] && a.grad_gate ? gate_target(a, blockIdx.x, r0, r1, gate_row) + size_t(column[i]) * V : nullptr;
+            float2* dst = on[i] && a.grad_gate ? reinterpret_cast<float2*>(gate_target(a, blockIdx.x, r0, r1, gate_row)) + size_t(column[i]) * P : nullptr;
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                if (dst) dst[e] = kFull ? fmaf(gain[e], acc_p[i][e], bias[e] * acc_q[i][e]) : gain[e] * acc_p[i][e];
-                acc_post[i][e] = fmaf(gate[e], acc_p[i][e], acc_post[i][e]);
-                acc_p[i][e] = 0.0f;
+            for (int e = 0; e < P; ++e) {
+                if (dst) dst[e] = kFull ? fma2(gain[e], acc_p[i][e], mul2(bias[e], acc_q[i][e])) : mul2(gain[e], acc_p[i][e]);
+                acc_post[i][e] = fma2(gate[e], acc_p[i][e], acc_post[i][e]);
+                acc_p[i][e] = twice(0.0f);
                 if constexpr (kFull) {
-                    acc_post_bias[i][e] = fmaf(gate[e], acc_q[i][e], acc_post_bias[i][e]);
-                    acc_q[i][e] = 0.0f;
+                    acc_post_bias[i][e] = fma2(gate[e], acc_q[i][e], acc_post_bias[i][e]);
+                    acc_q[i][e] = twice(0.0f);
                 }
             }
         }
@@ -504,7 +715,8 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
     uint32_t phase = 0;
     bool ok = true;
     for (size_t row = r0; row < r1 && ok; row += kR) {
-        float ds[kR][kI][V], hat[kR][kI][V], t[kSums * kR];
+        float2 ds[kR][kI][P], hat[kR][kI][P], t2[kSums * kR];
+        float t[kSums * kR];
         float4 st[kR];
         const bool two = kR == 1 || row + 1 < r1;
         const unsigned char* at[kR];
@@ -520,40 +732,42 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
             return on[i] && (k == 0 || two) ? *reinterpret_cast<const uint4*>(at[k] + tensor_at + column[i] * 16) : make_uint4(0, 0, 0, 0);
         };
 #pragma unroll
-        for (int k = 0; k < kSums * kR; ++k) t[k] = 0.0f;
+        for (int k = 0; k < kSums * kR; ++k) t2[k] = twice(0.0f);
         if (pre) {
             // d = dh g_pre and s^; their sums
 #pragma unroll
             for (int i = 0; i < kI; ++i) {
-                float w[V];
-                S::unpack(pre_gain[i], w);
+                float2 w[P];
+                widen<S>(pre_gain[i], w);
 #pragma unroll
                 for (int k = 0; k < kR; ++k) {
-                    S::unpack(in_ring(k, 0, i), ds[k][i]);
-                    S::unpack(in_ring(k, row_bytes, i), hat[k][i]);
+                    widen<S>(in_ring(k, 0, i), ds[k][i]);
+                    widen<S>(in_ring(k, row_bytes, i), hat[k][i]);
+                    normalise<kFull>(hat[k][i], st[k].z, st[k].w);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        hat[k][i][e] = kFull ? (hat[k][i][e] - st[k].z) * st[k].w : hat[k][i][e] * st[k].w;
-                        acc_pre[i][e] = fmaf(ds[k][i][e], hat[k][i][e], acc_pre[i][e]);
-                        if (kFull) acc_pre_bias[i][e] += ds[k][i][e];
-                        if (a.pre_gain) ds[k][i][e] *= w[e];
-                        t[kSums * k] = fmaf(ds[k][i][e], hat[k][i][e], t[kSums * k]);
-                        if (kFull) t[kSums * k + 1] += ds[k][i][e];
+                    for (int e = 0; e < P; ++e) {
+                        acc_pre[i][e] = fma2(ds[k][i][e], hat[k][i][e], acc_pre[i][e]);
+                        if (kFull) acc_pre_bias[i][e] = add2(acc_pre_bias[i][e], ds[k][i][e]);
+                        if (a.pre_gain) ds[k][i][e] = mul2(ds[k][i][e], w[e]);
+                        t2[kSums * k] = fma2(ds[k][i][e], hat[k][i][e], t2[kSums * k]);
+                        if (kFull) t2[kSums * k + 1] = add2(t2[kSums * k + 1], ds[k][i][e]);
                     }
                 }
             }
+#pragma unroll
+            for (int k = 0; k < kSums * kR; ++k) t[k] = t2[k].x + t2[k].y;
             sum(t);
 #pragma unroll
             for (int k = 0; k < kR; ++k) {
-                const float q = t[kSums * k] * a.inv_cols, m = kFull && a.pre == kNormLayer ? t[kSums * k + 1] * a.inv_cols : 0.0f;
+                const float2 q = twice(-t[kSums * k] * a.inv_cols), m = twice(kFull && a.pre == kNormLayer ? -t[kSums * k + 1] * a.inv_cols : 0.0f);
 #pragma unroll
                 for (int i = 0; i < kI; ++i) {
-                    float v[V];
-                    S::unpack(a.grad_s ? in_ring(k, at_gs, i) : make_uint4(0, 0, 0, 0), v);
+                    float2 v[P];
+                    widen<S>(a.grad_s ? in_ring(k, at_gs, i) : make_uint4(0, 0, 0, 0), v);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        const float c = fmaf(-hat[k][i][e], q, kFull ? ds[k][i][e] - m : ds[k][i][e]);
-                        ds[k][i][e] = fmaf(st[k].w, c, v[e]);
+                    for (int e = 0; e < P; ++e) {
+                        const float2 c = fma2(hat[k][i][e], q, kFull ? add2(ds[k][i][e], m) : ds[k][i][e]);
+                        ds[k][i][e] = fma2(twice(st[k].w), c, v[e]);
                     }
                 }
             }
@@ -561,11 +775,11 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
 #pragma unroll
             for (int k = 0; k < kR; ++k)
 #pragma unroll
-                for (int i = 0; i < kI; ++i) S::unpack(in_ring(k, at_gs, i), ds[k][i]);
+                for (int i = 0; i < kI; ++i) widen<S>(in_ring(k, at_gs, i), ds[k][i]);
         }
         // grad_r; then u^, P, Q and e = gate g_post ds, and the sums of the row
 #pragma unroll
-        for (int k = 0; k < kSums * kR; ++k) t[k] = 0.0f;
+        for (int k = 0; k < kSums * kR; ++k) t2[k] = twice(0.0f);
 #pragma unroll
         for (int k = 0; k < kR; ++k) {
             if (k > 0 && !two) break;
@@ -578,25 +792,27 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
 #pragma unroll
             for (int i = 0; i < kI; ++i) {
                 if (a.grad_r && on[i]) {
-                    float v[V];
+                    float2 v[P];
 #pragma unroll
-                    for (int e = 0; e < V; ++e) v[e] = a.alpha * ds[k][i][e];
-                    store_packet<true>(static_cast<uint4*>(a.grad_r) + (row + k) * a.packets + column[i], S::pack(v));
+                    for (int e = 0; e < P; ++e) v[e] = mul2(twice(a.alpha), ds[k][i][e]);
+                    store_packet<true>(static_cast<uint4*>(a.grad_r) + (row + k) * a.packets + column[i], narrow<S>(v));
                 }
                 if (post || kGate) {
-                    S::unpack(in_ring(k, at_u, i), hat[k][i]);
+                    widen<S>(in_ring(k, at_u, i), hat[k][i]);
+                    if (post) normalise<kFull>(hat[k][i], st[k].x, st[k].y);
 #pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        if (post) hat[k][i][e] = kFull ? (hat[k][i][e] - st[k].x) * st[k].y : hat[k][i][e] * st[k].y;
-                        acc_p[i][e] = fmaf(ds[k][i][e], hat[k][i][e], acc_p[i][e]);
-                        if (kFull) acc_q[i][e] += ds[k][i][e];
-                        ds[k][i][e] *= both[i][e];
-                        t[kSums * k] = fmaf(ds[k][i][e], hat[k][i][e], t[kSums * k]);
-                        if (kFull) t[kSums * k + 1] += ds[k][i][e];
+                    for (int e = 0; e < P; ++e) {
+                        acc_p[i][e] = fma2(ds[k][i][e], hat[k][i][e], acc_p[i][e]);
+                        if (kFull) acc_q[i][e] = add2(acc_q[i][e], ds[k][i][e]);
+                        ds[k][i][e] = mul2(ds[k][i][e], both[i][e]);
+                        t2[kSums * k] = fma2(ds[k][i][e], hat[k][i][e], t2[kSums * k]);
+                        if (kFull) t2[kSums * k + 1] = add2(t2[kSums * k + 1], ds[k][i][e]);
                     }
                 }
             }
         }
+#pragma unroll
+        for (int k = 0; k < kSums * kR; ++k) t[k] = t2[k].x + t2[k].y;
         if (post) sum(t);
         else __syncthreads();
         if (blockDim.x == 32) __syncwarp();
@@ -612,13 +828,14 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
 #pragma unroll
         for (int k = 0; k < kR; ++k) {
             if (k > 0 && !two) break;
-            const float q = t[kSums * k] * a.inv_cols, m = kFull && a.post == kNormLayer ? t[kSums * k + 1] * a.inv_cols : 0.0f;
+            const float2 q = twice(-t[kSums * k] * a.inv_cols), m = twice(kFull && a.post == kNormLayer ? -t[kSums * k + 1] * a.inv_cols : 0.0f);
 #pragma unroll
             for (int i = 0; i < kI; ++i) {
                 if (post)
 #pragma unroll
-                    for (int e = 0; e < V; ++e) ds[k][i][e] = st[k].y * fmaf(-hat[k][i][e], q, kFull ? ds[k][i][e] - m : ds[k][i][e]);
-                if (on[i]) store_packet<true>(static_cast<uint4*>(a.grad_u) + (row + k) * a.packets + column[i], S::pack(ds[k][i]));
+                    for (int e = 0; e < P; ++e)
+                        ds[k][i][e] = mul2(twice(st[k].y), fma2(hat[k][i][e], q, kFull ? add2(ds[k][i][e], m) : ds[k][i][e]));
+                if (on[i]) store_packet<true>(static_cast<uint4*>(a.grad_u) + (row + k) * a.packets + column[i], narrow<S>(ds[k][i]));
             }
         }
     }
@@ -631,12 +848,12 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
 #pragma unroll
     for (int i = 0; i < kI; ++i) {
         if (!on[i]) continue;
-        const size_t col = size_t(column[i]) * V;
-        auto keep = [&](int k, const float (&v)[V]) {
+        const size_t col = size_t(column[i]) * S::kVec;
+        auto keep = [&](int k, const float2 (&v)[P]) {
             if (!a.sums[k]) return;
             float4* dst = reinterpret_cast<float4*>(a.partial + (size_t(blockIdx.x) * kNormSums + k) * a.cols + col);
 #pragma unroll
-            for (int e = 0; e < V; e += 4) dst[e / 4] = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+            for (int e = 0; e < P; e += 2) dst[e / 2] = make_float4(v[e].x, v[e].y, v[e + 1].x, v[e + 1].y);
         };
         keep(kSumPreGain, acc_pre[i]);
         if constexpr (kGate) keep(kSumPostGain, acc_post[i]);
@@ -846,7 +1063,8 @@ cudaError_t launch_norm_backward_kernel(const NormBackwardArgs& a, const NormPla
 template <class S, int kI, int kR> cudaError_t launch_norm_backward_rows(const NormBackwardArgs& a, const NormPlan& p, cudaStream_t st)
 {
     const bool more = a.sums[kSumPreBias] || a.sums[kSumPostBias] || a.pre == kNormLayer || a.post == kNormLayer;
-    if (a.gate) return more ? launch_norm_backward_kernel<S, kI, kR, true, true>(a, p, st) : launch_norm_backward_kernel<S, kI, kR, true, false>(a, p, st);
+    // six sums for each column beside two rows spill (310 us for a LayerNorm pair with a gate on [16384, 4096] bf16): one row then
+    if (a.gate) return more ? launch_norm_backward_kernel<S, kI, 1, true, true>(a, p, st) : launch_norm_backward_kernel<S, kI, kR, true, false>(a, p, st);
     return more ? launch_norm_backward_kernel<S, kI, kR, false, true>(a, p, st) : launch_norm_backward_kernel<S, kI, kR, false, false>(a, p, st);
 }
 

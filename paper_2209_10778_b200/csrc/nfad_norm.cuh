@@ -867,38 +867,70 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
     if (threadIdx.x == 0 && gave_up_) atomicAdd(&g_norm_faults, 1u);
 }
 
-// Any shape, first kernel: the four row means that the gradients need, (mean d, mean d s^, mean e, mean e u^).
-template <class S> struct NormElement {
-    float d, shat, ds, uhat, a, da;
+// Any shape: two kernels.  A thread takes one column at a time, or a packet of them where rows are aligned (kVec: rows too long for
+// registers).
+template <class S, bool kVec> struct NormLanes {
+    static constexpr int V = kVec ? S::kVec : 1;
+    static __device__ __forceinline__ void load(const void* base, size_t i, float (&v)[V])
+    {
+        if constexpr (kVec) S::unpack(*reinterpret_cast<const uint4*>(static_cast<const typename S::elem*>(base) + i), v);
+        else v[0] = at<S>(base, i);
+    }
+    static __device__ __forceinline__ void store(void* base, size_t i, const float (&v)[V])
+    {
+        if constexpr (kVec) *reinterpret_cast<uint4*>(static_cast<typename S::elem*>(base) + i) = S::pack(v);
+        else put<S>(base, i, v[0]);
+    }
+    // everything of these columns up to da, from the row's statistics and (for ds) its first two means
+    float d[V], shat[V], ds[V], uhat[V], a[V], da[V], gain[V];
+    __device__ __forceinline__ void read(const NormBackwardArgs& g, size_t base, size_t gate, size_t c, float4 st, float m, float q)
+    {
+        float w[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) d[e] = shat[e] = ds[e] = uhat[e] = 0.0f, gain[e] = 1.0f;
+        if (g.grad_s) load(g.grad_s, base + c, ds);
+        if (g.pre != kNormNone) {
+            load(g.grad_h, base + c, d);
+            load(g.s, base + c, shat);
+#pragma unroll
+            for (int e = 0; e < V; ++e) w[e] = 1.0f;
+            if (g.pre_gain) load(g.pre_gain, c, w);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                shat[e] = (shat[e] - st.z) * st.w;
+                ds[e] = fmaf(st.w, d[e] * w[e] - m - shat[e] * q, ds[e]);
+            }
+        }
+        if (g.u) load(g.u, base + c, uhat);
+        if (g.post != kNormNone) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) uhat[e] = (uhat[e] - st.x) * st.y;
+            if (g.post_gain) load(g.post_gain, c, gain);
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            a[e] = uhat[e] * gain[e];
+            da[e] = ds[e];
+        }
+        if (g.gate) {
+            if (g.post != kNormNone && g.post_bias) {
+                load(g.post_bias, c, w);
+#pragma unroll
+                for (int e = 0; e < V; ++e) a[e] += w[e];
+            }
+            load(g.gate, gate + c, w);
+#pragma unroll
+            for (int e = 0; e < V; ++e) da[e] *= w[e];
+        }
+    }
 };
 
-// everything of one element up to e = da g_post, from the row's statistics and (for ds) its first two means
-template <class S>
-__device__ __forceinline__ NormElement<S> norm_element(const NormBackwardArgs& a, size_t base, size_t gate, uint32_t c, float4 st, float m, float q)
-{
-    NormElement<S> x;
-    x.d = x.shat = 0.0f;
-    x.ds = a.grad_s ? at<S>(a.grad_s, base + c) : 0.0f;
-    if (a.pre != kNormNone) {
-        x.d = at<S>(a.grad_h, base + c);
-        x.shat = (at<S>(a.s, base + c) - st.z) * st.w;
-        const float d = a.pre_gain ? x.d * at<S>(a.pre_gain, c) : x.d;
-        x.ds = fmaf(st.w, d - m - x.shat * q, x.ds);
-    }
-    x.uhat = a.u ? at<S>(a.u, base + c) : 0.0f;
-    if (a.post != kNormNone) x.uhat = (x.uhat - st.x) * st.y;
-    x.a = x.uhat;
-    if (a.post != kNormNone) {
-        if (a.post_gain) x.a *= at<S>(a.post_gain, c);
-        if (a.post_bias) x.a += at<S>(a.post_bias, c);
-    }
-    x.da = a.gate ? x.ds * at<S>(a.gate, gate + c) : x.ds;
-    return x;
-}
-
-template <class S>
+// First kernel: the four row means that the gradients need, (mean d, mean d s^, mean e, mean e u^).
+template <class S, bool kVec>
 __global__ void __launch_bounds__(kBlock) norm_backward_means_kernel(const __grid_constant__ NormBackwardArgs a)
 {
+    using L = NormLanes<S, kVec>;
+    constexpr int V = L::V;
     __shared__ float buf[2][2][32];
     RowSum<2, false> sum{buf, 0};
     for (size_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -907,11 +939,19 @@ __global__ void __launch_bounds__(kBlock) norm_backward_means_kernel(const __gri
         float t[2] = {0.0f, 0.0f};
         float4 out = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (a.pre != kNormNone) {
-            for (uint32_t c = threadIdx.x; c < a.cols; c += kBlock) {
-                float d = at<S>(a.grad_h, base + c);
-                if (a.pre_gain) d *= at<S>(a.pre_gain, c);
-                t[0] += d;
-                t[1] = fmaf(d, (at<S>(a.s, base + c) - st.z) * st.w, t[1]);
+            for (size_t c = threadIdx.x * V; c < a.cols; c += kBlock * V) {
+                float d[V], x[V], w[V];
+                L::load(a.grad_h, base + c, d);
+                L::load(a.s, base + c, x);
+#pragma unroll
+                for (int e = 0; e < V; ++e) w[e] = 1.0f;
+                if (a.pre_gain) L::load(a.pre_gain, c, w);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    d[e] *= w[e];
+                    t[0] += d[e];
+                    t[1] = fmaf(d[e], (x[e] - st.z) * st.w, t[1]);
+                }
             }
             sum(t);
             out.x = a.pre == kNormLayer ? t[0] * a.inv_cols : 0.0f;
@@ -919,11 +959,15 @@ __global__ void __launch_bounds__(kBlock) norm_backward_means_kernel(const __gri
         }
         if (a.post != kNormNone) {
             t[0] = t[1] = 0.0f;
-            for (uint32_t c = threadIdx.x; c < a.cols; c += kBlock) {
-                const NormElement<S> x = norm_element<S>(a, base, gate, c, st, out.x, out.y);
-                const float e = a.post_gain ? x.da * at<S>(a.post_gain, c) : x.da;
-                t[0] += e;
-                t[1] = fmaf(e, x.uhat, t[1]);
+            for (size_t c = threadIdx.x * V; c < a.cols; c += kBlock * V) {
+                L x;
+                x.read(a, base, gate, c, st, out.x, out.y);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float v = x.da[e] * x.gain[e];
+                    t[0] += v;
+                    t[1] = fmaf(v, x.uhat[e], t[1]);
+                }
             }
             sum(t);
             out.z = a.post == kNormLayer ? t[0] * a.inv_cols : 0.0f;
@@ -933,44 +977,72 @@ __global__ void __launch_bounds__(kBlock) norm_backward_means_kernel(const __gri
     }
 }
 
-// Any shape, second kernel: a thread owns one column of a chunk of rows, writes the two gradients and its column's sums.
-template <class S>
+// Second kernel: a thread owns its columns of a chunk of rows, writes the two gradients and its columns' sums.
+template <class S, bool kVec>
 __global__ void __launch_bounds__(kBlock) norm_backward_columns_kernel(const __grid_constant__ NormBackwardArgs a)
 {
-    const size_t col = size_t(blockIdx.x) * kBlock + threadIdx.x;
-    if (col >= a.cols) return;
-    const uint32_t c = uint32_t(col);
+    using L = NormLanes<S, kVec>;
+    constexpr int V = L::V;
+    const size_t c = (size_t(blockIdx.x) * kBlock + threadIdx.x) * V;
+    if (c >= a.cols) return;
     const size_t r0 = blockIdx.y * a.chunk_rows, r1 = r0 + a.chunk_rows < a.rows ? r0 + a.chunk_rows : a.rows;
     if (r0 >= r1) return;
-    float acc[kNormSums] = {0.0f, 0.0f, 0.0f, 0.0f}, accg = 0.0f;
+    float acc[kNormSums][V], accg[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+#pragma unroll
+        for (int k = 0; k < kNormSums; ++k) acc[k][e] = 0.0f;
+        accg[e] = 0.0f;
+    }
     size_t gate_row = a.gate ? r0 / a.rows_per_gate : 0, gate_end = (gate_row + 1) * a.rows_per_gate;
+    auto hand_over_gate = [&]() {
+        float* dst = a.grad_gate ? gate_target(a, blockIdx.y, r0, r1, gate_row) + c : nullptr;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            if (dst) dst[e] = accg[e];
+            accg[e] = 0.0f;
+        }
+    };
     for (size_t row = r0; row < r1; ++row) {
         if (a.gate && row == gate_end) {
-            if (a.grad_gate) gate_target(a, blockIdx.y, r0, r1, gate_row)[c] = accg;
-            accg = 0.0f;
+            hand_over_gate();
             ++gate_row;
             gate_end += a.rows_per_gate;
         }
-        const float4 st = a.stats[row], mean = a.row_means[row];
+        const float4 st = __ldg(a.stats + row), mean = a.row_means[row];
         const size_t base = row * a.cols;
-        const NormElement<S> x = norm_element<S>(a, base, gate_row * a.cols, c, st, mean.x, mean.y);
-        acc[kSumPreGain] = fmaf(x.d, x.shat, acc[kSumPreGain]);
-        acc[kSumPreBias] += x.d;
-        acc[kSumPostGain] = fmaf(x.da, x.uhat, acc[kSumPostGain]);
-        acc[kSumPostBias] += x.da;
-        accg = fmaf(x.ds, x.a, accg);
-        float du = x.da;
-        if (a.post != kNormNone) {
-            const float e = a.post_gain ? du * at<S>(a.post_gain, c) : du;
-            du = st.y * (e - mean.z - x.uhat * mean.w);
+        L x;
+        x.read(a, base, gate_row * a.cols, c, st, mean.x, mean.y);
+        float gr[V], gu[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            acc[kSumPreGain][e] = fmaf(x.d[e], x.shat[e], acc[kSumPreGain][e]);
+            acc[kSumPreBias][e] += x.d[e];
+            acc[kSumPostGain][e] = fmaf(x.da[e], x.uhat[e], acc[kSumPostGain][e]);
+            acc[kSumPostBias][e] += x.da[e];
+            accg[e] = fmaf(x.ds[e], x.a[e], accg[e]);
+            gr[e] = a.alpha * x.ds[e];
+            gu[e] = a.post != kNormNone ? st.y * (x.da[e] * x.gain[e] - mean.z - x.uhat[e] * mean.w) : x.da[e];
         }
-        if (a.grad_r) put<S>(a.grad_r, base + c, a.alpha * x.ds);
-        put<S>(a.grad_u, base + c, du);
+        if (a.grad_r) L::store(a.grad_r, base + c, gr);
+        L::store(a.grad_u, base + c, gu);
     }
 #pragma unroll
     for (int k = 0; k < kNormSums; ++k)
-        if (a.sums[k]) a.partial[(size_t(blockIdx.y) * kNormSums + k) * a.cols + c] = acc[k];
-    if (a.grad_gate) gate_target(a, blockIdx.y, r0, r1, gate_row)[c] = accg;
+        if (a.sums[k])
+#pragma unroll
+            for (int e = 0; e < V; ++e) a.partial[(size_t(blockIdx.y) * kNormSums + k) * a.cols + c + e] = acc[k][e];
+    if (a.gate) hand_over_gate();
+}
+
+template <class S, bool kVec> cudaError_t launch_norm_backward_any(const NormBackwardArgs& a, int sms, cudaStream_t st)
+{
+    const size_t cap = size_t(sms) * 8, lanes = size_t(kBlock) * NormLanes<S, kVec>::V;
+    norm_backward_means_kernel<S, kVec><<<(unsigned)(a.rows < cap ? a.rows : cap), kBlock, 0, st>>>(a);
+    cudaError_t e = cudaPeekAtLastError();
+    if (e != cudaSuccess) return e;
+    norm_backward_columns_kernel<S, kVec><<<dim3(unsigned((a.cols + lanes - 1) / lanes), a.chunks), kBlock, 0, st>>>(a);
+    return cudaPeekAtLastError();
 }
 
 // Adds the chunks' sums: blockIdx.y < kNormSums one of the parameters', beyond that a gate row's.  32 columns times 32 runs
@@ -1027,7 +1099,8 @@ template <class S> inline NormPlan norm_plan(size_t rows, size_t cols, int sm_co
     p.packets_per_thread = packets <= 512 ? 1 : 2;
     size_t block = ((packets + p.packets_per_thread - 1) / p.packets_per_thread + 31) / 32 * 32;
     p.block = unsigned(block < 512 ? block : 512);
-    const size_t target = size_t(sm_count) * (512 / p.block);
+    // CTAs that stay, one per 512 threads of an SM; rows longer than their registers go by strips of columns, several to a chunk
+    const size_t target = size_t(sm_count) * (packets <= 1024 ? 512 / p.block : 1);
     size_t chunks = rows < target ? rows : target;
     if (chunks == 0) chunks = 1;
     p.chunk_rows = (rows + chunks - 1) / chunks;
@@ -1091,15 +1164,10 @@ cudaError_t launch_norm_backward(const NormBackwardArgs& in, void* scratch, cuda
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];
     // the row in registers, two packets a thread at most (more spill beside the column sums)
-    if (norm_vector_ok<S>(ptr, 10, a.cols) && a.packets <= 1024) {
-        e = p.packets_per_thread == 1 ? launch_norm_backward_rows<S, 1, 2>(a, p, st) : launch_norm_backward_rows<S, 2, 1>(a, p, st);
-    } else {
-        const size_t cap = size_t(di.sm_count) * 8;
-        norm_backward_means_kernel<S><<<(unsigned)(a.rows < cap ? a.rows : cap), kBlock, 0, st>>>(a);
-        if ((e = cudaPeekAtLastError()) != cudaSuccess) return e;
-        norm_backward_columns_kernel<S><<<dim3((a.cols + kBlock - 1) / kBlock, p.chunks), kBlock, 0, st>>>(a);
-        e = cudaPeekAtLastError();
-    }
+    const bool vec = norm_vector_ok<S>(ptr, 10, a.cols);
+    if (vec && a.packets <= 512) e = launch_norm_backward_rows<S, 1, 2>(a, p, st);
+    else if (vec && a.packets <= 1024) e = launch_norm_backward_rows<S, 2, 1>(a, p, st);
+    else e = vec ? launch_norm_backward_any<S, true>(a, di.sm_count, st) : launch_norm_backward_any<S, false>(a, di.sm_count, st);
     if (e != cudaSuccess) return e;
     const size_t gate_rows = a.grad_gate && a.rows_per_gate > 1 ? a.rows / a.rows_per_gate : 0;
     bool any = gate_rows > 0;

@@ -231,7 +231,8 @@ template <bool kBytes, class S, int NT> cudaError_t launch_few_rows_tiles(const 
 // Whether there are few rows: 32 at most, or up to four for each expert.  Measured against the tiles on tcgen05: one token
 // 4096 -> 12288 in 8 bits 12.6 us (24.6), 16 tokens 4096 -> 4096 6.5 (14.0), 32 tokens 5120 -> 2048 11.9 (16.0), 64 of them 22.6 (16.1);
 // 24 rows over 64 experts 2048 -> 1408 bf16 24.8 (44.2), 256 of them 62.7 (65.7); 64 rows over 8 experts 2048 -> 4096 34.7 (28.7).
-inline bool few_rows(const ProdArgs& g) { return g.rows <= 32 || (g.rows <= kFewMaxRows && g.rows <= 4 * size_t(g.experts)); }
+// (Byte offsets inside a row are 32-bit there.)
+inline bool few_rows(const ProdArgs& g) { return g.in < (1u << 28) && (g.rows <= 32 || (g.rows <= kFewMaxRows && g.rows <= 4 * size_t(g.experts))); }
 
 // Tokens a job takes at once, by the rows an expert has on average: an expert with more is read once per such group.
 template <bool kBytes, class S> cudaError_t launch_few_rows(const ProdArgs& g, int sms, int early, cudaStream_t st)

@@ -302,6 +302,12 @@ __global__ void __launch_bounds__(512, kI == 1 ? 2 : 1) norm_forward_ring_kernel
     bool on[kI];
     uint4 pre_gain[kI];
     float gain[kI][V];                               // times the gate
+#pragma unroll
+    for (int i = 0; i < kI; ++i) {
+        column[i] = threadIdx.x + i * blockDim.x;
+        on[i] = column[i] < a.packets;
+        pre_gain[i] = on[i] && a.pre_gain ? __ldg(static_cast<const uint4*>(a.pre_gain) + column[i]) : make_uint4(0, 0, 0, 0);
+    }
     size_t gate_row = a.gate ? r0 / a.rows_per_gate : 0, gate_end = a.gate ? (gate_row + 1) * a.rows_per_gate : a.rows;
     auto parameter = [&](const void* base, size_t row, int i, float none, float (&v)[V]) {
         if (base && on[i]) {
@@ -322,12 +328,6 @@ __global__ void __launch_bounds__(512, kI == 1 ? 2 : 1) norm_forward_ring_kernel
             for (int e = 0; e < V; ++e) gain[i][e] *= w[e];
         }
     };
-#pragma unroll
-    for (int i = 0; i < kI; ++i) {
-        column[i] = threadIdx.x + i * blockDim.x;
-        on[i] = column[i] < a.packets;
-        pre_gain[i] = on[i] && a.pre_gain ? __ldg(static_cast<const uint4*>(a.pre_gain) + column[i]) : make_uint4(0, 0, 0, 0);
-    }
     set_gate();
     int stage = 0;
     uint32_t phase = 0;
@@ -646,6 +646,11 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
 
     uint32_t column[kI];
     bool on[kI];
+#pragma unroll
+    for (int i = 0; i < kI; ++i) {
+        column[i] = threadIdx.x + i * blockDim.x;
+        on[i] = column[i] < a.packets;
+    }
     uint4 pre_gain[kI];
     float2 both[kI][P];                              // gate g_post
     float2 acc_pre[kI][P], acc_pre_bias[kFull ? kI : 1][P], acc_p[kI][P], acc_q[kFull ? kI : 1][P];
@@ -677,8 +682,6 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
     };
 #pragma unroll
     for (int i = 0; i < kI; ++i) {
-        column[i] = threadIdx.x + i * blockDim.x;
-        on[i] = column[i] < a.packets;
         pre_gain[i] = on[i] && a.pre_gain ? __ldg(static_cast<const uint4*>(a.pre_gain) + column[i]) : make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int e = 0; e < P; ++e) {

@@ -29,8 +29,7 @@ namespace nfad {
 
 constexpr int kTileRows = 128;
 constexpr int kStepBytes = 128;                    // of the reduction, per stage
-constexpr int kResultWarps = 8;
-constexpr int kGatherWarps = 4;
+constexpr int kGatherWarps = 8;
 constexpr int kFirstResultWarp = 4;                // a warp reads the 32 tensor-memory lanes of its index modulo 4
 constexpr int kRingBytes = 163840;
 constexpr int kMaxStages = 9;
@@ -61,7 +60,13 @@ struct ProdShared {
     int tiles[kMaxExperts + 1];                     // row tiles before each expert
 };
 constexpr int kStageBytes = 32 * 128;             // a result warp's 32 rows of 128 bytes
-constexpr int kProdSmem = 1024 + kRingBytes + kResultWarps * kStageBytes + int(sizeof(ProdShared));
+constexpr int kMostResultWarps = 8;
+// Result warps: beside gathering warps four, whose registers those need.
+template <bool kGather> struct ProdWarps {
+    static constexpr int kResult = kGather ? 4 : kMostResultWarps;
+    static constexpr int kThreads = (kFirstResultWarp + kResult + (kGather ? kGatherWarps : 0)) * 32;
+};
+constexpr int kProdSmem = 1024 + kRingBytes + kMostResultWarps * kStageBytes + int(sizeof(ProdShared));
 
 // CTAs one of whose waits ran out; one counter for each translation unit that includes this file
 static __device__ unsigned g_product_faults;
@@ -79,7 +84,7 @@ struct ProdTileAt {
 constexpr uint32_t kBand = 16;
 template <int OP, int BN, bool kPair> struct TileWalk {
     uint32_t b_tiles, expert = 0;
-    __device__ __forceinline__ ProdTileAt at(const ProdArgs& g, const ProdShared& s, uint32_t t)
+    __device__ __forceinline__ ProdTileAt at(const ProdArgs& g, const int* start, const int* tiles, uint32_t t)
     {
         constexpr int kRows = ProdTile<BN, kPair>::kRows;
         ProdTileAt q;
@@ -89,15 +94,15 @@ template <int OP, int BN, bool kPair> struct TileWalk {
             expert = t / (a_tiles * b_tiles);
             local = t - expert * a_tiles * b_tiles;
         } else {
-            while (uint32_t(s.tiles[expert + 1]) * b_tiles <= t) ++expert;
-            a_tiles = s.tiles[expert + 1] - s.tiles[expert];
-            local = t - uint32_t(s.tiles[expert]) * b_tiles;
+            while (uint32_t(tiles[expert + 1]) * b_tiles <= t) ++expert;
+            a_tiles = tiles[expert + 1] - tiles[expert];
+            local = t - uint32_t(tiles[expert]) * b_tiles;
         }
         const uint32_t band = local / (kBand * b_tiles);
         const uint32_t in_band = local - band * kBand * b_tiles;
         const uint32_t height = min(kBand, a_tiles - band * kBand);
         const uint32_t bt = in_band / height, at = band * kBand + in_band - bt * height;
-        const int r0 = s.start[expert], r1 = s.start[expert + 1];
+        const int r0 = start[expert], r1 = start[expert + 1];
         q.expert = expert;
         q.b0 = int(bt) * BN;
         if (OP == kProdWeight) {
@@ -115,35 +120,124 @@ template <int OP, int BN, bool kPair> struct TileWalk {
     }
 };
 
+// One warp: the experts' row ranges, held inside [0, rows] whatever the offsets say, and the row tiles of kRows before each.
+template <int kRows> __device__ __forceinline__ void row_table(const ProdArgs& g, int* start, int* tiles, int lane)
+{
+    int before = 0, last = 0;
+    for (uint32_t e0 = 0; e0 <= g.experts; e0 += 32) {
+        const uint32_t e = e0 + lane;
+        int first = e < g.experts ? 0 : int(g.rows);
+        if (g.offsets && e <= g.experts) first = min(max(__ldg(g.offsets + e), 0), int(g.rows));
+        // ranges that run backwards are empty: an expert begins no earlier than the largest offset before it
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, first, o);
+            if (lane >= o) first = max(first, v);
+        }
+        first = max(first, last);
+        int prev = __shfl_up_sync(0xffffffffu, first, 1);
+        if (lane == 0) prev = e0 ? last : first;
+        int n = (first - prev + kRows - 1) / kRows;      // of the expert before this one
+        if (e > g.experts) n = 0;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, n, o);
+            if (lane >= o) n += v;
+        }
+        n += before;
+        if (e <= g.experts) {
+            start[e] = first;
+            tiles[e] = n;
+        }
+        before = __shfl_sync(0xffffffffu, n, 31);
+        last = __shfl_sync(0xffffffffu, first, 31);
+    }
+}
+
+// Clears reduction steps from `keep` on in `runs` boxes of `steps` 128-byte rows, by one warp.
+__device__ __forceinline__ void clear_runs(unsigned char* at, int runs, int keep, int steps, int lane)
+{
+    for (int j = 0; j < runs; ++j)
+        for (int i = keep * 8 + lane; i < steps * 8; i += 32) *reinterpret_cast<uint4*>(at + j * 64 * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+}
+
 // ---------------------------------------------------------------- gathering without tensor copies
 
-// `rows` runs of 128 bytes, swizzled as a tensor copy would leave them; elements outside [row, row_end) x [c, c_end) are zero
-template <int ES> __device__ __forceinline__ void gather_box(unsigned char* dst, const unsigned char* src, size_t pitch, int rows, int row, int row_end,
-                                                             int c, int c_end, int thread)
-{
-    constexpr int PER = 16 / ES;
-    for (int i = thread; i < rows * 8; i += kGatherWarps * 32) {
-        const int r = i >> 3, chunk = i & 7;
-        const int col = c + chunk * PER;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (row + r < row_end && col < c_end) {
-            const unsigned char* p = src + size_t(row + r) * pitch + size_t(col) * ES;
-            if (col + PER <= c_end && (reinterpret_cast<uintptr_t>(p) & 15u) == 0) {
-                v = __ldg(reinterpret_cast<const uint4*>(p));
-            } else {
+// One operand's 128 x 128 bytes of a stage, swizzled as tensor copies would leave them: 1024 packets of 16 bytes, four to a thread.
+// Not turned: 128 rows of the operand's own dimension, 128 bytes of the reduction.  Turned: two boxes of 64 reduction steps (128
+// for bytes there are none) by 128 bytes along the own dimension.  Elements outside read as zeros.  A packet that starts
+// anywhere comes from the two aligned ones that hold it, shifted; at the ends of a row and of the whole operand ([begin, end))
+// it comes element by element.
+struct GatherSource {
+    const unsigned char *begin, *end, *at;
+    uint32_t pitch;
+    int own, own_end, red, red_end;                  // first index and end along the own dimension and along the reduction
+};
+constexpr int kGatherPackets = 1024 / (kGatherWarps * 32);
+template <int ES, bool kTurn> struct GatherPackets {
+    static constexpr int PER = 16 / ES;
+    uint4 lo[kGatherPackets], hi[kGatherPackets];
+    uint32_t whole;
+    // where packet i of the box begins, and how many of its elements there are
+    static __device__ __forceinline__ const unsigned char* place(const GatherSource& src, int i, int* n)
+    {
+        const int row = kTurn ? src.red + ((i & 511) >> 3) : src.own + (i >> 3), end = kTurn ? src.red_end : src.own_end;
+        const int col = kTurn ? src.own + (i >> 9) * (128 / ES) + (i & 7) * PER : src.red + (i & 7) * PER, width = kTurn ? src.own_end : src.red_end;
+        *n = row < end ? width - col : 0;
+        return src.at + size_t(row) * src.pitch + size_t(col) * ES;
+    }
+    __device__ __forceinline__ void load(const GatherSource& src, int thread)
+    {
+        whole = 0;
+#pragma unroll
+        for (int j = 0; j < kGatherPackets; ++j) {
+            int n;
+            const unsigned char* p = place(src, thread + j * kGatherWarps * 32, &n);
+            const unsigned char* q = reinterpret_cast<const unsigned char*>(reinterpret_cast<uintptr_t>(p) & ~uintptr_t(15));
+            lo[j] = hi[j] = make_uint4(0, 0, 0, 0);
+            if (n >= PER && q >= src.begin && q + (p == q ? 16 : 32) <= src.end) {
+                whole |= 1u << j;
+                lo[j] = __ldg(reinterpret_cast<const uint4*>(q));
+                if (p != q) hi[j] = __ldg(reinterpret_cast<const uint4*>(q) + 1);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(unsigned char* dst, const GatherSource& src, int thread)
+    {
+#pragma unroll
+        for (int j = 0; j < kGatherPackets; ++j) {
+            const int i = thread + j * kGatherWarps * 32;
+            int n;
+            const unsigned char* p = place(src, i, &n);
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (whole >> j & 1) {
+                // bytes [s, s + 16) of the 32: whole words first, then within the words
+                const uint32_t s = uint32_t(reinterpret_cast<uintptr_t>(p)) & 15u, bits = (s & 3u) * 8;
+                uint32_t w[8] = {lo[j].x, lo[j].y, lo[j].z, lo[j].w, hi[j].x, hi[j].y, hi[j].z, hi[j].w};
+                if (s & 8u) {
+#pragma unroll
+                    for (int k = 0; k < 6; ++k) w[k] = w[k + 2];
+                }
+                if (s & 4u) {
+#pragma unroll
+                    for (int k = 0; k < 5; ++k) w[k] = w[k + 1];
+                }
+                v = make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+            } else if (n > 0) {
                 uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
                 for (int e = 0; e < PER; ++e)
-                    if (col + e < c_end) {
+                    if (e < n) {
                         if (ES == 2) w[e >> 1] |= uint32_t(__ldg(reinterpret_cast<const unsigned short*>(p) + e)) << (16 * (e & 1));
                         else w[e >> 2] |= uint32_t(__ldg(p + e)) << (8 * (e & 3));
                     }
                 v = make_uint4(w[0], w[1], w[2], w[3]);
             }
+            const int r = i >> 3;
+            *reinterpret_cast<uint4*>(dst + r * 128 + (((i & 7) ^ (r & 7)) << 4)) = v;
         }
-        *reinterpret_cast<uint4*>(dst + r * 128 + ((chunk ^ (r & 7)) << 4)) = v;
     }
-}
+};
 
 // ---------------------------------------------------------------- epilogue
 
@@ -174,6 +268,32 @@ template <bool kSlope> __device__ __forceinline__ void act32(int kind, float (&z
     }
 }
 
+// the same for one packet
+template <class K, bool kSlope> __device__ __forceinline__ void act8(float (&z)[8], float (&d)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        if (kSlope) {
+            const ActOut2 o = evaluate(K{}, Fast2{}, make_float2(z[e], z[e + 1]));
+            z[e] = o.y.x; z[e + 1] = o.y.y;
+            d[e] = o.dydx.x; d[e + 1] = o.dydx.y;
+        } else {
+            const float2 y = evaluate_value(K{}, Fast2{}, make_float2(z[e], z[e + 1]));
+            z[e] = y.x; z[e + 1] = y.y;
+        }
+    }
+}
+template <bool kSlope> __device__ __forceinline__ void act8(int kind, float (&z)[8], float (&d)[8])
+{
+    switch (kind) {
+    case kGeluErf:  act8<GeluErf, kSlope>(z, d); break;
+    case kGeluTanh: act8<GeluTanh, kSlope>(z, d); break;
+    case kSwish:    act8<Swish, kSlope>(z, d); break;
+    case kMish:     act8<Mish, kSlope>(z, d); break;
+    default: break;
+    }
+}
+
 // eight neighbours of a [*, width] tensor from column c on; past the width: 0 (unaligned rows: one by one)
 template <class S> __device__ __forceinline__ void load8(const void* base, size_t row, uint32_t width, uint32_t c, bool vec, float (&v)[8])
 {
@@ -185,14 +305,6 @@ template <class S> __device__ __forceinline__ void load8(const void* base, size_
         for (int e = 0; e < 8; ++e) v[e] = c + e < width ? S::load1(p + e) : 0.0f;
     }
 }
-template <class S> __device__ __forceinline__ void store8(void* base, size_t row, uint32_t width, uint32_t c, const float* v)
-{
-    typename S::elem* p = static_cast<typename S::elem*>(base) + row * width + c;
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (c + e < width) S::store1(p + e, v[e]);
-}
-
 template <class S> __device__ __forceinline__ uint4 pack8(const float (&z)[32], int p)
 {
     float o[8];
@@ -232,6 +344,23 @@ struct RowPackets {
         each<typename S::elem, kPackets>(static_cast<typename S::elem*>(base), col, first,
                                          [&](int, int place, typename S::elem* p) { *reinterpret_cast<uint4*>(p) = stage[place]; });
     }
+    // the same where rows start anywhere: kPackets * 8 elements of each row, one by one, neighbours by neighbouring lanes
+    template <class S, int kPackets> __device__ __forceinline__ void store_odd(void* base, uint32_t col, int first) const
+    {
+        using E = typename S::elem;
+        E* p = static_cast<E*>(base) + row0 * width + col;
+        for (int r = 0; r < rows; ++r, p += width)
+#pragma unroll
+            for (int e = lane; e < kPackets * 8; e += 32)
+                if (col + e < width) p[e] = reinterpret_cast<const E*>(stage + at(r, first + (e >> 3)))[e & 7];
+    }
+    template <class S> __device__ __forceinline__ void fetch_odd(const void* base, uint32_t col, int first) const
+    {
+        using E = typename S::elem;
+        const E* p = static_cast<const E*>(base) + row0 * width + col;
+        for (int r = 0; r < rows; ++r, p += width)
+            if (col + lane < width) reinterpret_cast<E*>(stage + at(r, first + (lane >> 3)))[lane & 7] = p[lane];
+    }
     // four packets of each row, on their way in
     template <class S> __device__ __forceinline__ void fetch(const void* base, uint32_t col, uint4 (&v)[4]) const
     {
@@ -247,10 +376,10 @@ struct RowPackets {
 };
 
 // rows that belong to no expert: zeros
-template <class S> __device__ __forceinline__ void clear_rows(const ProdArgs& g, int first, int end, uint32_t width, int thread)
+template <class S, int kThreads> __device__ __forceinline__ void clear_rows(const ProdArgs& g, int first, int end, uint32_t width, int thread)
 {
     const size_t n0 = size_t(first) * width, n1 = size_t(end) * width;
-    for (size_t i = n0 + size_t(blockIdx.x) * (kResultWarps * 32) + thread; i < n1; i += size_t(gridDim.x) * (kResultWarps * 32)) {
+    for (size_t i = n0 + size_t(blockIdx.x) * kThreads + thread; i < n1; i += size_t(gridDim.x) * kThreads) {
         S::store1(static_cast<typename S::elem*>(g.out) + i, 0.0f);
         if (g.slope) S::store1(static_cast<typename S::elem*>(g.slope) + i, 0.0f);
     }
@@ -259,17 +388,17 @@ template <class S> __device__ __forceinline__ void clear_rows(const ProdArgs& g,
 // ---------------------------------------------------------------- the kernel
 
 template <int OP, int BN, class S, bool kGather, bool kPair>
-__global__ void __launch_bounds__((kFirstResultWarp + kResultWarps + (kGather ? kGatherWarps : 0)) * 32, 1)
+__global__ void __launch_bounds__(ProdWarps<kGather>::kThreads, 1)
 product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b)
 {
     using Kind = ProdKind<OP>;
     using Tile = ProdTile<BN, kPair>;
     constexpr int kStages = Tile::kStages, kStep = Kind::kStep, kOwn = Tile::kOwnColumns;
     constexpr uint32_t kTmem = 2 * BN;
-    constexpr int kBoxRows = Tile::kBoxRows;
+    constexpr int kBoxRows = Tile::kBoxRows, kResultWarps = ProdWarps<kGather>::kResult;
     extern __shared__ unsigned char raw[];
     unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
-    ProdShared& s = *reinterpret_cast<ProdShared*>(ring + kRingBytes + kResultWarps * kStageBytes);
+    ProdShared& s = *reinterpret_cast<ProdShared*>(ring + kRingBytes + kMostResultWarps * kStageBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = kPair ? tc::rank_in_pair() : 0;
     const uint32_t unit = kPair ? blockIdx.x >> 1 : blockIdx.x, units = kPair ? gridDim.x >> 1 : gridDim.x;
@@ -304,38 +433,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    // the experts' row ranges, held inside [0, rows] whatever the offsets say, and the row tiles before each
-    if (warp == 3) {
-        int before = 0, last = 0;
-        for (uint32_t e0 = 0; e0 <= g.experts; e0 += 32) {
-            const uint32_t e = e0 + lane;
-            int first = e < g.experts ? 0 : int(g.rows);
-            if (g.offsets && e <= g.experts) first = min(max(__ldg(g.offsets + e), 0), int(g.rows));
-            // ranges that run backwards are empty: an expert begins no earlier than the largest offset before it
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int v = __shfl_up_sync(0xffffffffu, first, o);
-                if (lane >= o) first = max(first, v);
-            }
-            first = max(first, last);
-            int prev = __shfl_up_sync(0xffffffffu, first, 1);
-            if (lane == 0) prev = e0 ? last : first;
-            int n = (first - prev + Tile::kRows - 1) / Tile::kRows;      // of the expert before this one
-            if (e > g.experts) n = 0;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int v = __shfl_up_sync(0xffffffffu, n, o);
-                if (lane >= o) n += v;
-            }
-            n += before;
-            if (e <= g.experts) {
-                s.start[e] = first;
-                s.tiles[e] = n;
-            }
-            before = __shfl_sync(0xffffffffu, n, 31);
-            last = __shfl_sync(0xffffffffu, first, 31);
-        }
-    }
+    if (warp == 3) row_table<Tile::kRows>(g, s.start, s.tiles, lane);
     tc::fence_before_sync();
     __syncthreads();
     if (kPair) tc::pair_sync();                      // the other CTA's barriers exist
@@ -354,10 +452,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
     auto ragged = [&](const ProdTileAt& q, int r) { return OP == kProdWeight && !kGather && r + kStep > q.r_end; };
     // clears those rows in every 128-byte run of this CTA's two operands
     auto clear_ragged = [&](const ProdTileAt& q, int r, uint32_t stage) {
-        const int keep = q.r_end - r;
-        unsigned char* at = ring + stage * Tile::kStage;
-        for (int j = 0; j < 2 + kOwn / 64; ++j)
-            for (int i = keep * 8 + lane; i < kStep * 8; i += 32) *reinterpret_cast<uint4*>(at + j * 64 * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+        clear_runs(ring + stage * Tile::kStage, 2 + kOwn / 64, q.r_end - r, kStep, lane);
         tc::writes_to_async();
         if (kPair) tc::pair_fence();
         __syncwarp();
@@ -370,7 +465,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
         const bool for_a = warp == 0;
         if (lane == 0)
             for (uint32_t t = unit; t < total; t += units) {
-                const ProdTileAt q = walk.at(g, s, t);
+                const ProdTileAt q = walk.at(g, s.start, s.tiles, t);
                 const int a0 = q.a0 + int(rank) * kTileRows, b0 = q.b0 + (rank ? int(columns(q)) / 2 : 0);
                 const int a_rows = max(0, min(kTileRows, q.a_end - a0));
                 const int boxes = (a_rows + kBoxRows - 1) / kBoxRows;     // of A, when it is not turned
@@ -421,27 +516,35 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
         uint32_t stage = 0, phase = 0;
         bool ok = true;
         for (uint32_t t = unit; t < total && ok; t += units) {
-            const ProdTileAt q = walk.at(g, s, t);
+            const ProdTileAt q = walk.at(g, s.start, s.tiles, t);
+            static_assert(!kGather || BN == kTileRows, "both operands' boxes are 128 by 128 bytes");
+            constexpr int ES = Kind::kElem;
+            const int thread = threadIdx.x - (kFirstResultWarp + kResultWarps) * 32;
+            GatherSource a, b;
+            a.pitch = (OP == kProdInput || OP == kProdWeight ? g.outs : g.in) * ES;
+            b.pitch = g.in * ES;
+            const size_t weight = size_t(g.outs) * b.pitch;                       // bytes of an expert's
+            a.begin = a.at = static_cast<const unsigned char*>(g.a);
+            a.end = a.begin + g.rows * a.pitch;
+            a.own = q.a0;
+            a.own_end = q.a_end;
+            b.begin = static_cast<const unsigned char*>(g.b);
+            b.end = b.begin + (OP == kProdWeight ? g.rows * b.pitch : g.experts * weight);
+            b.at = b.begin + (OP == kProdWeight ? 0 : q.expert * weight);
+            b.own = q.b0;
+            b.own_end = int(width);
+            a.red_end = b.red_end = q.r_end;
             for (int r = q.r0; r < q.r_end; r += kStep) {
+                a.red = b.red = r;
+                // requested before the stage is free, so that the wait covers the loads
+                GatherPackets<ES, Kind::kTurnA> pa;
+                GatherPackets<ES, Kind::kTurnB> pb;
+                pa.load(a, thread);
+                pb.load(b, thread);
                 if (!(ok = tc::barrier_wait(empty(stage), phase ^ 1, gave_up))) break;
-                constexpr int ES = Kind::kElem;
-                unsigned char *da = ring + stage * Tile::kStage, *db = da + kTileRows * kStepBytes;
-                const int thread = threadIdx.x - (kFirstResultWarp + kResultWarps) * 32;
-                const unsigned char *pa = static_cast<const unsigned char*>(g.a), *pb = static_cast<const unsigned char*>(g.b);
-                if (Kind::kTurnA) {
-                    for (int j = 0; j < 2; ++j)
-                        gather_box<ES>(da + j * 64 * 128, pa, size_t(g.outs) * ES, kStep, r, q.r_end, q.a0 + j * 64, int(g.outs), thread);
-                } else {
-                    const uint32_t w = OP == kProdInput ? g.outs : g.in;
-                    gather_box<ES>(da, pa, size_t(w) * ES, kTileRows, q.a0, q.a_end, r, int(w), thread);
-                }
-                if (Kind::kTurnB) {
-                    const unsigned char* p = OP == kProdInput ? pb + size_t(q.expert) * g.outs * g.in * ES : pb;
-                    for (int j = 0; j < BN / 64; ++j)
-                        gather_box<ES>(db + j * 64 * 128, p, size_t(g.in) * ES, kStep, r, q.r_end, q.b0 + j * 64, int(g.in), thread);
-                } else {
-                    gather_box<ES>(db, pb + size_t(q.expert) * g.outs * g.in * ES, size_t(g.in) * ES, BN, q.b0, int(g.outs), r, int(g.in), thread);
-                }
+                unsigned char* at = ring + stage * Tile::kStage;
+                pa.store(at, a, thread);
+                pb.store(at + kTileRows * kStepBytes, b, thread);
                 tc::writes_to_async();
                 tc::barrier_arrive(full(stage));
                 if (++stage == kStages) { stage = 0; phase ^= 1; }
@@ -452,7 +555,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
         uint32_t stage = 0, phase = 0, turn = 0, turn_phase = 0, landed_phases = 0;              // landed_phases: a bit for each stage
         bool ok = true;
         for (uint32_t t = unit; t < total && ok; t += units) {
-            const ProdTileAt q = walk.at(g, s, t);
+            const ProdTileAt q = walk.at(g, s.start, s.tiles, t);
             if (!(ok = tc::barrier_wait(acc_empty(turn), turn_phase ^ 1, gave_up))) break;
             tc::fence_after_sync();
             const uint32_t what = tc::instruction(Kind::kBytes ? tc::kNumberS8 : IsBF16<S>::value ? tc::kNumberBF16 : tc::kNumberF16, Kind::kTurnA, Kind::kTurnB,
@@ -499,7 +602,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
         uint32_t stage = 0, landed_phases = 0;
         bool ok = true;
         for (uint32_t t = unit; t < total && ok; t += units) {
-            const ProdTileAt q = walk.at(g, s, t);
+            const ProdTileAt q = walk.at(g, s.start, s.tiles, t);
             for (int r = q.r0; r < q.r_end; r += kStep) {
                 if (ragged(q, r)) {
                     if (!(ok = tc::barrier_wait(landed(stage), landed_phases >> stage & 1, gave_up))) break;
@@ -514,8 +617,8 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
         // ------------------------------------------------ results
         const int lanes = (warp & 3) * 32, half = (warp - kFirstResultWarp) >> 2;
         if (OP != kProdWeight && g.offsets) {
-            clear_rows<S>(g, 0, s.start[0], width, threadIdx.x - kFirstResultWarp * 32);
-            clear_rows<S>(g, s.start[g.experts], int(g.rows), width, threadIdx.x - kFirstResultWarp * 32);
+            clear_rows<S, kResultWarps * 32>(g, 0, s.start[0], width, threadIdx.x - kFirstResultWarp * 32);
+            clear_rows<S, kResultWarps * 32>(g, s.start[g.experts], int(g.rows), width, threadIdx.x - kFirstResultWarp * 32);
         }
         // whole 16-byte packets: rows start on packets and no packet crosses a row's end
         const bool vec = width % 8 == 0 && ((reinterpret_cast<uintptr_t>(g.out) | reinterpret_cast<uintptr_t>(g.slope) | reinterpret_cast<uintptr_t>(g.bias) |
@@ -523,7 +626,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
         const bool vec_scale = Kind::kBytes && width % 8 == 0 && (reinterpret_cast<uintptr_t>(g.b_scale) & 15u) == 0;
         uint32_t turn = 0, turn_phase = 0;
         for (uint32_t t = unit; t < total; t += units) {
-            const ProdTileAt q = walk.at(g, s, t);
+            const ProdTileAt q = walk.at(g, s.start, s.tiles, t);
             const int row = q.a0 + int(rank) * kTileRows + lanes + lane;
             const bool mine = row < q.a_end, none = q.r0 >= q.r_end;
             const size_t out_row = OP == kProdWeight ? size_t(q.expert) * g.outs + row : size_t(row);
@@ -535,7 +638,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
             rows.row0 = out_row - lane;
             rows.stage = reinterpret_cast<uint4*>(ring + kRingBytes + (warp - kFirstResultWarp) * kStageBytes);
             // 32 columns at a time; without slopes two of them leave together; the factors of the next are fetched during the current
-            constexpr int kChunks = BN / 32, kOwnChunks = kChunks / 2;
+            constexpr int kChunks = BN / 32, kOwnChunks = kChunks / (kResultWarps / 4);
             constexpr bool kTwo = kOwnChunks > 1;
             const bool slopes = OP == kProdForward && g.slope;
             uint4 prev[4] = {};
@@ -582,20 +685,18 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
                 }
                 if (OP == kProdInput && g.prev) {
                     const int first = second ? 4 : 0;                 // the places that this chunk's results will take
-                    if (vec) {
-                        rows.settle(prev, first);
-                        __syncwarp();
-                        if (c + 1 < (half + 1) * kOwnChunks) rows.template fetch<S>(g.prev, col0 + 32, prev);
-                    }
+                    if (vec) rows.settle(prev, first);
+                    else rows.template fetch_odd<S>(g.prev, col0, first);
+                    __syncwarp();
+                    if (vec && c + 1 < (half + 1) * kOwnChunks) rows.template fetch<S>(g.prev, col0 + 32, prev);
 #pragma unroll
                     for (int p = 0; p < 4; ++p) {
                         float f[8];
-                        if (vec) S::unpack(rows.get(first + p), f);
-                        else load8<S>(g.prev, mine ? out_row : rows.row0, width, col0 + p * 8, false, f);
+                        S::unpack(rows.get(first + p), f);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) z[p * 8 + e] *= f[e];
                     }
-                    if (vec) __syncwarp();
+                    __syncwarp();
                 }
                 if constexpr (OP == kProdForward) {
                     if (slopes) act32<true>(g.act, z, d);
@@ -603,28 +704,25 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
                 } else if constexpr (OP == kProdBytes) {
                     act32<false>(g.act, z, d);
                 }
-                if (vec) {
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        rows.put((second ? 4 : 0) + p, pack8<S>(z, p));
-                        if (OP == kProdForward && slopes) rows.put(4 + p, pack8<S>(d, p));
-                    }
-                    if (kTwo && !slopes && !second && c + 1 < (half + 1) * kOwnChunks && col0 + 32 < width) continue;   // the next 32 first
-                    __syncwarp();
-                    if (kTwo && second) {
-                        rows.template store<S, 8>(g.out, col0 - 32, 0);
-                    } else {
-                        rows.template store<S, 4>(g.out, col0, 0);
-                        if (OP == kProdForward && slopes) rows.template store<S, 4>(g.slope, col0, 4);
-                    }
-                    __syncwarp();
-                } else if (mine) {
-#pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        store8<S>(g.out, out_row, width, col0 + p * 8, &z[p * 8]);
-                        if (OP == kProdForward && slopes) store8<S>(g.slope, out_row, width, col0 + p * 8, &d[p * 8]);
+                for (int p = 0; p < 4; ++p) {
+                    rows.put((second ? 4 : 0) + p, pack8<S>(z, p));
+                    if (OP == kProdForward && slopes) rows.put(4 + p, pack8<S>(d, p));
+                }
+                if (kTwo && !slopes && !second && c + 1 < (half + 1) * kOwnChunks && col0 + 32 < width) continue;   // the next 32 first
+                __syncwarp();
+                if (kTwo && second) {
+                    if (vec) rows.template store<S, 8>(g.out, col0 - 32, 0);
+                    else rows.template store_odd<S, 8>(g.out, col0 - 32, 0);
+                } else {
+                    if (vec) rows.template store<S, 4>(g.out, col0, 0);
+                    else rows.template store_odd<S, 4>(g.out, col0, 0);
+                    if (OP == kProdForward && slopes) {
+                        if (vec) rows.template store<S, 4>(g.slope, col0, 4);
+                        else rows.template store_odd<S, 4>(g.slope, col0, 4);
                     }
                 }
+                __syncwarp();
             }
             tc::fence_before_sync();
             __syncwarp();

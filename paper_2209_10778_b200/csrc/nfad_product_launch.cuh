@@ -6,6 +6,7 @@
 
 #include "nfad_few_rows.cuh"
 #include "nfad_product.cuh"
+#include "nfad_split.cuh"
 
 namespace nfad {
 
@@ -78,7 +79,7 @@ cudaError_t launch_product_tile(const ProdArgs& g, int sms, cudaStream_t st)
     if (kPair) grid *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(grid));
-    cfg.blockDim = dim3((kFirstResultWarp + kResultWarps + (kGather ? kGatherWarps : 0)) * 32);
+    cfg.blockDim = dim3(ProdWarps<kGather>::kThreads);
     cfg.dynamicSmemBytes = kProdSmem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -90,6 +91,56 @@ cudaError_t launch_product_tile(const ProdArgs& g, int sms, cudaStream_t st)
     cfg.attrs = attr;
     cfg.numAttrs = kPair ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, g, map_a, map_b);
+}
+
+template <int OP, class S> cudaError_t launch_split(const ProdArgs& g, unsigned ranks, cudaStream_t st)
+{
+    using Kind = ProdKind<OP>;
+    auto kernel = split_kernel<OP, S>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitSmem);
+    if (e != cudaSuccess) return e;
+    CUtensorMap map_a = {}, map_b = {};
+    const int number = Kind::kBytes ? tc::kNumberS8 : IsBF16<S>::value ? tc::kNumberBF16 : tc::kNumberF16;
+    e = make_map(&map_a, number, g.a, OP == kProdInput || OP == kProdWeight ? g.outs : g.in, g.rows, 0, Kind::kTurnA ? 64 : 32);
+    if (e != cudaSuccess) return e;
+    e = OP == kProdWeight ? make_map(&map_b, number, g.b, g.in, g.rows, 0, 64) : make_map(&map_b, number, g.b, g.in, g.outs, g.experts, 64);
+    if (e != cudaSuccess) return e;
+    const size_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs, b_tiles = (width + kSplitColumns - 1) / kSplitColumns;
+    const size_t a_tiles = OP == kProdWeight ? size_t(g.experts) * ((g.outs + kTileRows - 1) / kTileRows)
+                                             : (g.rows + kTileRows - 1) / kTileRows + (g.offsets ? g.experts : 0);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(a_tiles * b_tiles * ranks));          // at most this many tiles; clusters past the last leave
+    cfg.blockDim = dim3(kSplitThreads);
+    cfg.dynamicSmemBytes = kSplitSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ranks;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, g, map_a, map_b, uint32_t(ranks));
+}
+
+// Over how many CTAs a tile's reduction is split (0: not at all; single CTAs or pairs walk over the tiles): as many as two to an
+// SM allow, with ten steps left for each; and one when the tiles alone are between one and two to an SM.  Measured (us, against
+// tiles that are walked over): 77 rows 5120 -> 2048 in 8 bits over 4: 10.9 (16.2); 64 rows 4096 -> 4096 bf16 over 4: 16.7 (23.9); 128 rows
+// 4096 -> 12288 in 8 bits, over one: 19.6 (27.0); weight gradient 8192 rows of 256 x 256 over 8: 13.3 (41.8).  With eight steps each no gain
+// (1024 x 1024 x 1024 over 2: 10.8, 10.8); with more CTAs than fit twice what it was.
+template <int OP> unsigned split_ranks(const ProdArgs& g, int sms)
+{
+    const size_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs;
+    const uintptr_t results = reinterpret_cast<uintptr_t>(g.out) | reinterpret_cast<uintptr_t>(g.slope) | reinterpret_cast<uintptr_t>(g.bias) | reinterpret_cast<uintptr_t>(g.prev);
+    if (width % 8 || results % 16) return 0;         // its results go by packets
+    const size_t a_tiles = OP == kProdWeight ? size_t(g.experts) * ((g.outs + kTileRows - 1) / kTileRows)
+                                             : (g.rows + kTileRows - 1) / kTileRows + (g.offsets ? g.experts - 1 : 0);
+    const size_t tiles = a_tiles * ((width + kSplitColumns - 1) / kSplitColumns), fit = 2 * size_t(sms);
+    const size_t steps = (OP == kProdInput ? g.outs : OP == kProdWeight ? g.rows / g.experts : g.in) / ProdKind<OP>::kStep;
+    for (unsigned ranks = 8; ranks > 1; ranks /= 2)
+        if (tiles * ranks <= fit && steps >= 10 * ranks) return ranks;
+    return OP != kProdWeight && tiles > size_t(sms) && tiles <= fit ? 1 : 0;
 }
 
 // Columns of a tile: the widest of 256, 128 and 64 that still gives every SM a tile, by the tiles that the rows make when they
@@ -130,6 +181,7 @@ template <int OP, class S> cudaError_t launch_product_store(const ProdArgs& g, c
     if (low % 16 || reduction == 0) return launch_product_tile<OP, 128, S, true>(g, di.sm_count, st);
     if constexpr (OP == kProdForward || OP == kProdBytes)
         if (few_rows(g)) return launch_few_rows<Kind::kBytes, S>(g, di.sm_count, g.b_ready, st);
+    if (const unsigned ranks = split_ranks<OP>(g, di.sm_count)) return launch_split<OP, S>(g, ranks, st);
     if (product_pairs<OP>(g, di.sm_count)) return launch_product_tile<OP, 256, S, false, true>(g, di.sm_count, st);
     switch (product_width<OP>(g, di.sm_count)) {
     case 256: return launch_product_tile<OP, 256, S, false>(g, di.sm_count, st);

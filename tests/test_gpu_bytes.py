@@ -15,7 +15,9 @@ ACTS = [None, "gelu_erf", "gelu_tanh", "swish", "mish"]
 # rows, in, out: single tokens, few, a tile and its borders, many tiles; odd sizes (gathered); in a multiple of 4 and of 8 only
 SHAPES = [(1, 64, 64), (1, 4096, 1000), (2, 1040, 136), (3, 48, 24), (4, 2064, 520), (5, 128, 40), (8, 512, 256), (9, 512, 264), (16, 1024, 2048),
           (17, 96, 8), (64, 256, 320), (127, 144, 48), (128, 128, 128), (129, 1024, 512), (300, 2048, 1000), (1, 37, 51), (7, 33, 20), (3, 1001, 77),
-          (130, 100, 44), (20, 24, 8), (1, 1, 1), (40, 16, 1), (1, 5000, 3), (2, 20000, 40)]
+          (130, 100, 44), (20, 24, 8), (1, 1, 1), (40, 16, 1), (1, 5000, 3), (2, 20000, 40),
+          # the reduction over eight, four and two CTAs, one tile for each of two CTAs of an SM, pairs
+          (40, 10256, 72), (77, 5136, 136), (60, 2576, 200), (130, 272, 5120), (2600, 272, 2056)]
 
 
 def quantize(x):

@@ -153,6 +153,27 @@ def test_many_tiles(dtype):
     assert nfad.nfad_wait_faults() == 0
 
 
+# shapes that take the ways through the products which depend on size (B200, 148 SMs): pairs of CTAs on 256 x 256 tiles (each
+# product), the reduction split over two, four and eight CTAs, one tile for each of two CTAs of an SM, and few rows
+WAYS = [
+    ([1100, 700, 800], 0, 0, 2048, 264), ([1101, 701, 900], 1, 3, 1040, 1800), ([600, 1, 900], 0, 0, 1048, 2568),
+    ([40, 0, 37], 3, 2, 1288, 136), ([77], 0, 0, 2568, 72), ([33], 0, 0, 5128, 72), ([150], 0, 0, 72, 5128), ([40, 0, 60], 0, 5, 136, 2568),
+    ([5203], 0, 0, 72, 136), ([2570, 2571], 0, 1, 136, 72), ([260], 0, 0, 264, 5000), ([9, 0, 17, 3], 1, 2, 1032, 200), ([3, 1, 0, 2] * 40, 0, 0, 264, 136),
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("way", range(len(WAYS)))
+def test_ways(dtype, way):
+    x, w, b, off, o = _case(WAYS[way], dtype, 300 + way)
+    _check_forward("gelu_erf", x, w, b, o, *_forward("gelu_erf", x, w, b, off))
+    _check_forward(None, x, w, None, o, *_forward(None, x, w, None, off))
+    gz = W.normal(x.shape[0] * w.shape[1], dtype, 9, 1.0).view(x.shape[0], w.shape[1])
+    prev = W.uniform(x.numel(), dtype, 11, -0.2, 1.1).view(x.shape)
+    _check_backward(gz, x, w, o, prev, *_backward(gz, x, w, off, prev))
+    assert nfad.nfad_wait_faults() == 0
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_neighbours_do_not_mix(dtype):
     # infinities and NaN in one expert's rows and weights stay there: tiles and reduction steps reach into the neighbours
@@ -252,6 +273,37 @@ def test_graph_with_other_offsets():
         g.replay()
         torch.cuda.synchronize()
         _check_forward("swish", x, w, b, other, y, None)
+
+
+def test_elements_beyond_32_bits():
+    # results, and gradients of the input, whose element offsets pass 2^31: the last rows against the plain form
+    rows, n_in, n_out = 270000, 64, 8200
+    w, b = W.normal(n_out * n_in, "bf16", 2, 0.125).view(1, n_out, n_in), W.normal(n_out, "bf16", 3, 0.4).view(1, n_out)
+    x = torch.zeros(rows, n_in, dtype=torch.bfloat16, device=DEV)
+    tail = W.normal(5 * n_in, "bf16", 4, 1.0).view(5, n_in)
+    x[-5:] = tail.to(DEV)
+    off = torch.tensor([0, rows], dtype=torch.int32)
+    y, d = torch.empty(rows, n_out, dtype=torch.bfloat16, device=DEV), torch.empty(rows, n_out, dtype=torch.bfloat16, device=DEV)
+    nfad.nfad_expert_linear("swish", x, w.to(DEV), b.to(DEV), off.to(DEV), y, d)
+    _check_forward("swish", tail, w, b, [0, 5], y[-5:], d[-5:])
+    _check_forward("swish", torch.zeros(3, n_in, dtype=torch.bfloat16), w, b, [0, 3], y[100:103], d[100:103])
+    gx = torch.empty_like(x)
+    nfad.nfad_expert_linear_backward_input(y, w.to(DEV), off.to(DEV), None, gx)
+    g = y[-5:].cpu().double()
+    plain.check(gx[-5:], g @ w[0].double(), plain.dot_error(g.abs() @ w[0].double().abs(), n_out), "grad_x")
+    gz = torch.empty_like(y)
+    gb = torch.empty(1, n_out, device=DEV)
+    nfad.nfad_expert_act_backward(y, d, off.to(DEV), gz, gb, nfad.nfad_expert_act_backward_scratch(y))
+    assert torch.equal(gz[-5:], (y[-5:].double() * d[-5:].double()).bfloat16())
+    # gradients of many experts' weights: 2.2e9 elements
+    experts, n_in, n_out = 1024, 1024, 2056
+    gw = torch.full((experts, n_out, n_in), float("nan"), dtype=torch.bfloat16, device=DEV)
+    x, gz = W.normal(8 * n_in, "bf16", 5, 1.0).view(8, n_in), W.normal(8 * n_out, "bf16", 6, 1.0).view(8, n_out)
+    off = torch.zeros(experts + 1, dtype=torch.int32)
+    off[-1] = 8
+    nfad.nfad_expert_linear_backward_weight(gz.to(DEV), x.to(DEV), off.to(DEV), gw)
+    plain.check(gw[-1], gz.double().t() @ x.double(), plain.dot_error(gz.double().abs().t() @ x.double().abs(), 8), "grad_w")
+    assert not gw[:-1].any()
 
 
 def test_most_experts():

@@ -42,7 +42,7 @@ def _quantize(x):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_quantizer(dtype):
-    for i, (rows, cols) in enumerate([(1, 1), (3, 7), (5, 64), (2, 1000), (4, 4096), (300, 520), (2, 40001)]):
+    for i, (rows, cols) in enumerate([(1, 1), (3, 7), (5, 64), (2, 1000), (4, 4096), (300, 520), (2, 40001), (9, 200), (17, 256), (5, 512), (3, 1024), (4, 2056), (3, 8192), (2, 12000)]):
         x = W.normal(rows * cols, dtype, i, 1.5).view(rows, cols)
         q, s = _quantize(x)
         wq, ws = quantize(x)

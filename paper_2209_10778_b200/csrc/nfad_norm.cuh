@@ -122,10 +122,11 @@ __device__ __forceinline__ void row_statistics(const float (&v)[kR][kI][V], cons
 
 // kR consecutive rows per CTA, or per warp (kWarp), kI packets of each per thread; cols a multiple of the packet, every pointer on a
 // 16-byte boundary.  kMean: one of the norms is LAYER.  For 16-bit storage instructions are what is short (49 per element at
-// first, 4.1 TB/s on [16384, 4096] bf16 against 6.0 for fp32 storage, where they are half as many per byte): so two rows share
-// each parameter's load and widening and each barrier, the normalisation is one multiply-add, and no 64-bit division is left.
+// first, 4.1 TB/s on [16384, 4096] bf16 against 6.0 for fp32 storage, where they are half as many per byte): so rows share
+// each parameter's load and widening and each barrier, threads are few with much work each, and no 64-bit division is left.
+// (A ring of bulk copies kept ahead of CTAs that stay, as backward has it, came to 92 us where this takes 87.)
 template <class S, int kI, int kR, bool kWarp, bool kMean>
-__global__ void __launch_bounds__(kI == 1 || kWarp ? 512 : 1024) norm_forward_kernel(const __grid_constant__ NormForwardArgs a)
+__global__ void __launch_bounds__(kWarp ? 128 : kI == 1 ? 512 : 256) norm_forward_kernel(const __grid_constant__ NormForwardArgs a)
 {
     constexpr int V = S::kVec;
     __shared__ float buf[2][kR][32];
@@ -262,177 +263,6 @@ constexpr int kNormRingBytes = 200 * 1024;          // of an SM's shared memory,
 
 static __device__ unsigned g_norm_faults;           // CTAs whose wait ran out
 
-// Many rows: a CTA stays and takes kR consecutive rows at a time, through a ring in shared memory that bulk copies of whole rows
-// fill several rows ahead, so that reads are in flight while a row waits for its reductions.  A thread owns the same columns of
-// every row: gain times gate is formed once (per gate row).  RMS norms without biases only: with means and biases the registers
-// leave one CTA to an SM, and its barriers show (150 against 141 us for a LayerNorm pair on [16384, 4096] bf16).
-// Measured on bf16 RMS pairs with a gate against a CTA per two rows: [16384, 4096] 93 (113) us, [8192, 8192] 94 (112), [4096, 6144]
-// 46.5 (50.6), [32768, 2048] 100 (102), and on fp32 [8192, 4096] 98 (87).
-template <class S, int kI, int kR>
-__global__ void __launch_bounds__(512, kI == 1 ? 2 : 1) norm_forward_ring_kernel(const __grid_constant__ NormForwardArgs a, int stages)
-{
-    constexpr int V = S::kVec;
-    extern __shared__ __align__(128) unsigned char ring[];
-    __shared__ float buf[2][kR][32];
-    __shared__ uint64_t full[kNormMaxStages];
-    __shared__ uint32_t gave_up_;
-    volatile uint32_t* gave_up = &gave_up_;
-    const uint32_t row_bytes = a.packets * 16, stage_bytes = a.r ? 2 * row_bytes : row_bytes;
-    const bool post = a.post != kNormNone, pre = a.pre != kNormNone;
-    if (threadIdx.x == 0) {
-        gave_up_ = 0;
-        for (int i = 0; i < stages; ++i) tc::barrier_init(tc::shared_address(&full[i]), 1);
-        tc::barrier_init_done();
-    }
-    __syncthreads();
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    RowSum<kR, false> sum{buf, 0};
-    const size_t r0 = blockIdx.x * a.chunk_rows, r1 = r0 + a.chunk_rows < a.rows ? r0 + a.chunk_rows : a.rows;
-    if (r0 >= r1) return;
-    auto request = [&](size_t row, int stage) {                       // by one thread
-        const uint32_t bar = tc::shared_address(&full[stage]), dst = tc::shared_address(ring) + stage * stage_bytes;
-        tc::barrier_expect(bar, stage_bytes);
-        tc::load_run(dst, static_cast<const unsigned char*>(a.u) + row * row_bytes, row_bytes, bar);
-        if (a.r) tc::load_run(dst + row_bytes, static_cast<const unsigned char*>(a.r) + row * row_bytes, row_bytes, bar);
-    };
-    if (threadIdx.x == 0)
-        for (int i = 0; i < stages && r0 + i < r1; ++i) request(r0 + i, i);
-    uint32_t column[kI];
-    bool on[kI];
-    uint4 pre_gain[kI];
-    float gain[kI][V];                               // times the gate
-#pragma unroll
-    for (int i = 0; i < kI; ++i) {
-        column[i] = threadIdx.x + i * blockDim.x;
-        on[i] = column[i] < a.packets;
-        pre_gain[i] = on[i] && a.pre_gain ? __ldg(static_cast<const uint4*>(a.pre_gain) + column[i]) : make_uint4(0, 0, 0, 0);
-    }
-    size_t gate_row = a.gate ? r0 / a.rows_per_gate : 0, gate_end = a.gate ? (gate_row + 1) * a.rows_per_gate : a.rows;
-    auto parameter = [&](const void* base, size_t row, int i, float none, float (&v)[V]) {
-        if (base && on[i]) {
-            S::unpack(__ldg(static_cast<const uint4*>(base) + row * a.packets + column[i]), v);
-        } else {
-#pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = on[i] ? none : 0.0f;  // columns past the row: nothing
-        }
-    };
-    auto set_gate = [&]() {
-#pragma unroll
-        for (int i = 0; i < kI; ++i) {
-            float w[V];
-            parameter(post ? a.post_gain : nullptr, 0, i, 1.0f, gain[i]);
-            if (!a.gate) continue;
-            parameter(a.gate, gate_row, i, 1.0f, w);
-#pragma unroll
-            for (int e = 0; e < V; ++e) gain[i][e] *= w[e];
-        }
-    };
-    set_gate();
-    int stage = 0;
-    uint32_t phase = 0;
-    bool ok = true;
-    for (size_t row = r0; row < r1 && ok; row += kR) {
-        float v[kR][kI][V], mean[kR], rstd[kR], rstd2[kR];            // mean stays 0
-        const bool two = kR == 1 || row + 1 < r1;
-        const unsigned char* at[kR];
-#pragma unroll
-        for (int k = 0; k < kR; ++k) {                               // stages are a multiple of kR: no wrap inside
-            if (k == 0 || two) tc::barrier_wait(tc::shared_address(&full[stage + k]), phase, gave_up);
-            at[k] = ring + (stage + k) * stage_bytes;
-            mean[k] = rstd2[k] = 0.0f;
-            rstd[k] = post ? 0.0f : 1.0f;
-        }
-        // A thread whose wait ran out carries on to this row's last barrier, behind which all learn of it together.
-        // Columns past the row and rows past the chunk read as zeros, and are not stored.
-        auto in_ring = [&](int k, uint32_t tensor_at, int i) {
-            return on[i] && (k == 0 || two) ? *reinterpret_cast<const uint4*>(at[k] + tensor_at + column[i] * 16) : make_uint4(0, 0, 0, 0);
-        };
-#pragma unroll
-        for (int k = 0; k < kR; ++k)
-#pragma unroll
-            for (int i = 0; i < kI; ++i) S::unpack(in_ring(k, 0, i), v[k][i]);
-        if (post) row_statistics<V, kR, kI, false, false>(v, on, a.post, a.inv_cols, a.eps, sum, mean, rstd);
-#pragma unroll
-        for (int k = 0; k < kR; ++k) {
-            if (k > 0 && !two) break;
-            if (row + k == gate_end) {
-                ++gate_row;
-                gate_end += a.rows_per_gate;
-                set_gate();
-            }
-#pragma unroll
-            for (int i = 0; i < kI; ++i) {
-                float w[V];
-                S::unpack(a.r ? in_ring(k, row_bytes, i) : make_uint4(0, 0, 0, 0), w);
-#pragma unroll
-                for (int e = 0; e < V; ++e) v[k][i][e] = fmaf(v[k][i][e] * rstd[k], gain[i][e], a.alpha * w[e]);
-                if (a.s && on[i]) store_packet<true>(static_cast<uint4*>(a.s) + (row + k) * a.packets + column[i], S::pack(v[k][i]));
-            }
-        }
-        if (pre) row_statistics<V, kR, kI, false, false>(v, on, a.pre, a.inv_cols, a.eps, sum, mean, rstd2);
-        else __syncthreads();
-        if (blockDim.x == 32) __syncwarp();
-        ok = *gave_up == 0;
-        // every thread has read the rows: their places in the ring are free
-        if (threadIdx.x == 0 && ok) {
-#pragma unroll
-            for (int k = 0; k < kR; ++k)
-                if (row + k + stages < r1) request(row + k + stages, stage + k);
-        }
-        stage += kR;
-        if (stage >= stages) { stage = 0; phase ^= 1; }
-        if (pre) {
-#pragma unroll
-            for (int i = 0; i < kI; ++i) {
-                if (!on[i]) continue;
-                float w[V];
-                S::unpack(pre_gain[i], w);
-#pragma unroll
-                for (int k = 0; k < kR; ++k) {
-                    if (k > 0 && !two) break;
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        v[k][i][e] *= rstd2[k];
-                        if (a.pre_gain) v[k][i][e] *= w[e];
-                    }
-                    store_packet<true>(static_cast<uint4*>(a.h) + (row + k) * a.packets + column[i], S::pack(v[k][i]));
-                }
-            }
-        }
-        if (a.stats && threadIdx.x < kR && (threadIdx.x == 0 || two)) {
-            const bool last = kR > 1 && threadIdx.x == 1;
-            a.stats[row + threadIdx.x] = make_float4(0.0f, post ? (last ? rstd[kR - 1] : rstd[0]) : 0.0f, 0.0f, last ? rstd2[kR - 1] : rstd2[0]);
-        }
-    }
-    if (!ok) {
-        // copies in flight land before the CTA's memory goes away
-        const long long t0 = clock64();
-        while (clock64() - t0 < tc::kWaitDrain) {}
-    }
-    if (threadIdx.x == 0 && gave_up_) atomicAdd(&g_norm_faults, 1u);
-}
-
-template <class S, int kI, int kR> cudaError_t launch_norm_forward_ring(const NormForwardArgs& in, unsigned block, int sms, cudaStream_t st)
-{
-    NormForwardArgs a = in;
-    auto kernel = norm_forward_ring_kernel<S, kI, kR>;
-    const unsigned per_sm = (kI == 1 ? 1024 : 512) / block;
-    const size_t row = size_t(a.packets) * 16 * (a.r ? 2 : 1);
-    size_t stages = kNormRingBytes / per_sm / row;
-    if (stages > kNormMaxStages) stages = kNormMaxStages;
-    stages -= stages % kR;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(stages * row));
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute attr[1];
-    const size_t most = size_t(sms) * per_sm;
-    a.chunk_rows = (a.rows + most - 1) / most;
-    norm_launch_config(&cfg, attr, (a.rows + a.chunk_rows - 1) / a.chunk_rows, block, st);
-    cfg.dynamicSmemBytes = stages * row;
-    return cudaLaunchKernelEx(&cfg, kernel, a, int(stages));
-}
-
 // Element access of the any-shape kernels.
 template <class S> __device__ __forceinline__ float at(const void* base, size_t i) { return S::load1(static_cast<const typename S::elem*>(base) + i); }
 template <class S> __device__ __forceinline__ void put(void* base, size_t i, float v) { S::store1(static_cast<typename S::elem*>(base) + i, v); }
@@ -507,23 +337,29 @@ template <class S> inline bool norm_vector_ok(const void* const* p, int n, size_
     return true;
 }
 
-template <class S, bool kMean> cudaError_t launch_norm_forward_rows(const NormForwardArgs& a, cudaStream_t st)
+template <class S, int kI, int kR, bool kWarp, bool kMean> cudaError_t launch_norm_forward_kernel(const NormForwardArgs& a, cudaStream_t st)
 {
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];
-    if (a.packets <= 128) {                          // a warp per row (two when a lane has one packet of each), four warps
-        const size_t rows = a.packets <= 32 ? 8 : 4;
-        norm_launch_config(&cfg, attr, (a.rows + rows - 1) / rows, 128, st);
-        if (a.packets <= 32) return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 1, 2, true, kMean>, a);
-        if (a.packets <= 64) return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 2, 1, true, kMean>, a);
-        return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 4, 1, true, kMean>, a);
-    }
-    if (a.packets <= 512) {
-        norm_launch_config(&cfg, attr, (a.rows + 1) / 2, (a.packets + 31) / 32 * 32, st);
-        return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 1, 2, false, kMean>, a);
-    }
-    norm_launch_config(&cfg, attr, a.rows, ((a.packets + 1) / 2 + 31) / 32 * 32, st);
-    return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, 2, 1, false, kMean>, a);
+    const size_t rows = kWarp ? 4 * kR : kR;         // of a CTA
+    const unsigned block = kWarp ? 128 : ((a.packets + kI - 1) / kI + 31) / 32 * 32;
+    norm_launch_config(&cfg, attr, (a.rows + rows - 1) / rows, block, st);
+    return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, kI, kR, kWarp, kMean>, a);
+}
+
+// Packets a thread holds, and rows.  Few threads with much each: a row's reductions are shared by fewer warps, and its
+// parameters by more of the work.  bf16, us, against one packet of two rows a thread: [16384, 4096] RMS pair 87 (113), LayerNorm pair
+// by four packets 110 (141), [32768, 2048] 86 (102), [8192, 8192] by four 99 (112), [4096, 16384] by eight 105 (131 swept several times).
+// A warp per row below 65 packets: [65536, 512] LayerNorm pair 49 (52 by a CTA).  Fewer rows than SMs are a matter of latency: one
+// packet of one row, 2.9 us for three rows of 4096 (4.1).
+template <class S, bool kMean> cudaError_t launch_norm_forward_rows(const NormForwardArgs& a, int sms, cudaStream_t st)
+{
+    if (a.packets <= 32) return launch_norm_forward_kernel<S, 1, 2, true, kMean>(a, st);
+    if (a.packets <= 64) return launch_norm_forward_kernel<S, 2, 1, true, kMean>(a, st);
+    if (a.packets <= 512 && a.rows <= size_t(sms)) return launch_norm_forward_kernel<S, 1, 1, false, kMean>(a, st);
+    if (a.packets <= (kMean ? 255 : 512)) return launch_norm_forward_kernel<S, 2, 2, false, kMean>(a, st);
+    if (a.packets <= 1024) return launch_norm_forward_kernel<S, 4, 1, false, kMean>(a, st);
+    return launch_norm_forward_kernel<S, 8, 1, false, kMean>(a, st);
 }
 
 template <class S>
@@ -533,25 +369,17 @@ cudaError_t launch_norm_forward(const NormForwardArgs& in, cudaStream_t st)
     if (a.rows == 0 || a.cols == 0) return cudaSuccess;
     const void* p[9] = {a.u, a.r, a.post_gain, a.post_bias, a.gate, a.pre_gain, a.pre_bias, a.s, a.h};
     a.packets = a.cols / S::kVec;
-    // a row in registers: a warp of one to four packets per lane, or a CTA of one or two (up to 1024 threads)
+    DeviceInfo di;
+    cudaError_t e = device_info(&di);
+    if (e != cudaSuccess) return e;
+    // a row in registers, eight packets a thread at most
     if (!norm_vector_ok<S>(p, 9, a.cols) || a.packets > 2048) {
-        DeviceInfo di;
-        cudaError_t e = device_info(&di);
-        if (e != cudaSuccess) return e;
         const size_t cap = size_t(di.sm_count) * 8;
         norm_forward_any_kernel<S><<<(unsigned)(a.rows < cap ? a.rows : cap), kBlock, 0, st>>>(a);
         return cudaPeekAtLastError();
     }
     const bool mean = a.post == kNormLayer || a.pre == kNormLayer;
-    // long rows, many of them, 16-bit storage (fp32 storage is not short of instructions), no means and no biases
-    if (S::kVec == 8 && !mean && !a.post_bias && !a.pre_bias && a.packets >= 384 && a.packets <= 1024 && a.rows >= 2048) {
-        DeviceInfo di;
-        cudaError_t e = device_info(&di);
-        if (e != cudaSuccess) return e;
-        if (a.packets <= 512) return launch_norm_forward_ring<S, 1, 2>(a, (a.packets + 31) / 32 * 32, di.sm_count, st);
-        return launch_norm_forward_ring<S, 2, 1>(a, ((a.packets + 1) / 2 + 31) / 32 * 32, di.sm_count, st);
-    }
-    return mean ? launch_norm_forward_rows<S, true>(a, st) : launch_norm_forward_rows<S, false>(a, st);
+    return mean ? launch_norm_forward_rows<S, true>(a, di.sm_count, st) : launch_norm_forward_rows<S, false>(a, di.sm_count, st);
 }
 
 // ---------------------------------------------------------------- backward

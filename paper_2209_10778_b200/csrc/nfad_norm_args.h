@@ -13,7 +13,7 @@ struct NormForwardArgs {
     const void *u, *r, *post_gain, *post_bias, *gate, *pre_gain, *pre_bias;
     void *s, *h;
     float4* stats;
-    size_t rows, rows_per_gate, chunk_rows;          // chunk_rows: of a CTA that stays (many rows)
+    size_t rows, rows_per_gate;
     uint32_t cols, packets;
     int post, pre;
     float alpha, eps, inv_cols;

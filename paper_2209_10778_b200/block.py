@@ -9,7 +9,26 @@ from typing import Dict, Optional
 
 import torch
 
-from .binding import BlockNormDesc, BlockNormGrads, _check, _kind, _on_device, _stream, _tensor, _TORCH_TO_CODE, load
+from .binding import BlockNormDesc, BlockNormGrads, _check, _kind, _on_device, _stream, _tensor, _TORCH_TO_CODE, _raw_stream, load
+
+# small calls are a few microseconds on the device: what is looked up for each of them is looked up once
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_functions = {}
+
+
+def _call(name: str, t: torch.Tensor, *args) -> None:
+    """The library's function on t's device and its current stream (the last argument); raises on any status but 0."""
+    fn = _functions.get(name)
+    if fn is None:
+        fn = _functions[name] = getattr(load(), name)
+    index = t.get_device()
+    if index == _current_device():
+        rc = fn(*args, _raw_stream(index) if _raw_stream is not None else _stream(t))
+    else:
+        with _on_device(t.device):
+            rc = fn(*args, _stream(t))
+    if rc:
+        _check(rc, name)
 
 NORMS = {"none": 0, "rms": 1, "layer": 2}
 NO_ACT = -1
@@ -23,6 +42,8 @@ def _raw(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, shape, device
     """The address of an optional tensor that must have exactly this type, shape and device."""
     if t is None:
         return None
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.is_cuda and t.device == device:
+        return t.data_ptr()
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
     if t.dtype != dtype:
@@ -71,13 +92,23 @@ class BlockNorm:
 
     def _fits(self, x: torch.Tensor, name: str) -> int:
         p = _tensor(x, name)
-        if x.dim() == 0 or (self.cols is not None and (x.shape[-1] != self.cols or x.dtype != self.dtype or x.device != self.device)):
+        if x.dim() == 0 or (self.cols is not None and (x.size(-1) != self.cols or x.dtype is not self.dtype or x.device != self.device)):
             raise ValueError(f"{name} must be [..., {self.cols}] of the parameters' dtype and device")
         return p
 
 
-def _like(t: Optional[torch.Tensor], name: str, first: torch.Tensor) -> Optional[int]:
-    return None if t is None else _tensor(t, name, first)
+def _kin(first: torch.Tensor):
+    """What tensors like `first` share, for _like: looked up once a call."""
+    return first.dtype, first.numel(), first.get_device(), first
+
+
+def _like(t: Optional[torch.Tensor], name: str, kin) -> Optional[int]:
+    """The address of an optional contiguous tensor of the first one's type, size and device."""
+    if t is None:
+        return None
+    if type(t) is torch.Tensor and t.dtype is kin[0] and t.numel() == kin[1] and t.get_device() == kin[2] and t.is_contiguous():
+        return t.data_ptr()
+    return _tensor(t, name, kin[3])                  # a subclass, or it raises
 
 
 def nfad_block_norm_forward(norm: BlockNorm, u: torch.Tensor, r: Optional[torch.Tensor], s_out: Optional[torch.Tensor],
@@ -85,12 +116,12 @@ def nfad_block_norm_forward(norm: BlockNorm, u: torch.Tensor, r: Optional[torch.
     """s_out = residual_scale r + gate N_post(u), h = N_pre(s): tensors [..., cols]; stats: fp32 [rows, 4], or None in a
     pass that will not be differentiated."""
     pu = norm._fits(u, "u")
-    cols = u.shape[-1]
-    rows = u.numel() // cols if cols else 0
-    ps = _raw(stats, "stats", torch.float32, (rows, 4), u.device)
-    with _on_device(u.device):
-        _check(load().nfad_block_norm_forward(norm.ref, _TORCH_TO_CODE[u.dtype], pu, _like(r, "r", u), _like(s_out, "s_out", u),
-                                              _like(h, "h", u), ps, rows, cols, _stream(u)), "nfad_block_norm_forward")
+    kin = _kin(u)
+    cols = u.size(-1)
+    rows = kin[1] // cols if cols else 0
+    ps = None if stats is None else _raw(stats, "stats", torch.float32, (rows, 4), u.device)
+    _call("nfad_block_norm_forward", u, norm.ref, _TORCH_TO_CODE[kin[0]], pu, _like(r, "r", kin), _like(s_out, "s_out", kin), _like(h, "h", kin), ps,
+          rows, cols)
 
 
 def nfad_block_norm_backward_scratch_bytes(dtype, rows: int, cols: int, device=None) -> int:
@@ -120,12 +151,10 @@ def nfad_block_norm_backward(norm: BlockNorm, grad_h: Optional[torch.Tensor], gr
         shape = like.shape if like is not None else (cols,)
         setattr(out, name, _raw(t, "grads[" + name + "]", torch.float32, torch.Size(shape), grad_u.device))
     sp, sb = _scratch(scratch)
-    with _on_device(grad_u.device):
-        _check(load().nfad_block_norm_backward(norm.ref, _TORCH_TO_CODE[grad_u.dtype], _like(grad_h, "grad_h", grad_u),
-                                               _like(grad_s, "grad_s", grad_u), _like(u, "u", grad_u), _like(s, "s", grad_u),
-                                               _raw(stats, "stats", torch.float32, (rows, 4), grad_u.device), pg,
-                                               _like(grad_r, "grad_r", grad_u), ctypes.byref(out), sp, sb, rows, cols,
-                                               _stream(grad_u)), "nfad_block_norm_backward")
+    kin = _kin(grad_u)
+    _call("nfad_block_norm_backward", grad_u, norm.ref, _TORCH_TO_CODE[kin[0]], _like(grad_h, "grad_h", kin), _like(grad_s, "grad_s", kin),
+          _like(u, "u", kin), _like(s, "s", kin), _raw(stats, "stats", torch.float32, (rows, 4), grad_u.device), pg,
+          _like(grad_r, "grad_r", kin), ctypes.byref(out), sp, sb, rows, cols)
 
 
 # ---------------------------------------------------------------- products grouped by expert
@@ -165,9 +194,7 @@ def nfad_expert_linear(kind, x: torch.Tensor, w: torch.Tensor, bias: Optional[to
     shape = (rows, n_out)
     pb = _raw(bias, "bias", x.dtype, (experts, n_out), x.device)
     py, pd = _raw(y, "y", x.dtype, shape, x.device), _raw(dfdx, "dfdx", x.dtype, shape, x.device)
-    with _on_device(x.device):
-        _check(load().nfad_expert_linear(_act(kind), _TORCH_TO_CODE[x.dtype], px, pw, pb, _offsets(offsets, x.device), py, pd, rows, n_in, n_out,
-                                         experts, _stream(x)), "nfad_expert_linear")
+    _call("nfad_expert_linear", x, _act(kind), _TORCH_TO_CODE[x.dtype], px, pw, pb, _offsets(offsets, x.device), py, pd, rows, n_in, n_out, experts)
 
 
 def nfad_expert_act_backward_scratch_bytes(rows: int, out: int, device=None) -> int:
@@ -191,9 +218,8 @@ def nfad_expert_act_backward(grad_out: torch.Tensor, dfdx: Optional[torch.Tensor
     pz = _raw(grad_z, "grad_z", grad_out.dtype, grad_out.shape, grad_out.device)
     pb = _raw(grad_bias, "grad_bias", torch.float32, (experts, n_out), grad_out.device)
     sp, sb = _scratch(scratch)
-    with _on_device(grad_out.device):
-        _check(load().nfad_expert_act_backward(_TORCH_TO_CODE[grad_out.dtype], pg, pd, _offsets(offsets, grad_out.device), pz, pb, sp, sb, rows,
-                                               n_out, experts, _stream(grad_out)), "nfad_expert_act_backward")
+    _call("nfad_expert_act_backward", grad_out, _TORCH_TO_CODE[grad_out.dtype], pg, pd, _offsets(offsets, grad_out.device), pz, pb, sp, sb,
+          rows, n_out, experts)
 
 
 def nfad_expert_linear_backward_input(grad_z: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, dfdx_x: Optional[torch.Tensor],
@@ -208,9 +234,8 @@ def nfad_expert_linear_backward_input(grad_z: torch.Tensor, w: torch.Tensor, off
     shape = (rows, n_in)
     pd = _raw(dfdx_x, "dfdx_x", grad_z.dtype, shape, grad_z.device)
     px = _raw(grad_x, "grad_x", grad_z.dtype, shape, grad_z.device)
-    with _on_device(grad_z.device):
-        _check(load().nfad_expert_linear_backward_input(_TORCH_TO_CODE[grad_z.dtype], pg, pw, _offsets(offsets, grad_z.device), pd, px, rows, n_in,
-                                                        n_out, experts, _stream(grad_z)), "nfad_expert_linear_backward_input")
+    _call("nfad_expert_linear_backward_input", grad_z, _TORCH_TO_CODE[grad_z.dtype], pg, pw, _offsets(offsets, grad_z.device), pd, px, rows,
+          n_in, n_out, experts)
 
 
 def nfad_expert_linear_backward_weight(grad_z: torch.Tensor, x: torch.Tensor, offsets: torch.Tensor, grad_w: torch.Tensor) -> None:
@@ -220,9 +245,8 @@ def nfad_expert_linear_backward_weight(grad_z: torch.Tensor, x: torch.Tensor, of
     if x.shape[0] != rows or x.dtype != grad_z.dtype or x.device != grad_z.device:
         raise ValueError("x must have grad_z's rows, dtype and device")
     pw = _raw(grad_w, "grad_w", grad_z.dtype, (experts, n_out, n_in), grad_z.device)
-    with _on_device(grad_z.device):
-        _check(load().nfad_expert_linear_backward_weight(_TORCH_TO_CODE[grad_z.dtype], pg, px, _offsets(offsets, grad_z.device), pw, rows, n_in,
-                                                         n_out, experts, _stream(grad_z)), "nfad_expert_linear_backward_weight")
+    _call("nfad_expert_linear_backward_weight", grad_z, _TORCH_TO_CODE[grad_z.dtype], pg, px, _offsets(offsets, grad_z.device), pw, rows, n_in,
+          n_out, experts)
 
 
 # ---------------------------------------------------------------- the linear layer in 8-bit integers
@@ -231,8 +255,7 @@ def nfad_i8_quantize_rows(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor)
     """q (int8) and scale (fp32 [rows]) of x [rows, cols]: x = scale q up to half a step of the row's own scale."""
     px = _matrix(x, "x")
     pq, ps = _raw(q, "q", torch.int8, x.shape, x.device), _raw(scale, "scale", torch.float32, x.shape[:1], x.device)
-    with _on_device(x.device):
-        _check(load().nfad_i8_quantize_rows(_TORCH_TO_CODE[x.dtype], px, pq, ps, x.shape[0], x.shape[1], _stream(x)), "nfad_i8_quantize_rows")
+    _call("nfad_i8_quantize_rows", x, _TORCH_TO_CODE[x.dtype], px, pq, ps, x.shape[0], x.shape[1])
 
 
 def _i8_weight(wq: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor], y: torch.Tensor, n_in: int):
@@ -252,8 +275,7 @@ def nfad_i8_linear(kind, xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tens
     if y.shape != (rows, n_out):
         raise ValueError("y must be [rows, out]")
     px, pxs = _raw(xq, "xq", torch.int8, (rows, n_in), y.device), _raw(x_scale, "x_scale", torch.float32, (rows,), y.device)
-    with _on_device(y.device):
-        _check(load().nfad_i8_linear(_act(kind), _TORCH_TO_CODE[y.dtype], px, pxs, pw, pws, pb, py, rows, n_in, n_out, _stream(y)), "nfad_i8_linear")
+    _call("nfad_i8_linear", y, _act(kind), _TORCH_TO_CODE[y.dtype], px, pxs, pw, pws, pb, py, rows, n_in, n_out)
 
 
 def nfad_i8_linear_dynamic_scratch_bytes(rows: int, n_in: int) -> int:
@@ -274,9 +296,7 @@ def nfad_i8_linear_dynamic(kind, x: torch.Tensor, wq: torch.Tensor, w_scale: tor
     if y.shape != (rows, n_out) or y.dtype != x.dtype or y.device != x.device:
         raise ValueError("y must be [rows, out] of x's dtype and device")
     sp, sb = _scratch(scratch)
-    with _on_device(x.device):
-        _check(load().nfad_i8_linear_dynamic(_act(kind), _TORCH_TO_CODE[x.dtype], px, pw, pws, pb, py, sp, sb, rows, n_in, n_out, _stream(x)),
-               "nfad_i8_linear_dynamic")
+    _call("nfad_i8_linear_dynamic", x, _act(kind), _TORCH_TO_CODE[x.dtype], px, pw, pws, pb, py, sp, sb, rows, n_in, n_out)
 
 
 def nfad_wait_faults() -> int:

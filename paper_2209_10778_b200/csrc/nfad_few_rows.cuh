@@ -214,10 +214,11 @@ __global__ void __launch_bounds__(kFewWarps * 32, NT == 1 ? 4 : 3) few_rows_kern
 template <bool kBytes, class S, int NT> cudaError_t launch_few_rows_tiles(const ProdArgs& g, int sms, int early, cudaStream_t st)
 {
     const size_t live = g.rows < g.experts ? g.rows : g.experts;
-    size_t grid = (g.outs + kFewOutputs - 1) / kFewOutputs * live;
-    const size_t cap = size_t(sms) * (NT == 1 ? 4 : 3);              // more than fit at once; each then walks over its share
+    const size_t jobs = (g.outs + kFewOutputs - 1) / kFewOutputs * live, fit = size_t(sms) * (NT == 1 ? 4 : 3);
+    // one expert, whose jobs are known: as many for each CTA, rather than a last turn of a few (13.3 -> 12.6 us); else all that fit
+    const size_t turns = g.experts == 1 ? (jobs + fit - 1) / fit : 1, grid = (jobs + turns - 1) / turns;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(grid < cap ? grid : cap));
+    cfg.gridDim = dim3(unsigned(grid < fit ? grid : fit));
     cfg.blockDim = dim3(kFewWarps * 32);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -228,11 +229,11 @@ template <bool kBytes, class S, int NT> cudaError_t launch_few_rows_tiles(const 
     return cudaLaunchKernelEx(&cfg, few_rows_kernel<kBytes, S, NT>, g, early);
 }
 
-// Whether there are few rows: 32 at most, or up to four for each expert.  Measured against the tiles on tcgen05: one token
-// 4096 -> 12288 in 8 bits 12.6 us (24.6), 16 tokens 4096 -> 4096 6.5 (14.0), 32 tokens 5120 -> 2048 11.9 (16.0), 64 of them 22.6 (16.1);
-// 24 rows over 64 experts 2048 -> 1408 bf16 24.8 (44.2), 256 of them 62.7 (65.7); 64 rows over 8 experts 2048 -> 4096 34.7 (28.7).
+// Whether there are few rows: 16 at most, or up to four for each expert.  Measured against tiles on tcgen05 (us): one token
+// 4096 -> 12288 in 8 bits 12.6 (24.6), 16 tokens 4096 -> 4096 6.6 (14.0); 32 of them bf16 23.6 (16.5); 24 rows over 64 experts
+// 2048 -> 1408 bf16 24.8 (44.2), 256 of them 62.7 (65.7); 64 rows over 8 experts 2048 -> 4096 34.7 (28.7).
 // (Byte offsets inside a row are 32-bit there.)
-inline bool few_rows(const ProdArgs& g) { return g.in < (1u << 28) && (g.rows <= 32 || (g.rows <= kFewMaxRows && g.rows <= 4 * size_t(g.experts))); }
+inline bool few_rows(const ProdArgs& g) { return g.in < (1u << 28) && (g.rows <= 16 || (g.rows <= kFewMaxRows && g.rows <= 4 * size_t(g.experts))); }
 
 // Tokens a job takes at once, by the rows an expert has on average: an expert with more is read once per such group.
 template <bool kBytes, class S> cudaError_t launch_few_rows(const ProdArgs& g, int sms, int early, cudaStream_t st)

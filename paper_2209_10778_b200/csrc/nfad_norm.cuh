@@ -69,6 +69,50 @@ template <class S> __device__ __forceinline__ void load_parameter(const void* ba
     S::unpack(__ldg(static_cast<const uint4*>(base) + row * packets + p), v);
 }
 
+// Rows that do not start on 16-byte boundaries: a thread's packet of V elements is V / kUnit pieces of kUnit elements, the pieces of
+// neighbouring threads side by side.
+template <class S, int kUnit> struct RowColumns {
+    static constexpr int V = S::kVec, kPieces = V / kUnit;
+    using E = typename S::elem;
+    uint32_t lane, width, cols;
+    __device__ __forceinline__ uint32_t column(int i, int piece) const { return ((i * kPieces + piece) * width + lane) * kUnit; }
+    // one bit for each element that is inside the row (rows hold whole pieces)
+    __device__ __forceinline__ uint32_t mask(int i) const
+    {
+        uint32_t m = 0;
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j)
+            if (column(i, j) < cols) m |= ((1u << kUnit) - 1) << (j * kUnit);
+        return m;
+    }
+    // outside the row: zeros
+    __device__ __forceinline__ uint4 load(const void* base, size_t row, int i) const
+    {
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+            const E* at = static_cast<const E*>(base) + row * cols + column(i, j);
+            if (column(i, j) < cols) {
+                if constexpr (kUnit * sizeof(E) == 2) w[j >> 1] |= uint32_t(*reinterpret_cast<const unsigned short*>(at)) << (16 * (j & 1));
+                else w[j] = *reinterpret_cast<const unsigned*>(at);
+            }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __device__ __forceinline__ void store(void* base, size_t row, int i, const uint4& v) const
+    {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+            E* at = static_cast<E*>(base) + row * cols + column(i, j);
+            if (column(i, j) < cols) {
+                if constexpr (kUnit * sizeof(E) == 2) *reinterpret_cast<unsigned short*>(at) = (unsigned short)(w[j >> 1] >> (16 * (j & 1)));
+                else *reinterpret_cast<unsigned*>(at) = w[j];
+            }
+        }
+    }
+};
+
 // 1 / sqrt(x): the hardware's approximation and one Newton step, within two units in the last place
 __device__ __forceinline__ float reciprocal_root(float x)
 {
@@ -85,8 +129,8 @@ __device__ __forceinline__ size_t gate_row_of(size_t row, size_t rows_per_gate)
 }
 
 // Means and reciprocal deviations of kR rows whose threads hold kI packets each; packets past the row hold zeros.
-template <int V, int kR, int kI, bool kWarp, bool kMean>
-__device__ __forceinline__ void row_statistics(const float (&v)[kR][kI][V], const bool (&on)[kI], int kind, float inv_cols, float eps,
+template <int V, int kUnit, int kR, int kI, bool kWarp, bool kMean>
+__device__ __forceinline__ void row_statistics(const float (&v)[kR][kI][V], const uint32_t (&on)[kI], int kind, float inv_cols, float eps,
                                                RowSum<kR, kWarp>& sum, float (&mean)[kR], float (&rstd)[kR])
 {
     float t[kR];
@@ -111,7 +155,8 @@ __device__ __forceinline__ void row_statistics(const float (&v)[kR][kI][V], cons
             if (!kMean || on[i])
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float c = kMean ? v[k][i][e] - mean[k] : v[k][i][e];
+                    float c = kMean ? v[k][i][e] - mean[k] : v[k][i][e];
+                    if (kMean && kUnit < V && !(on[i] >> e & 1)) c = 0.0f;
                     t[k] = fmaf(c, c, t[k]);
                 }
     }
@@ -138,7 +183,8 @@ __global__ void __launch_bounds__(kWarp ? 128 : kI == 1 ? 512 : 256) norm_forwar
     for (size_t turn = blockIdx.x * per_cta + (kWarp ? threadIdx.x >> 5 : 0); turn * kR < a.rows; turn += gridDim.x * per_cta) {
         const size_t row = turn * kR;
         uint4 ru[kR][kI], rr[kR][kI];
-        bool on[kI], there[kR];
+        uint32_t on[kI];
+        bool there[kR];
 #pragma unroll
         for (int k = 0; k < kR; ++k) there[k] = k == 0 || row + k < a.rows;
 #pragma unroll
@@ -161,7 +207,7 @@ __global__ void __launch_bounds__(kWarp ? 128 : kI == 1 ? 512 : 256) norm_forwar
 #pragma unroll
             for (int i = 0; i < kI; ++i) S::unpack(ru[k][i], v[k][i]);
         }
-        if (a.post != kNormNone) row_statistics<V, kR, kI, kWarp, kMean>(v, on, a.post, a.inv_cols, a.eps, sum, mean, rstd);
+        if (a.post != kNormNone) row_statistics<V, V, kR, kI, kWarp, kMean>(v, on, a.post, a.inv_cols, a.eps, sum, mean, rstd);
         size_t gate_row[kR];
 #pragma unroll
         for (int k = 0; k < kR; ++k) gate_row[k] = a.gate ? gate_row_of(row + k, a.rows_per_gate) : 0;
@@ -210,7 +256,7 @@ __global__ void __launch_bounds__(kWarp ? 128 : kI == 1 ? 512 : 256) norm_forwar
             }
         }
         if (a.pre != kNormNone) {
-            row_statistics<V, kR, kI, kWarp, kMean>(v, on, a.pre, a.inv_cols, a.eps, sum, mean2, rstd2);
+            row_statistics<V, V, kR, kI, kWarp, kMean>(v, on, a.pre, a.inv_cols, a.eps, sum, mean2, rstd2);
 #pragma unroll
             for (int i = 0; i < kI; ++i) {
                 const uint32_t p = lane + i * width;
@@ -237,6 +283,132 @@ __global__ void __launch_bounds__(kWarp ? 128 : kI == 1 ? 512 : 256) norm_forwar
 #pragma unroll
                 for (int k = 0; k < kR; ++k)
                     if (there[k]) store_packet<true>(static_cast<uint4*>(a.h) + (row + k) * a.packets + p, S::pack(v[k][i]));
+            }
+        }
+        if (a.stats && lane == 0)
+#pragma unroll
+            for (int k = 0; k < kR; ++k)
+                if (there[k]) a.stats[row + k] = make_float4(mean[k], rstd[k], mean2[k], rstd2[k]);
+    }
+}
+
+// The same for rows off the 16-byte boundaries: packets of pieces, and a bit for each element that is inside the row.
+template <class S, int kUnit, int kI, int kR, bool kWarp, bool kMean>
+__global__ void __launch_bounds__(kWarp ? 128 : 256, kWarp ? 8 : kI == 4 ? 3 : 2) norm_forward_odd_kernel(const __grid_constant__ NormForwardArgs a)
+{
+    constexpr int V = S::kVec;
+    __shared__ float buf[2][kR][32];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const uint32_t lane = kWarp ? threadIdx.x & 31 : threadIdx.x, width = kWarp ? 32 : blockDim.x;
+    const size_t per_cta = kWarp ? blockDim.x >> 5 : 1;
+    RowSum<kR, kWarp> sum{buf, 0};
+    const RowColumns<S, kUnit> at{lane, width, a.cols};
+    uint32_t on[kI];
+#pragma unroll
+    for (int i = 0; i < kI; ++i) on[i] = at.mask(i);
+    auto parameter = [&](const void* base, size_t row, int i, float (&w)[V]) { S::unpack(at.load(base, row, i), w); };
+    for (size_t turn = blockIdx.x * per_cta + (kWarp ? threadIdx.x >> 5 : 0); turn * kR < a.rows; turn += gridDim.x * per_cta) {
+        const size_t row = turn * kR;
+        uint4 ru[kR][kI], rr[kR][kI];
+        bool there[kR];
+#pragma unroll
+        for (int k = 0; k < kR; ++k) there[k] = k == 0 || row + k < a.rows;
+#pragma unroll
+        for (int i = 0; i < kI; ++i)
+#pragma unroll
+            for (int k = 0; k < kR; ++k) {
+                ru[k][i] = rr[k][i] = make_uint4(0, 0, 0, 0);
+                if (there[k]) {
+                    ru[k][i] = at.load(a.u, row + k, i);
+                    if (a.r) rr[k][i] = at.load(a.r, row + k, i);
+                }
+            }
+        float v[kR][kI][V], mean[kR], rstd[kR], mean2[kR], rstd2[kR];
+#pragma unroll
+        for (int k = 0; k < kR; ++k) {
+            mean[k] = rstd[k] = mean2[k] = rstd2[k] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kI; ++i) S::unpack(ru[k][i], v[k][i]);
+        }
+        if (a.post != kNormNone) row_statistics<V, kUnit, kR, kI, kWarp, kMean>(v, on, a.post, a.inv_cols, a.eps, sum, mean, rstd);
+        size_t gate_row[kR];
+#pragma unroll
+        for (int k = 0; k < kR; ++k) gate_row[k] = a.gate ? gate_row_of(row + k, a.rows_per_gate) : 0;
+#pragma unroll
+        for (int i = 0; i < kI; ++i) {
+            if (!on[i]) continue;
+            float w[V];
+            if (a.post != kNormNone) {
+#pragma unroll
+                for (int k = 0; k < kR; ++k)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[k][i][e] = kMean ? (v[k][i][e] - mean[k]) * rstd[k] : v[k][i][e] * rstd[k];
+                if (a.post_gain) {
+                    parameter(a.post_gain, 0, i, w);
+#pragma unroll
+                    for (int k = 0; k < kR; ++k)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) v[k][i][e] *= w[e];
+                }
+                if (a.post_bias) {
+                    parameter(a.post_bias, 0, i, w);
+#pragma unroll
+                    for (int k = 0; k < kR; ++k)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) v[k][i][e] += w[e];
+                }
+            }
+            if (a.gate) {
+#pragma unroll
+                for (int k = 0; k < kR; ++k) {
+                    if (k > 0 && !there[k]) continue;
+                    if (k == 0 || gate_row[k] != gate_row[0]) parameter(a.gate, gate_row[k], i, w);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[k][i][e] *= w[e];
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kR; ++k) {
+                if (a.r) {
+                    S::unpack(rr[k][i], w);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[k][i][e] = fmaf(a.alpha, w[e], v[k][i][e]);
+                }
+                if (kMean && kUnit < V)                              // columns past the row hold nothing for the next mean
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        if (!(on[i] >> e & 1)) v[k][i][e] = 0.0f;
+                if (a.s && there[k]) at.store(a.s, row + k, i, S::pack(v[k][i]));
+            }
+        }
+        if (a.pre != kNormNone) {
+            row_statistics<V, kUnit, kR, kI, kWarp, kMean>(v, on, a.pre, a.inv_cols, a.eps, sum, mean2, rstd2);
+#pragma unroll
+            for (int i = 0; i < kI; ++i) {
+                if (!on[i]) continue;
+                float w[V];
+#pragma unroll
+                for (int k = 0; k < kR; ++k)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[k][i][e] = kMean ? (v[k][i][e] - mean2[k]) * rstd2[k] : v[k][i][e] * rstd2[k];
+                if (a.pre_gain) {
+                    parameter(a.pre_gain, 0, i, w);
+#pragma unroll
+                    for (int k = 0; k < kR; ++k)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) v[k][i][e] *= w[e];
+                }
+                if (a.pre_bias) {
+                    parameter(a.pre_bias, 0, i, w);
+#pragma unroll
+                    for (int k = 0; k < kR; ++k)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) v[k][i][e] += w[e];
+                }
+#pragma unroll
+                for (int k = 0; k < kR; ++k)
+                    if (there[k]) at.store(a.h, row + k, i, S::pack(v[k][i]));
             }
         }
         if (a.stats && lane == 0)
@@ -337,14 +509,16 @@ template <class S> inline bool norm_vector_ok(const void* const* p, int n, size_
     return true;
 }
 
-template <class S, int kI, int kR, bool kWarp, bool kMean> cudaError_t launch_norm_forward_kernel(const NormForwardArgs& a, cudaStream_t st)
+// kUnit == V: aligned rows
+template <class S, int kUnit, int kI, int kR, bool kWarp, bool kMean> cudaError_t launch_norm_forward_kernel(const NormForwardArgs& a, cudaStream_t st)
 {
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];
     const size_t rows = kWarp ? 4 * kR : kR;         // of a CTA
     const unsigned block = kWarp ? 128 : ((a.packets + kI - 1) / kI + 31) / 32 * 32;
     norm_launch_config(&cfg, attr, (a.rows + rows - 1) / rows, block, st);
-    return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, kI, kR, kWarp, kMean>, a);
+    if constexpr (kUnit == S::kVec) return cudaLaunchKernelEx(&cfg, norm_forward_kernel<S, kI, kR, kWarp, kMean>, a);
+    else return cudaLaunchKernelEx(&cfg, norm_forward_odd_kernel<S, kUnit, kI, kR, kWarp, kMean>, a);
 }
 
 // Packets a thread holds, and rows.  Few threads with much each: a row's reductions are shared by fewer warps, and its
@@ -354,12 +528,23 @@ template <class S, int kI, int kR, bool kWarp, bool kMean> cudaError_t launch_no
 // packet of one row, 2.9 us for three rows of 4096 (4.1).
 template <class S, bool kMean> cudaError_t launch_norm_forward_rows(const NormForwardArgs& a, int sms, cudaStream_t st)
 {
-    if (a.packets <= 32) return launch_norm_forward_kernel<S, 1, 2, true, kMean>(a, st);
-    if (a.packets <= 64) return launch_norm_forward_kernel<S, 2, 1, true, kMean>(a, st);
-    if (a.packets <= 512 && a.rows <= size_t(sms)) return launch_norm_forward_kernel<S, 1, 1, false, kMean>(a, st);
-    if (a.packets <= (kMean ? 255 : 512)) return launch_norm_forward_kernel<S, 2, 2, false, kMean>(a, st);
-    if (a.packets <= 1024) return launch_norm_forward_kernel<S, 4, 1, false, kMean>(a, st);
-    return launch_norm_forward_kernel<S, 8, 1, false, kMean>(a, st);
+    constexpr int V = S::kVec;
+    if (a.packets <= 32) return launch_norm_forward_kernel<S, V, 1, 2, true, kMean>(a, st);
+    if (a.packets <= 64) return launch_norm_forward_kernel<S, V, 2, 1, true, kMean>(a, st);
+    if (a.packets <= 512 && a.rows <= size_t(sms)) return launch_norm_forward_kernel<S, V, 1, 1, false, kMean>(a, st);
+    if (a.packets <= (kMean ? 255 : 512)) return launch_norm_forward_kernel<S, V, 2, 2, false, kMean>(a, st);
+    if (a.packets <= 1024) return launch_norm_forward_kernel<S, V, 4, 1, false, kMean>(a, st);
+    return launch_norm_forward_kernel<S, V, 8, 1, false, kMean>(a, st);
+}
+
+// Rows off the 16-byte boundaries, in pieces of 4 bytes where they begin on those (an even number of 16-bit columns), else element
+// by element.  bf16, us, against a CTA that sweeps its row from memory for each statistic: [14808, 100] 6 (47), [4000, 1021] 30 (43),
+// [8192, 4098] 95 (184), [8192, 4097] 191 (184), [5076, 14082] 375 (727).
+template <class S, int kUnit, bool kMean> cudaError_t launch_norm_forward_odd(const NormForwardArgs& a, cudaStream_t st)
+{
+    if (a.packets <= 32) return launch_norm_forward_kernel<S, kUnit, 1, 2, true, kMean>(a, st);
+    if (a.packets <= 1024) return launch_norm_forward_kernel<S, kUnit, 4, 1, false, kMean>(a, st);
+    return launch_norm_forward_kernel<S, kUnit, 8, 1, false, kMean>(a, st);
 }
 
 template <class S>
@@ -368,18 +553,23 @@ cudaError_t launch_norm_forward(const NormForwardArgs& in, cudaStream_t st)
     NormForwardArgs a = in;
     if (a.rows == 0 || a.cols == 0) return cudaSuccess;
     const void* p[9] = {a.u, a.r, a.post_gain, a.post_bias, a.gate, a.pre_gain, a.pre_bias, a.s, a.h};
-    a.packets = a.cols / S::kVec;
+    a.packets = (a.cols + S::kVec - 1) / S::kVec;
     DeviceInfo di;
     cudaError_t e = device_info(&di);
     if (e != cudaSuccess) return e;
     // a row in registers, eight packets a thread at most
-    if (!norm_vector_ok<S>(p, 9, a.cols) || a.packets > 2048) {
+    if (a.packets > 2048) {
         const size_t cap = size_t(di.sm_count) * 8;
         norm_forward_any_kernel<S><<<(unsigned)(a.rows < cap ? a.rows : cap), kBlock, 0, st>>>(a);
         return cudaPeekAtLastError();
     }
     const bool mean = a.post == kNormLayer || a.pre == kNormLayer;
-    return mean ? launch_norm_forward_rows<S, true>(a, di.sm_count, st) : launch_norm_forward_rows<S, false>(a, di.sm_count, st);
+    if (norm_vector_ok<S>(p, 9, a.cols)) return mean ? launch_norm_forward_rows<S, true>(a, di.sm_count, st) : launch_norm_forward_rows<S, false>(a, di.sm_count, st);
+    constexpr int kTwo = S::kVec == 8 ? 2 : 1;       // elements in 4 bytes
+    uintptr_t low = 0;
+    for (const void* q : p) low |= reinterpret_cast<uintptr_t>(q);
+    if (kTwo == 2 && a.cols % 2 == 0 && low % 4 == 0) return mean ? launch_norm_forward_odd<S, kTwo, true>(a, st) : launch_norm_forward_odd<S, kTwo, false>(a, st);
+    return mean ? launch_norm_forward_odd<S, 1, true>(a, st) : launch_norm_forward_odd<S, 1, false>(a, st);
 }
 
 // ---------------------------------------------------------------- backward

@@ -372,8 +372,8 @@ typedef struct { float *post_gain, *post_bias, *gate, *pre_gain, *pre_bias; } nf
  *   when pre is NONE;  stats [out] rows x 4 floats, 16-byte aligned: mean and 1/sqrt of u, then of s (0 where there is no
  *   norm or no mean) for nfad_block_norm_backward, or NULL in a pass that will not be differentiated.
  * s_out and h may each equal u or r (not both the same tensor).  The 128-bit path needs cols to be a multiple of the
- * packet (8 elements, 4 for fp32), 16-byte aligned tensors and at most 2048 packets in a row; otherwise a slower kernel takes
- * every element by itself.  cols must be below 2^31 (NFAD_E_TOO_LARGE).
+ * packet (8 elements, 4 for fp32), 16-byte aligned tensors and at most 2048 packets in a row; other rows go by 4 bytes or by
+ * single elements, and rows too long to be held on chip are read again for each pass.  cols must be below 2^31 (NFAD_E_TOO_LARGE).
  */
 NFAD_API int nfad_block_norm_forward(const nfad_block_norm* norm, int dtype, const void* u, const void* r, void* s_out, void* h,
                                      float* stats, size_t rows, size_t cols, nfad_stream_t stream);

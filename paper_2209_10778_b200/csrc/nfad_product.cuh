@@ -4,14 +4,14 @@
 // One CTA per SM stays for the whole launch and walks over result tiles of 128 x BN.  Its warps have roles:
 //   copy      (one thread) tensor copies of the operands' 128-byte wide boxes into a ring of stages;
 //   products  (one thread) 128 x BN x 64 (128 bytes of the reduction) per stage into one of two accumulators;
-//   results   (eight warps) read the other accumulator, apply the epilogue, store.
+//   results   (eight warps, four beside a gather) read the other accumulator, apply the epilogue, store.
 // So copies, products and epilogues of neighbouring tiles overlap.  Which rows a tile has comes from the offsets on the
 // device: every CTA builds the table of row ranges in shared memory and finds its tiles in it, with no word from the host.
 // A tile's last rows may belong to the next expert (forward, input gradient): they are computed and not stored, as rows do
 // not mix.  In the weight gradient rows are the reduction, so rows past the expert's end are cleared in shared memory
 // (both operands: 0 times a NaN of the neighbour would be one).
 //
-// Operands that no tensor copy can take (rows that do not start on 16-byte boundaries) are gathered by four further warps
+// Operands that no tensor copy can take (rows that do not start on 16-byte boundaries) are gathered by eight further warps
 // with plain loads into the same swizzled stages (kGather); everything behind the stages is shared.
 //
 // What bounds it: the tensor cores for long inputs (2 rows in out operations, 32 KB + 16 KB of operands for each 128 x 256 x

@@ -89,6 +89,36 @@ def test_forward(dtype, post, pre):
             _check_forward(p, u, r, *_forward(p, u, r))
 
 
+# rows that do not fill 16-byte packets: by 4 bytes, by single elements; few and many packets a thread; too long to be held
+ODD_SHAPES = [(40, 100), (33, 1002), (9, 4098), (6, 14082), (7, 12289), (2, 34007), (400, 202), (333, 997), (200, 6002)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", ODD_SHAPES)
+def test_rows_off_the_packets(dtype, rows, cols):
+    u, r = _tensors(rows, cols, dtype, cols)
+    dh, gs = _tensors(rows, cols, dtype, cols + 2)
+    for i, (post, pre) in enumerate(NORMS):
+        p = _parameters(dtype, cols, rows, post, pre, 1 if i % 2 else 0, i % 3 == 1, 3000 + i)
+        s, h, stats = _forward(p, u, r)
+        _check_forward(p, u, r, s, h, stats)
+        s = s.cpu()
+        _check_backward(p, dh if pre != "none" else None, gs, u, s, stats, *_backward(p, dh if pre != "none" else None, gs, u, s, stats))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [(400, 64), (700, 512), (333, 1024), (451, 4096), (310, 6144)])
+def test_more_rows_than_multiprocessors(dtype, rows, cols):
+    u, r = _tensors(rows, cols, dtype, cols)
+    dh, gs = _tensors(rows, cols, dtype, cols + 2)
+    for post, pre in (("rms", "rms"), ("layer", "layer"), ("none", "layer")):
+        p = _parameters(dtype, cols, rows, post, pre, 1, True, 4000)
+        s, h, stats = _forward(p, u, r)
+        _check_forward(p, u, r, s, h, stats)
+        s = s.cpu()
+        _check_backward(p, dh, gs, u, s, stats, *_backward(p, dh, gs, u, s, stats))
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_forward_without_stream_or_s(dtype):
     rows, cols = 17, 512

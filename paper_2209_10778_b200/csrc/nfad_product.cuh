@@ -154,11 +154,15 @@ template <int kRows> __device__ __forceinline__ void row_table(const ProdArgs& g
     }
 }
 
-// Clears reduction steps from `keep` on in `runs` boxes of `steps` 128-byte rows, by one warp.
-__device__ __forceinline__ void clear_runs(unsigned char* at, int runs, int keep, int steps, int lane)
+// The weight gradient's last step of an expert: `keep` of its 64 rows are the expert's.  Products are issued by 16 rows, as many as hold one of
+// them, so only the rows up to the next multiple of 16 have to be cleared: here, in `runs` boxes of 128-byte rows, by one warp.  (All 64
+// cleared and multiplied: 77 us for 61 experts of 67 rows, 1000 x 1416 f16; 46 us for 64 rows each.)
+constexpr int kProductRows = 16;
+__device__ __forceinline__ void clear_runs(unsigned char* at, int runs, int keep, int lane)
 {
+    const int end = (keep + kProductRows - 1) / kProductRows * kProductRows * 8;
     for (int j = 0; j < runs; ++j)
-        for (int i = keep * 8 + lane; i < steps * 8; i += 32) *reinterpret_cast<uint4*>(at + j * 64 * 128 + i * 16) = make_uint4(0, 0, 0, 0);
+        for (int i = keep * 8 + lane; i < end; i += 32) *reinterpret_cast<uint4*>(at + j * 64 * 128 + i * 16) = make_uint4(0, 0, 0, 0);
 }
 
 // ---------------------------------------------------------------- gathering without tensor copies
@@ -448,11 +452,11 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
         const uint32_t unit_n = kPair ? 32 : 16, left = (width - q.b0 + unit_n - 1) / unit_n * unit_n;
         return left < uint32_t(BN) ? left : uint32_t(BN);
     };
-    // a step of the weight gradient that holds rows past the expert's end (gathered operands come without them)
-    auto ragged = [&](const ProdTileAt& q, int r) { return OP == kProdWeight && !kGather && r + kStep > q.r_end; };
+    // a step of the weight gradient whose products reach past the expert's end (gathered operands come without those rows)
+    auto ragged = [&](const ProdTileAt& q, int r) { return OP == kProdWeight && !kGather && r + kStep > q.r_end && (q.r_end - r) % kProductRows; };
     // clears those rows in every 128-byte run of this CTA's two operands
     auto clear_ragged = [&](const ProdTileAt& q, int r, uint32_t stage) {
-        clear_runs(ring + stage * Tile::kStage, 2 + kOwn / 64, q.r_end - r, kStep, lane);
+        clear_runs(ring + stage * Tile::kStage, 2 + kOwn / 64, q.r_end - r, lane);
         tc::writes_to_async();
         if (kPair) tc::pair_fence();
         __syncwarp();
@@ -577,6 +581,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
                 if (lane == 0) {
 #pragma unroll
                     for (int k = 0; k < kStepBytes / 32; ++k) {
+                        if (OP == kProdWeight && k * kProductRows >= q.r_end - r) break;
                         // 32 bytes of the reduction: along the 128-byte rows, or 16 reduction steps of 128 bytes further
                         const uint64_t da = Kind::kTurnA ? tc::operand(at_a + k * 2048, 64 * 128, 1024) : tc::operand(at_a + k * 32, 16, 1024);
                         const uint64_t db = Kind::kTurnB ? tc::operand(at_b + k * 2048, 64 * 128, 1024) : tc::operand(at_b + k * 32, 16, 1024);

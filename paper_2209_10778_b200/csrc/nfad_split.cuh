@@ -83,7 +83,7 @@ split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtenso
         r1 = min(q.r_end, r0 + per * kStep);
     }
     const uint32_t n = min(uint32_t(kSplitColumns), (width - q.b0 + 15) / 16 * 16);
-    auto ragged = [&](int r) { return OP == kProdWeight && r + kStep > q.r_end; };
+    auto ragged = [&](int r) { return OP == kProdWeight && r + kStep > q.r_end && (q.r_end - r) % kProductRows; };
     bool ok = true;
     if (warp == 0 || warp == 3) {
         const bool for_a = warp == 0;
@@ -126,7 +126,7 @@ split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtenso
             if (ragged(r)) {
                 if (!(ok = tc::barrier_wait(landed(stage), landed_phases >> stage & 1, gave_up))) break;
                 landed_phases ^= 1u << stage;
-                clear_runs(ring + stage * kSplitStage, 2 + kSplitColumns / 64, q.r_end - r, kStep, lane);
+                clear_runs(ring + stage * kSplitStage, 2 + kSplitColumns / 64, q.r_end - r, lane);
                 tc::writes_to_async();
                 __syncwarp();
                 if (lane < 2) tc::barrier_arrive(full(stage));
@@ -137,6 +137,7 @@ split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtenso
             if (lane == 0) {
 #pragma unroll
                 for (int k = 0; k < kStepBytes / 32; ++k) {
+                    if (OP == kProdWeight && k * kProductRows >= q.r_end - r) break;
                     const uint64_t da = Kind::kTurnA ? tc::operand(at_a + k * 2048, 64 * 128, 1024) : tc::operand(at_a + k * 32, 16, 1024);
                     const uint64_t db = Kind::kTurnB ? tc::operand(at_b + k * 2048, 64 * 128, 1024) : tc::operand(at_b + k * 32, 16, 1024);
                     tc::product<Kind::kBytes, false>(tmem, da, db, what, r > r0 || k > 0);

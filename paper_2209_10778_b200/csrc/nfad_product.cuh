@@ -15,7 +15,7 @@
 // with plain loads into the same swizzled stages (kGather); everything behind the stages is shared.
 //
 // What bounds it: the tensor cores for long inputs (2 rows in out operations, 32 KB + 16 KB of operands for each 128 x 256 x
-// 64 step); the weights' bytes when an expert has few rows.  BN is chosen by how many tiles there are (see product_width).
+// 64 step); the weights' bytes when an expert has few rows.  BN is chosen by how many turns the tiles take (see product_tile).
 #pragma once
 
 #include "nfad_internal.h"

@@ -125,10 +125,9 @@ template <int OP, class S> cudaError_t launch_split(const ProdArgs& g, unsigned 
 }
 
 // Over how many CTAs a tile's reduction is split (0: not at all; single CTAs or pairs walk over the tiles): as many as two to an
-// SM allow, with ten steps left for each; and one when the tiles alone are between one and two to an SM.  Measured (us, against
-// tiles that are walked over): 77 rows 5120 -> 2048 in 8 bits over 4: 10.9 (16.2); 64 rows 4096 -> 4096 bf16 over 4: 16.7 (23.9); 128 rows
-// 4096 -> 12288 in 8 bits, over one: 19.6 (27.0); weight gradient 8192 rows of 256 x 256 over 8: 13.3 (41.8).  With eight steps each no gain
-// (1024 x 1024 x 1024 over 2: 10.8, 10.8); with more CTAs than fit twice what it was.
+// SM allow, with ten steps left for each.  Measured (us, against tiles that are walked over): 77 rows 5120 -> 2048 in 8 bits over 4:
+// 10.7 (16.2); 64 rows 4096 -> 4096 bf16 over 4: 15.7 (23.3); 200 rows over 2: 19.6 (25.1); weight gradient 8192 rows of 256 x 256 over
+// 8: 13.3 (41.8).  With eight steps each no gain (1024 x 1024 x 1024 over 2: 10.8, 10.8); with more CTAs than fit twice what it was.
 template <int OP> unsigned split_ranks(const ProdArgs& g, int sms)
 {
     const size_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs;
@@ -140,32 +139,38 @@ template <int OP> unsigned split_ranks(const ProdArgs& g, int sms)
     const size_t steps = (OP == kProdInput ? g.outs : OP == kProdWeight ? g.rows / g.experts : g.in) / ProdKind<OP>::kStep;
     for (unsigned ranks = 8; ranks > 1; ranks /= 2)
         if (tiles * ranks <= fit && steps >= 10 * ranks) return ranks;
-    return OP != kProdWeight && tiles > size_t(sms) && tiles <= fit ? 1 : 0;
+    return 0;
 }
 
-// Columns of a tile: the widest of 256, 128 and 64 that still gives every SM a tile, by the tiles that the rows make when they
-// spread evenly over the experts.  A wide tile reads operands from shared memory the fewest times per product; many narrow ones keep
-// every SM's loads in flight when there are few rows and the weights' bytes are what takes the time.
-template <int OP> int product_width(const ProdArgs& g, int sms)
+// Tiles of 128 rows by 256, 128 or 64 columns for single CTAs, or of 256 x 256 for pairs (kPairTile): what takes the fewest turns of
+// all SMs, each turn counted by the rows of operands that a CTA copies in a step (128 and the columns; 256 for half a pair).
+// Experts' tiles are counted with half a tile of padding each.  Measured (us, by 128 / 256 columns / pairs): 1024 rows 4096 -> 4096 bf16
+// 45 / 30 / 29, its gradient of the input 44 / 28 / 26; 512 rows 26 / 28 / 28 (by 64: 48), in 8 bits 17 / 21 / 21; 2048 x 2048 x 2048
+// 26 / 19 / 19; 512 rows 512 -> 2048 by 64: 7.1, by 128 8.1; 2000 rows of 16 experts 1024 -> 1024 16 / 14 / 15, 3000 of them 2048 -> 1408
+// 38 / 40 / 33; 61 experts of 67 rows 1000 -> 1416 47 / 46 / 56; 32768 rows of 8 experts 2048 -> 8192 by 256: 550, by pairs 450.
+// Pairs only where their second 128 rows are not empty as a rule (900 rows of 8 experts 4096 -> 4096: 56 us by 256, 63 by pairs) and, in the
+// weight gradient, where the reduction is long enough to pay for the pair's hand-shakes (128 to 256 rows an expert: 55 and 196 us in
+// pairs, 47 and 187 by single CTAs; 1024 and more: 377 against 410).
+constexpr int kPairTile = 512;
+template <int OP> int product_tile(const ProdArgs& g, int sms)
 {
     const size_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs;
     const size_t live = g.rows < g.experts ? g.rows : g.experts;
-    const size_t a_tiles = OP == kProdWeight ? size_t(g.experts) * ((g.outs + kTileRows - 1) / kTileRows)
-                                             : live * ((g.rows + live * kTileRows - 1) / (live * kTileRows));
-    for (int bn = 256; bn > 64; bn /= 2)
-        if (a_tiles * ((width + bn - 1) / bn) >= size_t(sms)) return bn;
-    return 64;
-}
-
-// Whether pairs of CTAs share tiles of 256 x 256: when every pair gets one, and the tile's second 128 rows are not empty as a
-// rule (forward, input gradient; 67 rows an expert: 56 us in pairs, 49 by single CTAs; 128 and more: pairs equal or faster, 450 against 550
-// us with 2048), and the reduction is long enough to pay for the pair's hand-shakes (weight gradient; 128 to 256 rows
-// an expert: 55 and 196 us in pairs, 47 and 187 by single CTAs; 1024 and more: 377 against 410 us).
-template <int OP> bool product_pairs(const ProdArgs& g, int sms)
-{
-    const size_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs, mean = g.rows / g.experts;
-    const size_t a_tiles = OP == kProdWeight ? size_t(g.experts) * ((g.outs + 255) / 256) : (g.rows + 255) / 256;
-    return mean >= (OP == kProdWeight ? 512 : 128) && a_tiles * ((width + 255) / 256) >= size_t(sms / 2);
+    auto turns = [&](size_t tile_rows, size_t columns, size_t workers) {
+        size_t a = (g.rows + tile_rows - 1) / tile_rows + (live > 1 ? live / 2 : 0);
+        if (a < live) a = live;
+        if (OP == kProdWeight) a = size_t(g.experts) * ((g.outs + tile_rows - 1) / tile_rows);
+        return (a * ((width + columns - 1) / columns) + workers - 1) / workers;
+    };
+    int best = 256;
+    size_t least = turns(128, 256, sms) * 384;
+    for (int columns = 128; columns >= 64; columns /= 2)
+        if (const size_t cost = turns(128, columns, sms) * (128 + columns); cost < least) {
+            least = cost;
+            best = columns;
+        }
+    if (g.rows / g.experts >= (OP == kProdWeight ? 512 : 128) && turns(256, 256, sms / 2) * 256 < least) best = kPairTile;
+    return best;
 }
 
 template <int OP, class S> cudaError_t launch_product_store(const ProdArgs& g, cudaStream_t st)
@@ -182,8 +187,8 @@ template <int OP, class S> cudaError_t launch_product_store(const ProdArgs& g, c
     if constexpr (OP == kProdForward || OP == kProdBytes)
         if (few_rows(g)) return launch_few_rows<Kind::kBytes, S>(g, di.sm_count, g.b_ready, st);
     if (const unsigned ranks = split_ranks<OP>(g, di.sm_count)) return launch_split<OP, S>(g, ranks, st);
-    if (product_pairs<OP>(g, di.sm_count)) return launch_product_tile<OP, 256, S, false, true>(g, di.sm_count, st);
-    switch (product_width<OP>(g, di.sm_count)) {
+    switch (product_tile<OP>(g, di.sm_count)) {
+    case kPairTile: return launch_product_tile<OP, 256, S, false, true>(g, di.sm_count, st);
     case 256: return launch_product_tile<OP, 256, S, false>(g, di.sm_count, st);
     case 128: return launch_product_tile<OP, 128, S, false>(g, di.sm_count, st);
     default:  return launch_product_tile<OP, 64, S, false>(g, di.sm_count, st);

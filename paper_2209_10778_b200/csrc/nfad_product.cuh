@@ -61,12 +61,17 @@ struct ProdShared {
 };
 constexpr int kStageBytes = 32 * 128;             // a result warp's 32 rows of 128 bytes
 constexpr int kMostResultWarps = 8;
+// The bias and the weights' scales of a result warp's columns, fetched while it waits for the tile: eight packets for each 32 columns
+// straight from memory cost a third of the epilogue (8192 x 8192 results of a reduction of 64, bf16, us: without activation 79, now
+// 51; GELU-erf and f' 157, now 130; of 1024: 181, now 150).
+constexpr int kColumns = 128;
+constexpr int kColumnBytes = kColumns * 2 * 4;
 // Result warps: beside gathering warps four, whose registers those need.
 template <bool kGather> struct ProdWarps {
     static constexpr int kResult = kGather ? 4 : kMostResultWarps;
     static constexpr int kThreads = (kFirstResultWarp + kResult + (kGather ? kGatherWarps : 0)) * 32;
 };
-constexpr int kProdSmem = 1024 + kRingBytes + kMostResultWarps * kStageBytes + int(sizeof(ProdShared));
+constexpr int kProdSmem = 1024 + kRingBytes + kMostResultWarps * (kStageBytes + kColumnBytes) + int(sizeof(ProdShared));
 
 // CTAs one of whose waits ran out; one counter for each translation unit that includes this file
 static __device__ unsigned g_product_faults;
@@ -298,16 +303,10 @@ template <bool kSlope> __device__ __forceinline__ void act8(int kind, float (&z)
     }
 }
 
-// eight neighbours of a [*, width] tensor from column c on; past the width: 0 (unaligned rows: one by one)
-template <class S> __device__ __forceinline__ void load8(const void* base, size_t row, uint32_t width, uint32_t c, bool vec, float (&v)[8])
+// eight neighbours of a [*, width] tensor from column c on
+template <class S> __device__ __forceinline__ void load8(const void* base, size_t row, uint32_t width, uint32_t c, float (&v)[8])
 {
-    const typename S::elem* p = static_cast<const typename S::elem*>(base) + row * width + c;
-    if (vec && c < width) {
-        S::unpack(*reinterpret_cast<const uint4*>(p), v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = c + e < width ? S::load1(p + e) : 0.0f;
-    }
+    S::unpack(*reinterpret_cast<const uint4*>(static_cast<const typename S::elem*>(base) + row * width + c), v);
 }
 template <class S> __device__ __forceinline__ uint4 pack8(const float (&z)[32], int p)
 {
@@ -320,13 +319,14 @@ template <class S> __device__ __forceinline__ uint4 pack8(const float (&z)[32], 
 // A lane holds results of its own row; memory wants whole lines.  So packets of eight go through the warp's 4 KB of shared
 // memory: 32 rows of eight packets, their places rotated so that neither side meets bank conflicts.  The eight packets are 64
 // neighbouring results (whole 128-byte lines on the way out), or 32 results and their 32 slopes, or 32 factors on the way in.
+// (Half rows of two neighbours are read together: the rotation puts them into different halves.)
 // Written straight from the rows, every access touched 32 lines, and the stores alone took 5 us a tile.
 struct RowPackets {
     int lane, rows;                                 // how many of the warp's 32 rows there are
     uint32_t width;
     size_t row0;                                    // the first one
     uint4* stage;
-    static __device__ __forceinline__ int at(int row, int packet) { return row * 8 + (packet ^ (row & 7)); }
+    static __device__ __forceinline__ int at(int row, int packet) { return row * 8 + (packet ^ (row << 2 & 4 | row >> 1 & 3)); }
     __device__ __forceinline__ void put(int packet, const uint4& v) const { stage[at(lane, packet)] = v; }
     __device__ __forceinline__ uint4 get(int packet) const { return stage[at(lane, packet)]; }
     // Calls f(i, place in the stage, address) for each packet of this lane that is inside: packet lane % kPackets, counted from
@@ -402,7 +402,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
     constexpr int kBoxRows = Tile::kBoxRows, kResultWarps = ProdWarps<kGather>::kResult;
     extern __shared__ unsigned char raw[];
     unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
-    ProdShared& s = *reinterpret_cast<ProdShared*>(ring + kRingBytes + kMostResultWarps * kStageBytes);
+    ProdShared& s = *reinterpret_cast<ProdShared*>(ring + kRingBytes + kMostResultWarps * (kStageBytes + kColumnBytes));
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = kPair ? tc::rank_in_pair() : 0;
     const uint32_t unit = kPair ? blockIdx.x >> 1 : blockIdx.x, units = kPair ? gridDim.x >> 1 : gridDim.x;
@@ -626,9 +626,8 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
             clear_rows<S, kResultWarps * 32>(g, s.start[g.experts], int(g.rows), width, threadIdx.x - kFirstResultWarp * 32);
         }
         // whole 16-byte packets: rows start on packets and no packet crosses a row's end
-        const bool vec = width % 8 == 0 && ((reinterpret_cast<uintptr_t>(g.out) | reinterpret_cast<uintptr_t>(g.slope) | reinterpret_cast<uintptr_t>(g.bias) |
-                                             reinterpret_cast<uintptr_t>(g.prev)) & 15u) == 0;
-        const bool vec_scale = Kind::kBytes && width % 8 == 0 && (reinterpret_cast<uintptr_t>(g.b_scale) & 15u) == 0;
+        const bool vec = width % 8 == 0 && ((reinterpret_cast<uintptr_t>(g.out) | reinterpret_cast<uintptr_t>(g.slope) | reinterpret_cast<uintptr_t>(g.prev)) & 15u) == 0;
+        float* columns = reinterpret_cast<float*>(ring + kRingBytes + kMostResultWarps * kStageBytes + (warp - kFirstResultWarp) * kColumnBytes);
         uint32_t turn = 0, turn_phase = 0;
         for (uint32_t t = unit; t < total; t += units) {
             const ProdTileAt q = walk.at(g, s.start, s.tiles, t);
@@ -648,6 +647,23 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
             const bool slopes = OP == kProdForward && g.slope;
             uint4 prev[4] = {};
             if (OP == kProdInput && g.prev && vec) rows.template fetch<S>(g.prev, q.b0 + half * kOwnChunks * 32, prev);
+            if constexpr (OP == kProdForward || OP == kProdBytes) {
+                static_assert(kOwnChunks * 32 <= kColumns, "a result warp's columns");
+                float bias[kOwnChunks], scales[kOwnChunks];
+#pragma unroll
+                for (int j = 0; j < kOwnChunks; ++j) {
+                    const uint32_t col = q.b0 + (half * kOwnChunks + j) * 32 + lane;
+                    const bool inside = col < width;
+                    bias[j] = g.bias && inside ? S::load1(static_cast<const typename S::elem*>(g.bias) + size_t(q.expert) * width + col) : 0.0f;
+                    scales[j] = Kind::kBytes && inside ? __ldg(g.b_scale + col) : 0.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < kOwnChunks; ++j) {
+                    columns[j * 32 + lane] = bias[j];
+                    if (Kind::kBytes) columns[kColumns + j * 32 + lane] = scales[j];
+                }
+                __syncwarp();
+            }
             if (!tc::barrier_wait(acc_full(turn), turn_phase, gave_up)) break;
             tc::fence_after_sync();
             for (int c = half * kOwnChunks; c < (half + 1) * kOwnChunks; ++c) {
@@ -663,29 +679,19 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
                 if (none)
 #pragma unroll
                     for (int e = 0; e < 32; ++e) z[e] = 0.0f;
+                const float4* own = reinterpret_cast<const float4*>(columns) + (c - half * kOwnChunks) * 8;
                 if (Kind::kBytes) {
 #pragma unroll
                     for (int p = 0; p < 8; ++p) {
-                        const uint32_t col = col0 + p * 4;
-                        float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        if (vec_scale) {
-                            if (col < width) w = __ldg(reinterpret_cast<const float4*>(g.b_scale + col));
-                        } else {
-                            if (col < width) w.x = __ldg(g.b_scale + col);
-                            if (col + 1 < width) w.y = __ldg(g.b_scale + col + 1);
-                            if (col + 2 < width) w.z = __ldg(g.b_scale + col + 2);
-                            if (col + 3 < width) w.w = __ldg(g.b_scale + col + 3);
-                        }
+                        const float4 w = own[kColumns / 4 + p];
                         z[p * 4] *= scale * w.x; z[p * 4 + 1] *= scale * w.y; z[p * 4 + 2] *= scale * w.z; z[p * 4 + 3] *= scale * w.w;
                     }
                 }
                 if ((OP == kProdForward || OP == kProdBytes) && g.bias) {
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        float b[8];
-                        load8<S>(g.bias, q.expert, width, col0 + p * 8, vec, b);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) z[p * 8 + e] += b[e];
+                    for (int p = 0; p < 8; ++p) {
+                        const float4 b = own[p];
+                        z[p * 4] += b.x; z[p * 4 + 1] += b.y; z[p * 4 + 2] += b.z; z[p * 4 + 3] += b.w;
                     }
                 }
                 if (OP == kProdInput && g.prev) {

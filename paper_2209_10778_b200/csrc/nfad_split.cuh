@@ -204,12 +204,12 @@ split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtenso
             }
             float f[8];
             if ((OP == kProdForward || OP == kProdBytes) && g.bias) {
-                load8<S>(g.bias, q.expert, width, col, true, f);
+                load8<S>(g.bias, q.expert, width, col, f);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) z[e] += f[e];
             }
             if (OP == kProdInput && g.prev) {
-                load8<S>(g.prev, out_row, width, col, true, f);
+                load8<S>(g.prev, out_row, width, col, f);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) z[e] *= f[e];
             }

@@ -154,7 +154,7 @@ def test_many_tiles(dtype):
 
 
 # shapes that take the ways through the products which depend on size (B200, 148 SMs): pairs of CTAs on 256 x 256 tiles (each
-# product), the reduction split over two, four and eight CTAs, one tile for each of two CTAs of an SM, and few rows
+# product), the reduction split over two, four and eight CTAs, tiles of each width, and few rows
 WAYS = [
     ([1100, 700, 800], 0, 0, 2048, 264), ([1101, 701, 900], 1, 3, 1040, 1800), ([600, 1, 900], 0, 0, 1048, 2568),
     ([40, 0, 37], 3, 2, 1288, 136), ([77], 0, 0, 2568, 72), ([33], 0, 0, 5128, 72), ([150], 0, 0, 72, 5128), ([40, 0, 60], 0, 5, 136, 2568),
@@ -171,6 +171,25 @@ def test_ways(dtype, way):
     gz = W.normal(x.shape[0] * w.shape[1], dtype, 9, 1.0).view(x.shape[0], w.shape[1])
     prev = W.uniform(x.numel(), dtype, 11, -0.2, 1.1).view(x.shape)
     _check_backward(gz, x, w, o, prev, *_backward(gz, x, w, off, prev))
+    assert nfad.nfad_wait_faults() == 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("counts,n_in,n_out", [(list(range(1, 67)), 264, 136), ([513, 527, 528, 529, 545, 575, 576, 577], 1040, 776)])
+def test_runs_that_end_anywhere(dtype, counts, n_in, n_out):
+    # the weights' gradient multiplies whole groups of rows: what follows an expert's last row must not reach it
+    x, w, _, off, o = _case((counts, 3, 2, n_in, n_out), dtype, 17)
+    gz = W.normal(x.shape[0] * n_out, dtype, 9, 1.0).view(x.shape[0], n_out)
+    gx, gw = _backward(gz, x, w, off)
+    _check_backward(gz, x, w, o, None, gx, gw)
+    for third in range(3):
+        bad_gz, bad_x = gz.clone(), x.clone()
+        bad_gz[:o[0]], bad_x[o[-1]:] = float("nan"), float("inf")
+        for e in range(third, len(counts), 3):
+            bad_gz[o[e]:o[e + 1]], bad_x[o[e]:o[e + 1]] = float("inf"), float("nan")
+        _, got = _backward(bad_gz, bad_x, w, off)
+        keep = [e for e in range(len(counts)) if e % 3 != third]
+        assert torch.equal(got[keep], gw[keep])
     assert nfad.nfad_wait_faults() == 0
 
 

@@ -621,8 +621,8 @@ template <bool kMean, int P> __device__ __forceinline__ void normalise(float2 (&
 //   grad gate = g_post P + b_post Q, grad g_post += gate P, grad b_post += gate Q.
 // Measured on [32768, 4096] bf16, RMS norms and a gate (1.6 GB): next row prefetched into registers 418 us, this ring 355 us, these
 // sums 290 us, pairs of values in one instruction 283 us, with norm_reduce_kernel as it is now 278 us.
-// kI packets per thread, kR rows at a time; kGate: there is a gate; kFull: means and bias sums are kept too (without: RMS norms
-// and no bias sums).  Aligned rows of up to 512 kI packets.  Dynamic shared memory: `stages` rows of the tensors that are there.
+// kI packets per thread, kR rows at a time; kGate: there is a gate; kFull: means and bias sums are kept too (without: RMS norms,
+// no bias sums, and no post_bias in a gate's gradient that is asked for).  Aligned rows of up to 512 kI packets.  Dynamic shared memory: `stages` rows of the tensors that are there.
 template <class S, int kI, int kR, bool kGate, bool kFull>
 __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constant__ NormBackwardArgs a, int stages)
 {
@@ -1165,7 +1165,8 @@ cudaError_t launch_norm_backward_kernel(const NormBackwardArgs& a, const NormPla
 
 template <class S, int kI, int kR> cudaError_t launch_norm_backward_rows(const NormBackwardArgs& a, const NormPlan& p, cudaStream_t st)
 {
-    const bool more = a.sums[kSumPreBias] || a.sums[kSumPostBias] || a.pre == kNormLayer || a.post == kNormLayer;
+    // (the gate's gradient holds post_bias times the sum of ds, whether or not post_bias has a gradient of its own)
+    const bool more = a.sums[kSumPreBias] || a.sums[kSumPostBias] || (a.grad_gate && a.post_bias) || a.pre == kNormLayer || a.post == kNormLayer;
     // six sums for each column beside two rows spill (310 us for a LayerNorm pair with a gate on [16384, 4096] bf16): one row then
     if (a.gate) return more ? launch_norm_backward_kernel<S, kI, 1, true, true>(a, p, st) : launch_norm_backward_kernel<S, kI, kR, true, false>(a, p, st);
     return more ? launch_norm_backward_kernel<S, kI, kR, false, true>(a, p, st) : launch_norm_backward_kernel<S, kI, kR, false, false>(a, p, st);

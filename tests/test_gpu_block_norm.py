@@ -360,3 +360,31 @@ def test_refusals():
     q = nfad.BlockNorm(post="none", pre="rms", pre_gain=gain)
     assert status(lambda: nfad.nfad_block_norm_backward(q, h, None, u, s, st, s.clone(), None, {"post_gain": torch.empty(cols, device=DEV)}, scratch)) == 11
     assert status(lambda: nfad.nfad_block_norm_backward(norm, None, h, u, s, st, s.clone(), None, None, scratch)) == 3
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [64, 1000, 6144, 1021, 20000])
+def test_every_subset_of_the_parameters_gradients(dtype, cols):
+    # what is not asked for changes nothing in what is: a frozen bias behind the block still stands in the gate's gradient
+    rows = 24
+    u, r = _tensors(rows, cols, dtype, 61)
+    dh, gs = _tensors(rows, cols, dtype, 63)
+    for post, pre, gates in (("rms", "rms", 1), ("rms", "rms", 6), ("rms", "layer", rows), ("layer", "rms", 4), ("rms", "none", 2), ("none", "rms", 3)):
+        p = _parameters(dtype, cols, rows, post, pre, gates, True, 6000)
+        norm = _module(p)
+        s, _, stats = _forward(p, u, r)
+        a, du, dgs = dh.to(DEV) if pre != "none" else None, u.to(DEV), gs.to(DEV)
+        scratch = nfad.nfad_block_norm_backward_scratch(norm, du)
+        want = plain.block_norm_backward(p, dh if pre != "none" else None, gs, u, s.cpu(), stats.cpu())
+        k = plain.EPS32 * 2 * plain.depth(cols)
+        names = [n for n in nfad.BlockNorm.PARAMETERS if norm.tensors[n] is not None]
+        for count in range(len(names) + 1):
+            for some in itertools.combinations(names, count):
+                scratch.fill_(0xff)
+                gu, gr = torch.full_like(du, 9.0), torch.full_like(du, 9.0)
+                grads = {n: torch.full(norm.tensors[n].shape, 9.0, device=DEV) for n in some}
+                nfad.nfad_block_norm_backward(norm, a, dgs, du, s, stats, gu, gr, grads, scratch)
+                plain.check(gu, want["u"][0], 2 * k * want["u"][1], f"grad_u with {some}")
+                plain.check(gr, want["r"][0], k * want["r"][1], f"grad_r with {some}")
+                for n in some:
+                    plain.check(grads[n], want[n][0], (2 * k + plain.EPS32 * (rows + 64)) * want[n][1], f"grad {n} with {some}, {post} {pre}")

@@ -128,3 +128,28 @@ def test_example_command():
                          capture_output=True, text=True, timeout=300)
     assert out.returncode == 0, out.stderr
     assert "rows in 8 bits" in out.stdout
+
+
+@pytest.mark.parametrize("frozen", [["post_gain"], ["post_bias"], ["gate"], ["pre_gain"], ["pre_bias"], ["post_bias", "pre_bias"], ["post_gain", "post_bias", "pre_bias"]])
+@pytest.mark.parametrize("cols", [256, 203])
+def test_block_norm_wrapper_with_frozen_parameters(frozen, cols):
+    rows = 24
+    t = {k: W.normal(n, "f32", 30 + i, 0.5, DEV) for i, (k, n) in enumerate(dict(u=rows * cols, r=rows * cols, post_gain=cols, post_bias=cols, gate=3 * cols,
+                                                                               pre_gain=cols, pre_bias=cols).items())}
+    t["u"], t["r"], t["gate"] = t["u"].view(rows, cols), t["r"].view(rows, cols), t["gate"].view(3, cols)
+    leaf = {k: v.clone().requires_grad_(k not in frozen) for k, v in t.items()}
+    s, h = autograd.block_norm(leaf["u"], leaf["r"], post="rms", pre="rms", **{k: leaf[k] for k in list(t)[2:]})
+    ws, wh = (W.normal(rows * cols, "f32", 40 + i, 1.0, DEV).view(s.shape) for i in range(2))
+    ((s * ws).sum() + (h * wh).sum()).backward()
+    ref = {k: v.double().requires_grad_(k not in frozen) for k, v in t.items()}
+    rms = lambda x: x / (x.square().mean(-1, keepdim=True) + 1e-5).sqrt()
+    a = rms(ref["u"]) * ref["post_gain"] + ref["post_bias"]
+    s64 = ref["r"] + (a.view(3, -1, cols) * ref["gate"][:, None]).view(a.shape)
+    h64 = rms(s64) * ref["pre_gain"] + ref["pre_bias"]
+    ((s64 * ws.double()).sum() + (h64 * wh.double()).sum()).backward()
+    for k in t:
+        if k in frozen:
+            assert leaf[k].grad is None
+            continue
+        rel = float((leaf[k].grad.double() - ref[k].grad).norm() / ref[k].grad.norm())
+        assert rel < 1e-5, (k, rel)

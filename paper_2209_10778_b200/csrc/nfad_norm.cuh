@@ -718,10 +718,15 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
             parameter(a.gate, gate_row, i, 0.0f, gate);
             parameter(post ? a.post_gain : nullptr, 0, i, 1.0f, gain);
             parameter(post ? a.post_bias : nullptr, 0, i, 0.0f, bias);
-            float2* dst = on[i] && a.grad_gate ? reinterpret_cast<float2*>(gate_target(a, blockIdx.x, r0, r1, gate_row)) + size_t(column[i]) * P : nullptr;
+            // the caller's tensor may begin on any float: single stores
+            float* dst = on[i] && a.grad_gate ? gate_target(a, blockIdx.x, r0, r1, gate_row) + size_t(column[i]) * S::kVec : nullptr;
 #pragma unroll
             for (int e = 0; e < P; ++e) {
-                if (dst) dst[e] = kFull ? fma2(gain[e], acc_p[i][e], mul2(bias[e], acc_q[i][e])) : mul2(gain[e], acc_p[i][e]);
+                if (dst) {
+                    const float2 v = kFull ? fma2(gain[e], acc_p[i][e], mul2(bias[e], acc_q[i][e])) : mul2(gain[e], acc_p[i][e]);
+                    dst[2 * e] = v.x;
+                    dst[2 * e + 1] = v.y;
+                }
                 acc_post[i][e] = fma2(gate[e], acc_p[i][e], acc_post[i][e]);
                 acc_p[i][e] = twice(0.0f);
                 if constexpr (kFull) {

@@ -388,3 +388,36 @@ def test_every_subset_of_the_parameters_gradients(dtype, cols):
                 plain.check(gr, want["r"][0], k * want["r"][1], f"grad_r with {some}")
                 for n in some:
                     plain.check(grads[n], want[n][0], (2 * k + plain.EPS32 * (rows + 64)) * want[n][1], f"grad {n} with {some}, {post} {pre}")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [64, 1000, 4096, 6144, 515])
+def test_gradients_that_begin_on_any_float(dtype, cols):
+    # the parameters' gradients as pieces of one flat buffer, as an optimizer keeps them; gate rows that end inside a chunk of rows
+    rows = 360
+    u, r = _tensors(rows, cols, dtype, 71)
+    dh, gs = _tensors(rows, cols, dtype, 73)
+    for gates in (rows, rows // 2, 3, 1):
+        for post, pre, bias in (("rms", "rms", False), ("layer", "layer", True), ("none", "rms", False)):
+            p = _parameters(dtype, cols, rows, post, pre, gates, bias, 7000)
+            norm = _module(p)
+            s, _, stats = _forward(p, u, r)
+            want = _backward(p, dh, gs, u, s.cpu(), stats)
+            for shift in (1, 2, 3):
+                names = list(want[2])
+                flat = torch.full((shift + sum(norm.tensors[n].numel() + 1 for n in names),), 5.0, device=DEV)
+                grads, at = {}, shift
+                for n in names:
+                    t = norm.tensors[n]
+                    grads[n] = flat[at:at + t.numel()].view(t.shape)
+                    at += t.numel() + 1                               # one float between them, which nothing writes
+                du = u.to(DEV)
+                gu, gr = torch.empty_like(du), torch.empty_like(du)
+                nfad.nfad_block_norm_backward(norm, dh.to(DEV), gs.to(DEV), du, s, stats, gu, gr, grads, nfad.nfad_block_norm_backward_scratch(norm, du))
+                assert torch.equal(gu, want[0]) and torch.equal(gr, want[1])
+                at = shift
+                for n in names:
+                    assert torch.equal(grads[n], want[2][n]), n
+                    at += norm.tensors[n].numel() + 1
+                    assert flat[at - 1] == 5.0
+                assert (flat[:shift] == 5.0).all()

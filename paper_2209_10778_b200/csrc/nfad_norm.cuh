@@ -1159,7 +1159,8 @@ cudaError_t launch_norm_backward_kernel(const NormBackwardArgs& a, const NormPla
     size_t stages = kNormRingBytes / (512 / p.block) / row;
     if (stages > kNormMaxStages) stages = kNormMaxStages;
     stages -= stages % kR;                           // rows are taken kR at a time (at least two turns: see the rule below)
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(stages * row));
+    // the same limit whatever the call: one that followed the shape could be lowered by another host thread before this launch
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormRingBytes);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];

@@ -421,3 +421,43 @@ def test_gradients_that_begin_on_any_float(dtype, cols):
                     at += norm.tensors[n].numel() + 1
                     assert flat[at - 1] == 5.0
                 assert (flat[:shift] == 5.0).all()
+
+
+def test_threads_with_different_widths():
+    # calls from several host threads at once, rows of different lengths through the same kernel: each gets its own answer
+    import ctypes
+    import threading
+    from paper_2209_10778_b200 import binding
+    call = binding.load().nfad_block_norm_backward                    # the library's own calls, one behind the other
+    jobs = []
+    for cols in (256, 4096, 1024, 4088):
+        rows = 64
+        u, r = _tensors(rows, cols, "bf16", cols)
+        dh, gs = _tensors(rows, cols, "bf16", cols + 1)
+        p = _parameters("bf16", cols, rows, "rms", "rms", 1, False, 3)
+        s, _, stats = _forward(p, u, r)
+        want = _backward(p, dh, gs, u, s.cpu(), stats)
+        norm, du = _module(p), u.to(DEV)
+        given = [dh.to(DEV), gs.to(DEV), du, s, stats, torch.empty_like(du), torch.empty_like(du)]
+        grads = {k: torch.empty(norm.tensors[k].shape, device=DEV) for k in want[2]}
+        out = binding.BlockNormGrads(**{k: g.data_ptr() for k, g in grads.items()})
+        scratch, stream = nfad.nfad_block_norm_backward_scratch(norm, du), torch.cuda.Stream()
+        args = (norm.ref, binding.DTYPES["bf16"], *(t.data_ptr() for t in given), ctypes.byref(out), scratch.data_ptr(),
+                scratch.numel(), rows, cols, stream.cuda_stream)
+        jobs.append((args, given, grads, want, (norm, out, scratch, stream)))
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(args):
+        torch.cuda.set_device(0)
+        failed.extend(rc for rc in (call(*args) for _ in range(4000)) if rc)
+
+    threads = [threading.Thread(target=work, args=j[:1]) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed, (len(failed), failed[0])
+    for _, given, grads, want, _ in jobs:
+        assert torch.equal(given[5], want[0]) and torch.equal(given[6], want[1]) and all(torch.equal(grads[k], want[2][k]) for k in grads)

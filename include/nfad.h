@@ -399,8 +399,8 @@ NFAD_API size_t nfad_block_norm_backward_scratch_bytes(int dtype, size_t rows, s
  * x is [rows, in], its rows sorted by expert; w is [experts, out, in] (each expert's weight as a linear layer keeps it);
  * offsets is a DEVICE array of experts + 1 ints: expert e has the rows from offsets[e] up to offsets[e + 1].  The runs may be
  * ragged and empty.  Nothing is read back: the call does not synchronise, and a CUDA graph may be replayed with other
- * offsets.  Offsets are held to [0, rows] and to ascending order on the device, so that no value of theirs reaches memory outside the
- * tensors.  Rows before offsets[0] and from offsets[experts] on belong to no expert: they are not read and their results are 0.
+ * offsets.  Offsets are held to [0, rows] and to ascending order on the device (an expert begins no earlier than the largest offset
+ * before it, for every call below alike), so that no value of theirs reaches memory outside the tensors.  Rows before offsets[0] and from offsets[experts] on belong to no expert: they are not read and their results are 0.
  * experts is at most NFAD_MAX_EXPERTS (NFAD_E_TOO_LARGE); one expert with offsets {0, rows} is an ordinary linear layer.
  * dtype is NFAD_BF16 or NFAD_F16 (NFAD_E_DTYPE otherwise); products are exact and summed in fp32 by the tensor cores, and
  * every result is rounded once.  in, out and rows must be below 2^31.  Tensors whose rows do not start on 16-byte

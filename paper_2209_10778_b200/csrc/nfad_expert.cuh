@@ -2,12 +2,13 @@
 //
 // A thread owns one column packet of a chunk of consecutive rows, as in the bias-fused backward.  An expert's rows may begin
 // and end anywhere in a chunk: at each border the thread hands its column sums over, straight to the result when the
-// expert's rows all lie in the chunk, else to the chunk's slot 0 (the expert that the chunk begins in) or 1 (the one it
-// ends in); a second kernel adds the slots of an expert in row order.  The sums are of the unrounded products (exact in
+// expert's rows all lie in the chunk, else to the chunk's slot 0 (an expert whose rows begin before the chunk) or 1 (one whose rows
+// begin in it and go on); a second kernel adds the slots of an expert in row order.  The sums are of the unrounded products (exact in
 // fp32 for 16-bit factors), in fp32 and in a fixed order.  Three tensors of traffic bound it.
 #pragma once
 
 #include "nfad_bias.cuh"
+#include "nfad_product_args.h"
 
 namespace nfad {
 
@@ -15,44 +16,63 @@ struct ExpertActArgs {
     const void *g, *d;                   // d null: f' = 1
     void* gz;                            // may be null when d is null
     float *grad_bias, *partial;          // grad_bias null: not wanted; partial [chunks][2][cols]
+    int* begin;                          // [experts + 1] where each expert's rows begin, for the second kernel
     const int* offsets;
     size_t rows;
     uint32_t cols, row_packets, chunk_rows, chunks, experts;
 };
 
-__device__ __forceinline__ size_t expert_offset(const ExpertActArgs& a, uint32_t e)
+// Offsets mean what they mean to the products: they are held to [0, rows], and an expert begins no earlier than the largest offset before
+// it.  So a row belongs to the expert in front of the first offset above it, whose rows end at that offset.
+__device__ __forceinline__ int expert_offset(const ExpertActArgs& a, uint32_t e) { return min(max(__ldg(a.offsets + e), 0), int(a.rows)); }
+
+struct ExpertRun {
+    uint32_t next;                       // the first offset above the run's rows: they are expert next - 1's (0 or experts + 1: nobody's)
+    int end;                             // behind its last row
+    bool here;                           // its first row is in this chunk
+};
+
+// The run that holds `row`, found by a warp together, 32 kWide offsets at a time; no offset before `from` is above it.  here: it begins at `row`.
+template <int kWide> __device__ __forceinline__ ExpertRun expert_run(const ExpertActArgs& a, int row, uint32_t from)
 {
-    const int v = __ldg(a.offsets + e);
-    return v < 0 ? 0 : size_t(v) < a.rows ? size_t(v) : a.rows;
+    const int lane = threadIdx.x & 31;
+    uint32_t at_row = 0;
+    for (uint32_t i0 = from; i0 <= a.experts; i0 += 32 * kWide) {
+        int v[kWide];
+#pragma unroll
+        for (int j = 0; j < kWide; ++j) v[j] = i0 + j * 32 + lane <= a.experts ? expert_offset(a, i0 + j * 32 + lane) : -1;
+#pragma unroll
+        for (int j = 0; j < kWide; ++j) {
+            const uint32_t above = __ballot_sync(0xffffffffu, v[j] > row);
+            at_row |= __ballot_sync(0xffffffffu, v[j] == row) & (above - 1 & ~above);       // those in front of the first above
+            if (above) {
+                const int first = __ffs(above) - 1;
+                return {i0 + j * 32 + first, __shfl_sync(0xffffffffu, v[j], first), at_row != 0};
+            }
+        }
+    }
+    return {a.experts + 1, int(a.rows), at_row != 0};
 }
 
-// The expert that `row` belongs to (experts when none) and where its run of rows ends (always past `row`).
-__device__ __forceinline__ uint32_t expert_of(const ExpertActArgs& a, size_t row, size_t* end)
+// By one warp: where each expert's rows begin.
+__device__ __forceinline__ void expert_begins(const ExpertActArgs& a)
 {
-    if (row < expert_offset(a, 0)) {
-        *end = expert_offset(a, 0);
-        return a.experts;
+    const uint32_t lane = threadIdx.x & 31;
+    int last = 0;
+    for (uint32_t i0 = 0; i0 <= a.experts; i0 += 32) {
+        int v = i0 + lane <= a.experts ? max(expert_offset(a, i0 + lane), last) : last;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int w = __shfl_up_sync(0xffffffffu, v, o);
+            if (lane >= o) v = max(v, w);
+        }
+        if (i0 + lane <= a.experts) a.begin[i0 + lane] = v;
+        last = __shfl_sync(0xffffffffu, v, 31);
     }
-    uint32_t lo = 0, hi = a.experts + 1;
-    while (hi - lo > 1) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (expert_offset(a, mid) <= row) lo = mid;
-        else hi = mid;
-    }
-    *end = lo < a.experts ? expert_offset(a, lo + 1) : a.rows;
-    if (*end <= row) *end = row + 1;
-    return lo;
-}
-
-__device__ __forceinline__ float* expert_target(const ExpertActArgs& a, size_t chunk, size_t r0, size_t r1, uint32_t e)
-{
-    const size_t g0 = expert_offset(a, e), g1 = expert_offset(a, e + 1);
-    if (g0 >= r0 && g1 <= r1) return a.grad_bias + size_t(e) * a.cols;
-    return a.partial + (chunk * 2 + (g0 <= r0 ? 0 : 1)) * a.cols;
 }
 
 // kVec: whole 16-byte packets; else one column a thread.  The rows go by fours, whatever experts they belong to, so that the
-// loads of a group are all in flight before the first is used and an expert's border costs a thread one look at the offsets.
+// loads of a group are all in flight before the first is used and an expert's border costs a warp one look at the offsets.
 template <class S, bool kVec> struct ExpertPacket { uint4 v; };
 template <class S> struct ExpertPacket<S, false> { typename S::elem v; };
 
@@ -65,8 +85,9 @@ __global__ void __launch_bounds__(kBiasMaxBlock, 4) expert_act_kernel(const __gr
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t cp = blockIdx.x * blockDim.x + threadIdx.x;
-    if (cp >= a.row_packets) return;
-    const size_t r0 = size_t(blockIdx.y) * a.chunk_rows, r1 = r0 + a.chunk_rows < a.rows ? r0 + a.chunk_rows : a.rows;
+    if ((cp & ~31u) >= a.row_packets) return;                         // whole warps only: a warp looks at the offsets together
+    const bool on = cp < a.row_packets;
+    const int r0 = int(blockIdx.y * a.chunk_rows), r1 = int(min(size_t(r0) + a.chunk_rows, a.rows));      // rows are below 2^31
     if (r0 >= r1) return;
     auto load = [&](const void* base, size_t row) {
         Packet p;
@@ -81,34 +102,37 @@ __global__ void __launch_bounds__(kBiasMaxBlock, 4) expert_act_kernel(const __gr
     float acc[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = 0.0f;
-    uint32_t e = a.experts;
-    size_t end = r0;                                                  // of the run of rows that `row` is in
+    ExpertRun run = {0, r0, false};                                   // of the row at hand
+    // straight to the result when all of the expert's rows are in the chunk; else to slot 0 (they begin before it) or 1
     auto hand_over = [&]() {
-        if (a.grad_bias && e < a.experts) {
-            float* dst = expert_target(a, blockIdx.y, r0, r1, e) + size_t(cp) * V;
+        const uint32_t e = run.next - 1;
+        if (a.grad_bias && on && e < a.experts) {
+            float* dst = (run.here && run.end <= r1 ? a.grad_bias + size_t(e) * a.cols : a.partial + (size_t(blockIdx.y) * 2 + run.here) * a.cols) + size_t(cp) * V;
 #pragma unroll
             for (int i = 0; i < V; ++i) dst[i] = acc[i];
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] = 0.0f;
     };
-    for (size_t row = r0; row < r1; row += U) {
+    for (int row = r0; row < r1; row += U) {
         Packet g[U], d[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (row + u < r1) {
+            if (on && row + u < r1) {
                 g[u] = load(a.g, row + u);
                 if (a.d) d[u] = load(a.d, row + u);
             }
+        if (row == r0) run = expert_run<4>(a, row, 0);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (row + u >= r1) break;
-            if (row + u == end) {
-                if (row + u > r0) hand_over();
-                e = expert_of(a, row + u, &end);
+            if (row + u == run.end) {
+                hand_over();
+                run = expert_run<1>(a, row + u, run.next);
+                run.here = true;                                     // the offset that ended the run before is this row
             }
             float v[V];
-            if (e < a.experts) {
+            if (run.next - 1 < a.experts) {
                 widen(g[u], v);
                 if (a.d) {
                     float f[V];
@@ -122,13 +146,14 @@ __global__ void __launch_bounds__(kBiasMaxBlock, 4) expert_act_kernel(const __gr
 #pragma unroll
                 for (int i = 0; i < V; ++i) v[i] = 0.0f;
             }
-            if (a.gz) {
-                if constexpr (kVec) store_packet<true>(static_cast<uint4*>(a.gz) + (row + u) * a.row_packets + cp, S::pack(v));
-                else S::store1(static_cast<E*>(a.gz) + (row + u) * a.cols + cp, v[0]);
+            if (a.gz && on) {
+                if constexpr (kVec) store_packet<true>(static_cast<uint4*>(a.gz) + size_t(row + u) * a.row_packets + cp, S::pack(v));
+                else S::store1(static_cast<E*>(a.gz) + size_t(row + u) * a.cols + cp, v[0]);
             }
         }
     }
     hand_over();
+    if (a.grad_bias && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 32) expert_begins(a);
 }
 
 // The experts whose rows lie in several chunks, and those without rows.  32 columns times kExpertGroups runs of consecutive
@@ -141,7 +166,7 @@ static __global__ void __launch_bounds__(32 * kExpertGroups) expert_reduce_kerne
     const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
     const size_t col = size_t(blockIdx.x) * 32 + lane;
     const uint32_t e = blockIdx.y;
-    const size_t g0 = expert_offset(a, e), g1 = expert_offset(a, e + 1);
+    const size_t g0 = a.rows ? a.begin[e] : 0, g1 = a.rows ? a.begin[e + 1] : 0;
     float* out = a.grad_bias + size_t(e) * a.cols;
     if (g1 <= g0) {
         if (group == 0 && col < a.cols) out[col] = 0.0f;
@@ -157,7 +182,7 @@ static __global__ void __launch_bounds__(32 * kExpertGroups) expert_reduce_kerne
             float v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                v[j] = k + j < k1 ? a.partial[((k + j) * 2 + (g0 <= (k + j) * a.chunk_rows ? 0 : 1)) * a.cols + col] : 0.0f;
+                v[j] = k + j < k1 ? a.partial[((k + j) * 2 + (g0 < (k + j) * a.chunk_rows ? 0 : 1)) * a.cols + col] : 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (k + j < k1) s = __fadd_rn(s, v[j]);
@@ -187,7 +212,7 @@ inline size_t expert_act_scratch_bytes(size_t rows, size_t cols, int sms)
 {
     if (rows == 0 || cols == 0) return 0;
     const size_t n = expert_chunk_rows(rows, cols, sms);
-    return (rows + n - 1) / n * 2 * cols * sizeof(float);
+    return (rows + n - 1) / n * 2 * cols * sizeof(float) + (kMaxExperts + 1) * sizeof(int);
 }
 
 template <class S> cudaError_t launch_expert_act(const ExpertActArgs& in, cudaStream_t st)
@@ -200,6 +225,7 @@ template <class S> cudaError_t launch_expert_act(const ExpertActArgs& in, cudaSt
     cudaLaunchAttribute attr[1];
     a.chunk_rows = expert_chunk_rows(a.rows, a.cols, di.sm_count);
     a.chunks = uint32_t((a.rows + a.chunk_rows - 1) / a.chunk_rows);
+    a.begin = reinterpret_cast<int*>(a.partial + size_t(a.chunks) * 2 * a.cols);
     if (a.rows) {
         const bool vec = a.cols % 8 == 0 && aligned16(a.g) && aligned16(a.d) && aligned16(a.gz);
         a.row_packets = vec ? a.cols / 8 : a.cols;

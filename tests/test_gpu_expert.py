@@ -376,3 +376,34 @@ def test_refusals():
     scratch = nfad.nfad_expert_act_backward_scratch(big)
     assert status(lambda: nfad.nfad_expert_act_backward(big, None, off, None, gb, scratch[:16])) == 7
     assert status(lambda: nfad.nfad_expert_act_backward(big, None, off, None, gb, None)) == 3
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [24, 25, 1416])
+@pytest.mark.parametrize("off", [[0, 60, 20, 80], [0, 10, 5, 20], [5, 3, 10], [70, 0, 80], [-7, 1 << 30, 20], [40, 30, 20, 10], [0, 600, 200, 900, 100, 1500, 2600],
+                                 [0] + [100, 40] * 300 + [2500], [3000, 0, 5]])
+def test_offsets_out_of_order_mean_the_same_everywhere(dtype, cols, off):
+    # an expert begins no earlier than the largest offset before it, in Eq. 4 and its bias sums as in the products
+    rows = 80 if len(off) < 5 and max(off) <= 80 else 2600
+    held, last = [], 0
+    for v in off:
+        last = max(last, min(max(v, 0), rows))
+        held.append(last)
+    experts = len(off) - 1
+    g, d = W.normal(rows * cols, dtype, 15, 1.0).view(rows, cols), W.uniform(rows * cols, dtype, 16, -0.2, 1.1).view(rows, cols)
+    exact = g.double() * d.double()
+    gz, gb = _act_backward(g, d, torch.tensor(off, dtype=torch.int32), experts)
+    assert torch.equal(gz[held[0]:held[-1]], exact[held[0]:held[-1]].to(gz.dtype))
+    assert not gz[:held[0]].any() and not gz[held[-1]:].any()
+    for e in range(experts):
+        part = exact[held[e]:held[e + 1]]
+        plain.check(gb[e], part.sum(0), plain.EPS32 * (part.shape[0] + 40) * part.abs().sum(0), f"bias of expert {e}")
+    gz2, gb2 = _act_backward(g, d, torch.tensor(held, dtype=torch.int32), experts)
+    assert torch.equal(gz, gz2) and torch.equal(gb, gb2)
+    # the products' rows of the same offsets
+    x = W.normal(rows * 16, dtype, 17, 1.0).view(rows, 16)
+    w = W.normal(experts * cols * 16, dtype, 18, 0.25).view(experts, cols, 16)
+    a, b = (_backward(gz, x, w, torch.tensor(o, dtype=torch.int32)) for o in (off, held))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    ya, yb = (_forward("swish", x, w, None, torch.tensor(o, dtype=torch.int32)) for o in (off, held))
+    assert torch.equal(ya[0], yb[0]) and torch.equal(ya[1], yb[1])

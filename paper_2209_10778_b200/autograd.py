@@ -100,21 +100,22 @@ class FadSequence(torch.autograd.Function):
 
 
 class BlockNormFunction(torch.autograd.Function):
-    """(s, h) of the norms around a block; saved: u, s and four statistics a row."""
+    """(s, h) of the norms around a block; saved: u, s, four statistics a row, and the parameters."""
 
     @staticmethod
     def forward(ctx, u, r, post_gain, post_bias, gate, pre_gain, pre_bias, post, pre, residual_scale, eps):
         given = dict(post_gain=post_gain, post_bias=post_bias, gate=gate, pre_gain=pre_gain, pre_bias=pre_bias)
-        norm = block.BlockNorm(post=post, pre=pre, residual_scale=residual_scale, eps=eps,
-                               **{k: None if t is None else t.detach().contiguous() for k, t in given.items()})
+        given = {k: t.contiguous() for k, t in given.items() if t is not None}
+        settings = dict(post=post, pre=pre, residual_scale=residual_scale, eps=eps)
+        norm = block.BlockNorm(**given, **settings)
         uc, rc = u.contiguous(), None if r is None else r.contiguous()
         s = torch.empty_like(uc)
         h = torch.empty_like(uc) if norm.pre else None
         stats = torch.empty(uc.numel() // max(1, uc.shape[-1]), 4, device=uc.device)
         block.nfad_block_norm_forward(norm, uc, rc, s, h, stats)
-        ctx.save_for_backward(uc, s, stats)
+        ctx.save_for_backward(uc, s, stats, *given.values())
         ctx.set_materialize_grads(False)             # a result that nothing used costs no read of zeros
-        ctx.norm, ctx.dtypes = norm, {k: t.dtype for k, t in given.items() if t is not None}
+        ctx.names, ctx.settings = list(given), settings
         if h is None:
             h = s.new_empty(0)
             ctx.mark_non_differentiable(h)
@@ -122,8 +123,8 @@ class BlockNormFunction(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, grad_s, grad_h):
-        u, s, stats = ctx.saved_tensors
-        norm = ctx.norm
+        u, s, stats, *given = ctx.saved_tensors
+        norm = block.BlockNorm(**dict(zip(ctx.names, given)), **ctx.settings)
         if norm.pre and grad_h is None or not norm.pre and grad_s is None:
             zeros = torch.zeros_like(s)
             grad_h, grad_s = (zeros, grad_s) if norm.pre else (None, zeros)
@@ -136,7 +137,7 @@ class BlockNormFunction(torch.autograd.Function):
         gr = torch.empty_like(u) if ctx.needs_input_grad[1] else None
         block.nfad_block_norm_backward(norm, grad_h.contiguous() if norm.pre else None, None if grad_s is None else grad_s.contiguous(), u, s, stats, gu, gr, grads,
                                        block.nfad_block_norm_backward_scratch(norm, u))
-        return (gu, gr, *(grads[k].to(ctx.dtypes[k]) if k in grads else None for k in names), None, None, None, None)
+        return (gu, gr, *(grads[k].to(u.dtype) if k in grads else None for k in names), None, None, None, None)
 
 
 def block_norm(u, r=None, post="none", pre="rms", post_gain=None, post_bias=None, gate=None, pre_gain=None, pre_bias=None,

@@ -153,3 +153,31 @@ def test_block_norm_wrapper_with_frozen_parameters(frozen, cols):
             continue
         rel = float((leaf[k].grad.double() - ref[k].grad).norm() / ref[k].grad.norm())
         assert rel < 1e-5, (k, rel)
+
+
+@pytest.mark.parametrize("name", ["post_gain", "post_bias", "gate", "pre_gain", "pre_bias"])
+def test_block_norm_parameters_changed_before_backward(name):
+    rows, cols = 8, 64
+    u = W.normal(rows * cols, "bf16", 1, 1.0, DEV).view(rows, cols).requires_grad_(True)
+    par = {k: W.normal(cols, "bf16", 2 + i, 0.5, DEV).requires_grad_(True) for i, k in enumerate(("post_gain", "post_bias", "gate", "pre_gain", "pre_bias"))}
+    s, h = autograd.block_norm(u, None, post="rms", pre="rms", **par)
+    with torch.no_grad():
+        par[name].mul_(2.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        (s.float().sum() + h.float().sum()).backward()
+
+
+def test_block_norm_parameters_pass_saved_tensor_hooks():
+    rows, cols = 8, 64
+    u = W.normal(rows * cols, "bf16", 1, 1.0, DEV).view(rows, cols).requires_grad_(True)
+    gain = W.normal(cols, "bf16", 2, 0.5, DEV).requires_grad_(True)
+    seen = []
+    # kept on the host between the passes
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: (seen.append(t.data_ptr()), t.cpu())[1], lambda t: t.to(DEV)):
+        s, h = autograd.block_norm(u, None, post="none", pre="rms", pre_gain=gain)
+    h.float().sum().backward()
+    assert gain.data_ptr() in seen
+    want, want_u = gain.grad.clone(), u.grad.clone()
+    gain.grad = u.grad = None
+    autograd.block_norm(u, None, post="none", pre="rms", pre_gain=gain)[1].float().sum().backward()
+    assert torch.equal(gain.grad, want) and torch.equal(u.grad, want_u)

@@ -352,6 +352,8 @@ NFAD_API size_t nfad_bias_act_backward_scratch_bytes(int dtype, size_t rows, siz
  * channel; the number of sequences: one for each sequence).  Parameters have the tensors' dtype; each may be NULL (gain
  * 1, bias 0, gate 1), and then gate_rows is ignored.  gate_rows must divide rows and eps must be > 0 and finite (NFAD_E_VALUE).
  * A row that holds a NaN or an infinity spoils its own results only.
+ * A finite row whose sum of squares passes fp32's range (elements from about 2^64 on) has 1/sqrt = 0: its normalised values are 0
+ * (NaN where a LayerNorm's plain sum overflows as well).
  */
 typedef enum { NFAD_NORM_NONE = 0, NFAD_NORM_RMS = 1, NFAD_NORM_LAYER = 2 } nfad_norm;
 

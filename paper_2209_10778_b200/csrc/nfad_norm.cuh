@@ -113,11 +113,13 @@ template <class S, int kUnit> struct RowColumns {
     }
 };
 
-// 1 / sqrt(x): the hardware's approximation and one Newton step, within two units in the last place
+// 1 / sqrt(x): the hardware's approximation y and one Newton step, y + y (1 - x y^2) / 2, within one unit in the last place; 0 for a
+// sum of squares that has overflowed (its row's normalised values are 0 then; the step alone would make NaN of it).  The intrinsic that
+// rounds exactly takes a tenth longer on short rows ([65536, 128] bf16 20.6 us for 18.8, [14808, 100] 6.2 for 5.6).
 __device__ __forceinline__ float reciprocal_root(float x)
 {
-    const float y = rsqrtf(x);
-    return y * fmaf(-0.5f * x * y, y, 1.5f);
+    const float y = rsqrtf(x), root = fmaf(0.5f * y, fmaf(-x * y, y, 1.0f), y);
+    return x > 3.40282347e+38f ? 0.0f : root;
 }
 
 // which gate row governs a row; divisions of 64 bits cost as much as a row's arithmetic, and are rarely needed

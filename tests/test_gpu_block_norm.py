@@ -461,3 +461,35 @@ def test_threads_with_different_widths():
     assert not failed, (len(failed), failed[0])
     for _, given, grads, want, _ in jobs:
         assert torch.equal(given[5], want[0]) and torch.equal(given[6], want[1]) and all(torch.equal(grads[k], want[2][k]) for k in grads)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [64, 1000, 4096, 14336, 1021, 4098, 20000])
+def test_rows_whose_squares_overflow(dtype, cols):
+    # finite values from about 2^64 on: the sum of their squares is infinite in fp32, its reciprocal root 0, and so is the normalised row
+    rows = 9
+    u, r = _tensors(rows, cols, dtype, 81)
+    sign = torch.ones(cols)
+    sign[1::2] = -1
+    for post, pre in (("rms", "rms"), ("layer", "layer"), ("none", "rms"), ("rms", "none")):
+        p = _parameters(dtype, cols, rows, post, pre, 1, True, 8000)
+        clean = _forward(p, u, r)
+        big_u, big_r = u.clone(), r.clone()
+        big_u[2], big_r[6] = (sign * 1e25).to(u.dtype), (sign * 1e25).to(u.dtype)
+        s, h, stats = _forward(p, big_u, big_r)
+        keep = [i for i in range(rows) if i not in (2, 6)]
+        assert torch.equal(s[keep], clean[0][keep]) and torch.equal(stats[keep], clean[2][keep])
+        assert torch.isfinite(s).all()
+        if post != "none":
+            assert stats[2, 1] == 0
+            a = p["post_bias"].double() * p["gate"][0].double()       # what is left of a row whose normalised values are 0
+            want = p["alpha"] * r[2].double() + a
+            plain.check(s[2], want, 4 * plain.EPS32 * (abs(p["alpha"]) * r[2].double().abs() + a.abs()), "s")
+        if pre != "none":
+            for i in (2, 6) if post == "none" else (6,):
+                assert stats[i, 3] == 0
+                assert torch.equal(h[i].float().cpu(), p["pre_bias"].float())
+            assert torch.isfinite(h).all()
+        dh, gs = _tensors(rows, cols, dtype, 83)
+        gu, gr, grads = _backward(p, dh if pre != "none" else None, gs, big_u, s.cpu(), stats)
+        assert torch.isfinite(gu).all() and torch.isfinite(gr).all() and all(torch.isfinite(g).all() for g in grads.values())

@@ -55,11 +55,13 @@ def _raw(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, shape, device
     return t.data_ptr()
 
 
-def _scratch(t: Optional[torch.Tensor]):
+def _scratch(t: Optional[torch.Tensor], device):
     if t is None:
         return None, 0
     if not t.is_cuda or not t.is_contiguous():
         raise TypeError("scratch must be a contiguous CUDA tensor")
+    if t.device != device:
+        raise ValueError(f"scratch must be on {device}")
     return t.data_ptr(), t.numel() * t.element_size()
 
 
@@ -150,7 +152,7 @@ def nfad_block_norm_backward(norm: BlockNorm, grad_h: Optional[torch.Tensor], gr
         like = norm.tensors[name]
         shape = like.shape if like is not None else (cols,)
         setattr(out, name, _raw(t, "grads[" + name + "]", torch.float32, torch.Size(shape), grad_u.device))
-    sp, sb = _scratch(scratch)
+    sp, sb = _scratch(scratch, grad_u.device)
     kin = _kin(grad_u)
     _call("nfad_block_norm_backward", grad_u, norm.ref, _TORCH_TO_CODE[kin[0]], _like(grad_h, "grad_h", kin), _like(grad_s, "grad_s", kin),
           _like(u, "u", kin), _like(s, "s", kin), _raw(stats, "stats", torch.float32, (rows, 4), grad_u.device), pg,
@@ -217,7 +219,7 @@ def nfad_expert_act_backward(grad_out: torch.Tensor, dfdx: Optional[torch.Tensor
     pd = _raw(dfdx, "dfdx", grad_out.dtype, grad_out.shape, grad_out.device)
     pz = _raw(grad_z, "grad_z", grad_out.dtype, grad_out.shape, grad_out.device)
     pb = _raw(grad_bias, "grad_bias", torch.float32, (experts, n_out), grad_out.device)
-    sp, sb = _scratch(scratch)
+    sp, sb = _scratch(scratch, grad_out.device)
     _call("nfad_expert_act_backward", grad_out, _TORCH_TO_CODE[grad_out.dtype], pg, pd, _offsets(offsets, grad_out.device), pz, pb, sp, sb,
           rows, n_out, experts)
 
@@ -295,7 +297,7 @@ def nfad_i8_linear_dynamic(kind, x: torch.Tensor, wq: torch.Tensor, w_scale: tor
     n_out, pw, pws, pb = _i8_weight(wq, w_scale, bias, y, n_in)
     if y.shape != (rows, n_out) or y.dtype != x.dtype or y.device != x.device:
         raise ValueError("y must be [rows, out] of x's dtype and device")
-    sp, sb = _scratch(scratch)
+    sp, sb = _scratch(scratch, x.device)
     _call("nfad_i8_linear_dynamic", x, _act(kind), _TORCH_TO_CODE[x.dtype], px, pw, pws, pb, py, sp, sb, rows, n_in, n_out)
 
 

@@ -493,3 +493,27 @@ def test_rows_whose_squares_overflow(dtype, cols):
         dh, gs = _tensors(rows, cols, dtype, 83)
         gu, gr, grads = _backward(p, dh if pre != "none" else None, gs, big_u, s.cpu(), stats)
         assert torch.isfinite(gu).all() and torch.isfinite(gr).all() and all(torch.isfinite(g).all() for g in grads.values())
+
+
+class _Elsewhere(torch.Tensor):
+    """A tensor that says it lives on another GPU."""
+    device = property(lambda self: torch.device("cuda", 1))
+
+
+def test_scratch_on_another_device_is_refused():
+    rows, cols = 8, 64
+    u, r = (t.to(DEV) for t in _tensors(rows, cols, "bf16", 1))
+    gain = torch.ones(cols, dtype=torch.bfloat16, device=DEV)
+    norm = nfad.BlockNorm(post="rms", pre="rms", pre_gain=gain)
+    s, h, st = torch.empty_like(u), torch.empty_like(u), torch.empty(rows, 4, device=DEV)
+    nfad.nfad_block_norm_forward(norm, u, r, s, h, st)
+    away = nfad.nfad_block_norm_backward_scratch(norm, u).as_subclass(_Elsewhere)
+    with pytest.raises(ValueError):
+        nfad.nfad_block_norm_backward(norm, h, None, u, s, st, torch.empty_like(u), None, None, away)
+    offsets = torch.tensor([0, rows], dtype=torch.int32, device=DEV)
+    with pytest.raises(ValueError):
+        nfad.nfad_expert_act_backward(u, None, offsets, None, torch.empty(1, cols, device=DEV), nfad.nfad_expert_act_backward_scratch(u).as_subclass(_Elsewhere))
+    q, qs = torch.zeros(16, cols, dtype=torch.int8, device=DEV), torch.ones(16, device=DEV)
+    with pytest.raises(ValueError):
+        nfad.nfad_i8_linear_dynamic(None, u, q, qs, None, torch.empty(rows, 16, dtype=u.dtype, device=DEV),
+                                    nfad.nfad_i8_linear_dynamic_scratch(u).as_subclass(_Elsewhere))

@@ -115,7 +115,7 @@ class BlockNormFunction(torch.autograd.Function):
         block.nfad_block_norm_forward(norm, uc, rc, s, h, stats)
         ctx.save_for_backward(uc, s, stats, *given.values())
         ctx.set_materialize_grads(False)             # a result that nothing used costs no read of zeros
-        ctx.names, ctx.settings = list(given), settings
+        ctx.names, ctx.settings, ctx.r_shape = list(given), settings, None if r is None else r.shape
         if h is None:
             h = s.new_empty(0)
             ctx.mark_non_differentiable(h)
@@ -134,7 +134,7 @@ class BlockNormFunction(torch.autograd.Function):
         grads = {k: torch.empty(norm.tensors[k].shape, device=u.device) for i, k in enumerate(names)
                  if norm.tensors[k] is not None and has[k] and ctx.needs_input_grad[2 + i]}
         gu = torch.empty_like(u)
-        gr = torch.empty_like(u) if ctx.needs_input_grad[1] else None
+        gr = torch.empty(ctx.r_shape, dtype=u.dtype, device=u.device) if ctx.needs_input_grad[1] else None
         block.nfad_block_norm_backward(norm, grad_h.contiguous() if norm.pre else None, None if grad_s is None else grad_s.contiguous(), u, s, stats, gu, gr, grads,
                                        block.nfad_block_norm_backward_scratch(norm, u))
         return (gu, gr, *(grads[k].to(u.dtype) if k in grads else None for k in names), None, None, None, None)

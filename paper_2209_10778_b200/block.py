@@ -101,16 +101,19 @@ class BlockNorm:
 
 def _kin(first: torch.Tensor):
     """What tensors like `first` share, for _like: looked up once a call."""
-    return first.dtype, first.numel(), first.get_device(), first
+    return first.dtype, first.shape, first.get_device(), first
 
 
 def _like(t: Optional[torch.Tensor], name: str, kin) -> Optional[int]:
-    """The address of an optional contiguous tensor of the first one's type, size and device."""
+    """The address of an optional contiguous tensor of the first one's type, size, row length and device."""
     if t is None:
         return None
-    if type(t) is torch.Tensor and t.dtype is kin[0] and t.numel() == kin[1] and t.get_device() == kin[2] and t.is_contiguous():
+    if type(t) is torch.Tensor and t.dtype is kin[0] and t.shape == kin[1] and t.get_device() == kin[2] and t.is_contiguous():
         return t.data_ptr()
-    return _tensor(t, name, kin[3])                  # a subclass, or it raises
+    p = _tensor(t, name, kin[3])                     # a subclass, the same rows in another shape, or it raises
+    if t.shape[-1:] != kin[1][-1:]:
+        raise ValueError(f"{name} must have rows of {kin[1][-1]}")
+    return p
 
 
 def nfad_block_norm_forward(norm: BlockNorm, u: torch.Tensor, r: Optional[torch.Tensor], s_out: Optional[torch.Tensor],
@@ -119,8 +122,8 @@ def nfad_block_norm_forward(norm: BlockNorm, u: torch.Tensor, r: Optional[torch.
     pass that will not be differentiated."""
     pu = norm._fits(u, "u")
     kin = _kin(u)
-    cols = u.size(-1)
-    rows = kin[1] // cols if cols else 0
+    cols = kin[1][-1]
+    rows = u.numel() // cols if cols else 0
     ps = None if stats is None else _raw(stats, "stats", torch.float32, (rows, 4), u.device)
     _call("nfad_block_norm_forward", u, norm.ref, _TORCH_TO_CODE[kin[0]], pu, _like(r, "r", kin), _like(s_out, "s_out", kin), _like(h, "h", kin), ps,
           rows, cols)

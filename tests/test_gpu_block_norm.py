@@ -517,3 +517,22 @@ def test_scratch_on_another_device_is_refused():
     with pytest.raises(ValueError):
         nfad.nfad_i8_linear_dynamic(None, u, q, qs, None, torch.empty(rows, 16, dtype=u.dtype, device=DEV),
                                     nfad.nfad_i8_linear_dynamic_scratch(u).as_subclass(_Elsewhere))
+
+
+def test_rows_of_another_length_are_refused():
+    # as many elements in rows of another length would be read as other rows
+    rows, cols = 8, 64
+    u, r = (t.to(DEV) for t in _tensors(rows, cols, "bf16", 1))
+    norm = nfad.BlockNorm(post="rms", pre="rms")
+    turned = lambda: torch.empty(cols, rows, dtype=u.dtype, device=DEV)
+    s, h, st = torch.empty_like(u), torch.empty_like(u), torch.empty(rows, 4, device=DEV)
+    for bad in ((u, turned(), s, h), (u, r, turned(), h), (u, r, s, turned())):
+        with pytest.raises(ValueError):
+            nfad.nfad_block_norm_forward(norm, *bad, st)
+    nfad.nfad_block_norm_forward(norm, u.view(2, 4, cols), r, s, h, st)               # the rows are the same
+    scratch, gu = nfad.nfad_block_norm_backward_scratch(norm, u), torch.empty_like(u)
+    for i in range(5):
+        args = [h, r, u, s, torch.empty_like(u)]
+        args[i] = turned()
+        with pytest.raises(ValueError):
+            nfad.nfad_block_norm_backward(norm, *args[:4], st, gu, args[4], None, scratch)

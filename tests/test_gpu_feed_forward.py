@@ -181,3 +181,11 @@ def test_block_norm_parameters_pass_saved_tensor_hooks():
     gain.grad = u.grad = None
     autograd.block_norm(u, None, post="none", pre="rms", pre_gain=gain)[1].float().sum().backward()
     assert torch.equal(gain.grad, want) and torch.equal(u.grad, want_u)
+
+
+def test_block_norm_stream_in_another_shape():
+    u, r = W.normal(12 * 64, "f32", 1, 1.0, DEV).view(2, 6, 64).requires_grad_(True), W.normal(12 * 64, "f32", 2, 1.0, DEV).view(12, 64).requires_grad_(True)
+    s, h = autograd.block_norm(u, r, residual_scale=0.5)
+    s.sum().backward()
+    assert u.grad.shape == u.shape and r.grad.shape == r.shape
+    assert torch.equal(u.grad, torch.ones_like(u)) and torch.equal(r.grad, torch.full_like(r, 0.5))

@@ -6,6 +6,7 @@ and call the CUDA library.
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as nfad
 from . import block
@@ -122,6 +123,7 @@ class BlockNormFunction(torch.autograd.Function):
         return s, h
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_s, grad_h):
         u, s, stats, *given = ctx.saved_tensors
         norm = block.BlockNorm(**dict(zip(ctx.names, given)), **ctx.settings)
@@ -170,6 +172,7 @@ class ExpertLinear(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_out):
         x, w, offsets, *d = ctx.saved_tensors
         gz, gb = _expert_grad_bias(grad_out.contiguous(), d[0] if d else None, offsets, ctx.needs_input_grad[2])
@@ -205,6 +208,7 @@ class ExpertFeedForward(torch.autograd.Function):
         return y2
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_out):
         x, y1, d1, w1, w2, offsets = ctx.saved_tensors
         need = ctx.needs_input_grad

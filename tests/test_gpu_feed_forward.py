@@ -189,3 +189,15 @@ def test_block_norm_stream_in_another_shape():
     s.sum().backward()
     assert u.grad.shape == u.shape and r.grad.shape == r.shape
     assert torch.equal(u.grad, torch.ones_like(u)) and torch.equal(r.grad, torch.full_like(r, 0.5))
+
+
+def test_second_derivatives_are_refused():
+    # the wrappers' backward passes are kernels without a derivative of their own
+    off = torch.tensor([0, 8], dtype=torch.int32, device=DEV)
+    x = W.normal(8 * 64, "bf16", 1, 1.0, DEV).view(8, 64).requires_grad_(True)
+    w1, w2 = (W.normal(64 * 64, "bf16", 2 + i, 0.1, DEV).view(1, 64, 64) for i in range(2))
+    for out in (autograd.block_norm(x, None)[1], autograd.expert_linear(x, w1, None, off, "swish"), autograd.expert_feed_forward(x, w1, None, w2, None, off)):
+        # a factor that depends on x, so that the first derivative is differentiable as a whole
+        g, = torch.autograd.grad((out.float() * x.float()).sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            g.float().sum().backward()

@@ -42,7 +42,8 @@ class FeedForwardBlock(torch.nn.Module):
 
 class ServingBlock:
     """A one-expert block's value-only pass with its weights in 8-bit integers: a scale for each output channel, formed here once,
-    and for each token, formed on the way.  Keeps its buffers for the largest number of rows seen."""
+    and for each token, formed on the way.  Everything is a copy: training the block on changes nothing here.  Keeps its buffers for
+    the largest number of rows seen."""
 
     def __init__(self, block: FeedForwardBlock):
         if block.w1.shape[0] != 1:
@@ -52,9 +53,9 @@ class ServingBlock:
             ops.nfad_i8_quantize_rows(w.detach()[0], q, s)
             return q, s
         (self.q1, self.s1), (self.q2, self.s2) = quantized(block.w1), quantized(block.w2)
-        self.b1, self.b2 = (b.detach()[0].contiguous() for b in (block.b1, block.b2))
-        self.norm = ops.BlockNorm(post="rms", pre="rms", post_gain=block.post_gain.detach(), gate=block.gate.detach(),
-                                  pre_gain=block.pre_gain.detach(), residual_scale=block.residual_scale)
+        self.b1, self.b2 = (b.detach()[0].clone() for b in (block.b1, block.b2))
+        self.norm = ops.BlockNorm(post="rms", pre="rms", residual_scale=block.residual_scale,
+                                  **{k: getattr(block, k).detach().clone() for k in ("post_gain", "gate", "pre_gain")})
         self.kind, self.dtype = block.kind, block.w1.dtype
         self._rows = 0
 

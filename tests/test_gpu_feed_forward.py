@@ -201,3 +201,20 @@ def test_second_derivatives_are_refused():
         g, = torch.autograd.grad((out.float() * x.float()).sum(), x, create_graph=True)
         with pytest.raises(RuntimeError, match="once_differentiable"):
             g.float().sum().backward()
+
+
+def test_serving_keeps_the_weights_it_was_made_of():
+    torch.manual_seed(1)
+    block = feed_forward.FeedForwardBlock(64, 128, 1, kind="swish")
+    with torch.no_grad():
+        for b in (block.b1, block.b2):
+            b.normal_()
+    x = W.normal(4 * 64, "bf16", 1, 1.0, DEV).view(4, 64)
+    serve = block.serving()
+    want_s = x.clone()
+    want_h = serve(want_s, x).clone()
+    with torch.no_grad():
+        for p in block.parameters():                                  # training goes on
+            p.add_(0.5)
+    s = x.clone()
+    assert torch.equal(serve(s, x), want_h) and torch.equal(s, want_s)

@@ -1083,7 +1083,7 @@ static __global__ void __launch_bounds__(32 * kNormGroups) norm_reduce_kernel(co
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
     const size_t col = size_t(blockIdx.x) * 32 + lane;
-    const size_t gate_rows = a.grad_gate ? a.rows / a.rows_per_gate : 0;
+    const size_t gate_rows = a.grad_gate && a.rows_per_gate > 1 ? a.rows / a.rows_per_gate : 0;          // as the launch counts them
     for (size_t job = blockIdx.y; job < kNormSums + gate_rows; job += gridDim.y) {
         const bool gate = job >= kNormSums;
         float* out = gate ? a.grad_gate + (job - kNormSums) * a.cols : a.sums[job];

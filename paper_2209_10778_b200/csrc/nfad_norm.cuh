@@ -526,8 +526,10 @@ template <class S, int kUnit, int kI, int kR, bool kWarp, bool kMean> cudaError_
 // Packets a thread holds, and rows.  Few threads with much each: a row's reductions are shared by fewer warps, and its
 // parameters by more of the work.  bf16, us, against one packet of two rows a thread: [16384, 4096] RMS pair 87 (113), LayerNorm pair
 // by four packets 110 (141), [32768, 2048] 86 (102), [8192, 8192] by four 99 (112), [4096, 16384] by eight 105 (131 swept several times).
+// LayerNorm pairs from 256 packets on by four of one row, against two of two rows: [6000, 2560] f16 30.4 (32.0), [16384, 2560] 75.3 (79.8),
+// [16384, 4096] 105.6 (112.4), fp32 [16384, 1024] 48.2 (45.7) and [16384, 2048] 86 (85); with 2048 columns the threshold itself: 56.1 (57.1).
 // A warp per row below 65 packets: [65536, 512] LayerNorm pair 49 (52 by a CTA).  Fewer rows than SMs are a matter of latency: one
-// packet of one row, 2.9 us for three rows of 4096 (4.1).
+// packet of one row, against two of two: three rows of 4096 2.8 (4.0), 148 of them 3.0 (4.1), their LayerNorm pair 3.5 (5.7).
 template <class S, bool kMean> cudaError_t launch_norm_forward_rows(const NormForwardArgs& a, int sms, cudaStream_t st)
 {
     constexpr int V = S::kVec;
@@ -621,10 +623,12 @@ template <bool kMean, int P> __device__ __forceinline__ void normalise(float2 (&
 // gains and the gate are constants, so the inner loop keeps few sums:
 //   grad g_pre = sum dh s^;   P = sum ds u^, Q = sum ds over the rows of one gate row, from which at its end
 //   grad gate = g_post P + b_post Q, grad g_post += gate P, grad b_post += gate Q.
-// Measured on [32768, 4096] bf16, RMS norms and a gate (1.6 GB): next row prefetched into registers 418 us, this ring 355 us, these
-// sums 290 us, pairs of values in one instruction 283 us, with norm_reduce_kernel as it is now 278 us.
+// Measured on [32768, 4096] bf16, RMS norms and a gate (1.6 GB), graph replays: next row prefetched into registers 418 us, this ring
+// 355 us, these sums 290 us, pairs of values in one instruction 283 us, with norm_reduce_kernel as it is now 279 us (calls between
+// other kernels: 303 us).
 // kI packets per thread, kR rows at a time; kGate: there is a gate; kFull: means and bias sums are kept too (without: RMS norms,
-// no bias sums, and no post_bias in a gate's gradient that is asked for).  Aligned rows of up to 512 kI packets.  Dynamic shared memory: `stages` rows of the tensors that are there.
+// no bias sums, and no post_bias in a gate's gradient that is asked for).  Aligned rows of up to 512 kI packets.  Dynamic shared
+// memory: `stages` rows of the tensors that are there.
 template <class S, int kI, int kR, bool kGate, bool kFull>
 __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constant__ NormBackwardArgs a, int stages)
 {
@@ -1202,7 +1206,8 @@ cudaError_t launch_norm_backward(const NormBackwardArgs& in, void* scratch, cuda
     const void* ptr[10] = {a.grad_h, a.grad_s, a.u, a.s, a.post_gain, a.post_bias, a.gate, a.pre_gain, a.grad_u, a.grad_r};
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];
-    // the row in registers, two packets a thread at most (more spill beside the column sums)
+    // the row in registers, two packets a thread at most (beside the sums of a gate and means two already spill 280 bytes a thread for
+    // bf16 and 460 for f16: [4096, 6144] f16, LayerNorm pair, 124 us)
     const bool vec = norm_vector_ok<S>(ptr, 10, a.cols);
     if (vec && a.packets <= 512) e = launch_norm_backward_rows<S, 1, 2>(a, p, st);
     else if (vec && a.packets <= 1024) e = launch_norm_backward_rows<S, 2, 1>(a, p, st);

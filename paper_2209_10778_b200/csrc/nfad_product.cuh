@@ -85,7 +85,8 @@ struct ProdTileAt {
 
 // Tile t, for one role's walk over its tiles (t ascending).  Within an expert, bands of kBand tiles along A's dimension, B's tile
 // changing slowest inside a band: the CTAs that run at one time then share a few tiles of each operand through L2.  32-bit
-// arithmetic throughout: tiles are counted below 2^31 (the launch sees to it), and every role does this once per tile.
+// arithmetic throughout: tiles are counted below 2^31 (the launch sees to it), and every role does this once per tile.  Bands of 8, 16
+// and 64 tiles, us, 8192 rows 2048 -> 8192 bf16: forward 187, 185, 183; gradient of the input 199, 203, 211; of the weights 221, 221, 228.
 constexpr uint32_t kBand = 16;
 template <int OP, int BN, bool kPair> struct TileWalk {
     uint32_t b_tiles, expert = 0;

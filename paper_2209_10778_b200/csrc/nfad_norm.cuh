@@ -624,7 +624,7 @@ template <bool kMean, int P> __device__ __forceinline__ void normalise(float2 (&
 //   grad g_pre = sum dh s^;   P = sum ds u^, Q = sum ds over the rows of one gate row, from which at its end
 //   grad gate = g_post P + b_post Q, grad g_post += gate P, grad b_post += gate Q.
 // Measured on [32768, 4096] bf16, RMS norms and a gate (1.6 GB), graph replays: next row prefetched into registers 418 us, this ring
-// 355 us, these sums 290 us, pairs of values in one instruction 283 us, with norm_reduce_kernel as it is now 279 us (calls between
+// 355 us, these sums 290 us, pairs of values in one instruction 283 us, with norm_reduce_kernel as it is now 276 us (calls between
 // other kernels: 303 us).
 // kI packets per thread, kR rows at a time; kGate: there is a gate; kFull: means and bias sums are kept too (without: RMS norms,
 // no bias sums, and no post_bias in a gate's gradient that is asked for).  Aligned rows of up to 512 kI packets.  Dynamic shared
@@ -724,14 +724,19 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
             parameter(a.gate, gate_row, i, 0.0f, gate);
             parameter(post ? a.post_gain : nullptr, 0, i, 1.0f, gain);
             parameter(post ? a.post_bias : nullptr, 0, i, 0.0f, bias);
-            // the caller's tensor may begin on any float: single stores
+            // pairs where the place begins on eight bytes (by single floats throughout: 647 us for a gate row for each row of [32768, 4096] bf16, not
+            // 617); the caller's tensor may begin on any float
             float* dst = on[i] && a.grad_gate ? gate_target(a, blockIdx.x, r0, r1, gate_row) + size_t(column[i]) * S::kVec : nullptr;
 #pragma unroll
             for (int e = 0; e < P; ++e) {
                 if (dst) {
                     const float2 v = kFull ? fma2(gain[e], acc_p[i][e], mul2(bias[e], acc_q[i][e])) : mul2(gain[e], acc_p[i][e]);
-                    dst[2 * e] = v.x;
-                    dst[2 * e + 1] = v.y;
+                    if (reinterpret_cast<uintptr_t>(dst) & 7u) {
+                        dst[2 * e] = v.x;
+                        dst[2 * e + 1] = v.y;
+                    } else {
+                        reinterpret_cast<float2*>(dst)[e] = v;
+                    }
                 }
                 acc_post[i][e] = fma2(gate[e], acc_p[i][e], acc_post[i][e]);
                 acc_p[i][e] = twice(0.0f);

@@ -432,6 +432,30 @@ NFAD_API int nfad_expert_linear_backward_weight(int dtype, const void* grad_z, c
                                                 size_t in, size_t out, size_t experts, nfad_stream_t stream);
 
 /*
+ * Gated layers, grouped by expert like the products above (the same rules for offsets, rows of nobody, types and alignment).
+ *
+ * Forward: w is [experts, 2, out, in], bias [experts, 2, out] or NULL: the gate's weight, then the other one's.
+ *   a = x w_e0^T + bias_e0,  u = x w_e1^T + bias_e1,  y = f(a) u,
+ *   both projections, the activation and the product in one kernel; a and u never reach memory.  kind NFAD_NO_ACT: y = a u.  y is
+ *   a function of two variables, and nested forward differentiation gives both its derivatives with it:
+ *   partials [rows, 2, out] or NULL: dy/da = f'(a) u, then dy/du = f(a), each rounded once: all that the layer's backward keeps.
+ * Backward: grad_z = [grad_y dy/da, grad_y dy/du], [rows, 2, out], the gradient of both projections at once.  From there on the layer
+ *   is a linear one with 2 out outputs: nfad_expert_linear_backward_input and _weight with grad_z, w and out doubled.
+ * nfad_expert_gated_backward: grad_out [rows, out] is the gradient of y.  grad_bias [experts, 2, out] or NULL: the column sums of the
+ *   unrounded products (fp32, fixed order).  grad_z may equal partials.  scratch as for nfad_expert_act_backward with 2 out columns; needed for
+ *   grad_bias only.
+ * nfad_expert_linear_backward_gated: the same where the layer behind is a linear one, w [experts, out, in] and grad_z [rows, out] the
+ *   gradient of its result: its input's gradient g = grad_z w_e stays in the kernel, and grad [rows, 2, in] = [g dy/da, g dy/du],
+ *   rounded once.  grad may equal partials [rows, 2, in].
+ */
+NFAD_API int nfad_expert_gated_linear(int kind, int dtype, const void* x, const void* w, const void* bias, const int* offsets, void* y, void* partials,
+                                      size_t rows, size_t in, size_t out, size_t experts, nfad_stream_t stream);
+NFAD_API int nfad_expert_gated_backward(int dtype, const void* grad_out, const void* partials, const int* offsets, void* grad_z, float* grad_bias,
+                                        void* scratch, size_t scratch_bytes, size_t rows, size_t out, size_t experts, nfad_stream_t stream);
+NFAD_API int nfad_expert_linear_backward_gated(int dtype, const void* grad_z, const void* w, const int* offsets, const void* partials, void* grad,
+                                               size_t rows, size_t in, size_t out, size_t experts, nfad_stream_t stream);
+
+/*
  * Linear layer in 8-bit integers, with a scale for each token (row of x) and for each output channel (row of w).
  *
  * nfad_i8_quantize_rows: scale[r] = amax / 127, q = rint(x (127 / amax)) in [-127, 127], amax the row's largest magnitude.

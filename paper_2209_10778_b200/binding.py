@@ -37,6 +37,7 @@ EXPORTS = (
     "nfad_block_norm_forward", "nfad_block_norm_backward", "nfad_block_norm_backward_scratch_bytes",
     "nfad_expert_linear", "nfad_expert_act_backward", "nfad_expert_act_backward_scratch_bytes",
     "nfad_expert_linear_backward_input", "nfad_expert_linear_backward_weight",
+    "nfad_expert_gated_linear", "nfad_expert_gated_backward", "nfad_expert_linear_backward_gated",
     "nfad_i8_quantize_rows", "nfad_i8_linear", "nfad_i8_linear_dynamic", "nfad_i8_linear_dynamic_scratch_bytes",
     "nfad_wait_faults",
 )
@@ -122,6 +123,9 @@ def load() -> ctypes.CDLL:
                 ("nfad_expert_act_backward_scratch_bytes", [sz, sz], sz),
                 ("nfad_expert_linear_backward_input", [ci, vp, vp, vp, vp, vp, sz, sz, sz, sz, vp], ci),
                 ("nfad_expert_linear_backward_weight", [ci, vp, vp, vp, vp, sz, sz, sz, sz, vp], ci),
+                ("nfad_expert_gated_linear", [ci, ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, sz, vp], ci),
+                ("nfad_expert_gated_backward", [ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, sz, vp], ci),
+                ("nfad_expert_linear_backward_gated", [ci, vp, vp, vp, vp, vp, sz, sz, sz, sz, vp], ci),
                 ("nfad_i8_quantize_rows", [ci, vp, vp, vp, sz, sz, vp], ci),
                 ("nfad_i8_linear", [ci, ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, vp], ci),
                 ("nfad_i8_linear_dynamic", [ci, ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, sz, vp], ci),

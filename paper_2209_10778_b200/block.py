@@ -254,6 +254,55 @@ def nfad_expert_linear_backward_weight(grad_z: torch.Tensor, x: torch.Tensor, of
           n_out, experts)
 
 
+# ---------------------------------------------------------------- gated layers grouped by expert
+
+def nfad_expert_gated_linear(kind, x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor], offsets: torch.Tensor, y: torch.Tensor,
+                             partials: Optional[torch.Tensor] = None) -> None:
+    """y = f(a) u, a = x w_e0^T + bias_e0, u = x w_e1^T + bias_e1: x [rows, in] sorted by expert, w [experts, 2, out, in], bias
+    [experts, 2, out]; partials [rows, 2, out] = (f'(a) u, f(a)), y's two derivatives.  kind None: y = a u."""
+    px, pw = _matrix(x, "x"), _matrix(w, "w", 4)
+    (rows, n_in), (experts, two, n_out, w_in) = x.shape, w.shape
+    if w_in != n_in or two != 2 or w.dtype != x.dtype or w.device != x.device:
+        raise ValueError("w must be [experts, 2, out, in] of x's dtype and device")
+    if offsets.numel() != experts + 1:
+        raise ValueError("offsets must hold experts + 1 values")
+    pb = _raw(bias, "bias", x.dtype, (experts, 2, n_out), x.device)
+    py, pp = _raw(y, "y", x.dtype, (rows, n_out), x.device), _raw(partials, "partials", x.dtype, (rows, 2, n_out), x.device)
+    _call("nfad_expert_gated_linear", x, _act(kind), _TORCH_TO_CODE[x.dtype], px, pw, pb, _offsets(offsets, x.device), py, pp, rows, n_in, n_out, experts)
+
+
+def nfad_expert_gated_backward(grad_out: torch.Tensor, partials: torch.Tensor, offsets: torch.Tensor, grad_z: torch.Tensor,
+                               grad_bias: Optional[torch.Tensor], scratch: Optional[torch.Tensor]) -> None:
+    """grad_z [rows, 2, out] = grad_out times both partials; grad_bias (fp32 [experts, 2, out]) = each expert's column sums of the
+    unrounded products.  scratch: nfad_expert_act_backward_scratch of grad_z.flatten(1)."""
+    pg = _matrix(grad_out, "grad_out")
+    rows, n_out = grad_out.shape
+    experts, both = offsets.numel() - 1, (rows, 2, n_out)
+    if partials is None or grad_z is None:
+        raise TypeError("partials and grad_z must be CUDA tensors")
+    pp, pz = _raw(partials, "partials", grad_out.dtype, both, grad_out.device), _raw(grad_z, "grad_z", grad_out.dtype, both, grad_out.device)
+    pb = _raw(grad_bias, "grad_bias", torch.float32, (experts, 2, n_out), grad_out.device)
+    sp, sb = _scratch(scratch, grad_out.device)
+    _call("nfad_expert_gated_backward", grad_out, _TORCH_TO_CODE[grad_out.dtype], pg, pp, _offsets(offsets, grad_out.device), pz, pb, sp, sb,
+          rows, n_out, experts)
+
+
+def nfad_expert_linear_backward_gated(grad_z: torch.Tensor, w: torch.Tensor, offsets: torch.Tensor, partials: torch.Tensor, grad: torch.Tensor) -> None:
+    """grad [rows, 2, in] = (grad_z w_e) times both partials: the gradient of a linear layer's input, taken on through the gated layer
+    that made it."""
+    pg, pw = _matrix(grad_z, "grad_z"), _matrix(w, "w", 3)
+    (rows, n_out), (experts, w_out, n_in) = grad_z.shape, w.shape
+    if w_out != n_out or w.dtype != grad_z.dtype or w.device != grad_z.device:
+        raise ValueError("w must be [experts, out, in] of grad_z's dtype and device")
+    if offsets.numel() != experts + 1:
+        raise ValueError("offsets must hold experts + 1 values")
+    if partials is None or grad is None:
+        raise TypeError("partials and grad must be CUDA tensors")
+    pp, px = (_raw(t, name, grad_z.dtype, (rows, 2, n_in), grad_z.device) for t, name in ((partials, "partials"), (grad, "grad")))
+    _call("nfad_expert_linear_backward_gated", grad_z, _TORCH_TO_CODE[grad_z.dtype], pg, pw, _offsets(offsets, grad_z.device), pp, px, rows, n_in,
+          n_out, experts)
+
+
 # ---------------------------------------------------------------- the linear layer in 8-bit integers
 
 def nfad_i8_quantize_rows(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor) -> None:

@@ -35,6 +35,8 @@ UNITS = [
     ("nfad_kernels_prod_input.cu", ["-fmad=true"]),
     ("nfad_kernels_prod_weight.cu", ["-fmad=true"]),
     ("nfad_kernels_prod_bytes.cu", ["-fmad=true"]),
+    ("nfad_kernels_prod_gated.cu", ["-fmad=true"]),
+    ("nfad_kernels_prod_input_gated.cu", ["-fmad=true"]),
     ("nfad_kernels_expert.cu", ["-fmad=true"]),
     ("nfad_api.cu", ["-fmad=false"]),
     ("nfad_api_block.cu", ["-fmad=false"]),

@@ -72,6 +72,13 @@ int check_product(int kind, int dtype, size_t rows, size_t in, size_t out, size_
     return NFAD_OK;
 }
 
+// the same for a layer with two weights [out, in]
+int check_gated(int kind, int dtype, size_t rows, size_t in, size_t out, size_t experts)
+{
+    if (out >= (size_t(1) << 31)) return NFAD_E_TOO_LARGE;
+    return check_product(kind, dtype, rows, in, 2 * out, experts);
+}
+
 int check_norm(const nfad_block_norm* norm, int dtype, size_t rows, size_t cols, size_t* n)
 {
     if (!norm) return NFAD_E_NULL;
@@ -251,6 +258,63 @@ int nfad_expert_linear_backward_weight(int dtype, const void* grad_z, const void
     return finish(nfad::launch_product_weight(dtype, g, static_cast<cudaStream_t>(stream)));
 }
 
+int nfad_expert_gated_linear(int kind, int dtype, const void* x, const void* w, const void* bias, const int* offsets, void* y, void* partials,
+                             size_t rows, size_t in, size_t out, size_t experts, nfad_stream_t stream)
+{
+    int rc = check_gated(kind, dtype, rows, in, out, experts);
+    if (rc) return rc;
+    if (rows == 0 || out == 0) return NFAD_OK;
+    if ((in && (!x || !w)) || !offsets || !y) return NFAD_E_NULL;
+    const Span sx{x, rows * in * 2, 2}, sw{w, experts * 2 * out * in * 2, 2}, sb{bias, experts * 2 * out * 2, 2}, so{offsets, (experts + 1) * 4, 4};
+    const Span oy{y, rows * out * 2, 2}, op{partials, rows * 2 * out * 2, 2};
+    if ((rc = aligned({sx, sw, sb, so, oy, op}))) return rc;
+    if ((rc = aliasing({oy, op}, {}, {sx, sw, sb, so}))) return rc;
+    nfad::ProdArgs g = {};
+    g.a = x; g.b = w; g.bias = bias; g.offsets = offsets; g.out = y; g.slope = partials;
+    g.rows = rows; g.in = uint32_t(in); g.outs = uint32_t(out); g.experts = uint32_t(experts); g.act = kind;
+    return finish(nfad::launch_product_gated(dtype, g, static_cast<cudaStream_t>(stream)));
+}
+
+int nfad_expert_gated_backward(int dtype, const void* grad_out, const void* partials, const int* offsets, void* grad_z, float* grad_bias, void* scratch,
+                               size_t scratch_bytes, size_t rows, size_t out, size_t experts, nfad_stream_t stream)
+{
+    int rc = check_gated(nfad::kNoAct, dtype, rows, 0, out, experts);
+    if (rc) return rc;
+    if (out == 0 || experts == 0) return NFAD_OK;
+    const size_t bytes = rows * out * 2;
+    if (!offsets || (bytes && (!grad_out || !partials || !grad_z))) return NFAD_E_NULL;
+    size_t need = 0;
+    if (grad_bias && bytes) {
+        if ((rc = finish(nfad::expert_act_backward_scratch(rows, 2 * out, &need)))) return rc;
+        if (!scratch) return NFAD_E_NULL;
+        if (scratch_bytes < need) return NFAD_E_SCRATCH;
+    }
+    const Span sg{grad_out, bytes, 2}, sp{partials, 2 * bytes, 2}, so{offsets, (experts + 1) * 4, 4};
+    const Span oz{grad_z, 2 * bytes, 2}, ob{grad_bias, experts * 2 * out * 4, 4}, sc{need ? scratch : nullptr, need, 16};
+    if ((rc = aligned({sg, sp, so, oz, ob, sc}))) return rc;
+    if ((rc = aliasing({oz}, {sp}, {sg, so, ob, sc}))) return rc;
+    if ((rc = aliasing({ob, sc}, {}, {sg, sp, so}))) return rc;
+    return finish(nfad::launch_expert_gated_backward(dtype, grad_out, partials, offsets, grad_z, grad_bias, scratch, rows, uint32_t(out),
+                                                     uint32_t(experts), static_cast<cudaStream_t>(stream)));
+}
+
+int nfad_expert_linear_backward_gated(int dtype, const void* grad_z, const void* w, const int* offsets, const void* partials, void* grad, size_t rows,
+                                      size_t in, size_t out, size_t experts, nfad_stream_t stream)
+{
+    int rc = check_gated(nfad::kNoAct, dtype, rows, out, in, experts);            // `in` is the gated layer's width here
+    if (rc) return rc;
+    if (rows == 0 || in == 0) return NFAD_OK;
+    if ((out && (!grad_z || !w)) || !offsets || !partials || !grad) return NFAD_E_NULL;
+    const Span sg{grad_z, rows * out * 2, 2}, sw{w, experts * out * in * 2, 2}, so{offsets, (experts + 1) * 4, 4}, sp{partials, rows * 2 * in * 2, 2};
+    const Span ox{grad, rows * 2 * in * 2, 2};
+    if ((rc = aligned({sg, sw, so, sp, ox}))) return rc;
+    if ((rc = aliasing({ox}, {sp}, {sg, sw, so}))) return rc;
+    nfad::ProdArgs g = {};
+    g.a = grad_z; g.b = w; g.prev = partials; g.offsets = offsets; g.out = grad;
+    g.rows = rows; g.in = uint32_t(in); g.outs = uint32_t(out); g.experts = uint32_t(experts); g.act = nfad::kNoAct;
+    return finish(nfad::launch_product_input_gated(dtype, g, static_cast<cudaStream_t>(stream)));
+}
+
 int nfad_i8_quantize_rows(int dtype, const void* x, signed char* q, float* scale, size_t rows, size_t cols, nfad_stream_t stream)
 {
     if (dtype < 0 || dtype > 2) return NFAD_E_DTYPE;
@@ -319,7 +383,8 @@ int nfad_i8_linear_dynamic(int kind, int dtype, const void* x, const signed char
 int nfad_wait_faults(void)
 {
     unsigned total = 0;
-    for (auto count : {nfad::wait_faults_norm, nfad::product_faults_forward, nfad::product_faults_input, nfad::product_faults_weight, nfad::product_faults_bytes}) {
+    for (auto count : {nfad::wait_faults_norm, nfad::product_faults_forward, nfad::product_faults_input, nfad::product_faults_weight, nfad::product_faults_bytes,
+                       nfad::product_faults_gated, nfad::product_faults_input_gated}) {
         unsigned n = 0;
         if (int rc = finish(count(&n))) return -rc;
         total += n;

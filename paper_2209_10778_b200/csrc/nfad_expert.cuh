@@ -5,6 +5,9 @@
 // expert's rows all lie in the chunk, else to the chunk's slot 0 (an expert whose rows begin before the chunk) or 1 (one whose rows
 // begin in it and go on); a second kernel adds the slots of an expert in row order.  The sums are of the unrounded products (exact in
 // fp32 for 16-bit factors), in fp32 and in a fixed order.  Three tensors of traffic bound it.
+//
+// Gated layers have two derivatives to a result, [rows, 2, cols] like gz and as wide as both: a thread multiplies its packet of
+// grad_out with both and keeps both sums.  Five tensors of traffic; two rows at a time, which are as many loads in flight as four of the other.
 #pragma once
 
 #include "nfad_bias.cuh"
@@ -15,7 +18,7 @@ namespace nfad {
 struct ExpertActArgs {
     const void *g, *d;                   // d null: f' = 1
     void* gz;                            // may be null when d is null
-    float *grad_bias, *partial;          // grad_bias null: not wanted; partial [chunks][2][cols]
+    float *grad_bias, *partial;          // grad_bias null: not wanted; partial [chunks][2][cols] (gated: [chunks][2][2 cols])
     int* begin;                          // [experts + 1] where each expert's rows begin, for the second kernel
     const int* offsets;
     size_t rows;
@@ -76,10 +79,10 @@ __device__ __forceinline__ void expert_begins(const ExpertActArgs& a)
 template <class S, bool kVec> struct ExpertPacket { uint4 v; };
 template <class S> struct ExpertPacket<S, false> { typename S::elem v; };
 
-template <class S, bool kVec>
+template <class S, bool kVec, bool kGated>
 __global__ void __launch_bounds__(kBiasMaxBlock, 4) expert_act_kernel(const __grid_constant__ ExpertActArgs a)
 {
-    constexpr int V = kVec ? S::kVec : 1, U = kBiasRows;
+    constexpr int V = kVec ? S::kVec : 1, G = kGated ? 2 : 1, U = kBiasRows / G;
     using E = typename S::elem;
     using Packet = ExpertPacket<S, kVec>;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -89,6 +92,7 @@ __global__ void __launch_bounds__(kBiasMaxBlock, 4) expert_act_kernel(const __gr
     const bool on = cp < a.row_packets;
     const int r0 = int(blockIdx.y * a.chunk_rows), r1 = int(min(size_t(r0) + a.chunk_rows, a.rows));      // rows are below 2^31
     if (r0 >= r1) return;
+    // `row` of a tensor of rows of cols: row G r + j is row r's part j where there are G parts
     auto load = [&](const void* base, size_t row) {
         Packet p;
         if constexpr (kVec) p.v = load_packet(static_cast<const uint4*>(base) + row * a.row_packets + cp);
@@ -99,28 +103,37 @@ __global__ void __launch_bounds__(kBiasMaxBlock, 4) expert_act_kernel(const __gr
         if constexpr (kVec) S::unpack(p.v, v);
         else v[0] = S::load1(&p.v);
     };
-    float acc[V];
+    float acc[G][V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+    for (int j = 0; j < G; ++j)
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[j][i] = 0.0f;
     ExpertRun run = {0, r0, false};                                   // of the row at hand
     // straight to the result when all of the expert's rows are in the chunk; else to slot 0 (they begin before it) or 1
     auto hand_over = [&]() {
         const uint32_t e = run.next - 1;
         if (a.grad_bias && on && e < a.experts) {
-            float* dst = (run.here && run.end <= r1 ? a.grad_bias + size_t(e) * a.cols : a.partial + (size_t(blockIdx.y) * 2 + run.here) * a.cols) + size_t(cp) * V;
+            const size_t wide = size_t(a.cols) * G;
+            float* dst = (run.here && run.end <= r1 ? a.grad_bias + size_t(e) * wide : a.partial + (size_t(blockIdx.y) * 2 + run.here) * wide) + size_t(cp) * V;
 #pragma unroll
-            for (int i = 0; i < V; ++i) dst[i] = acc[i];
+            for (int j = 0; j < G; ++j)
+#pragma unroll
+                for (int i = 0; i < V; ++i) dst[size_t(j) * a.cols + i] = acc[j][i];
         }
 #pragma unroll
-        for (int i = 0; i < V; ++i) acc[i] = 0.0f;
+        for (int j = 0; j < G; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) acc[j][i] = 0.0f;
     };
     for (int row = r0; row < r1; row += U) {
-        Packet g[U], d[U];
+        Packet g[U], d[U][G];
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (on && row + u < r1) {
                 g[u] = load(a.g, row + u);
-                if (a.d) d[u] = load(a.d, row + u);
+#pragma unroll
+                for (int j = 0; j < G; ++j)
+                    if (kGated || a.d) d[u][j] = load(a.d, size_t(row + u) * G + j);
             }
         if (row == r0) run = expert_run<4>(a, row, 0);
 #pragma unroll
@@ -131,24 +144,28 @@ __global__ void __launch_bounds__(kBiasMaxBlock, 4) expert_act_kernel(const __gr
                 run = expert_run<1>(a, row + u, run.next);
                 run.here = true;                                     // the offset that ended the run before is this row
             }
-            float v[V];
-            if (run.next - 1 < a.experts) {
-                widen(g[u], v);
-                if (a.d) {
-                    float f[V];
-                    widen(d[u], f);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) v[i] = __fmul_rn(v[i], f[i]);
+            for (int j = 0; j < G; ++j) {
+                float v[V];
+                if (run.next - 1 < a.experts) {
+                    widen(g[u], v);
+                    if (kGated || a.d) {
+                        float f[V];
+                        widen(d[u][j], f);
+#pragma unroll
+                        for (int i = 0; i < V; ++i) v[i] = __fmul_rn(v[i], f[i]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < V; ++i) acc[j][i] = __fadd_rn(acc[j][i], v[i]);
+                } else {                                             // nobody's row, whatever it holds
+#pragma unroll
+                    for (int i = 0; i < V; ++i) v[i] = 0.0f;
                 }
-#pragma unroll
-                for (int i = 0; i < V; ++i) acc[i] = __fadd_rn(acc[i], v[i]);
-            } else {                                                 // nobody's row, whatever it holds
-#pragma unroll
-                for (int i = 0; i < V; ++i) v[i] = 0.0f;
-            }
-            if (a.gz && on) {
-                if constexpr (kVec) store_packet<true>(static_cast<uint4*>(a.gz) + size_t(row + u) * a.row_packets + cp, S::pack(v));
-                else S::store1(static_cast<E*>(a.gz) + size_t(row + u) * a.cols + cp, v[0]);
+                if (a.gz && on) {
+                    const size_t at = size_t(row + u) * G + j;
+                    if constexpr (kVec) store_packet<true>(static_cast<uint4*>(a.gz) + at * a.row_packets + cp, S::pack(v));
+                    else S::store1(static_cast<E*>(a.gz) + at * a.cols + cp, v[0]);
+                }
             }
         }
     }
@@ -215,7 +232,7 @@ inline size_t expert_act_scratch_bytes(size_t rows, size_t cols, int sms)
     return (rows + n - 1) / n * 2 * cols * sizeof(float) + (kMaxExperts + 1) * sizeof(int);
 }
 
-template <class S> cudaError_t launch_expert_act(const ExpertActArgs& in, cudaStream_t st)
+template <class S, bool kGated = false> cudaError_t launch_expert_act(const ExpertActArgs& in, cudaStream_t st)
 {
     ExpertActArgs a = in;
     DeviceInfo di;
@@ -223,19 +240,21 @@ template <class S> cudaError_t launch_expert_act(const ExpertActArgs& in, cudaSt
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];
-    a.chunk_rows = expert_chunk_rows(a.rows, a.cols, di.sm_count);
+    const uint32_t wide = a.cols * (kGated ? 2 : 1); // columns that are summed
+    a.chunk_rows = expert_chunk_rows(a.rows, wide, di.sm_count);
     a.chunks = uint32_t((a.rows + a.chunk_rows - 1) / a.chunk_rows);
-    a.begin = reinterpret_cast<int*>(a.partial + size_t(a.chunks) * 2 * a.cols);
+    a.begin = reinterpret_cast<int*>(a.partial + size_t(a.chunks) * 2 * wide);
     if (a.rows) {
         const bool vec = a.cols % 8 == 0 && aligned16(a.g) && aligned16(a.d) && aligned16(a.gz);
         a.row_packets = vec ? a.cols / 8 : a.cols;
         const unsigned block = bias_block(a.row_packets);
         bias_launch_config(&cfg, attr, (a.row_packets + block - 1) / block, block, st, true);
         cfg.gridDim.y = a.chunks;
-        e = vec ? cudaLaunchKernelEx(&cfg, expert_act_kernel<S, true>, a) : cudaLaunchKernelEx(&cfg, expert_act_kernel<S, false>, a);
+        e = vec ? cudaLaunchKernelEx(&cfg, expert_act_kernel<S, true, kGated>, a) : cudaLaunchKernelEx(&cfg, expert_act_kernel<S, false, kGated>, a);
         if (e != cudaSuccess) return e;
     }
     if (!a.grad_bias) return cudaSuccess;
+    a.cols = wide;
     bias_launch_config(&cfg, attr, (a.cols + 31) / 32, 32 * kExpertGroups, st, true);
     cfg.gridDim.y = a.experts;
     return cudaLaunchKernelEx(&cfg, expert_reduce_kernel, a);

@@ -54,17 +54,20 @@ __device__ __forceinline__ void act1(int kind, float z, float* y, float* d)
     *d = o.dydx;
 }
 
-// kBytes: 8-bit integers, one expert.  early: the weights may be read before the kernel in front has ended
+// OP: kProdForward, kProdBytes (8-bit integers, one expert) or kProdGated, whose CTA takes eight outputs of each of the two weights: the
+// lower and the upper half of the instruction's 16 rows.  early: the weights may be read before the kernel in front has ended
 // (it is the quantiser of the same call, which starts this one only after everything before it is complete).
-template <bool kBytes, class S, int NT>
+template <int OP, class S, int NT>
 __global__ void __launch_bounds__(kFewWarps * 32, NT == 1 ? 4 : 3) few_rows_kernel(const __grid_constant__ ProdArgs g, int early)
 {
+    constexpr bool kBytes = OP == kProdBytes, kGated = OP == kProdGated;
+    constexpr int kOutputs = kFewOutputs / ProdKind<OP>::kPerResult;           // a job's
     constexpr int kNumber = kBytes ? tc::kNumberS8 : IsBF16<S>::value ? tc::kNumberBF16 : tc::kNumberF16;
     constexpr int ES = kBytes ? 1 : 2;
     __shared__ uint32_t sums[kFewWarps][kFewOutputs][8 * NT + 1];
     __shared__ int live[kFewMaxRows], first[kFewMaxRows], rows[kFewMaxRows], lives, bounds[2];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, quad = lane & 3;
-    const uint32_t groups = (g.outs + kFewOutputs - 1) / kFewOutputs;
+    const uint32_t groups = (g.outs + kOutputs - 1) / kOutputs;
     const uint32_t pitch = g.in * ES;                // bytes of a row of either operand
     const uint32_t blocks = (pitch + kFewSteps * 64 - 1) / (kFewSteps * 64);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -110,7 +113,12 @@ __global__ void __launch_bounds__(kFewWarps * 32, NT == 1 ? 4 : 3) few_rows_kern
             const int r = int(i / g.outs);
             if (r >= bounds[0] && r < bounds[1]) continue;
             S::store1(static_cast<typename S::elem*>(g.out) + i, 0.0f);
-            if (g.slope) S::store1(static_cast<typename S::elem*>(g.slope) + i, 0.0f);
+            if (g.slope && kGated) {
+                S::store1(static_cast<typename S::elem*>(g.slope) + i + size_t(r) * g.outs, 0.0f);
+                S::store1(static_cast<typename S::elem*>(g.slope) + i + size_t(r + 1) * g.outs, 0.0f);
+            } else if (g.slope) {
+                S::store1(static_cast<typename S::elem*>(g.slope) + i, 0.0f);
+            }
         }
     } else {
         if (threadIdx.x == 0) lives = (int(g.rows) + 8 * NT - 1) / (8 * NT);
@@ -128,11 +136,11 @@ __global__ void __launch_bounds__(kFewWarps * 32, NT == 1 ? 4 : 3) few_rows_kern
     const uint32_t jobs = groups * uint32_t(lives);
     uint4 lo[kFewSteps], hi[kFewSteps];
     auto request = [&](uint32_t job, uint32_t b) {
-        const uint32_t slot = job / groups, o0 = (job - slot * groups) * kFewOutputs;
-        const unsigned char* w = static_cast<const unsigned char*>(g.b) + (size_t(live[slot]) * g.outs + o0) * pitch;
+        const uint32_t slot = job / groups, o0 = (job - slot * groups) * kOutputs;
+        const unsigned char* w = static_cast<const unsigned char*>(g.b) + (size_t(live[slot]) * g.outs * ProdKind<OP>::kPerResult + o0) * pitch;
         // rows past the last output repeat it: their sums are not used
         const unsigned char* w_lo = w + size_t(min(uint32_t(gid), g.outs - 1 - o0)) * pitch;
-        const unsigned char* w_hi = w + size_t(min(uint32_t(gid) + 8, g.outs - 1 - o0)) * pitch;
+        const unsigned char* w_hi = kGated ? w_lo + size_t(g.outs) * pitch : w + size_t(min(uint32_t(gid) + 8, g.outs - 1 - o0)) * pitch;
         const uint32_t k0 = b * (kFewSteps * 64) + quad * 16;         // this lane's first byte
 #pragma unroll
         for (int i = 0; i < kFewSteps; ++i) {
@@ -147,7 +155,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, NT == 1 ? 4 : 3) few_rows_kern
     if (job < jobs && uint32_t(warp) < blocks) request(job, warp);
     for (; job < jobs; job += gridDim.x) {
         const int slot = int(job / groups);
-        const uint32_t o0 = (job - slot * groups) * kFewOutputs;
+        const uint32_t o0 = (job - slot * groups) * kOutputs;
         const int m = rows[slot];
         const unsigned char* x = static_cast<const unsigned char*>(g.a) + size_t(first[slot]) * pitch;
         uint32_t acc[NT][4];
@@ -184,21 +192,42 @@ __global__ void __launch_bounds__(kFewWarps * 32, NT == 1 ? 4 : 3) few_rows_kern
             sums[warp][gid + 8][n * 8 + quad * 2 + 1] = acc[n][3];
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < kFewOutputs * m; i += kFewWarps * 32) {
-            const int token = i / kFewOutputs;
-            const uint32_t o = o0 + i % kFewOutputs;
+        for (int i = threadIdx.x; i < kOutputs * m; i += kFewWarps * 32) {
+            const int token = i / kOutputs;
+            const uint32_t o = o0 + i % kOutputs;
             if (o >= g.outs) continue;
             const size_t row = first[slot] + token;
+            if constexpr (kGated) {
+                float z = 0.0f, u = 0.0f, f, d;
+#pragma unroll
+                for (int k = 0; k < kFewWarps; ++k) {
+                    z += __uint_as_float(sums[k][i % kOutputs][token]);
+                    u += __uint_as_float(sums[k][i % kOutputs + kOutputs][token]);
+                }
+                if (g.bias) {
+                    const typename S::elem* b = static_cast<const typename S::elem*>(g.bias) + size_t(live[slot]) * 2 * g.outs + o;
+                    z += S::load1(b);
+                    u += S::load1(b + g.outs);
+                }
+                act1(g.act, z, &f, &d);
+                S::store1(static_cast<typename S::elem*>(g.out) + row * g.outs + o, f * u);
+                if (g.slope) {
+                    typename S::elem* both = static_cast<typename S::elem*>(g.slope) + row * 2 * g.outs + o;
+                    S::store1(both, d * u);
+                    S::store1(both + g.outs, f);
+                }
+                continue;
+            }
             float z;
             if (kBytes) {
                 int t = 0;
 #pragma unroll
-                for (int k = 0; k < kFewWarps; ++k) t += int(sums[k][i % kFewOutputs][token]);
+                for (int k = 0; k < kFewWarps; ++k) t += int(sums[k][i % kOutputs][token]);
                 z = float(t) * (g.a_scale[row] * __ldg(g.b_scale + o));
             } else {
                 z = 0.0f;
 #pragma unroll
-                for (int k = 0; k < kFewWarps; ++k) z += __uint_as_float(sums[k][i % kFewOutputs][token]);
+                for (int k = 0; k < kFewWarps; ++k) z += __uint_as_float(sums[k][i % kOutputs][token]);
             }
             if (g.bias) z += S::load1(static_cast<const typename S::elem*>(g.bias) + size_t(live[slot]) * g.outs + o);
             float y, d;
@@ -211,10 +240,11 @@ __global__ void __launch_bounds__(kFewWarps * 32, NT == 1 ? 4 : 3) few_rows_kern
     if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");   // a CTA without work ends in order too
 }
 
-template <bool kBytes, class S, int NT> cudaError_t launch_few_rows_tiles(const ProdArgs& g, int sms, int early, cudaStream_t st)
+template <int OP, class S, int NT> cudaError_t launch_few_rows_tiles(const ProdArgs& g, int sms, int early, cudaStream_t st)
 {
     const size_t live = g.rows < g.experts ? g.rows : g.experts;
-    const size_t jobs = (g.outs + kFewOutputs - 1) / kFewOutputs * live, fit = size_t(sms) * (NT == 1 ? 4 : 3);
+    constexpr int kOutputs = kFewOutputs / ProdKind<OP>::kPerResult;
+    const size_t jobs = (g.outs + kOutputs - 1) / kOutputs * live, fit = size_t(sms) * (NT == 1 ? 4 : 3);
     // one expert, whose jobs are known: as many for each CTA, rather than a last turn of a few (13.3 -> 12.6 us); else all that fit
     const size_t turns = g.experts == 1 ? (jobs + fit - 1) / fit : 1, grid = (jobs + turns - 1) / turns;
     cudaLaunchConfig_t cfg = {};
@@ -226,7 +256,7 @@ template <bool kBytes, class S, int NT> cudaError_t launch_few_rows_tiles(const 
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, few_rows_kernel<kBytes, S, NT>, g, early);
+    return cudaLaunchKernelEx(&cfg, few_rows_kernel<OP, S, NT>, g, early);
 }
 
 // Whether there are few rows: 16 at most, or up to four for each expert.  Measured against tiles on tcgen05 (us): one token
@@ -236,11 +266,11 @@ template <bool kBytes, class S, int NT> cudaError_t launch_few_rows_tiles(const 
 inline bool few_rows(const ProdArgs& g) { return g.in < (1u << 28) && (g.rows <= 16 || (g.rows <= kFewMaxRows && g.rows <= 4 * size_t(g.experts))); }
 
 // Tokens a job takes at once, by the rows an expert has on average: an expert with more is read once per such group.
-template <bool kBytes, class S> cudaError_t launch_few_rows(const ProdArgs& g, int sms, int early, cudaStream_t st)
+template <int OP, class S> cudaError_t launch_few_rows(const ProdArgs& g, int sms, int early, cudaStream_t st)
 {
     const size_t mean = (g.rows + g.experts - 1) / g.experts;
-    if (mean <= 8) return launch_few_rows_tiles<kBytes, S, 1>(g, sms, early, st);
-    return launch_few_rows_tiles<kBytes, S, 2>(g, sms, early, st);
+    if (mean <= 8) return launch_few_rows_tiles<OP, S, 1>(g, sms, early, st);
+    return launch_few_rows_tiles<OP, S, 2>(g, sms, early, st);
 }
 
 }  // namespace nfad

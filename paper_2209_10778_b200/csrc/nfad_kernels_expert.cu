@@ -5,13 +5,27 @@
 
 namespace nfad {
 
-cudaError_t launch_expert_act_backward(int dtype, const void* g, const void* d, const int* offsets, void* gz, float* grad_bias, void* scratch,
-                                       size_t rows, uint32_t cols, uint32_t experts, cudaStream_t st)
+static ExpertActArgs expert_args(const void* g, const void* d, const int* offsets, void* gz, float* grad_bias, void* scratch, size_t rows, uint32_t cols,
+                                 uint32_t experts)
 {
     ExpertActArgs a = {};
     a.g = g; a.d = d; a.gz = gz; a.grad_bias = grad_bias; a.partial = static_cast<float*>(scratch);
     a.offsets = offsets; a.rows = rows; a.cols = cols; a.experts = experts;
+    return a;
+}
+
+cudaError_t launch_expert_act_backward(int dtype, const void* g, const void* d, const int* offsets, void* gz, float* grad_bias, void* scratch,
+                                       size_t rows, uint32_t cols, uint32_t experts, cudaStream_t st)
+{
+    const ExpertActArgs a = expert_args(g, d, offsets, gz, grad_bias, scratch, rows, cols, experts);
     return dtype == kBF16 ? launch_expert_act<StoreBF16>(a, st) : launch_expert_act<StoreF16>(a, st);
+}
+
+cudaError_t launch_expert_gated_backward(int dtype, const void* g, const void* d, const int* offsets, void* gz, float* grad_bias, void* scratch,
+                                         size_t rows, uint32_t cols, uint32_t experts, cudaStream_t st)
+{
+    const ExpertActArgs a = expert_args(g, d, offsets, gz, grad_bias, scratch, rows, cols, experts);
+    return dtype == kBF16 ? launch_expert_act<StoreBF16, true>(a, st) : launch_expert_act<StoreF16, true>(a, st);
 }
 
 cudaError_t expert_act_backward_scratch(size_t rows, size_t cols, size_t* bytes)

@@ -36,8 +36,12 @@ constexpr int kMaxStages = 9;
 
 template <int OP> struct ProdKind {
     static constexpr bool kBytes = OP == kProdBytes;
+    static constexpr bool kGated = OP == kProdGated;                      // half of a tile's columns are a's, half are u's of the same outputs
+    static constexpr bool kInput = OP == kProdInput || OP == kProdInputGated;
+    static constexpr bool kForward = OP == kProdForward || OP == kProdBytes || kGated;
     static constexpr bool kTurnA = OP == kProdWeight;                     // operand A runs along its rows' dimension in memory
-    static constexpr bool kTurnB = OP == kProdWeight || OP == kProdInput;
+    static constexpr bool kTurnB = OP == kProdWeight || kInput;
+    static constexpr int kPerResult = kGated ? 2 : 1;                     // a tile's columns for each column of the result
     static constexpr int kElem = kBytes ? 1 : 2;
     static constexpr int kStep = kStepBytes / kElem;                      // reduction steps per stage: 64, 128 for bytes
 };
@@ -110,7 +114,7 @@ template <int OP, int BN, bool kPair> struct TileWalk {
         const uint32_t bt = in_band / height, at = band * kBand + in_band - bt * height;
         const int r0 = start[expert], r1 = start[expert + 1];
         q.expert = expert;
-        q.b0 = int(bt) * BN;
+        q.b0 = int(bt) * (BN / ProdKind<OP>::kPerResult);
         if (OP == kProdWeight) {
             q.a0 = int(at) * kRows;
             q.a_end = int(g.outs);
@@ -120,7 +124,7 @@ template <int OP, int BN, bool kPair> struct TileWalk {
             q.a0 = r0 + int(at) * kRows;
             q.a_end = r1;
             q.r0 = 0;
-            q.r_end = int(OP == kProdInput ? g.outs : g.in);
+            q.r_end = int(ProdKind<OP>::kInput ? g.outs : g.in);
         }
         return q;
     }
@@ -182,19 +186,21 @@ struct GatherSource {
     const unsigned char *begin, *end, *at;
     uint32_t pitch;
     int own, own_end, red, red_end;                  // first index and end along the own dimension and along the reduction
+    size_t second;                                   // kHalves: bytes from the first half of the box's rows to the second
 };
 constexpr int kGatherPackets = 1024 / (kGatherWarps * 32);
-template <int ES, bool kTurn> struct GatherPackets {
+// kHalves: the box's second 64 rows have the first ones' indices in another matrix (the two weights of a gated layer)
+template <int ES, bool kTurn, bool kHalves = false> struct GatherPackets {
     static constexpr int PER = 16 / ES;
     uint4 lo[kGatherPackets], hi[kGatherPackets];
     uint32_t whole;
     // where packet i of the box begins, and how many of its elements there are
     static __device__ __forceinline__ const unsigned char* place(const GatherSource& src, int i, int* n)
     {
-        const int row = kTurn ? src.red + ((i & 511) >> 3) : src.own + (i >> 3), end = kTurn ? src.red_end : src.own_end;
+        const int row = kTurn ? src.red + ((i & 511) >> 3) : src.own + (kHalves ? (i & 511) >> 3 : i >> 3), end = kTurn ? src.red_end : src.own_end;
         const int col = kTurn ? src.own + (i >> 9) * (128 / ES) + (i & 7) * PER : src.red + (i & 7) * PER, width = kTurn ? src.own_end : src.red_end;
         *n = row < end ? width - col : 0;
-        return src.at + size_t(row) * src.pitch + size_t(col) * ES;
+        return src.at + size_t(row) * src.pitch + size_t(col) * ES + (kHalves && i >= 512 ? src.second : 0);
     }
     __device__ __forceinline__ void load(const GatherSource& src, int thread)
     {
@@ -326,6 +332,7 @@ struct RowPackets {
     int lane, rows;                                 // how many of the warp's 32 rows there are
     uint32_t width;
     size_t row0;                                    // the first one
+    size_t pitch;                                   // elements from one row to the next
     uint4* stage;
     static __device__ __forceinline__ int at(int row, int packet) { return row * 8 + (packet ^ (row << 2 & 4 | row >> 1 & 3)); }
     __device__ __forceinline__ void put(int packet, const uint4& v) const { stage[at(lane, packet)] = v; }
@@ -336,8 +343,8 @@ struct RowPackets {
     {
         const int r0 = lane / kPackets, c = lane % kPackets;
         if (col + c * 8 >= width) return;
-        E* p = base + ((row0 + r0) * width + col + c * 8);
-        const size_t step = size_t(32 / kPackets) * width;
+        E* p = base + ((row0 + r0) * pitch + col + c * 8);
+        const size_t step = size_t(32 / kPackets) * pitch;
 #pragma unroll
         for (int i = 0; i < kPackets; ++i, p += step) {
             const int r = r0 + i * (32 / kPackets);
@@ -353,8 +360,8 @@ struct RowPackets {
     template <class S, int kPackets> __device__ __forceinline__ void store_odd(void* base, uint32_t col, int first) const
     {
         using E = typename S::elem;
-        E* p = static_cast<E*>(base) + row0 * width + col;
-        for (int r = 0; r < rows; ++r, p += width)
+        E* p = static_cast<E*>(base) + row0 * pitch + col;
+        for (int r = 0; r < rows; ++r, p += pitch)
 #pragma unroll
             for (int e = lane; e < kPackets * 8; e += 32)
                 if (col + e < width) p[e] = reinterpret_cast<const E*>(stage + at(r, first + (e >> 3)))[e & 7];
@@ -362,8 +369,8 @@ struct RowPackets {
     template <class S> __device__ __forceinline__ void fetch_odd(const void* base, uint32_t col, int first) const
     {
         using E = typename S::elem;
-        const E* p = static_cast<const E*>(base) + row0 * width + col;
-        for (int r = 0; r < rows; ++r, p += width)
+        const E* p = static_cast<const E*>(base) + row0 * pitch + col;
+        for (int r = 0; r < rows; ++r, p += pitch)
             if (col + lane < width) reinterpret_cast<E*>(stage + at(r, first + (lane >> 3)))[lane & 7] = p[lane];
     }
     // four packets of each row, on their way in
@@ -380,14 +387,18 @@ struct RowPackets {
     }
 };
 
-// rows that belong to no expert: zeros
-template <class S, int kThreads> __device__ __forceinline__ void clear_rows(const ProdArgs& g, int first, int end, uint32_t width, int thread)
+// rows that belong to no expert: zeros (kGated: `slope` has two such rows to each of `out`; kInputGated: `out` does)
+template <class S, int kThreads, int OP> __device__ __forceinline__ void clear_rows(const ProdArgs& g, int first, int end, uint32_t result_width, int thread)
 {
+    const size_t width = OP == kProdInputGated ? size_t(result_width) * 2 : result_width;
     const size_t n0 = size_t(first) * width, n1 = size_t(end) * width;
     for (size_t i = n0 + size_t(blockIdx.x) * kThreads + thread; i < n1; i += size_t(gridDim.x) * kThreads) {
         S::store1(static_cast<typename S::elem*>(g.out) + i, 0.0f);
-        if (g.slope) S::store1(static_cast<typename S::elem*>(g.slope) + i, 0.0f);
+        if (!ProdKind<OP>::kGated && g.slope) S::store1(static_cast<typename S::elem*>(g.slope) + i, 0.0f);
     }
+    if (ProdKind<OP>::kGated && g.slope)
+        for (size_t i = 2 * n0 + size_t(blockIdx.x) * kThreads + thread; i < 2 * n1; i += size_t(gridDim.x) * kThreads)
+            S::store1(static_cast<typename S::elem*>(g.slope) + i, 0.0f);
 }
 
 // ---------------------------------------------------------------- the kernel
@@ -444,12 +455,14 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
     if (kPair) tc::pair_sync();                      // the other CTA's barriers exist
     tc::fence_after_sync();
     const uint32_t tmem = s.tmem;
-    const uint32_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs;       // of a result's row
+    const uint32_t width = Kind::kInput || OP == kProdWeight ? g.in : g.outs;       // of a result's row
+    constexpr uint32_t kResults = BN / Kind::kPerResult;                             // a tile's
     TileWalk<OP, BN, kPair> walk;
-    walk.b_tiles = (width + BN - 1) / BN;
+    walk.b_tiles = (width + kResults - 1) / kResults;
     const uint32_t total = (OP == kProdWeight ? g.experts * ((g.outs + Tile::kRows - 1) / Tile::kRows) : uint32_t(s.tiles[g.experts])) * walk.b_tiles;
     // the last tile along a result's row is a narrower product (a multiple of 16 columns, of 32 for a pair, which halves it)
     auto columns = [&](const ProdTileAt& q) {
+        if (Kind::kGated) return uint32_t(BN);       // u's columns keep their place: what lies behind the last output is zeros, times x
         const uint32_t unit_n = kPair ? 32 : 16, left = (width - q.b0 + unit_n - 1) / unit_n * unit_n;
         return left < uint32_t(BN) ? left : uint32_t(BN);
     };
@@ -471,7 +484,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
         if (lane == 0)
             for (uint32_t t = unit; t < total; t += units) {
                 const ProdTileAt q = walk.at(g, s.start, s.tiles, t);
-                const int a0 = q.a0 + int(rank) * kTileRows, b0 = q.b0 + (rank ? int(columns(q)) / 2 : 0);
+                const int a0 = q.a0 + int(rank) * kTileRows, b0 = q.b0 + (rank && !Kind::kGated ? int(columns(q)) / 2 : 0);
                 const int a_rows = max(0, min(kTileRows, q.a_end - a0));
                 const int boxes = (a_rows + kBoxRows - 1) / kBoxRows;     // of A, when it is not turned
                 const uint32_t bytes = !for_a ? kOwn * kStepBytes : Kind::kTurnA ? kTileRows * kStepBytes : uint32_t(boxes) * kBoxRows * kStepBytes;
@@ -504,6 +517,10 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
                     } else if (Kind::kTurnB) {
 #pragma unroll
                         for (int j = 0; j < kOwn / 64; ++j) tc::load_box<kPair>(at_b + j * 64 * 128, &map_b, bar, b0 + j * 64, r, int(q.expert));
+                    } else if (Kind::kGated) {
+                        // a pair's first CTA holds a's columns, the second u's
+                        tc::load_box<kPair>(at_b, &map_b, bar, r, b0, int(q.expert * 2 + rank));
+                        if (!kPair) tc::load_box<kPair>(at_b + kOwn / 2 * kStepBytes, &map_b, bar, r, b0, int(q.expert * 2 + 1));
                     } else {
                         tc::load_box<kPair>(at_b, &map_b, bar, r, b0, int(q.expert));
                     }
@@ -526,9 +543,10 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
             constexpr int ES = Kind::kElem;
             const int thread = threadIdx.x - (kFirstResultWarp + kResultWarps) * 32;
             GatherSource a, b;
-            a.pitch = (OP == kProdInput || OP == kProdWeight ? g.outs : g.in) * ES;
+            a.pitch = (Kind::kInput || OP == kProdWeight ? g.outs : g.in) * ES;
             b.pitch = g.in * ES;
-            const size_t weight = size_t(g.outs) * b.pitch;                       // bytes of an expert's
+            b.second = size_t(g.outs) * b.pitch;
+            const size_t weight = Kind::kPerResult * b.second;                    // bytes of an expert's
             a.begin = a.at = static_cast<const unsigned char*>(g.a);
             a.end = a.begin + g.rows * a.pitch;
             a.own = q.a0;
@@ -543,7 +561,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
                 a.red = b.red = r;
                 // requested before the stage is free, so that the wait covers the loads
                 GatherPackets<ES, Kind::kTurnA> pa;
-                GatherPackets<ES, Kind::kTurnB> pb;
+                GatherPackets<ES, Kind::kTurnB, Kind::kGated> pb;
                 pa.load(a, thread);
                 pb.load(b, thread);
                 if (!(ok = tc::barrier_wait(empty(stage), phase ^ 1, gave_up))) break;
@@ -623,8 +641,8 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
         // ------------------------------------------------ results
         const int lanes = (warp & 3) * 32, half = (warp - kFirstResultWarp) >> 2;
         if (OP != kProdWeight && g.offsets) {
-            clear_rows<S, kResultWarps * 32>(g, 0, s.start[0], width, threadIdx.x - kFirstResultWarp * 32);
-            clear_rows<S, kResultWarps * 32>(g, s.start[g.experts], int(g.rows), width, threadIdx.x - kFirstResultWarp * 32);
+            clear_rows<S, kResultWarps * 32, OP>(g, 0, s.start[0], width, threadIdx.x - kFirstResultWarp * 32);
+            clear_rows<S, kResultWarps * 32, OP>(g, s.start[g.experts], int(g.rows), width, threadIdx.x - kFirstResultWarp * 32);
         }
         // whole 16-byte packets: rows start on packets and no packet crosses a row's end
         const bool vec = width % 8 == 0 && ((reinterpret_cast<uintptr_t>(g.out) | reinterpret_cast<uintptr_t>(g.slope) | reinterpret_cast<uintptr_t>(g.prev)) & 15u) == 0;
@@ -640,28 +658,37 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
             rows.lane = lane;
             rows.rows = min(32, q.a_end - (row - lane));
             rows.width = width;
+            rows.pitch = OP == kProdInputGated ? size_t(width) * 2 : width;
             rows.row0 = out_row - lane;
             rows.stage = reinterpret_cast<uint4*>(ring + kRingBytes + (warp - kFirstResultWarp) * kStageBytes);
             // 32 columns at a time; without slopes two of them leave together; the factors of the next are fetched during the current
-            constexpr int kChunks = BN / 32, kOwnChunks = kChunks / (kResultWarps / 4);
+            constexpr int kChunks = kResults / 32, kOwnChunks = kChunks / (kResultWarps / 4);
+            static_assert(kOwnChunks > 0, "results for every result warp");
             constexpr bool kTwo = kOwnChunks > 1;
-            const bool slopes = OP == kProdForward && g.slope;
-            uint4 prev[4] = {};
+            const bool slopes = (OP == kProdForward || Kind::kGated) && g.slope;
+            uint4 prev[4] = {}, prev_u[4] = {};
+            if constexpr (OP == kProdInputGated)
+                if (vec) {
+                    rows.template fetch<S>(g.prev, q.b0 + half * kOwnChunks * 32, prev);
+                    rows.template fetch<S>(static_cast<const typename S::elem*>(g.prev) + width, q.b0 + half * kOwnChunks * 32, prev_u);
+                }
             if (OP == kProdInput && g.prev && vec) rows.template fetch<S>(g.prev, q.b0 + half * kOwnChunks * 32, prev);
-            if constexpr (OP == kProdForward || OP == kProdBytes) {
+            if constexpr (Kind::kForward) {
                 static_assert(kOwnChunks * 32 <= kColumns, "a result warp's columns");
-                float bias[kOwnChunks], scales[kOwnChunks];
+                float bias[kOwnChunks], scales[kOwnChunks];           // kGated: a's bias and u's
 #pragma unroll
                 for (int j = 0; j < kOwnChunks; ++j) {
                     const uint32_t col = q.b0 + (half * kOwnChunks + j) * 32 + lane;
                     const bool inside = col < width;
-                    bias[j] = g.bias && inside ? S::load1(static_cast<const typename S::elem*>(g.bias) + size_t(q.expert) * width + col) : 0.0f;
-                    scales[j] = Kind::kBytes && inside ? __ldg(g.b_scale + col) : 0.0f;
+                    const typename S::elem* own = static_cast<const typename S::elem*>(g.bias) + size_t(q.expert) * width * Kind::kPerResult + col;
+                    bias[j] = g.bias && inside ? S::load1(own) : 0.0f;
+                    if (Kind::kGated) scales[j] = g.bias && inside ? S::load1(own + width) : 0.0f;
+                    else scales[j] = Kind::kBytes && inside ? __ldg(g.b_scale + col) : 0.0f;
                 }
 #pragma unroll
                 for (int j = 0; j < kOwnChunks; ++j) {
                     columns[j * 32 + lane] = bias[j];
-                    if (Kind::kBytes) columns[kColumns + j * 32 + lane] = scales[j];
+                    if (Kind::kBytes || Kind::kGated) columns[kColumns + j * 32 + lane] = scales[j];
                 }
                 __syncwarp();
             }
@@ -670,9 +697,75 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
             for (int c = half * kOwnChunks; c < (half + 1) * kOwnChunks; ++c) {
                 const uint32_t col0 = q.b0 + c * 32;
                 if (col0 >= width || rows.rows <= 0) break;     // past the result's columns; a warp without rows
-                const bool second = kTwo && !slopes && (c & 1);
+                const bool second = kTwo && !slopes && OP != kProdInputGated && (c & 1);
                 uint32_t v[32];
                 tc::tmem_load32(tmem + (uint32_t(lanes) << 16) + turn * BN + c * 32, v);
+                if constexpr (Kind::kGated) {
+                    const float4* own = reinterpret_cast<const float4*>(columns) + (c - half * kOwnChunks) * 8;
+                    uint32_t w[32];
+                    tc::tmem_load32(tmem + (uint32_t(lanes) << 16) + turn * BN + kResults + c * 32, w);
+                    tc::tmem_load_wait();
+                    float z[32], u[32], d[32];
+#pragma unroll
+                    for (int p = 0; p < 8; ++p) {
+                        const float4 ba = own[p], bu = own[kColumns / 4 + p];
+                        const float add_a[4] = {ba.x, ba.y, ba.z, ba.w}, add_u[4] = {bu.x, bu.y, bu.z, bu.w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int e = p * 4 + k;
+                            z[e] = (none ? 0.0f : __uint_as_float(v[e])) + add_a[k];
+                            u[e] = (none ? 0.0f : __uint_as_float(w[e])) + add_u[k];
+                            d[e] = 1.0f;             // of no activation
+                        }
+                    }
+                    if (slopes) {
+                        act32<true>(g.act, z, d);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) d[e] *= u[e];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) u[e] *= z[e];
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) {
+                            rows.put(p, pack8<S>(u, p));
+                            rows.put(4 + p, pack8<S>(d, p));
+                        }
+                        __syncwarp();
+                        RowPackets both = rows;      // the derivatives' rows
+                        both.pitch = size_t(width) * 2;
+                        typename S::elem* by_u = static_cast<typename S::elem*>(g.slope) + width;
+                        if (vec) {
+                            rows.template store<S, 4>(g.out, col0, 0);
+                            both.template store<S, 4>(g.slope, col0, 4);
+                        } else {
+                            rows.template store_odd<S, 4>(g.out, col0, 0);
+                            both.template store_odd<S, 4>(g.slope, col0, 4);
+                        }
+                        __syncwarp();
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) rows.put(p, pack8<S>(z, p));
+                        __syncwarp();
+                        if (vec) both.template store<S, 4>(by_u, col0, 0);
+                        else both.template store_odd<S, 4>(by_u, col0, 0);
+                        __syncwarp();
+                        continue;
+                    }
+                    act32<false>(g.act, z, d);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) u[e] *= z[e];
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) rows.put((second ? 4 : 0) + p, pack8<S>(u, p));
+                    if (kTwo && !second && c + 1 < (half + 1) * kOwnChunks && col0 + 32 < width) continue;
+                    __syncwarp();
+                    if (kTwo && second) {
+                        if (vec) rows.template store<S, 8>(g.out, col0 - 32, 0);
+                        else rows.template store_odd<S, 8>(g.out, col0 - 32, 0);
+                    } else {
+                        if (vec) rows.template store<S, 4>(g.out, col0, 0);
+                        else rows.template store_odd<S, 4>(g.out, col0, 0);
+                    }
+                    __syncwarp();
+                    continue;
+                }
                 tc::tmem_load_wait();
                 float z[32], d[32];
 #pragma unroll
@@ -709,6 +802,41 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
                         for (int e = 0; e < 8; ++e) z[p * 8 + e] *= f[e];
                     }
                     __syncwarp();
+                }
+                if constexpr (OP == kProdInputGated) {
+                    // both factors in, both products out, through this lane's own places
+                    typename S::elem* by_u = static_cast<typename S::elem*>(g.out) + width;
+                    const typename S::elem* prev_by_u = static_cast<const typename S::elem*>(g.prev) + width;
+                    if (vec) {
+                        rows.settle(prev, 0);
+                        rows.settle(prev_u, 4);
+                    } else {
+                        rows.template fetch_odd<S>(g.prev, col0, 0);
+                        rows.template fetch_odd<S>(prev_by_u, col0, 4);
+                    }
+                    __syncwarp();
+                    if (vec && c + 1 < (half + 1) * kOwnChunks) {
+                        rows.template fetch<S>(g.prev, col0 + 32, prev);
+                        rows.template fetch<S>(prev_by_u, col0 + 32, prev_u);
+                    }
+#pragma unroll
+                    for (int p = 0; p < 8; ++p) {
+                        float f[8];
+                        S::unpack(rows.get(p), f);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) f[e] *= z[(p & 3) * 8 + e];
+                        rows.put(p, S::pack(f));
+                    }
+                    __syncwarp();
+                    if (vec) {
+                        rows.template store<S, 4>(g.out, col0, 0);
+                        rows.template store<S, 4>(by_u, col0, 4);
+                    } else {
+                        rows.template store_odd<S, 4>(g.out, col0, 0);
+                        rows.template store_odd<S, 4>(by_u, col0, 4);
+                    }
+                    __syncwarp();
+                    continue;
                 }
                 if constexpr (OP == kProdForward) {
                     if (slopes) act32<true>(g.act, z, d);

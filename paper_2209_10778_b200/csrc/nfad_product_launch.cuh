@@ -64,13 +64,16 @@ cudaError_t launch_product_tile(const ProdArgs& g, int sms, cudaStream_t st)
     CUtensorMap map_a = {}, map_b = {};
     if (!kGather) {
         const int number = Kind::kBytes ? tc::kNumberS8 : IsBF16<S>::value ? tc::kNumberBF16 : tc::kNumberF16;
-        const uint64_t pitch_a = OP == kProdInput || OP == kProdWeight ? g.outs : g.in;
+        const uint64_t pitch_a = Kind::kInput || OP == kProdWeight ? g.outs : g.in;
         e = make_map(&map_a, number, g.a, pitch_a, g.rows, 0, Kind::kTurnA ? 64 : Tile::kBoxRows);
         if (e != cudaSuccess) return e;
-        e = OP == kProdWeight ? make_map(&map_b, number, g.b, g.in, g.rows, 0, 64) : make_map(&map_b, number, g.b, g.in, g.outs, g.experts, Kind::kTurnB ? 64 : Tile::kOwnColumns);
+        e = OP == kProdWeight ? make_map(&map_b, number, g.b, g.in, g.rows, 0, 64)
+            : Kind::kGated    ? make_map(&map_b, number, g.b, g.in, g.outs, uint64_t(g.experts) * 2, BN / 2)
+                              : make_map(&map_b, number, g.b, g.in, g.outs, g.experts, Kind::kTurnB ? 64 : Tile::kOwnColumns);
         if (e != cudaSuccess) return e;
     }
-    const size_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs, b_tiles = (width + BN - 1) / BN;
+    constexpr size_t kResults = BN / Kind::kPerResult;
+    const size_t width = Kind::kInput || OP == kProdWeight ? g.in : g.outs, b_tiles = (width + kResults - 1) / kResults;
     const size_t a_tiles = OP == kProdWeight ? size_t(g.experts) * ((g.outs + Tile::kRows - 1) / Tile::kRows)
                                              : (g.rows + Tile::kRows - 1) / Tile::kRows + (g.offsets ? g.experts : 0);
     size_t grid = a_tiles * b_tiles;                 // at most this many tiles
@@ -101,11 +104,14 @@ template <int OP, class S> cudaError_t launch_split(const ProdArgs& g, unsigned 
     if (e != cudaSuccess) return e;
     CUtensorMap map_a = {}, map_b = {};
     const int number = Kind::kBytes ? tc::kNumberS8 : IsBF16<S>::value ? tc::kNumberBF16 : tc::kNumberF16;
-    e = make_map(&map_a, number, g.a, OP == kProdInput || OP == kProdWeight ? g.outs : g.in, g.rows, 0, Kind::kTurnA ? 64 : 32);
+    e = make_map(&map_a, number, g.a, Kind::kInput || OP == kProdWeight ? g.outs : g.in, g.rows, 0, Kind::kTurnA ? 64 : 32);
     if (e != cudaSuccess) return e;
-    e = OP == kProdWeight ? make_map(&map_b, number, g.b, g.in, g.rows, 0, 64) : make_map(&map_b, number, g.b, g.in, g.outs, g.experts, 64);
+    e = OP == kProdWeight ? make_map(&map_b, number, g.b, g.in, g.rows, 0, 64)
+        : Kind::kGated    ? make_map(&map_b, number, g.b, g.in, g.outs, uint64_t(g.experts) * 2, kSplitColumns / 2)
+                          : make_map(&map_b, number, g.b, g.in, g.outs, g.experts, 64);
     if (e != cudaSuccess) return e;
-    const size_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs, b_tiles = (width + kSplitColumns - 1) / kSplitColumns;
+    constexpr size_t kResults = kSplitColumns / Kind::kPerResult;
+    const size_t width = Kind::kInput || OP == kProdWeight ? g.in : g.outs, b_tiles = (width + kResults - 1) / kResults;
     const size_t a_tiles = OP == kProdWeight ? size_t(g.experts) * ((g.outs + kTileRows - 1) / kTileRows)
                                              : (g.rows + kTileRows - 1) / kTileRows + (g.offsets ? g.experts : 0);
     cudaLaunchConfig_t cfg = {};
@@ -130,13 +136,15 @@ template <int OP, class S> cudaError_t launch_split(const ProdArgs& g, unsigned 
 // 8: 13.3 (41.8).  With eight steps each no gain (1024 x 1024 x 1024 over 2: 10.8, 10.8); with more CTAs than fit twice what it was.
 template <int OP> unsigned split_ranks(const ProdArgs& g, int sms)
 {
-    const size_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs;
+    using Kind = ProdKind<OP>;
+    constexpr size_t kResults = kSplitColumns / Kind::kPerResult;
+    const size_t width = Kind::kInput || OP == kProdWeight ? g.in : g.outs;
     const uintptr_t results = reinterpret_cast<uintptr_t>(g.out) | reinterpret_cast<uintptr_t>(g.slope) | reinterpret_cast<uintptr_t>(g.bias) | reinterpret_cast<uintptr_t>(g.prev);
     if (width % 8 || results % 16) return 0;         // its results go by packets
     const size_t a_tiles = OP == kProdWeight ? size_t(g.experts) * ((g.outs + kTileRows - 1) / kTileRows)
                                              : (g.rows + kTileRows - 1) / kTileRows + (g.offsets ? g.experts - 1 : 0);
-    const size_t tiles = a_tiles * ((width + kSplitColumns - 1) / kSplitColumns), fit = 2 * size_t(sms);
-    const size_t steps = (OP == kProdInput ? g.outs : OP == kProdWeight ? g.rows / g.experts : g.in) / ProdKind<OP>::kStep;
+    const size_t tiles = a_tiles * ((width + kResults - 1) / kResults), fit = 2 * size_t(sms);
+    const size_t steps = (Kind::kInput ? g.outs : OP == kProdWeight ? g.rows / g.experts : g.in) / ProdKind<OP>::kStep;
     for (unsigned ranks = 8; ranks > 1; ranks /= 2)
         if (tiles * ranks <= fit && steps >= 10 * ranks) return ranks;
     return 0;
@@ -154,7 +162,8 @@ template <int OP> unsigned split_ranks(const ProdArgs& g, int sms)
 constexpr int kPairTile = 512;
 template <int OP> int product_tile(const ProdArgs& g, int sms)
 {
-    const size_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs;
+    using Kind = ProdKind<OP>;
+    const size_t width = (Kind::kInput || OP == kProdWeight ? g.in : g.outs) * size_t(Kind::kPerResult);
     const size_t live = g.rows < g.experts ? g.rows : g.experts;
     auto turns = [&](size_t tile_rows, size_t columns, size_t workers) {
         size_t a = (g.rows + tile_rows - 1) / tile_rows + (live > 1 ? live / 2 : 0);
@@ -164,7 +173,7 @@ template <int OP> int product_tile(const ProdArgs& g, int sms)
     };
     int best = 256;
     size_t least = turns(128, 256, sms) * 384;
-    for (int columns = 128; columns >= 64; columns /= 2)
+    for (int columns = 128; columns >= (Kind::kGated ? 128 : 64); columns /= 2)       // a gated tile has results for two warps of each lane quarter
         if (const size_t cost = turns(128, columns, sms) * (128 + columns); cost < least) {
             least = cost;
             best = columns;
@@ -179,19 +188,21 @@ template <int OP, class S> cudaError_t launch_product_store(const ProdArgs& g, c
     DeviceInfo di;
     cudaError_t e = device_info(&di);
     if (e != cudaSuccess) return e;
-    const size_t reduction = OP == kProdInput ? g.outs : OP == kProdWeight ? g.rows : g.in;
+    const size_t reduction = Kind::kInput ? g.outs : OP == kProdWeight ? g.rows : g.in;
     const uintptr_t low = reinterpret_cast<uintptr_t>(g.a) | reinterpret_cast<uintptr_t>(g.b) | uintptr_t(g.in) * Kind::kElem |
                           (Kind::kTurnB ? uintptr_t(g.outs) * Kind::kElem : 0);
     // a tensor copy needs rows that begin on 16-byte boundaries (and something to copy)
     if (low % 16 || reduction == 0) return launch_product_tile<OP, 128, S, true>(g, di.sm_count, st);
-    if constexpr (OP == kProdForward || OP == kProdBytes)
-        if (few_rows(g)) return launch_few_rows<Kind::kBytes, S>(g, di.sm_count, g.b_ready, st);
+    if constexpr (Kind::kForward)
+        if (few_rows(g)) return launch_few_rows<OP, S>(g, di.sm_count, g.b_ready, st);
     if (const unsigned ranks = split_ranks<OP>(g, di.sm_count)) return launch_split<OP, S>(g, ranks, st);
     switch (product_tile<OP>(g, di.sm_count)) {
     case kPairTile: return launch_product_tile<OP, 256, S, false, true>(g, di.sm_count, st);
     case 256: return launch_product_tile<OP, 256, S, false>(g, di.sm_count, st);
     case 128: return launch_product_tile<OP, 128, S, false>(g, di.sm_count, st);
-    default:  return launch_product_tile<OP, 64, S, false>(g, di.sm_count, st);
+    default:
+        if constexpr (!Kind::kGated) return launch_product_tile<OP, 64, S, false>(g, di.sm_count, st);
+        return cudaErrorInvalidValue;
     }
 }
 

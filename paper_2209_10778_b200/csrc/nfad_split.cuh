@@ -69,9 +69,10 @@ split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtenso
     __syncthreads();
     tc::fence_after_sync();
     const uint32_t tmem = s.tmem;
-    const uint32_t width = OP == kProdInput || OP == kProdWeight ? g.in : g.outs;
+    const uint32_t width = Kind::kInput || OP == kProdWeight ? g.in : g.outs;
+    constexpr uint32_t kResults = kSplitColumns / Kind::kPerResult;          // a tile's
     TileWalk<OP, kSplitColumns, false> walk;
-    walk.b_tiles = (width + kSplitColumns - 1) / kSplitColumns;
+    walk.b_tiles = (width + kResults - 1) / kResults;
     const uint32_t total = (OP == kProdWeight ? g.experts * ((g.outs + kTileRows - 1) / kTileRows) : uint32_t(s.tiles[g.experts])) * walk.b_tiles;
     const bool mine = tile < total;                  // the same for every CTA of the cluster
     ProdTileAt q = {};
@@ -82,7 +83,7 @@ split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtenso
         r0 = min(q.r_end, q.r0 + int(rank) * per * kStep);
         r1 = min(q.r_end, r0 + per * kStep);
     }
-    const uint32_t n = min(uint32_t(kSplitColumns), (width - q.b0 + 15) / 16 * 16);
+    const uint32_t n = Kind::kGated ? kSplitColumns : min(uint32_t(kSplitColumns), (width - q.b0 + 15) / 16 * 16);
     auto ragged = [&](int r) { return OP == kProdWeight && r + kStep > q.r_end && (q.r_end - r) % kProductRows; };
     bool ok = true;
     if (warp == 0 || warp == 3) {
@@ -108,6 +109,9 @@ split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtenso
                     tc::load_box<false>(at_b, &map_b, bar, q.b0, r);
                 } else if (Kind::kTurnB) {
                     tc::load_box<false>(at_b, &map_b, bar, q.b0, r, int(q.expert));
+                } else if (Kind::kGated) {
+                    tc::load_box<false>(at_b, &map_b, bar, r, q.b0, int(q.expert * 2));
+                    tc::load_box<false>(at_b + kSplitColumns / 2 * kStepBytes, &map_b, bar, r, q.b0, int(q.expert * 2 + 1));
                 } else {
                     tc::load_box<false>(at_b, &map_b, bar, r, q.b0, int(q.expert));
                 }
@@ -177,25 +181,59 @@ split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtenso
     if (mine) {
         // packets of eight results, shared out over the cluster
         const int rows = min(kTileRows, q.a_end - q.a0);
-        for (int i = rank * kSplitThreads + threadIdx.x; i < rows * (kSplitColumns / 8); i += ranks * kSplitThreads) {
-            const int row = i / (kSplitColumns / 8), p = i % (kSplitColumns / 8);
+        constexpr int kOut = kResults / 8;                            // packets of a row
+        for (int i = rank * kSplitThreads + threadIdx.x; i < rows * kOut; i += ranks * kSplitThreads) {
+            const int row = i / kOut, p = i % kOut;
             const uint32_t col = q.b0 + p * 8;
             if (col >= width) continue;
             float z[8];
             int t[8];
+            auto sums = [&](int p) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { z[e] = 0.0f; t[e] = 0; }
-            for (uint32_t k = 0; k < ranks; ++k)
+                for (int e = 0; e < 8; ++e) { z[e] = 0.0f; t[e] = 0; }
+                for (uint32_t k = 0; k < ranks; ++k)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint4 w = peer_packet(ring_at + place(row, p * 2 + h), k);
-                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+                    for (int h = 0; h < 2; ++h) {
+                        const uint4 w = peer_packet(ring_at + place(row, p * 2 + h), k);
+                        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (Kind::kBytes) t[h * 4 + e] += int(u[e]);
-                        else z[h * 4 + e] += __uint_as_float(u[e]);
+                        for (int e = 0; e < 4; ++e) {
+                            if (Kind::kBytes) t[h * 4 + e] += int(u[e]);
+                            else z[h * 4 + e] += __uint_as_float(u[e]);
+                        }
                     }
+            };
+            if constexpr (Kind::kGated) {
+                float u[8], f[8], d[8];
+                sums(p + kOut);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { u[e] = z[e]; d[e] = 1.0f; }
+                sums(p);
+                if (g.bias) {
+                    load8<S>(g.bias, q.expert * 2, width, col, f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] += f[e];
+                    load8<S>(g.bias, q.expert * 2 + 1, width, col, f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) u[e] += f[e];
                 }
+                const size_t r = size_t(q.a0) + row;
+                if (g.slope) {
+                    act8<true>(g.act, z, d);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) d[e] *= u[e];
+                    typename S::elem* both = static_cast<typename S::elem*>(g.slope) + r * 2 * width + col;
+                    *reinterpret_cast<uint4*>(both) = S::pack(d);
+                    *reinterpret_cast<uint4*>(both + width) = S::pack(z);
+                } else {
+                    act8<false>(g.act, z, d);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[e] *= u[e];
+                *reinterpret_cast<uint4*>(static_cast<typename S::elem*>(g.out) + r * width + col) = S::pack(z);
+                continue;
+            }
+            sums(p);
             const size_t out_row = OP == kProdWeight ? size_t(q.expert) * g.outs + q.a0 + row : size_t(q.a0) + row, at = out_row * width + col;
             if (Kind::kBytes) {
                 const float scale = g.a_scale[q.a0 + row];
@@ -203,10 +241,20 @@ split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtenso
                 for (int e = 0; e < 8; ++e) z[e] = float(t[e]) * (scale * __ldg(g.b_scale + col + e));
             }
             float f[8];
-            if ((OP == kProdForward || OP == kProdBytes) && g.bias) {
+            if (Kind::kForward && g.bias) {
                 load8<S>(g.bias, q.expert, width, col, f);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) z[e] += f[e];
+            }
+            if constexpr (OP == kProdInputGated) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    load8<S>(g.prev, out_row * 2 + j, width, col, f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[e] *= z[e];
+                    *reinterpret_cast<uint4*>(static_cast<typename S::elem*>(g.out) + (out_row * 2 + j) * width + col) = S::pack(f);
+                }
+                continue;
             }
             if (OP == kProdInput && g.prev) {
                 load8<S>(g.prev, out_row, width, col, f);
@@ -225,8 +273,8 @@ split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtenso
         }
     }
     if (OP != kProdWeight && g.offsets) {
-        clear_rows<S, kSplitThreads>(g, 0, s.start[0], width, threadIdx.x);
-        clear_rows<S, kSplitThreads>(g, s.start[g.experts], int(g.rows), width, threadIdx.x);
+        clear_rows<S, kSplitThreads, OP>(g, 0, s.start[0], width, threadIdx.x);
+        clear_rows<S, kSplitThreads, OP>(g, s.start[g.experts], int(g.rows), width, threadIdx.x);
     }
     __syncthreads();
     tc::pair_sync();                                 // no CTA reads this one's sums any more

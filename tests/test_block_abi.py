@@ -115,3 +115,30 @@ def test_binding_refuses_host_tensors():
                  lambda: nfad.BlockNorm(pre_gain=torch.ones(16))):
         with pytest.raises(TypeError):
             call()
+
+
+def test_gated(lib):
+    x, w, b, off, y, d = (p(a << 20) for a in range(1, 7))
+    f = lib.nfad_expert_gated_linear
+    assert f(4, BF16, x, w, b, off, y, d, 8, 16, 24, 2, None) == 1
+    assert f(0, F32, x, w, b, off, y, d, 8, 16, 24, 2, None) == 2
+    assert f(0, BF16, x, w, b, None, y, d, 8, 16, 24, 2, None) == 3
+    assert f(0, BF16, x, None, b, off, y, d, 8, 16, 24, 2, None) == 3
+    assert f(0, BF16, x, w, b, off, y, y, 8, 16, 24, 2, None) == 4
+    assert f(0, BF16, x, w, b, off, y, x, 8, 16, 24, 2, None) == 4
+    assert f(0, BF16, x, w, b, off, p((5 << 20) + 1), d, 8, 16, 24, 2, None) == 6
+    assert f(0, BF16, x, w, b, off, y, d, 8, 16, 24, 1025, None) == 9
+    assert f(0, BF16, x, w, b, off, y, d, 8, 16, 1 << 30, 2, None) == 9             # twice as many outputs
+    assert f(0, BF16, x, w, b, off, y, d, 8, 16, (1 << 63) + 8, 2, None) == 9
+    assert f(0, BF16, x, w, b, off, y, d, 8, 16, 24, 0, None) == 11
+    assert f(0, BF16, None, None, None, None, None, None, 0, 16, 24, 2, None) == 0
+    g = lib.nfad_expert_gated_backward
+    assert g(F32, x, d, off, y, None, None, 0, 8, 24, 2, None) == 2
+    assert g(BF16, x, None, off, y, None, None, 0, 8, 24, 2, None) == 3
+    assert g(BF16, x, d, off, None, None, None, 0, 8, 24, 2, None) == 3
+    assert g(BF16, x, d, off, x, None, None, 0, 8, 24, 2, None) == 4                   # only the partials' place is as large
+    assert g(BF16, x, d, off, p((6 << 20) + 32), None, None, 0, 8, 24, 2, None) == 4
+    h = lib.nfad_expert_linear_backward_gated
+    assert h(BF16, x, w, off, None, y, 8, 16, 24, 2, None) == 3
+    assert h(BF16, x, w, off, d, x, 8, 16, 24, 2, None) == 4
+    assert h(BF16, x, w, off, d, y, 8, 1 << 30, 24, 2, None) == 9

@@ -396,6 +396,29 @@ NFAD_API int nfad_block_norm_backward(const nfad_block_norm* norm, int dtype, co
 NFAD_API size_t nfad_block_norm_backward_scratch_bytes(int dtype, size_t rows, size_t cols);
 
 /*
+ * Dropout whose mask is drawn from a counter and never stored: who needs it again draws it again.
+ *
+ * Element i of a call is dropped when 16 random bits are below T = rint(65536 p), else multiplied by s = 65536 / (65536 - T): p is held to a
+ * multiple of 2^-16, and the scale is the one of what is drawn (T = 65536: everything is dropped).  The bits come from Philox
+ * 4x32 with ten rounds: the call's key is `seed` (low word first), its counter {i / 8 (two words), offset + *step (two words)}; element i has
+ * the lower (even i) or upper half of result word (i % 8) / 2.  They depend on these numbers and i alone: not on the type, the device or the
+ * launch.  Calls whose masks shall be independent differ in seed or in offset + step.  step is a DEVICE pointer to one 64-bit
+ * number, read when the call runs, or NULL (0): a captured graph that counts it up draws another mask at every replay.
+ *
+ * nfad_dropout: y = residual + m x, m the mask times s; residual [n] or NULL.  A dropped element is 0 (or the residual) whatever x
+ *   holds.  Formed in fp32 and rounded once.  The backward pass is this call on the gradient with the same mask and no residual (whose
+ *   gradient is the gradient itself).  y may equal x or residual.
+ * nfad_bias_act_dropout_forward: z = x + bias (bias [cols] or NULL), y = m f(z) and dfdx = m f'(z): the derivative carries the mask, and
+ *   the backward pass is nfad_bias_act_backward (nfad_act_backward without a bias) on dfdx, with nothing drawn again.  f and f' are
+ *   those of nfad_bias_act_forward; for fp32 storage the scale is a second rounding.  y and dfdx may each equal x.
+ * p outside [0, 1] gives NFAD_E_VALUE; step must be aligned to 8 bytes and lie outside the results.
+ */
+typedef struct { double p; unsigned long long seed, offset; const unsigned long long* step; } nfad_dropout_mask;
+NFAD_API int nfad_dropout(int dtype, const nfad_dropout_mask* mask, const void* x, const void* residual, void* y, size_t n, nfad_stream_t stream);
+NFAD_API int nfad_bias_act_dropout_forward(int kind, int dtype, const nfad_dropout_mask* mask, const void* x, const void* bias, void* y, void* dfdx,
+                                           size_t rows, size_t cols, nfad_stream_t stream);
+
+/*
  * Matrix products grouped by expert, with the nested activation in their epilogue.
  *
  * x is [rows, in], its rows sorted by expert; w is [experts, out, in] (each expert's weight as a linear layer keeps it);

@@ -14,7 +14,8 @@ from .binding import (  # noqa: F401
     nfad_status_string, nfad_version,
 )
 from .block import (  # noqa: F401
-    NORMS, BlockNorm, nfad_block_norm_backward, nfad_block_norm_backward_scratch, nfad_block_norm_backward_scratch_bytes,
+    NORMS, BlockNorm, Dropout, nfad_bias_act_dropout_forward, nfad_dropout,
+    nfad_block_norm_backward, nfad_block_norm_backward_scratch, nfad_block_norm_backward_scratch_bytes,
     nfad_block_norm_forward,
     nfad_expert_act_backward, nfad_expert_act_backward_scratch, nfad_expert_act_backward_scratch_bytes, nfad_expert_linear,
     nfad_expert_linear_backward_input, nfad_expert_linear_backward_weight,

@@ -38,6 +38,7 @@ EXPORTS = (
     "nfad_expert_linear", "nfad_expert_act_backward", "nfad_expert_act_backward_scratch_bytes",
     "nfad_expert_linear_backward_input", "nfad_expert_linear_backward_weight",
     "nfad_expert_gated_linear", "nfad_expert_gated_backward", "nfad_expert_linear_backward_gated",
+    "nfad_dropout", "nfad_bias_act_dropout_forward",
     "nfad_i8_quantize_rows", "nfad_i8_linear", "nfad_i8_linear_dynamic", "nfad_i8_linear_dynamic_scratch_bytes",
     "nfad_wait_faults",
 )
@@ -60,6 +61,11 @@ class BlockNormDesc(ctypes.Structure):
 class BlockNormGrads(ctypes.Structure):
     """`nfad_block_norm_grads` of the C interface."""
     _fields_ = [(name, ctypes.c_void_p) for name in ("post_gain", "post_bias", "gate", "pre_gain", "pre_bias")]
+
+
+class DropoutMask(ctypes.Structure):
+    """`nfad_dropout_mask` of the C interface."""
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_ulonglong), ("offset", ctypes.c_ulonglong), ("step", ctypes.c_void_p)]
 
 
 NOALLOC_SCRATCH_BYTES = 8388608
@@ -110,7 +116,7 @@ def load() -> ctypes.CDLL:
         lib.nfad_bias_act_backward.restype = ci
         lib.nfad_bias_act_backward_scratch_bytes.argtypes = [ci, sz, sz]
         lib.nfad_bias_act_backward_scratch_bytes.restype = sz
-        norm = ctypes.POINTER(BlockNormDesc)
+        norm, mask = ctypes.POINTER(BlockNormDesc), ctypes.POINTER(DropoutMask)
         lib.nfad_block_norm_forward.argtypes = [norm, ci, vp, vp, vp, vp, vp, sz, sz, vp]
         lib.nfad_block_norm_forward.restype = ci
         lib.nfad_block_norm_backward.argtypes = [norm, ci, vp, vp, vp, vp, vp, vp, vp, ctypes.POINTER(BlockNormGrads), vp, sz, sz, sz, vp]
@@ -126,6 +132,8 @@ def load() -> ctypes.CDLL:
                 ("nfad_expert_gated_linear", [ci, ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, sz, vp], ci),
                 ("nfad_expert_gated_backward", [ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, sz, vp], ci),
                 ("nfad_expert_linear_backward_gated", [ci, vp, vp, vp, vp, vp, sz, sz, sz, sz, vp], ci),
+                ("nfad_dropout", [ci, mask, vp, vp, vp, sz, vp], ci),
+                ("nfad_bias_act_dropout_forward", [ci, ci, mask, vp, vp, vp, vp, sz, sz, vp], ci),
                 ("nfad_i8_quantize_rows", [ci, vp, vp, vp, sz, sz, vp], ci),
                 ("nfad_i8_linear", [ci, ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, vp], ci),
                 ("nfad_i8_linear_dynamic", [ci, ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, sz, vp], ci),

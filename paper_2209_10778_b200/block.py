@@ -9,7 +9,7 @@ from typing import Dict, Optional
 
 import torch
 
-from .binding import BlockNormDesc, BlockNormGrads, _check, _kind, _on_device, _stream, _tensor, _TORCH_TO_CODE, _raw_stream, load
+from .binding import BlockNormDesc, BlockNormGrads, DropoutMask, _check, _kind, _on_device, _stream, _tensor, _TORCH_TO_CODE, _raw_stream, load
 
 # small calls are a few microseconds on the device: what is looked up for each of them is looked up once
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
@@ -160,6 +160,55 @@ def nfad_block_norm_backward(norm: BlockNorm, grad_h: Optional[torch.Tensor], gr
     _call("nfad_block_norm_backward", grad_u, norm.ref, _TORCH_TO_CODE[kin[0]], _like(grad_h, "grad_h", kin), _like(grad_s, "grad_s", kin),
           _like(u, "u", kin), _like(s, "s", kin), _raw(stats, "stats", torch.float32, (rows, 4), grad_u.device), pg,
           _like(grad_r, "grad_r", kin), ctypes.byref(out), sp, sb, rows, cols)
+
+
+# ---------------------------------------------------------------- dropout
+
+class Dropout:
+    """A mask: ``nfad_dropout_mask`` with the tensor it points to.
+
+    p in [0, 1] (held to a multiple of 2^-16); seed and offset: 64-bit integers; step: None, or an int64 CUDA tensor of one value that is
+    added to offset when a call runs.  The same numbers give the same mask; layers and steps differ in offset (or step).
+    """
+
+    def __init__(self, p: float, seed: int, offset: int = 0, step: Optional[torch.Tensor] = None):
+        self.p, self.seed, self.offset, self.step = float(p), int(seed), int(offset), step
+        if not 0.0 <= self.p <= 1.0:
+            raise ValueError("p must be in [0, 1]")
+        if not (0 <= self.seed < 2 ** 64 and 0 <= self.offset < 2 ** 64):
+            raise ValueError("seed and offset must be 64-bit numbers")
+        if step is not None:
+            if not isinstance(step, torch.Tensor) or step.dtype != torch.int64 or not step.is_cuda:
+                raise TypeError("step must be an int64 CUDA tensor")
+            if step.numel() != 1:
+                raise ValueError("step must hold one value")
+        self.desc = DropoutMask(self.p, self.seed, self.offset, None if step is None else step.data_ptr())
+        self.ref = ctypes.byref(self.desc)
+
+
+def _mask(drop: Dropout, x: torch.Tensor):
+    if not isinstance(drop, Dropout):
+        raise TypeError("drop must be a Dropout")
+    if drop.step is not None and drop.step.get_device() != x.get_device():
+        raise ValueError("the mask's step must be on the tensors' device")
+    return drop.ref
+
+
+def nfad_dropout(drop: Dropout, x: torch.Tensor, residual: Optional[torch.Tensor], y: torch.Tensor) -> None:
+    """y = residual + m x (m x without a residual), m the mask times its scale: tensors of one type and shape.  On the gradient, with the same
+    mask and no residual, it is its own backward pass."""
+    px = _tensor(x, "x")
+    _call("nfad_dropout", x, _TORCH_TO_CODE[x.dtype], _mask(drop, x), px, None if residual is None else _tensor(residual, "residual", x),
+          _tensor(y, "y", x), x.numel())
+
+
+def nfad_bias_act_dropout_forward(kind, drop: Dropout, x: torch.Tensor, bias: Optional[torch.Tensor], y: torch.Tensor, dfdx: torch.Tensor) -> None:
+    """y = m f(x + bias), dfdx = m f'(x + bias): x, y, dfdx [..., cols], bias [cols] or None.  The backward pass is that of
+    nfad_bias_act_forward (without a bias nfad_act_forward): dfdx carries the mask."""
+    px, py, pd = _tensor(x, "x"), _tensor(y, "y", x), _tensor(dfdx, "dfdx", x)
+    cols = x.shape[-1] if x.dim() else 1
+    pb = _raw(bias, "bias", x.dtype, (cols,), x.device)
+    _call("nfad_bias_act_dropout_forward", x, _kind(kind), _TORCH_TO_CODE[x.dtype], _mask(drop, x), px, pb, py, pd, x.numel() // cols if cols else 0, cols)
 
 
 # ---------------------------------------------------------------- products grouped by expert

@@ -30,6 +30,8 @@ UNITS = [
     ("nfad_kernels_16.cu", ["-fmad=true"]),
     ("nfad_kernels_seq.cu", ["-fmad=true"]),
     ("nfad_kernels_bias.cu", ["-fmad=false"]),
+    ("nfad_kernels_dropout_16.cu", ["-fmad=true"]),
+    ("nfad_kernels_dropout_f32.cu", ["-fmad=false"]),
     ("nfad_kernels_norm.cu", ["-fmad=true"]),
     ("nfad_kernels_prod_forward.cu", ["-fmad=true"]),
     ("nfad_kernels_prod_input.cu", ["-fmad=true"]),

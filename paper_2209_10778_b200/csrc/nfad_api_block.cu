@@ -6,6 +6,7 @@
 #include <initializer_list>
 
 #include "../../include/nfad.h"
+#include "nfad_dropout_args.h"
 #include "nfad_internal.h"
 #include "nfad_norm_args.h"
 #include "nfad_product_args.h"
@@ -77,6 +78,21 @@ int check_gated(int kind, int dtype, size_t rows, size_t in, size_t out, size_t 
 {
     if (out >= (size_t(1) << 31)) return NFAD_E_TOO_LARGE;
     return check_product(kind, dtype, rows, in, 2 * out, experts);
+}
+
+int check_mask(const nfad_dropout_mask* mask, int dtype, nfad::DropoutArgs* a)
+{
+    if (!mask) return NFAD_E_NULL;
+    if (dtype < 0 || dtype > 2) return NFAD_E_DTYPE;
+    if (!(mask->p >= 0.0 && mask->p <= 1.0)) return NFAD_E_VALUE;
+    const uint32_t dropped = uint32_t(rint(mask->p * 65536.0));
+    a->dropped = dropped < 65536 ? dropped << 16 : 0xffffffffu;
+    a->live = dropped < 65536 ? 0xffffffffu : 0;
+    a->scale = dropped < 65536 ? float(65536.0 / double(65536 - dropped)) : 0.0f;
+    a->seed = mask->seed;
+    a->offset = mask->offset;
+    a->step = mask->step;
+    return NFAD_OK;
 }
 
 int check_norm(const nfad_block_norm* norm, int dtype, size_t rows, size_t cols, size_t* n)
@@ -175,6 +191,42 @@ int nfad_block_norm_backward(const nfad_block_norm* norm, int dtype, const void*
         if (e != cudaSuccess) return finish(e);
     }
     return finish(nfad::launch_norm_backward(dtype, a, scratch, static_cast<cudaStream_t>(stream)));
+}
+
+int nfad_dropout(int dtype, const nfad_dropout_mask* mask, const void* x, const void* residual, void* y, size_t n, nfad_stream_t stream)
+{
+    nfad::DropoutArgs a = {};
+    int rc = check_mask(mask, dtype, &a);
+    if (rc) return rc;
+    if (n > ~size_t(0) / 64) return NFAD_E_TOO_LARGE;
+    if (n == 0) return NFAD_OK;
+    if (!x || !y) return NFAD_E_NULL;
+    const size_t es = elem_size(dtype);
+    const Span sx{x, n * es, es}, sr{residual, n * es, es}, ss{a.step, 8, 8}, oy{y, n * es, es};
+    if ((rc = aligned({sx, sr, ss, oy}))) return rc;
+    if ((rc = aliasing({oy}, {sx, sr}, {ss}))) return rc;
+    a.x = x; a.other = residual; a.y = y; a.n = n;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return finish(dtype == NFAD_F32 ? nfad::launch_dropout_f32(nfad::kNoAct, a, st) : nfad::launch_dropout_16(nfad::kNoAct, dtype, a, st));
+}
+
+int nfad_bias_act_dropout_forward(int kind, int dtype, const nfad_dropout_mask* mask, const void* x, const void* bias, void* y, void* dfdx, size_t rows,
+                                  size_t cols, nfad_stream_t stream)
+{
+    if (kind < 0 || kind > 3) return NFAD_E_KIND;
+    nfad::DropoutArgs a = {};
+    size_t n = 0;
+    int rc = check_mask(mask, dtype, &a);
+    if (rc || (rc = element_count(rows, cols, &n))) return rc;
+    if (n == 0) return NFAD_OK;
+    if (!x || !y || !dfdx) return NFAD_E_NULL;
+    const size_t es = elem_size(dtype);
+    const Span sx{x, n * es, es}, sb{bias, cols * es, es}, ss{a.step, 8, 8}, oy{y, n * es, es}, od{dfdx, n * es, es};
+    if ((rc = aligned({sx, sb, ss, oy, od}))) return rc;
+    if ((rc = aliasing({oy, od}, {sx}, {sb, ss}))) return rc;
+    a.x = x; a.other = bias; a.y = y; a.slope = dfdx; a.n = n; a.cols = uint32_t(cols);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return finish(dtype == NFAD_F32 ? nfad::launch_dropout_f32(kind, a, st) : nfad::launch_dropout_16(kind, dtype, a, st));
 }
 
 int nfad_expert_linear(int kind, int dtype, const void* x, const void* w, const void* bias, const int* offsets, void* y, void* dfdx, size_t rows,

@@ -66,6 +66,11 @@ cudaError_t launch_bias_backward(int dtype, const void* g, const void* d, void* 
                                  size_t rows, size_t cols, cudaStream_t st);
 cudaError_t bias_backward_scratch(int dtype, size_t rows, size_t cols, size_t* bytes);   // on the current device
 
+// Dropout (nfad_dropout.cuh); kind -1: no activation.
+struct DropoutArgs;
+cudaError_t launch_dropout_f32(int kind, const DropoutArgs& a, cudaStream_t st);
+cudaError_t launch_dropout_16(int kind, int dtype, const DropoutArgs& a, cudaStream_t st);
+
 // The norms around a block (nfad_norm.cuh).
 struct NormForwardArgs;
 struct NormBackwardArgs;

@@ -142,3 +142,34 @@ def test_gated(lib):
     assert h(BF16, x, w, off, None, y, 8, 16, 24, 2, None) == 3
     assert h(BF16, x, w, off, d, x, 8, 16, 24, 2, None) == 4
     assert h(BF16, x, w, off, d, y, 8, 1 << 30, 24, 2, None) == 9
+
+
+def test_dropout(lib):
+    x, r, y, d, b = (p(a << 20) for a in range(1, 6))
+
+    def mask(prob=0.5, step=None):
+        return ctypes.byref(binding.DropoutMask(prob, 1, 2, step))
+
+    f = lib.nfad_dropout
+    assert f(BF16, None, x, r, y, 64, None) == 3
+    assert f(3, mask(), x, r, y, 64, None) == 2
+    for prob in (-0.1, 1.1, float("nan"), float("inf")):
+        assert f(BF16, mask(prob), x, r, y, 64, None) == 11
+    assert f(BF16, mask(), None, r, y, 64, None) == 3
+    assert f(BF16, mask(), x, r, None, 64, None) == 3
+    assert f(BF16, mask(), x, r, p((1 << 20) + 16), 64, None) == 4
+    assert f(BF16, mask(step=(3 << 20) + 8), x, r, y, 64, None) == 4                      # the step among the results
+    assert f(BF16, mask(step=(6 << 20) + 4), x, r, y, 64, None) == 6
+    assert f(BF16, mask(), x, p((2 << 20) + 1), y, 64, None) == 6
+    assert f(BF16, mask(), x, r, y, 1 << 62, None) == 9
+    assert f(BF16, mask(), None, None, None, 0, None) == 0
+    g = lib.nfad_bias_act_dropout_forward
+    assert g(-1, BF16, mask(), x, b, y, d, 4, 16, None) == 1
+    assert g(0, BF16, mask(2.0), x, b, y, d, 4, 16, None) == 11
+    assert g(0, BF16, mask(), x, b, y, None, 4, 16, None) == 3
+    assert g(0, BF16, mask(), x, b, y, y, 4, 16, None) == 4
+    assert g(0, BF16, mask(), x, b, b, d, 4, 16, None) == 4
+    assert g(0, BF16, mask(), x, b, y, d, 4, 1 << 31, None) == 9
+    assert g(0, BF16, mask(), None, None, None, None, 0, 16, None) == 0
+    with pytest.raises(TypeError):
+        nfad.nfad_dropout(nfad.Dropout(0.5, 1), torch.zeros(8), None, torch.zeros(8))

@@ -500,6 +500,38 @@ NFAD_API int nfad_i8_linear_dynamic(int kind, int dtype, const void* x, const si
 NFAD_API size_t nfad_i8_linear_dynamic_scratch_bytes(size_t rows, size_t in);
 
 /*
+ * Linear layer in 8-bit floating point (four exponent bits, three of the significand, largest 448; torch's float8_e4m3fn), with a scale for
+ * each block of NFAD_F8_BLOCK = 128: of 128 values along a row of x, of 128 x 128 of the weight.  With B = ceil(in / 128):
+ *
+ * nfad_f8_quantize_rows: x [rows, cols] of any dtype, q [rows, cols] bytes, scale fp32 [ceil(cols / 128), rows] (a block's scales of
+ *   neighbouring rows are neighbours, as the products read them): scale = amax / 448, q = 448 x / amax to nearest even, amax the block's largest
+ *   magnitude.  For 16-bit x the exact quotient is rounded, once; for fp32 the quotient as fp32 arithmetic has it.  Blocks with amax below
+ *   2^-110 get scale 0 and q 0; blocks that hold an infinity or a NaN get scale NaN and q 0.  The last block of a row may be shorter.
+ * nfad_f8_quantize_blocks: the same of `matrices` matrices [rows, cols] by blocks of 128 x 128; scale [matrices, ceil(rows / 128), ceil(cols / 128)].
+ * nfad_f8_linear: z[r, o] = sum_b x_scale[b, r] w_scale[o / 128, b] sum_{k in block b} xq[r, k] wq[o, k] + bias[o], y = f(z): products exact, sums
+ *   fp32, rounded once to dtype (NFAD_BF16 or NFAD_F16).  wq [out, in], w_scale [ceil(out / 128), B]; bias [out] of dtype, or NULL; kind
+ *   NFAD_NO_ACT: no activation; value only.  The two byte values that stand for NaN give NaN.
+ * nfad_f8_gated_linear: the gated layer y = f(a) u with a and u such sums of two weights: wq [2, out, in], w_scale [2, ceil(out / 128), B],
+ *   bias [2, out] or NULL; the gate's first.
+ * nfad_f8_linear_dynamic, nfad_f8_gated_linear_dynamic: the same from x itself [rows, in] of dtype, quantised on the way.  scratch: device
+ *   memory, 16-byte aligned, of nfad_f8_linear_dynamic_scratch_bytes() bytes, contents irrelevant before and after.
+ * Rows of xq and wq that do not start on 16-byte boundaries (in not a multiple of 16) go through a slower gather.
+ */
+#define NFAD_F8_BLOCK 128
+NFAD_API int nfad_f8_quantize_rows(int dtype, const void* x, unsigned char* q, float* scale, size_t rows, size_t cols, nfad_stream_t stream);
+NFAD_API int nfad_f8_quantize_blocks(int dtype, const void* x, unsigned char* q, float* scale, size_t matrices, size_t rows, size_t cols,
+                                     nfad_stream_t stream);
+NFAD_API int nfad_f8_linear(int kind, int dtype, const unsigned char* xq, const float* x_scale, const unsigned char* wq, const float* w_scale,
+                            const void* bias, void* y, size_t rows, size_t in, size_t out, nfad_stream_t stream);
+NFAD_API int nfad_f8_gated_linear(int kind, int dtype, const unsigned char* xq, const float* x_scale, const unsigned char* wq, const float* w_scale,
+                                  const void* bias, void* y, size_t rows, size_t in, size_t out, nfad_stream_t stream);
+NFAD_API int nfad_f8_linear_dynamic(int kind, int dtype, const void* x, const unsigned char* wq, const float* w_scale, const void* bias, void* y,
+                                    void* scratch, size_t scratch_bytes, size_t rows, size_t in, size_t out, nfad_stream_t stream);
+NFAD_API int nfad_f8_gated_linear_dynamic(int kind, int dtype, const void* x, const unsigned char* wq, const float* w_scale, const void* bias, void* y,
+                                          void* scratch, size_t scratch_bytes, size_t rows, size_t in, size_t out, nfad_stream_t stream);
+NFAD_API size_t nfad_f8_linear_dynamic_scratch_bytes(size_t rows, size_t in);
+
+/*
  * How many CTAs of the kernels above have given up waiting for their own copies or products since the library was loaded
  * on the current device (0 in a healthy process; a launch that gave up leaves its results undefined instead of hanging the
  * device), or a negative nfad_status.  Synchronises the device: a diagnostic, not for a hot path.

@@ -20,6 +20,8 @@ from .block import (  # noqa: F401
     nfad_expert_act_backward, nfad_expert_act_backward_scratch, nfad_expert_act_backward_scratch_bytes, nfad_expert_linear,
     nfad_expert_linear_backward_input, nfad_expert_linear_backward_weight,
     nfad_expert_gated_backward, nfad_expert_gated_linear, nfad_expert_linear_backward_gated,
+    nfad_f8_gated_linear, nfad_f8_gated_linear_dynamic, nfad_f8_linear, nfad_f8_linear_dynamic, nfad_f8_linear_dynamic_scratch,
+    nfad_f8_linear_dynamic_scratch_bytes, nfad_f8_quantize_blocks, nfad_f8_quantize_rows,
     nfad_i8_linear, nfad_i8_linear_dynamic, nfad_i8_linear_dynamic_scratch, nfad_i8_linear_dynamic_scratch_bytes,
     nfad_i8_quantize_rows, nfad_wait_faults,
 )

@@ -40,6 +40,8 @@ EXPORTS = (
     "nfad_expert_gated_linear", "nfad_expert_gated_backward", "nfad_expert_linear_backward_gated",
     "nfad_dropout", "nfad_bias_act_dropout_forward",
     "nfad_i8_quantize_rows", "nfad_i8_linear", "nfad_i8_linear_dynamic", "nfad_i8_linear_dynamic_scratch_bytes",
+    "nfad_f8_quantize_rows", "nfad_f8_quantize_blocks", "nfad_f8_linear", "nfad_f8_gated_linear", "nfad_f8_linear_dynamic",
+    "nfad_f8_gated_linear_dynamic", "nfad_f8_linear_dynamic_scratch_bytes",
     "nfad_wait_faults",
 )
 OPCODES = {"add": 0, "mul": 1, "scale": 2, "add_const": 3, "exp": 4, "log1p": 5, "tanh": 6, "erf": 7, "softplus": 8,
@@ -137,6 +139,13 @@ def load() -> ctypes.CDLL:
                 ("nfad_i8_quantize_rows", [ci, vp, vp, vp, sz, sz, vp], ci),
                 ("nfad_i8_linear", [ci, ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, vp], ci),
                 ("nfad_i8_linear_dynamic", [ci, ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, sz, vp], ci),
+                ("nfad_f8_quantize_rows", [ci, vp, vp, vp, sz, sz, vp], ci),
+                ("nfad_f8_quantize_blocks", [ci, vp, vp, vp, sz, sz, sz, vp], ci),
+                ("nfad_f8_linear", [ci, ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, vp], ci),
+                ("nfad_f8_gated_linear", [ci, ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, vp], ci),
+                ("nfad_f8_linear_dynamic", [ci, ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, sz, vp], ci),
+                ("nfad_f8_gated_linear_dynamic", [ci, ci, vp, vp, vp, vp, vp, vp, sz, sz, sz, sz, vp], ci),
+                ("nfad_f8_linear_dynamic_scratch_bytes", [sz, sz], sz),
                 ("nfad_i8_linear_dynamic_scratch_bytes", [sz, sz], sz), ("nfad_wait_faults", [], ci)):
             getattr(lib, name).argtypes, getattr(lib, name).restype = args, res
         lib.nfad_seq_set_executor.argtypes = [ci]

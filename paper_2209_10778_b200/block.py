@@ -402,6 +402,105 @@ def nfad_i8_linear_dynamic(kind, x: torch.Tensor, wq: torch.Tensor, w_scale: tor
     _call("nfad_i8_linear_dynamic", x, _act(kind), _TORCH_TO_CODE[x.dtype], px, pw, pws, pb, py, sp, sb, rows, n_in, n_out)
 
 
+# ---------------------------------------------------------------- the linear layer in 8-bit floating point
+
+F8 = torch.float8_e4m3fn
+F8_BLOCK = 128
+
+
+def f8_blocks(n: int) -> int:
+    """Blocks of 128 along a dimension of n."""
+    return -(-n // F8_BLOCK)
+
+
+def nfad_f8_quantize_rows(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor) -> None:
+    """q (float8_e4m3fn [rows, cols]) and scale (fp32 [blocks of cols, rows]) of x [rows, cols]: blocks of 128 along a row."""
+    px = _matrix(x, "x")
+    rows, cols = x.shape
+    pq, ps = _raw(q, "q", F8, (rows, cols), x.device), _raw(scale, "scale", torch.float32, (f8_blocks(cols), rows), x.device)
+    _call("nfad_f8_quantize_rows", x, _TORCH_TO_CODE[x.dtype], px, pq, ps, rows, cols)
+
+
+def nfad_f8_quantize_blocks(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor) -> None:
+    """q and scale (fp32 [..., blocks of rows, blocks of cols]) of the matrices x [..., rows, cols]: blocks of 128 x 128."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError("x must be a CUDA tensor")
+    if x.dim() < 2:
+        raise ValueError("x must be a matrix or a stack of them")
+    px = _matrix(x, "x", x.dim())
+    *lead, rows, cols = x.shape
+    pq = _raw(q, "q", F8, x.shape, x.device)
+    ps = _raw(scale, "scale", torch.float32, (*lead, f8_blocks(rows), f8_blocks(cols)), x.device)
+    matrices = 1
+    for n in lead:
+        matrices *= n
+    _call("nfad_f8_quantize_blocks", x, _TORCH_TO_CODE[x.dtype], px, pq, ps, matrices, rows, cols)
+
+
+def _f8_weight(wq: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor], y: torch.Tensor, n_in: int, lead: tuple):
+    if not isinstance(wq, torch.Tensor) or wq.dim() != 2 + len(lead) or wq.shape[:-2] != lead or wq.shape[-1] != n_in:
+        raise ValueError(f"wq must be [{'2, ' if lead else ''}out, in]")
+    n_out = wq.shape[-2]
+    return (n_out, _raw(wq, "wq", F8, wq.shape, y.device), _raw(w_scale, "w_scale", torch.float32, (*lead, f8_blocks(n_out), f8_blocks(n_in)), y.device),
+            _raw(bias, "bias", y.dtype, (*lead, n_out), y.device))
+
+
+def _f8_linear(name, lead, kind, xq, x_scale, wq, w_scale, bias, y) -> None:
+    py = _matrix(y, "y")
+    if not isinstance(xq, torch.Tensor) or xq.dim() != 2:
+        raise ValueError("xq must be [rows, in]")
+    rows, n_in = xq.shape
+    n_out, pw, pws, pb = _f8_weight(wq, w_scale, bias, y, n_in, lead)
+    if y.shape != (rows, n_out):
+        raise ValueError("y must be [rows, out]")
+    px, pxs = _raw(xq, "xq", F8, (rows, n_in), y.device), _raw(x_scale, "x_scale", torch.float32, (f8_blocks(n_in), rows), y.device)
+    _call(name, y, _act(kind), _TORCH_TO_CODE[y.dtype], px, pxs, pw, pws, pb, py, rows, n_in, n_out)
+
+
+def nfad_f8_linear(kind, xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor],
+                   y: torch.Tensor) -> None:
+    """y = f(xq wq^T, each block of 128 along the reduction times its scales, + bias): xq [rows, in] and wq [out, in] float8_e4m3fn, scales as
+    the quantisers leave them, bias and y 16-bit."""
+    _f8_linear("nfad_f8_linear", (), kind, xq, x_scale, wq, w_scale, bias, y)
+
+
+def nfad_f8_gated_linear(kind, xq: torch.Tensor, x_scale: torch.Tensor, wq: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor],
+                         y: torch.Tensor) -> None:
+    """The gated layer y = f(a) u of such products: wq [2, out, in], w_scale [2, ...], bias [2, out]; the gate's first."""
+    _f8_linear("nfad_f8_gated_linear", (2,), kind, xq, x_scale, wq, w_scale, bias, y)
+
+
+def nfad_f8_linear_dynamic_scratch_bytes(rows: int, n_in: int) -> int:
+    return int(load().nfad_f8_linear_dynamic_scratch_bytes(rows, n_in))
+
+
+def nfad_f8_linear_dynamic_scratch(x: torch.Tensor) -> torch.Tensor:
+    """A scratch tensor for nfad_f8_linear_dynamic and nfad_f8_gated_linear_dynamic on inputs like x."""
+    return torch.empty(max(nfad_f8_linear_dynamic_scratch_bytes(*x.shape), 16), dtype=torch.uint8, device=x.device)
+
+
+def _f8_dynamic(name, lead, kind, x, wq, w_scale, bias, y, scratch) -> None:
+    px, py = _matrix(x, "x"), _matrix(y, "y")
+    rows, n_in = x.shape
+    n_out, pw, pws, pb = _f8_weight(wq, w_scale, bias, y, n_in, lead)
+    if y.shape != (rows, n_out) or y.dtype != x.dtype or y.device != x.device:
+        raise ValueError("y must be [rows, out] of x's dtype and device")
+    sp, sb = _scratch(scratch, x.device)
+    _call(name, x, _act(kind), _TORCH_TO_CODE[x.dtype], px, pw, pws, pb, py, sp, sb, rows, n_in, n_out)
+
+
+def nfad_f8_linear_dynamic(kind, x: torch.Tensor, wq: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor], y: torch.Tensor,
+                           scratch: torch.Tensor) -> None:
+    """nfad_f8_linear from the 16-bit x [rows, in], quantised on the way."""
+    _f8_dynamic("nfad_f8_linear_dynamic", (), kind, x, wq, w_scale, bias, y, scratch)
+
+
+def nfad_f8_gated_linear_dynamic(kind, x: torch.Tensor, wq: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor], y: torch.Tensor,
+                                 scratch: torch.Tensor) -> None:
+    """nfad_f8_gated_linear from the 16-bit x [rows, in], quantised on the way."""
+    _f8_dynamic("nfad_f8_gated_linear_dynamic", (2,), kind, x, wq, w_scale, bias, y, scratch)
+
+
 def nfad_wait_faults() -> int:
     """How many CTAs of the products have given up waiting since the library was loaded (0 in a healthy process).  Synchronises."""
     n = int(load().nfad_wait_faults())

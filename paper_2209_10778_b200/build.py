@@ -39,6 +39,9 @@ UNITS = [
     ("nfad_kernels_prod_bytes.cu", ["-fmad=true"]),
     ("nfad_kernels_prod_gated.cu", ["-fmad=true"]),
     ("nfad_kernels_prod_input_gated.cu", ["-fmad=true"]),
+    ("nfad_kernels_prod_scaled.cu", ["-fmad=true"]),
+    ("nfad_kernels_prod_scaled_gated.cu", ["-fmad=true"]),
+    ("nfad_kernels_blocks.cu", ["-fmad=true"]),
     ("nfad_kernels_expert.cu", ["-fmad=true"]),
     ("nfad_api.cu", ["-fmad=false"]),
     ("nfad_api_block.cu", ["-fmad=false"]),

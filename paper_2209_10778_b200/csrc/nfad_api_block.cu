@@ -107,6 +107,61 @@ int check_norm(const nfad_block_norm* norm, int dtype, size_t rows, size_t cols,
     return NFAD_OK;
 }
 
+// ---- 8-bit floating point; weights: 1, or 2 for a gated layer
+
+size_t f8_blocks(size_t n) { return (n + NFAD_F8_BLOCK - 1) / NFAD_F8_BLOCK; }
+
+int f8_launch(int weights, int kind, int dtype, const void* xq, const float* x_scale, const void* wq, const float* w_scale, const void* bias, void* y,
+              size_t rows, size_t in, size_t out, int b_ready, cudaStream_t st)
+{
+    nfad::ProdArgs g = {};
+    g.a = xq; g.b = wq; g.bias = bias; g.a_scale = x_scale; g.b_scale = w_scale; g.out = y;
+    g.rows = rows; g.in = uint32_t(in); g.outs = uint32_t(out); g.experts = 1; g.act = kind; g.b_ready = b_ready;
+    return finish(weights == 2 ? nfad::launch_product_scaled_gated(dtype, g, st) : nfad::launch_product_scaled(dtype, g, st));
+}
+
+int check_f8(int weights, int kind, int dtype, size_t rows, size_t in, size_t out)
+{
+    return weights == 2 ? check_gated(kind, dtype, rows, in, out, 1) : check_product(kind, dtype, rows, in, out, 1);
+}
+
+int f8_product(int weights, int kind, int dtype, const unsigned char* xq, const float* x_scale, const unsigned char* wq, const float* w_scale,
+               const void* bias, void* y, size_t rows, size_t in, size_t out, nfad_stream_t stream)
+{
+    int rc = check_f8(weights, kind, dtype, rows, in, out);
+    if (rc) return rc;
+    if (rows == 0 || out == 0) return NFAD_OK;
+    if ((in && (!xq || !wq || !x_scale || !w_scale)) || !y) return NFAD_E_NULL;
+    const Span sx{xq, rows * in, 1}, sxs{x_scale, f8_blocks(in) * rows * 4, 4}, sw{wq, weights * out * in, 1},
+        sws{w_scale, weights * f8_blocks(out) * f8_blocks(in) * 4, 4}, sb{bias, weights * out * 2, 2};
+    const Span oy{y, rows * out * 2, 2};
+    if ((rc = aligned({sx, sxs, sw, sws, sb, oy}))) return rc;
+    if ((rc = aliasing({oy}, {}, {sx, sxs, sw, sws, sb}))) return rc;
+    return f8_launch(weights, kind, dtype, xq, x_scale, wq, w_scale, bias, y, rows, in, out, 0, static_cast<cudaStream_t>(stream));
+}
+
+int f8_dynamic(int weights, int kind, int dtype, const void* x, const unsigned char* wq, const float* w_scale, const void* bias, void* y, void* scratch,
+               size_t scratch_bytes, size_t rows, size_t in, size_t out, nfad_stream_t stream)
+{
+    int rc = check_f8(weights, kind, dtype, rows, in, out);
+    if (rc) return rc;
+    if (rows == 0 || out == 0) return NFAD_OK;
+    const size_t need = nfad_f8_linear_dynamic_scratch_bytes(rows, in);
+    if ((in && (!x || !wq || !w_scale)) || !y || (need && !scratch)) return NFAD_E_NULL;
+    const Span sx{x, rows * in * 2, 2}, sw{wq, weights * out * in, 1}, sws{w_scale, weights * f8_blocks(out) * f8_blocks(in) * 4, 4},
+        sb{bias, weights * out * 2, 2};
+    const Span oy{y, rows * out * 2, 2}, sc{need ? scratch : nullptr, need, 16};
+    if ((rc = aligned({sx, sw, sws, sb, oy, sc}))) return rc;
+    if (scratch_bytes < need) return NFAD_E_SCRATCH;
+    if ((rc = aliasing({oy, sc}, {}, {sx, sw, sws, sb}))) return rc;
+    unsigned char* q = static_cast<unsigned char*>(scratch);
+    float* scale = reinterpret_cast<float*>(q + ((rows * in + 15) & ~size_t(15)));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (in && (rc = finish(nfad::launch_f8_groups(dtype, x, q, scale, rows, uint32_t(in), st)))) return rc;
+    // the quantiser lets its successor start only after its own wait
+    return f8_launch(weights, kind, dtype, q, scale, wq, w_scale, bias, y, rows, in, out, 1, st);
+}
+
 }  // namespace
 
 extern "C" {
@@ -432,11 +487,74 @@ int nfad_i8_linear_dynamic(int kind, int dtype, const void* x, const signed char
     return finish(nfad::launch_product_bytes(dtype, g, st));
 }
 
+int nfad_f8_quantize_rows(int dtype, const void* x, unsigned char* q, float* scale, size_t rows, size_t cols, nfad_stream_t stream)
+{
+    if (dtype < 0 || dtype > 2) return NFAD_E_DTYPE;
+    size_t n = 0;
+    int rc = element_count(rows, cols, &n);
+    if (rc) return rc;
+    if (n == 0) return NFAD_OK;
+    if (cols > (size_t(1) << 31) - 256) return NFAD_E_TOO_LARGE;
+    if (!x || !q || !scale) return NFAD_E_NULL;
+    const size_t es = elem_size(dtype);
+    const Span sx{x, n * es, es}, oq{q, n, 1}, os{scale, f8_blocks(cols) * rows * 4, 4};
+    if ((rc = aligned({sx, oq, os}))) return rc;
+    if ((rc = aliasing({oq, os}, {}, {sx}))) return rc;
+    return finish(nfad::launch_f8_groups(dtype, x, q, scale, rows, uint32_t(cols), static_cast<cudaStream_t>(stream)));
+}
+
+int nfad_f8_quantize_blocks(int dtype, const void* x, unsigned char* q, float* scale, size_t matrices, size_t rows, size_t cols, nfad_stream_t stream)
+{
+    if (dtype < 0 || dtype > 2) return NFAD_E_DTYPE;
+    size_t n = 0, all = 0;
+    int rc = element_count(rows, cols, &n);
+    if (rc) return rc;
+    if (n == 0 || matrices == 0) return NFAD_OK;
+    if (rows > (size_t(1) << 31) - 256 || cols > (size_t(1) << 31) - 256 || matrices > (~size_t(0) / 64) / n) return NFAD_E_TOO_LARGE;
+    all = matrices * n;
+    if (!x || !q || !scale) return NFAD_E_NULL;
+    const size_t es = elem_size(dtype);
+    const Span sx{x, all * es, es}, oq{q, all, 1}, os{scale, matrices * f8_blocks(rows) * f8_blocks(cols) * 4, 4};
+    if ((rc = aligned({sx, oq, os}))) return rc;
+    if ((rc = aliasing({oq, os}, {}, {sx}))) return rc;
+    return finish(nfad::launch_f8_blocks(dtype, x, q, scale, matrices, uint32_t(rows), uint32_t(cols), static_cast<cudaStream_t>(stream)));
+}
+
+int nfad_f8_linear(int kind, int dtype, const unsigned char* xq, const float* x_scale, const unsigned char* wq, const float* w_scale, const void* bias,
+                   void* y, size_t rows, size_t in, size_t out, nfad_stream_t stream)
+{
+    return f8_product(1, kind, dtype, xq, x_scale, wq, w_scale, bias, y, rows, in, out, stream);
+}
+
+int nfad_f8_gated_linear(int kind, int dtype, const unsigned char* xq, const float* x_scale, const unsigned char* wq, const float* w_scale, const void* bias,
+                         void* y, size_t rows, size_t in, size_t out, nfad_stream_t stream)
+{
+    return f8_product(2, kind, dtype, xq, x_scale, wq, w_scale, bias, y, rows, in, out, stream);
+}
+
+size_t nfad_f8_linear_dynamic_scratch_bytes(size_t rows, size_t in)
+{
+    if (rows >= (size_t(1) << 31) || in >= (size_t(1) << 31)) return 0;
+    return ((rows * in + 15) & ~size_t(15)) + f8_blocks(in) * rows * sizeof(float);   // the bytes, then the scales
+}
+
+int nfad_f8_linear_dynamic(int kind, int dtype, const void* x, const unsigned char* wq, const float* w_scale, const void* bias, void* y, void* scratch,
+                           size_t scratch_bytes, size_t rows, size_t in, size_t out, nfad_stream_t stream)
+{
+    return f8_dynamic(1, kind, dtype, x, wq, w_scale, bias, y, scratch, scratch_bytes, rows, in, out, stream);
+}
+
+int nfad_f8_gated_linear_dynamic(int kind, int dtype, const void* x, const unsigned char* wq, const float* w_scale, const void* bias, void* y, void* scratch,
+                                 size_t scratch_bytes, size_t rows, size_t in, size_t out, nfad_stream_t stream)
+{
+    return f8_dynamic(2, kind, dtype, x, wq, w_scale, bias, y, scratch, scratch_bytes, rows, in, out, stream);
+}
+
 int nfad_wait_faults(void)
 {
     unsigned total = 0;
     for (auto count : {nfad::wait_faults_norm, nfad::product_faults_forward, nfad::product_faults_input, nfad::product_faults_weight, nfad::product_faults_bytes,
-                       nfad::product_faults_gated, nfad::product_faults_input_gated}) {
+                       nfad::product_faults_gated, nfad::product_faults_input_gated, nfad::product_faults_scaled, nfad::product_faults_scaled_gated}) {
         unsigned n = 0;
         if (int rc = finish(count(&n))) return -rc;
         total += n;

@@ -84,6 +84,8 @@ cudaError_t launch_product_forward(int dtype, const ProdArgs& g, cudaStream_t st
 cudaError_t launch_product_input(int dtype, const ProdArgs& g, cudaStream_t st);
 cudaError_t launch_product_weight(int dtype, const ProdArgs& g, cudaStream_t st);
 cudaError_t launch_product_bytes(int dtype, const ProdArgs& g, cudaStream_t st);
+cudaError_t launch_product_scaled(int dtype, const ProdArgs& g, cudaStream_t st);
+cudaError_t launch_product_scaled_gated(int dtype, const ProdArgs& g, cudaStream_t st);
 cudaError_t launch_product_gated(int dtype, const ProdArgs& g, cudaStream_t st);
 cudaError_t launch_product_input_gated(int dtype, const ProdArgs& g, cudaStream_t st);
 cudaError_t wait_faults_norm(unsigned* n);
@@ -91,6 +93,8 @@ cudaError_t product_faults_forward(unsigned* n);
 cudaError_t product_faults_input(unsigned* n);
 cudaError_t product_faults_weight(unsigned* n);
 cudaError_t product_faults_bytes(unsigned* n);
+cudaError_t product_faults_scaled(unsigned* n);
+cudaError_t product_faults_scaled_gated(unsigned* n);
 cudaError_t product_faults_gated(unsigned* n);
 cudaError_t product_faults_input_gated(unsigned* n);
 cudaError_t launch_expert_act_backward(int dtype, const void* g, const void* d, const int* offsets, void* gz, float* grad_bias, void* scratch,
@@ -98,6 +102,8 @@ cudaError_t launch_expert_act_backward(int dtype, const void* g, const void* d, 
 cudaError_t launch_expert_gated_backward(int dtype, const void* g, const void* d, const int* offsets, void* gz, float* grad_bias, void* scratch,
                                          size_t rows, uint32_t cols, uint32_t experts, cudaStream_t st);
 cudaError_t expert_act_backward_scratch(size_t rows, size_t cols, size_t* bytes);        // on the current device
+cudaError_t launch_f8_groups(int dtype, const void* x, unsigned char* q, float* scale, size_t rows, uint32_t cols, cudaStream_t st);
+cudaError_t launch_f8_blocks(int dtype, const void* x, unsigned char* q, float* scale, size_t matrices, uint32_t rows, uint32_t cols, cudaStream_t st);
 cudaError_t launch_quantize_rows(int dtype, const void* x, signed char* q, float* scale, size_t rows, uint32_t cols, cudaStream_t st);
 
 }  // namespace nfad

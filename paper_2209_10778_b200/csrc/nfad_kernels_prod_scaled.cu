@@ -1,0 +1,8 @@
+#include "nfad_scaled_launch.cuh"
+
+namespace nfad {
+
+cudaError_t launch_product_scaled(int dtype, const ProdArgs& g, cudaStream_t st) { return launch_scaled_op<kProdScaled>(dtype, g, st); }
+cudaError_t product_faults_scaled(unsigned* n) { return product_faults_here(n); }
+
+}  // namespace nfad

@@ -36,13 +36,14 @@ constexpr int kMaxStages = 9;
 
 template <int OP> struct ProdKind {
     static constexpr bool kBytes = OP == kProdBytes;
-    static constexpr bool kGated = OP == kProdGated;                      // half of a tile's columns are a's, half are u's of the same outputs
+    static constexpr bool kScaled = OP == kProdScaled || OP == kProdScaledGated;
+    static constexpr bool kGated = OP == kProdGated || OP == kProdScaledGated;                      // half of a tile's columns are a's, half are u's of the same outputs
     static constexpr bool kInput = OP == kProdInput || OP == kProdInputGated;
-    static constexpr bool kForward = OP == kProdForward || OP == kProdBytes || kGated;
+    static constexpr bool kForward = OP == kProdForward || OP == kProdBytes || kGated || kScaled;
     static constexpr bool kTurnA = OP == kProdWeight;                     // operand A runs along its rows' dimension in memory
     static constexpr bool kTurnB = OP == kProdWeight || kInput;
     static constexpr int kPerResult = kGated ? 2 : 1;                     // a tile's columns for each column of the result
-    static constexpr int kElem = kBytes ? 1 : 2;
+    static constexpr int kElem = kBytes || kScaled ? 1 : 2;
     static constexpr int kStep = kStepBytes / kElem;                      // reduction steps per stage: 64, 128 for bytes
 };
 template <class S> struct IsBF16 { static constexpr bool value = false; };
@@ -177,7 +178,7 @@ __device__ __forceinline__ void clear_runs(unsigned char* at, int runs, int keep
 
 // ---------------------------------------------------------------- gathering without tensor copies
 
-// One operand's 128 x 128 bytes of a stage, swizzled as tensor copies would leave them: 1024 packets of 16 bytes, four to a thread.
+// One operand's 128 (kRows) x 128 bytes of a stage, swizzled as tensor copies would leave them: 1024 packets of 16 bytes, four to a thread.
 // Not turned: 128 rows of the operand's own dimension, 128 bytes of the reduction.  Turned: two boxes of 64 reduction steps (128
 // for bytes there are none) by 128 bytes along the own dimension.  Elements outside read as zeros.  A packet that starts
 // anywhere comes from the two aligned ones that hold it, shifted; at the ends of a row and of the whole operand ([begin, end))
@@ -188,19 +189,19 @@ struct GatherSource {
     int own, own_end, red, red_end;                  // first index and end along the own dimension and along the reduction
     size_t second;                                   // kHalves: bytes from the first half of the box's rows to the second
 };
-constexpr int kGatherPackets = 1024 / (kGatherWarps * 32);
-// kHalves: the box's second 64 rows have the first ones' indices in another matrix (the two weights of a gated layer)
-template <int ES, bool kTurn, bool kHalves = false> struct GatherPackets {
+// kHalves: the second half of the box's kRows rows has the first one's indices in another matrix (the two weights of a gated layer)
+template <int ES, bool kTurn, bool kHalves = false, int kRows = kTileRows> struct GatherPackets {
+    static constexpr int kGatherPackets = kRows * 8 / (kGatherWarps * 32);
     static constexpr int PER = 16 / ES;
     uint4 lo[kGatherPackets], hi[kGatherPackets];
     uint32_t whole;
     // where packet i of the box begins, and how many of its elements there are
     static __device__ __forceinline__ const unsigned char* place(const GatherSource& src, int i, int* n)
     {
-        const int row = kTurn ? src.red + ((i & 511) >> 3) : src.own + (kHalves ? (i & 511) >> 3 : i >> 3), end = kTurn ? src.red_end : src.own_end;
+        const int row = kTurn ? src.red + ((i & 511) >> 3) : src.own + (kHalves ? i % (kRows * 4) >> 3 : i >> 3), end = kTurn ? src.red_end : src.own_end;
         const int col = kTurn ? src.own + (i >> 9) * (128 / ES) + (i & 7) * PER : src.red + (i & 7) * PER, width = kTurn ? src.own_end : src.red_end;
         *n = row < end ? width - col : 0;
-        return src.at + size_t(row) * src.pitch + size_t(col) * ES + (kHalves && i >= 512 ? src.second : 0);
+        return src.at + size_t(row) * src.pitch + size_t(col) * ES + (kHalves && i >= kRows * 4 ? src.second : 0);
     }
     __device__ __forceinline__ void load(const GatherSource& src, int thread)
     {

@@ -36,8 +36,9 @@ inline cudaError_t make_map(CUtensorMap* m, int number, const void* p, uint64_t 
     EncodeTiled encode;
     cudaError_t e = encode_function(&encode);
     if (e != cudaSuccess) return e;
-    const uint32_t es = number == tc::kNumberS8 ? 1 : 2;
-    const CUtensorMapDataType type = number == tc::kNumberS8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+    const bool bytes = number == tc::kNumberS8 || number == tc::kNumberE4M3;
+    const uint32_t es = bytes ? 1 : 2;
+    const CUtensorMapDataType type = bytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8
                                      : number == tc::kNumberBF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     const cuuint64_t dims[3] = {d0, d1, d2}, strides[2] = {d0 * es, d0 * d1 * es};
     const cuuint32_t box[3] = {128 / es, b1, 1}, step[3] = {1, 1, 1};

@@ -1,0 +1,74 @@
+// nfad_scaled_launch.cuh -- launches of the products in 8-bit floating point with block scales.
+#pragma once
+
+#include "nfad_product_launch.cuh"
+#include "nfad_scaled.cuh"
+
+namespace nfad {
+
+template <int OP, int BN, class S, bool kGather, bool kPair = false>
+cudaError_t launch_scaled_tile(const ProdArgs& g, int sms, cudaStream_t st)
+{
+    using Kind = ProdKind<OP>;
+    using Tile = ProdTile<BN, kPair>;
+    auto kernel = scaled_kernel<OP, BN, S, kGather, kPair>;
+    static std::atomic<bool> ready[64] = {};         // the shared-memory opt-in of this kernel, by device (setting it twice is harmless)
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64 || !ready[dev]) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kScaledSmem);
+        if (e != cudaSuccess) return e;
+        if (dev >= 0 && dev < 64) ready[dev] = true;
+    }
+    CUtensorMap map_a = {}, map_b = {};
+    if (!kGather) {
+        e = make_map(&map_a, tc::kNumberE4M3, g.a, g.in, g.rows, 0, Tile::kBoxRows);
+        if (e != cudaSuccess) return e;
+        e = make_map(&map_b, tc::kNumberE4M3, g.b, g.in, g.outs, Kind::kPerResult, Kind::kGated ? BN / 2 : Tile::kOwnColumns);
+        if (e != cudaSuccess) return e;
+    }
+    constexpr size_t kResults = BN / Kind::kPerResult;
+    size_t grid = ((g.rows + Tile::kRows - 1) / Tile::kRows) * ((g.outs + kResults - 1) / kResults);
+    if (grid >= (size_t(1) << 31)) return cudaErrorInvalidValue;     // beyond what any device's memory holds
+    if (grid > size_t(sms / (kPair ? 2 : 1))) grid = sms / (kPair ? 2 : 1);
+    if (kPair) grid *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(grid));
+    cfg.blockDim = dim3(ScaledWarps<kGather>::kThreads);
+    cfg.dynamicSmemBytes = kScaledSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = kPair ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, g, map_a, map_b);
+}
+
+template <int OP, class S> cudaError_t launch_scaled_store(const ProdArgs& g, cudaStream_t st)
+{
+    DeviceInfo di;
+    cudaError_t e = device_info(&di);
+    if (e != cudaSuccess) return e;
+    const uintptr_t low = reinterpret_cast<uintptr_t>(g.a) | reinterpret_cast<uintptr_t>(g.b) | uintptr_t(g.in);
+    // a tensor copy needs rows that begin on 16-byte boundaries (and something to copy)
+    if (low % 16 || g.in == 0) return launch_scaled_tile<OP, 64, S, true>(g, di.sm_count, st);
+    switch (product_tile<OP>(g, di.sm_count)) {
+    case kPairTile: return launch_scaled_tile<OP, 256, S, false, true>(g, di.sm_count, st);
+    case 256: return launch_scaled_tile<OP, 256, S, false>(g, di.sm_count, st);
+    default:  return launch_scaled_tile<OP, 128, S, false>(g, di.sm_count, st);
+    }
+}
+
+template <int OP> cudaError_t launch_scaled_op(int dtype, const ProdArgs& g, cudaStream_t st)
+{
+    if (dtype == kBF16) return launch_scaled_store<OP, StoreBF16>(g, st);
+    if (dtype == kF16) return launch_scaled_store<OP, StoreF16>(g, st);
+    return cudaErrorInvalidValue;
+}
+
+}  // namespace nfad

@@ -144,6 +144,16 @@ NFAD_TC void tmem_load32(uint32_t at, uint32_t (&v)[32])
           "=r"(v[30]), "=r"(v[31])
         : "r"(at));
 }
+// the same wait, which the values that it waits for pass through: nothing that uses them can come to stand before it
+NFAD_TC void tmem_load_wait(uint32_t (&v)[32])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+                   "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]),
+                   "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]),
+                   "+r"(v[30]), "+r"(v[31])
+                 :: "memory");
+}
 NFAD_TC void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // Shared-memory operand with 128-byte swizzle.  Reduction-major: rows of 128 bytes along the reduction, eight rows to a
@@ -155,13 +165,14 @@ NFAD_TC uint64_t operand(uint32_t address, uint32_t lead, uint32_t stride)
            (1ull << 46) | (2ull << 61);
 }
 
-enum Number { kNumberF16 = 0, kNumberBF16 = 1, kNumberS8 = 2 };
+// (In a floating-point product of 8 bits, operand type 0 is the one with four exponent bits.)
+enum Number { kNumberF16 = 0, kNumberBF16 = 1, kNumberS8 = 2, kNumberE4M3 = 3 };
 
 // The instruction's description: accumulator type, operand types, which operands run along their own dimension in shared
 // memory instead of along the reduction, and the tile's shape.
 NFAD_TC uint32_t instruction(int number, bool a_turned, bool b_turned, uint32_t m, uint32_t n)
 {
-    const uint32_t acc = number == kNumberS8 ? 2 : 1, in = number == kNumberF16 ? 0 : 1;
+    const uint32_t acc = number == kNumberS8 ? 2 : 1, in = number == kNumberF16 || number == kNumberE4M3 ? 0 : 1;
     return (acc << 4) | (in << 7) | (in << 10) | (uint32_t(a_turned) << 15) | (uint32_t(b_turned) << 16) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
 
@@ -176,6 +187,16 @@ template <bool kBytes, bool kPair> NFAD_TC void product(uint32_t acc, uint64_t a
     else if (kBytes) NFAD_PRODUCT("1", "i8");
     else if (kPair) NFAD_PRODUCT("2", "f16");
     else NFAD_PRODUCT("1", "f16");
+#undef NFAD_PRODUCT
+}
+// the same of 8-bit floating-point numbers, 32 of them to a product
+template <bool kPair> NFAD_TC void product_e4m3(uint32_t acc, uint64_t a, uint64_t b, uint32_t what, bool add)
+{
+#define NFAD_PRODUCT(group)                                                                                                             \
+    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::" group ".kind::f8f6f4 [%0], %1, %2, %3, p;\n}" \
+                 ::"r"(acc), "l"(a), "l"(b), "r"(what), "r"(uint32_t(add)) : "memory")
+    if (kPair) NFAD_PRODUCT("2");
+    else NFAD_PRODUCT("1");
 #undef NFAD_PRODUCT
 }
 

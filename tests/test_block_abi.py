@@ -173,3 +173,43 @@ def test_dropout(lib):
     assert g(0, BF16, mask(), None, None, None, None, 0, 16, None) == 0
     with pytest.raises(TypeError):
         nfad.nfad_dropout(nfad.Dropout(0.5, 1), torch.zeros(8), None, torch.zeros(8))
+
+
+def test_f8(lib):
+    x, xs, w, ws, b, y, sc = (p(a << 20) for a in range(1, 8))
+    q = lib.nfad_f8_quantize_rows
+    assert q(3, x, w, xs, 4, 16, None) == 2
+    assert q(BF16, None, w, xs, 4, 16, None) == 3
+    assert q(BF16, x, w, None, 4, 16, None) == 3
+    assert q(BF16, x, x, xs, 4, 16, None) == 4
+    assert q(BF16, p((1 << 20) + 1), w, xs, 4, 16, None) == 6
+    assert q(BF16, x, w, p((2 << 20) + 2), 4, 16, None) == 6
+    assert q(BF16, x, w, xs, 4, 1 << 31, None) == 9
+    assert q(BF16, None, None, None, 0, 16, None) == 0
+    m = lib.nfad_f8_quantize_blocks
+    assert m(3, x, w, ws, 2, 4, 16, None) == 2
+    assert m(BF16, x, None, ws, 2, 4, 16, None) == 3
+    assert m(BF16, x, w, p((1 << 20) + 64), 2, 4, 16, None) == 4
+    assert m(BF16, x, w, ws, 1 << 62, 4, 16, None) == 9
+    assert m(BF16, None, None, None, 0, 4, 16, None) == 0
+    for f in (lib.nfad_f8_linear, lib.nfad_f8_gated_linear):
+        assert f(9, BF16, x, xs, w, ws, b, y, 4, 16, 8, None) == 1
+        assert f(-1, F32, x, xs, w, ws, b, y, 4, 16, 8, None) == 2
+        assert f(-1, BF16, x, None, w, ws, b, y, 4, 16, 8, None) == 3
+        assert f(-1, BF16, x, xs, w, None, b, y, 4, 16, 8, None) == 3
+        assert f(-1, BF16, x, xs, w, ws, b, b, 4, 16, 8, None) == 4
+        assert f(-1, BF16, x, xs, w, ws, b, p((3 << 20) + 64), 4, 16, 8, None) == 4
+        assert f(-1, BF16, x, p((2 << 20) + 2), w, ws, b, y, 4, 16, 8, None) == 6
+        assert f(-1, BF16, x, xs, w, ws, b, p((6 << 20) + 1), 4, 16, 8, None) == 6
+        assert f(-1, BF16, x, xs, w, ws, b, y, 1 << 31, 16, 8, None) == 9
+        assert f(-1, BF16, None, None, None, None, None, None, 0, 16, 8, None) == 0
+    assert lib.nfad_f8_gated_linear(-1, BF16, x, xs, w, ws, b, y, 4, 16, 1 << 30, None) == 9
+    need = lib.nfad_f8_linear_dynamic_scratch_bytes(4, 130)
+    assert need == 528 + 32                                           # 4 x 130 bytes to the next 16, two blocks of four rows
+    for g in (lib.nfad_f8_linear_dynamic, lib.nfad_f8_gated_linear_dynamic):
+        assert g(-1, BF16, x, w, ws, b, y, sc, need - 1, 4, 130, 8, None) == 7
+        assert g(-1, BF16, x, w, ws, b, y, None, need, 4, 130, 8, None) == 3
+        assert g(-1, BF16, x, w, ws, b, y, p((7 << 20) + 8), need, 4, 130, 8, None) == 6
+        assert g(-1, BF16, x, w, ws, b, y, x, need, 4, 130, 8, None) == 4
+    with pytest.raises(TypeError):
+        nfad.nfad_f8_quantize_rows(torch.zeros(4, 16), torch.zeros(4, 16).to(torch.float8_e4m3fn), torch.zeros(1, 4))

@@ -21,7 +21,14 @@ cudaError_t launch_scaled_tile(const ProdArgs& g, int sms, cudaStream_t st)
         if (e != cudaSuccess) return e;
         if (dev >= 0 && dev < 64) ready[dev] = true;
     }
-    CUtensorMap map_a = {}, map_b = {};
+    CUtensorMap map_a = {}, map_b = {}, map_out = {};
+    // results leave by tensor copies of 64 to a row where rows of them begin on 16-byte boundaries and a warp has as many
+    const int kOut = BN / Kind::kPerResult / (ScaledWarps<kGather>::kResult / 4);
+    const int out_copies = kOut >= 64 && g.outs % 8 == 0 && reinterpret_cast<uintptr_t>(g.out) % 16 == 0;
+    if (out_copies) {
+        e = make_map(&map_out, IsBF16<S>::value ? tc::kNumberBF16 : tc::kNumberF16, g.out, g.outs, g.rows, 0, 32);
+        if (e != cudaSuccess) return e;
+    }
     if (!kGather) {
         e = make_map(&map_a, tc::kNumberE4M3, g.a, g.in, g.rows, 0, Tile::kBoxRows);
         if (e != cudaSuccess) return e;
@@ -46,7 +53,7 @@ cudaError_t launch_scaled_tile(const ProdArgs& g, int sms, cudaStream_t st)
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = kPair ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kernel, g, map_a, map_b);
+    return cudaLaunchKernelEx(&cfg, kernel, g, map_a, map_b, map_out, out_copies);
 }
 
 template <int OP, class S> cudaError_t launch_scaled_store(const ProdArgs& g, cudaStream_t st)

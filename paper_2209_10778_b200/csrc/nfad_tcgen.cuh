@@ -60,6 +60,15 @@ NFAD_TC bool barrier_try(uint32_t bar, uint32_t parity)
     return ok != 0;
 }
 
+// whether the phase has completed, at once
+NFAD_TC bool barrier_test(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+
 // A wait that ends: when the barrier's phase completes (true), when another role of the CTA has given up, or after about ten
 // seconds of SM cycles (false; nothing that a correct launch waits for takes a hundredth of that).
 constexpr long long kWaitCycles = 20000000000ll;
@@ -76,6 +85,16 @@ NFAD_TC bool barrier_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave
         }
     }
     return true;
+}
+
+// The same wait for a phase that is expected within some hundred cycles: looked at again and again before the thread sleeps (a look takes
+// 17 cycles, a sleep that need not have been 59, and being woken more).
+constexpr int kLooks = 64;
+NFAD_TC bool barrier_poll(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up)
+{
+    for (int i = 0; i < kLooks; ++i)
+        if (barrier_test(bar, parity)) return true;
+    return barrier_wait(bar, parity, gave_up);
 }
 
 // plain shared-memory writes become visible to the asynchronous copies and products that follow
@@ -104,6 +123,17 @@ template <bool kPair> NFAD_TC void load_box(uint32_t dst, const CUtensorMap* m, 
         asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                      ::"r"(dst), "l"(m), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
+
+// The other way: a box of this CTA's shared memory, written before (writes_to_async and a warp's barrier behind the writes), to rows from c1 and
+// elements from c0 on; what lies outside the tensor is left out.  By the thread that later waits: stores_read before the memory is
+// written again, stores_done before the CTA ends.
+NFAD_TC void store_box(const CUtensorMap* m, uint32_t src, int c0, int c1)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(m), "r"(src), "r"(c0), "r"(c1) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+NFAD_TC void stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+NFAD_TC void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // `bytes` (a multiple of 16) between 16-byte boundaries, no tensor map
 NFAD_TC void load_run(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
@@ -143,6 +173,21 @@ NFAD_TC void tmem_load32(uint32_t at, uint32_t (&v)[32])
           "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]),
           "=r"(v[30]), "=r"(v[31])
         : "r"(at));
+}
+NFAD_TC void tmem_load16(uint32_t at, uint32_t (&v)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+          "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(at));
+}
+NFAD_TC void tmem_load_wait(uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]),
+                   "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+                 :: "memory");
 }
 // the same wait, which the values that it waits for pass through: nothing that uses them can come to stand before it
 NFAD_TC void tmem_load_wait(uint32_t (&v)[32])

@@ -235,6 +235,156 @@ def expert_feed_forward(x, w1, b1, w2, b2, offsets, kind="gelu_erf"):
     return ExpertFeedForward.apply(x, w1, b1, w2, b2, offsets, kind)
 
 
+class ExpertGatedLinear(torch.autograd.Function):
+    """y = f(a) u, a and u the products with the two weights, for rows grouped by expert; saved: x, w and y's two derivatives (no a, no u)."""
+
+    @staticmethod
+    def forward(ctx, x, w, bias, offsets, kind):
+        xc, wc, bc = x.contiguous(), w.contiguous(), None if bias is None else bias.contiguous()
+        y = torch.empty(xc.shape[0], wc.shape[2], dtype=xc.dtype, device=xc.device)
+        both = torch.empty(xc.shape[0], 2, wc.shape[2], dtype=xc.dtype, device=xc.device)
+        block.nfad_expert_gated_linear(kind, xc, wc, bc, offsets, y, both)
+        ctx.save_for_backward(xc, wc, offsets, both)
+        ctx.bias_dtype = None if bias is None else bias.dtype
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_out):
+        x, w, offsets, both = ctx.saved_tensors
+        gz, gb = torch.empty_like(both), None
+        if ctx.needs_input_grad[2]:
+            gb = torch.empty(*w.shape[:3], device=x.device)
+        scratch = block.nfad_expert_act_backward_scratch(gz.flatten(1)) if gb is not None else None
+        block.nfad_expert_gated_backward(grad_out.contiguous(), both, offsets, gz, gb, scratch)
+        gx, gw = _gated_products(gz, x, w, offsets, ctx.needs_input_grad[:2])
+        return gx, gw, None if gb is None else gb.to(ctx.bias_dtype), None, None
+
+
+def _gated_products(gz, x, w, offsets, need):
+    """The gradients of a gated layer's input and weights: those of a linear layer with twice the outputs."""
+    gx = gw = None
+    if need[0]:
+        gx = torch.empty_like(x)
+        block.nfad_expert_linear_backward_input(gz.flatten(1), w.flatten(1, 2), offsets, None, gx)
+    if need[1]:
+        gw = torch.empty_like(w)
+        block.nfad_expert_linear_backward_weight(gz.flatten(1), x, offsets, gw.view(w.shape[0], -1, w.shape[3]))
+    return gx, gw
+
+
+def expert_gated_linear(x, w, bias, offsets, kind="swish"):
+    """x [rows, in] sorted by expert, w [experts, 2, out, in] (the gate's first), bias [experts, 2, out] or None, offsets int32 [experts + 1]."""
+    return ExpertGatedLinear.apply(x, w, bias, offsets, kind)
+
+
+class ExpertGatedFeedForward(torch.autograd.Function):
+    """w2 (f(a) u) + b2, a and u the products of x with w1's two weights.  Saved: x, y1 = f(a) u, its two derivatives and the weights; on the way
+    back the second layer's input gradient leaves its product already multiplied by both."""
+
+    @staticmethod
+    def forward(ctx, x, w1, b1, w2, b2, offsets, kind):
+        xc, w1c, w2c = x.contiguous(), w1.contiguous(), w2.contiguous()
+        rows, hidden = xc.shape[0], w1c.shape[2]
+        y1 = torch.empty(rows, hidden, dtype=xc.dtype, device=xc.device)
+        both = torch.empty(rows, 2, hidden, dtype=xc.dtype, device=xc.device)
+        block.nfad_expert_gated_linear(kind, xc, w1c, None if b1 is None else b1.contiguous(), offsets, y1, both)
+        y2 = torch.empty(rows, w2c.shape[1], dtype=xc.dtype, device=xc.device)
+        block.nfad_expert_linear(None, y1, w2c, None if b2 is None else b2.contiguous(), offsets, y2)
+        ctx.save_for_backward(xc, y1, both, w1c, w2c, offsets)
+        ctx.bias_dtypes = [None if b is None else b.dtype for b in (b1, b2)]
+        return y2
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_out):
+        x, y1, both, w1, w2, offsets = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        g2, gb2 = _expert_grad_bias(grad_out.contiguous(), None, offsets, need[4])
+        gw2 = None
+        if need[3]:
+            gw2 = torch.empty_like(w2)
+            block.nfad_expert_linear_backward_weight(g2, y1, offsets, gw2)
+        gz = gb1 = gx = gw1 = None
+        if any(need[:3]):
+            gz = torch.empty_like(both)
+            block.nfad_expert_linear_backward_gated(g2, w2, offsets, both, gz)
+            _, gb1 = _expert_grad_bias(gz.flatten(1), None, offsets, need[2])
+            gx, gw1 = _gated_products(gz, x, w1, offsets, need[:2])
+        gb1 = None if gb1 is None else gb1.view(w1.shape[:3]).to(ctx.bias_dtypes[0])
+        return gx, gw1, gb1, gw2, None if gb2 is None else gb2.to(ctx.bias_dtypes[1]), None, None
+
+
+def expert_gated_feed_forward(x, w1, b1, w2, b2, offsets, kind="swish"):
+    """A gated layer and a linear one: w1 [experts, 2, hidden, in] (the gate's first), w2 [experts, out, hidden]."""
+    return ExpertGatedFeedForward.apply(x, w1, b1, w2, b2, offsets, kind)
+
+
+class Dropout(torch.autograd.Function):
+    """residual + m x; nothing is saved but what names the mask: the backward pass draws it again."""
+
+    @staticmethod
+    def forward(ctx, x, residual, drop):
+        xc = x.contiguous()
+        y = torch.empty_like(xc)
+        block.nfad_dropout(drop, xc, None if residual is None else residual.contiguous(), y)
+        ctx.numbers = drop.p, drop.seed, drop.offset
+        # with autograd, which refuses a backward pass after the step has been counted up in place
+        ctx.save_for_backward(*([] if drop.step is None else [drop.step]))
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_out):
+        gx = None
+        if ctx.needs_input_grad[0]:
+            g = grad_out.contiguous()
+            gx = torch.empty_like(g)
+            block.nfad_dropout(block.Dropout(*ctx.numbers, *ctx.saved_tensors), g, None, gx)
+        return gx, grad_out if ctx.needs_input_grad[1] else None, None
+
+
+def dropout(x, drop, residual=None):
+    """m x, or residual + m x, with the mask of a ``block.Dropout``."""
+    if residual is not None and residual.shape != x.shape:
+        raise ValueError("residual must have x's shape")
+    return Dropout.apply(x, residual, drop)
+
+
+class NestedBiasActivationDropout(torch.autograd.Function):
+    """m f(x + bias) for x [..., cols]; m f'(x + bias) is the only saved tensor and carries the mask: the backward pass is that of the activation
+    without dropout."""
+
+    @staticmethod
+    def forward(ctx, x, bias, kind, drop):
+        xc = x.contiguous()
+        y, d = torch.empty_like(xc), torch.empty_like(xc)
+        block.nfad_bias_act_dropout_forward(kind, drop, xc, None if bias is None else bias.contiguous(), y, d)
+        ctx.save_for_backward(d)
+        ctx.kind, ctx.bias_dtype, ctx.cols = kind, None if bias is None else bias.dtype, xc.shape[-1] if xc.dim() else 1
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_out):
+        (d,) = ctx.saved_tensors
+        g = grad_out.contiguous()
+        gin = torch.empty_like(g)
+        if not ctx.needs_input_grad[1]:
+            nfad.nfad_act_backward(ctx.kind, g.view(-1), d.view(-1), gin.view(-1))
+            return gin, None, None, None
+        gb = torch.empty(ctx.cols, dtype=torch.float32, device=g.device)
+        nb = nfad.nfad_bias_act_backward_scratch_bytes(g.dtype, g.numel() // max(1, ctx.cols), ctx.cols, g.device)
+        scratch = torch.empty(nb, dtype=torch.uint8, device=g.device) if nb else None
+        nfad.nfad_bias_act_backward(ctx.kind, g.view(-1), d.view(-1), gin.view(-1), gb, scratch)
+        return gin, gb.to(ctx.bias_dtype), None, None
+
+
+def bias_act_dropout(x, bias, kind, drop):
+    """Dropout of f(x + bias) (bias [cols] or None), with the mask of a ``block.Dropout``."""
+    return NestedBiasActivationDropout.apply(x, bias, kind, drop)
+
+
 def bias_gelu(x, bias, approximate: str = "none"):
     return NestedBiasActivation.apply(x, bias, "gelu_tanh" if approximate == "tanh" else "gelu_erf")
 

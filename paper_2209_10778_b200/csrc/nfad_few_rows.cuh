@@ -19,6 +19,18 @@ constexpr int kFewOutputs = 16;
 constexpr int kFewSteps = 4;                        // of 64 bytes of each row: what a warp has in flight
 constexpr int kFewMaxRows = 256;
 
+// d += a b of four 8-bit floating-point values each, as two pairs of halves, which hold them exactly.  (The instruction for 8-bit operands itself
+// spills 172 bytes a thread and took 46 us for one token, 4096 -> 2 x 14336, where this takes 32.)
+__device__ __forceinline__ void few_product_e4m3(float (&f)[4], uint32_t lo, uint32_t hi, uint32_t x)
+{
+    asm volatile("{\n .reg .b16 l, h;\n .reg .b32 a0, a1, a2, a3, b0, b1;\n"
+        " mov.b32 {l, h}, %4;\n cvt.rn.f16x2.e4m3x2 a0, l;\n cvt.rn.f16x2.e4m3x2 a2, h;\n"
+        " mov.b32 {l, h}, %5;\n cvt.rn.f16x2.e4m3x2 a1, l;\n cvt.rn.f16x2.e4m3x2 a3, h;\n"
+        " mov.b32 {l, h}, %6;\n cvt.rn.f16x2.e4m3x2 b0, l;\n cvt.rn.f16x2.e4m3x2 b1, h;\n"
+        " mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {a0, a1, a2, a3}, {b0, b1}, {%0, %1, %2, %3};\n}"
+        : "+f"(f[0]), "+f"(f[1]), "+f"(f[2]), "+f"(f[3]) : "r"(lo), "r"(hi), "r"(x));
+}
+
 // d += a b: 16 outputs x 8 tokens, 32 bytes of the reduction
 template <int kNumber> __device__ __forceinline__ void few_product(uint32_t (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
@@ -29,7 +41,10 @@ template <int kNumber> __device__ __forceinline__ void few_product(uint32_t (&d)
         float f[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(d[i]);
-        if (kNumber == tc::kNumberBF16)
+        if (kNumber == tc::kNumberE4M3) {
+            few_product_e4m3(f, a0, a1, b0);
+            few_product_e4m3(f, a2, a3, b1);
+        } else if (kNumber == tc::kNumberBF16)
             asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                 : "+f"(f[0]), "+f"(f[1]), "+f"(f[2]), "+f"(f[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
         else
@@ -54,22 +69,26 @@ __device__ __forceinline__ void act1(int kind, float z, float* y, float* d)
     *d = o.dydx;
 }
 
-// OP: kProdForward, kProdBytes (8-bit integers, one expert) or kProdGated, whose CTA takes eight outputs of each of the two weights: the
+// Of operands with block scales a warp's block of 256 bytes is two scaled blocks: each one's products start from zero and are added with
+// their scale.
+// OP: kProdForward, kProdBytes (8-bit integers, one expert), kProdScaled or a gated one, whose CTA takes eight outputs of each of the two weights: the
 // lower and the upper half of the instruction's 16 rows.  early: the weights may be read before the kernel in front has ended
 // (it is the quantiser of the same call, which starts this one only after everything before it is complete).
+template <int OP, int NT> struct FewResident { static constexpr int value = NT == 1 && !ProdKind<OP>::kScaled ? 4 : 3; };     // CTAs to an SM (scaled: two conversions a word, 80 registers)
 template <int OP, class S, int NT>
-__global__ void __launch_bounds__(kFewWarps * 32, NT == 1 ? 4 : 3) few_rows_kernel(const __grid_constant__ ProdArgs g, int early)
+__global__ void __launch_bounds__(kFewWarps * 32, FewResident<OP, NT>::value) few_rows_kernel(const __grid_constant__ ProdArgs g, int early)
 {
-    constexpr bool kBytes = OP == kProdBytes, kGated = OP == kProdGated;
+    constexpr bool kBytes = OP == kProdBytes, kGated = ProdKind<OP>::kGated, kScaled = ProdKind<OP>::kScaled;
+    static_assert(kFewSteps * 64 == 256, "two scaled blocks");
     constexpr int kOutputs = kFewOutputs / ProdKind<OP>::kPerResult;           // a job's
-    constexpr int kNumber = kBytes ? tc::kNumberS8 : IsBF16<S>::value ? tc::kNumberBF16 : tc::kNumberF16;
-    constexpr int ES = kBytes ? 1 : 2;
+    constexpr int kNumber = kBytes ? tc::kNumberS8 : kScaled ? tc::kNumberE4M3 : IsBF16<S>::value ? tc::kNumberBF16 : tc::kNumberF16;
+    constexpr int ES = kBytes || kScaled ? 1 : 2;
     __shared__ uint32_t sums[kFewWarps][kFewOutputs][8 * NT + 1];
     __shared__ int live[kFewMaxRows], first[kFewMaxRows], rows[kFewMaxRows], lives, bounds[2];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, quad = lane & 3;
     const uint32_t groups = (g.outs + kOutputs - 1) / kOutputs;
     const uint32_t pitch = g.in * ES;                // bytes of a row of either operand
-    const uint32_t blocks = (pitch + kFewSteps * 64 - 1) / (kFewSteps * 64);
+    const uint32_t blocks = (pitch + kFewSteps * 64 - 1) / (kFewSteps * 64), in_blocks = (g.in + 127) / 128;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (!early) asm volatile("griddepcontrol.wait;" ::: "memory");
     if (g.offsets) {
@@ -167,14 +186,47 @@ __global__ void __launch_bounds__(kFewWarps * 32, NT == 1 ? 4 : 3) few_rows_kern
         }
         for (uint32_t b = warp; b < blocks; b += kFewWarps) {
             const uint32_t k0 = b * (kFewSteps * 64) + quad * 16;
+            // rows of the sums are outputs, of one block of weights (gated: the lower and the upper half of one of each weight)
+            float sw[2][2];
+            if (kScaled)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        if (!kGated && e) sw[h][e] = sw[h][0];
+                        else sw[h][e] = b * 2 + h < in_blocks ? __ldg(g.b_scale + (size_t(e ? (g.outs + 127) / 128 : 0) + o0 / 128) * in_blocks + b * 2 + h) : 0.0f;
+                    }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 if (n * 8 >= m) break;
+                // columns of the sums are tokens, two to a lane; past the row's last block all sums are 0, whatever they are scaled by
+                float sx[2][2];
+                if (kScaled)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            sx[h][e] = b * 2 + h < in_blocks ? g.a_scale[size_t(b * 2 + h) * g.rows + first[slot] + min(n * 8 + int(quad) * 2 + e, m - 1)] : 0.0f;
                 // tokens past the last one repeat it
                 const unsigned char* row = x + size_t(min(n * 8 + gid, m - 1)) * pitch + k0;
                 uint4 v[kFewSteps];
 #pragma unroll
                 for (int i = 0; i < kFewSteps; ++i) v[i] = k0 + i * 64 < pitch ? *reinterpret_cast<const uint4*>(row + i * 64) : make_uint4(0, 0, 0, 0);
+                if constexpr (kScaled) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t part[4] = {0, 0, 0, 0};
+#pragma unroll
+                        for (int i = 2 * h; i < 2 * h + 2; ++i) {
+                            few_product<kNumber>(part, lo[i].x, hi[i].x, lo[i].y, hi[i].y, v[i].x, v[i].y);
+                            few_product<kNumber>(part, lo[i].z, hi[i].z, lo[i].w, hi[i].w, v[i].z, v[i].w);
+                        }
+                        const float scale[4] = {sx[h][0] * sw[h][0], sx[h][1] * sw[h][0], sx[h][0] * sw[h][1], sx[h][1] * sw[h][1]};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[n][e] = __float_as_uint(fmaf(__uint_as_float(part[e]), scale[e], __uint_as_float(acc[n][e])));
+                    }
+                    continue;
+                }
 #pragma unroll
                 for (int i = 0; i < kFewSteps; ++i) {
                     few_product<kNumber>(acc[n], lo[i].x, hi[i].x, lo[i].y, hi[i].y, v[i].x, v[i].y);
@@ -244,7 +296,7 @@ template <int OP, class S, int NT> cudaError_t launch_few_rows_tiles(const ProdA
 {
     const size_t live = g.rows < g.experts ? g.rows : g.experts;
     constexpr int kOutputs = kFewOutputs / ProdKind<OP>::kPerResult;
-    const size_t jobs = (g.outs + kOutputs - 1) / kOutputs * live, fit = size_t(sms) * (NT == 1 ? 4 : 3);
+    const size_t jobs = (g.outs + kOutputs - 1) / kOutputs * live, fit = size_t(sms) * FewResident<OP, NT>::value;
     // one expert, whose jobs are known: as many for each CTA, rather than a last turn of a few (13.3 -> 12.6 us); else all that fit
     const size_t turns = g.experts == 1 ? (jobs + fit - 1) / fit : 1, grid = (jobs + turns - 1) / turns;
     cudaLaunchConfig_t cfg = {};

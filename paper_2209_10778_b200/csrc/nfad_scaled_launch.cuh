@@ -3,6 +3,7 @@
 
 #include "nfad_product_launch.cuh"
 #include "nfad_scaled.cuh"
+#include "nfad_scaled_split.cuh"
 
 namespace nfad {
 
@@ -56,6 +57,50 @@ cudaError_t launch_scaled_tile(const ProdArgs& g, int sms, cudaStream_t st)
     return cudaLaunchKernelEx(&cfg, kernel, g, map_a, map_b, map_out, out_copies);
 }
 
+template <int OP, class S> cudaError_t launch_scaled_split(const ProdArgs& g, unsigned ranks, cudaStream_t st)
+{
+    using Kind = ProdKind<OP>;
+    auto kernel = scaled_split_kernel<OP, S>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kThinSmem);
+    if (e != cudaSuccess) return e;
+    CUtensorMap map_a = {}, map_b = {};
+    e = make_map(&map_a, tc::kNumberE4M3, g.a, g.in, g.rows, 0, 32);
+    if (e != cudaSuccess) return e;
+    e = make_map(&map_b, tc::kNumberE4M3, g.b, g.in, g.outs, Kind::kPerResult, kSplitColumns / Kind::kPerResult);
+    if (e != cudaSuccess) return e;
+    constexpr size_t kResults = kSplitColumns / Kind::kPerResult;
+    const size_t tiles = ((g.rows + kTileRows - 1) / kTileRows) * ((g.outs + kResults - 1) / kResults);
+    if (tiles * ranks >= (size_t(1) << 31)) return cudaErrorInvalidValue;     // beyond what any device's memory holds
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(tiles * ranks));
+    cfg.blockDim = dim3(kSplitThreads);
+    cfg.dynamicSmemBytes = kThinSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ranks;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, g, map_a, map_b, uint32_t(ranks));
+}
+
+// Over how many CTAs a tile's reduction is split (0: not at all; tiles of another size, which CTAs walk over): as many as one to an SM allows,
+// with eight blocks left for each.  Measured (us, against tiles that are walked over): 100 rows 4096 -> 2048 over 4: 14.3 (22.5), over 8: 20.6;
+// 400 rows 4096 -> 1024 over 2: 17.2 (22.5); 40 rows 8192 -> 4096 over 2: 22.5 (33.7); gated 200 rows 4096 -> 2 x 1024 over 2: 18.4 (20.4).
+// One CTA to a tile of this size was never the fastest (40 rows 4096 -> 28672: 45, by tiles of 128 34.8).
+template <int OP> unsigned scaled_split_ranks(const ProdArgs& g, int sms)
+{
+    if (g.outs % 8 || (reinterpret_cast<uintptr_t>(g.out) | reinterpret_cast<uintptr_t>(g.bias)) % 16) return 0;      // its results go by packets
+    constexpr size_t kResults = kSplitColumns / ProdKind<OP>::kPerResult;
+    const size_t tiles = ((g.rows + kTileRows - 1) / kTileRows) * ((g.outs + kResults - 1) / kResults), blocks = (g.in + kScaleBlock - 1) / kScaleBlock;
+    for (unsigned ranks = 8; ranks > 1; ranks /= 2)
+        if (tiles * ranks <= size_t(sms) && blocks >= 8 * ranks) return ranks;
+    return 0;
+}
+
 template <int OP, class S> cudaError_t launch_scaled_store(const ProdArgs& g, cudaStream_t st)
 {
     DeviceInfo di;
@@ -64,6 +109,10 @@ template <int OP, class S> cudaError_t launch_scaled_store(const ProdArgs& g, cu
     const uintptr_t low = reinterpret_cast<uintptr_t>(g.a) | reinterpret_cast<uintptr_t>(g.b) | uintptr_t(g.in);
     // a tensor copy needs rows that begin on 16-byte boundaries (and something to copy)
     if (low % 16 || g.in == 0) return launch_scaled_tile<OP, 64, S, true>(g, di.sm_count, st);
+    // Up to eight rows, a column each of the small matrix instruction.  Against tiles (us): 8 rows 4096 -> 4096 10.3 (14.3 split over 4), gated
+    // 4096 -> 2 x 14336 36.9 (34.8), 1 row of it 32.4 (36.7); with two such groups 16 rows of it took 57 (34.8).
+    if (few_rows(g) && g.rows <= 8) return launch_few_rows_tiles<OP, S, 1>(g, di.sm_count, g.b_ready, st);
+    if (const unsigned ranks = scaled_split_ranks<OP>(g, di.sm_count)) return launch_scaled_split<OP, S>(g, ranks, st);
     switch (product_tile<OP>(g, di.sm_count)) {
     case kPairTile: return launch_scaled_tile<OP, 256, S, false, true>(g, di.sm_count, st);
     case 256: return launch_scaled_tile<OP, 256, S, false>(g, di.sm_count, st);

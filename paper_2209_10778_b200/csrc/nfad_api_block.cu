@@ -86,9 +86,8 @@ int check_mask(const nfad_dropout_mask* mask, int dtype, nfad::DropoutArgs* a)
     if (dtype < 0 || dtype > 2) return NFAD_E_DTYPE;
     if (!(mask->p >= 0.0 && mask->p <= 1.0)) return NFAD_E_VALUE;
     const uint32_t dropped = uint32_t(rint(mask->p * 65536.0));
-    a->dropped = dropped < 65536 ? dropped << 16 : 0xffffffffu;
-    a->live = dropped < 65536 ? 0xffffffffu : 0;
-    a->scale = dropped < 65536 ? float(65536.0 / double(65536 - dropped)) : 0.0f;
+    a->dropped = dropped << 16;
+    a->scale = dropped < 65536 ? float(65536.0 / double(65536 - dropped)) : 0.0f;          // 0: everything is dropped
     a->seed = mask->seed;
     a->offset = mask->offset;
     a->step = mask->step;
@@ -262,6 +261,10 @@ int nfad_dropout(int dtype, const nfad_dropout_mask* mask, const void* x, const 
     if ((rc = aliasing({oy}, {sx, sr}, {ss}))) return rc;
     a.x = x; a.other = residual; a.y = y; a.n = n;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (a.scale == 0.0f) {
+        if (residual == y) return NFAD_OK;
+        return finish(residual ? cudaMemcpyAsync(y, residual, n * es, cudaMemcpyDeviceToDevice, st) : cudaMemsetAsync(y, 0, n * es, st));
+    }
     return finish(dtype == NFAD_F32 ? nfad::launch_dropout_f32(nfad::kNoAct, a, st) : nfad::launch_dropout_16(nfad::kNoAct, dtype, a, st));
 }
 
@@ -281,6 +284,10 @@ int nfad_bias_act_dropout_forward(int kind, int dtype, const nfad_dropout_mask* 
     if ((rc = aliasing({oy, od}, {sx}, {sb, ss}))) return rc;
     a.x = x; a.other = bias; a.y = y; a.slope = dfdx; a.n = n; a.cols = uint32_t(cols);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (a.scale == 0.0f) {
+        if ((rc = finish(cudaMemsetAsync(y, 0, n * es, st)))) return rc;
+        return finish(cudaMemsetAsync(dfdx, 0, n * es, st));
+    }
     return finish(dtype == NFAD_F32 ? nfad::launch_dropout_f32(kind, a, st) : nfad::launch_dropout_16(kind, dtype, a, st));
 }
 

@@ -16,7 +16,7 @@ struct DropoutArgs {
     uint32_t cols, row_packets;      // with a bias
     uint64_t seed, offset;
     const unsigned long long* step;  // on the device, added to offset; or null
-    uint32_t dropped, live;          // see kept()
+    uint32_t dropped;                // see kept()
     float scale;
 };
 

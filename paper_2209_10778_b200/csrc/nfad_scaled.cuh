@@ -15,6 +15,8 @@
 // for a tile without an activation, 5.2 with Swish (two special-function results an element).
 #pragma once
 
+#include <stddef.h>
+
 #include "nfad_dropout_args.h"
 #include "nfad_product.cuh"
 
@@ -69,6 +71,13 @@ template <class K, class S, bool kGated> __device__ __forceinline__ uint4 finish
         y[e + 1] = z.y;
     }
     return S::pack(y);
+}
+
+// a value whose origin the compiler does not see: it is formed where this stands, and what is formed of it further down
+__device__ __forceinline__ uint32_t fresh(uint32_t v)
+{
+    asm volatile("" : "+r"(v));
+    return v;
 }
 
 // A load that stays where it stands: left to itself it sinks to its use, a step later, and every step waits for it (500 of 1000 cycles).
@@ -208,13 +217,25 @@ scaled_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtens
     } else if (warp < kFirstResultWarp + kResultWarps) {
         if (kMoveRegisters) asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
         // ------------------------------------------------ results.  Little besides the sums may live through the steps.
+        // What the roles share is formed anew here, hidden from the compiler: a value that lives across the roles is put into local memory
+        // and fetched from there in every step.
+        const uint32_t thread = fresh(threadIdx.x), warp = thread >> 5, lane = thread & 31;
+        const uint32_t rows = fresh(uint32_t(g.rows)), width = fresh(g.outs), blocks = (fresh(g.in) + kScaleBlock - 1) / kScaleBlock;
+        const uint32_t rank = kPair ? fresh(tc::rank_in_pair()) : 0, block = fresh(blockIdx.x), step = fresh(gridDim.x);
+        const uint32_t unit = kPair ? block >> 1 : block, units = kPair ? step >> 1 : step;
+        const uint32_t a_tiles = (rows + Tile::kRows - 1) / Tile::kRows, b_tiles = (width + kResults - 1) / kResults, total = a_tiles * b_tiles;
+        const uint32_t base = fresh(tc::shared_address(raw)), shared_at = ((base + 1023) & ~1023u) + kRingBytes + kMostResultWarps * kOutBytes;
+        auto done = [&](int i) { return shared_at + uint32_t(offsetof(ScaledShared, done)) + i * 8; };
+        auto taken = [&](int i) { return shared_at + uint32_t(offsetof(ScaledShared, taken)) + i * 8; };
+        uint32_t tmem;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(tmem) : "r"(shared_at + uint32_t(offsetof(ScaledShared, tmem))));
         const int lanes = (warp & 3) * 32, half = (warp - kFirstResultWarp) >> 2;
         constexpr int kOut = kColumns / Kind::kPerResult;                    // this warp's results of a row, from half kOut on
         // chunk c's first column in a buffer: a gated warp has columns of a first, then those of u
         auto column = [&](int c) { return Kind::kGated && c >= kChunks / 2 ? int(kResults) + half * kOut + (c - kChunks / 2) * kChunk : half * kOut + c * kChunk; };
         uint32_t turn = 0, stage = 0, phase = 0;
         for (uint32_t t = unit; t < total; t += units) {
-            const ScaledAt q = tile_at(t);
+            const ScaledAt q = scaled_at(t, a_tiles, b_tiles, Tile::kRows, kResults);
             const uint32_t row0 = q.a0 + rank * kTileRows + lanes;            // this warp's first row
             const uint32_t first = q.b0 + half * kOut;                        // and result: all of its results are in one block of outputs
             float2 acc[kColumns / 2];
@@ -230,19 +251,15 @@ scaled_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtens
                 if (Kind::kGated) next_u = load_now(g.b_scale + ((size_t((width + kScaleBlock - 1) / kScaleBlock) + sw) * blocks + b));
             };
             request(0);
-            // the bias of this warp's results, kMine neighbours to a lane: fetched in the epilogue, it cost 3 us a tile
-            constexpr int kMine = kOut / 32;
-            float bias[kMine], bias_u[kMine];
-#pragma unroll
-            for (int i = 0; i < kMine; ++i) {
-                const uint32_t c = first + lane * kMine + i;
-                const typename S::elem* p = static_cast<const typename S::elem*>(g.bias) + c;
-                bias[i] = g.bias && c < width ? S::load1(p) : 0.0f;
-                bias_u[i] = Kind::kGated && g.bias && c < width ? S::load1(p + width) : 0.0f;
+            if (g.bias && first + lane * (kOut / 32) < width) {
+                // needed behind the steps; not held through them
+                const typename S::elem* bias = static_cast<const typename S::elem*>(g.bias) + first + lane * (kOut / 32);
+                asm volatile("prefetch.global.L1 [%0];" ::"l"(bias));
+                if (Kind::kGated) asm volatile("prefetch.global.L1 [%0];" ::"l"(bias + width));
             }
             bool ok = true;
             for (uint32_t b = 0; b < blocks; ++b) {
-                if (!(ok = tc::barrier_poll(done(stage), phase, gave_up))) break;
+                if (!(ok = tc::barrier_wait(done(stage), phase, gave_up))) break;
                 tc::fence_after_sync();
                 const uint32_t at = tmem + (uint32_t(lanes) << 16) + turn * BN;
                 uint32_t v[2][kChunk];
@@ -270,11 +287,19 @@ scaled_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtens
             }
             if (!ok) break;
             if (first < width && row0 < rows) {
+                // the bias of this warp's results, kMine neighbours to a lane: fetched packet by packet, it cost 3 us a tile
+                constexpr int kMine = kOut / 32;
+                float bias[kMine], bias_u[kMine];
+#pragma unroll
+                for (int i = 0; i < kMine; ++i) {
+                    const uint32_t c = first + lane * kMine + i;
+                    const typename S::elem* p = static_cast<const typename S::elem*>(g.bias) + c;
+                    bias[i] = g.bias && c < width ? S::load1(p) : 0.0f;
+                    bias_u[i] = Kind::kGated && g.bias && c < width ? S::load1(p + width) : 0.0f;
+                }
                 // from here on by a copy of the thread's number that is made here, so that no address of this part lives through the steps
-                uint32_t thread = threadIdx.x;
-                asm volatile("" : "+r"(thread));
-                const uint32_t place = thread & 31;
-                unsigned char* boxes = ring + kRingBytes + ((thread >> 5) - kFirstResultWarp) * kOutBytes;
+                const uint32_t again = fresh(threadIdx.x), place = again & 31;
+                unsigned char* boxes = ring + kRingBytes + ((again >> 5) - kFirstResultWarp) * kOutBytes;
                 RowPackets packets;
                 packets.lane = place;
                 packets.rows = min(32, int(rows - row0));

@@ -99,27 +99,33 @@ scaled_split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ 
         // the tail of the launch order: whatever read ahead waits here
         if (g.b_ready && warp == 3) asm volatile("griddepcontrol.wait;" ::: "memory");
     } else if (warp == 1) {
-        if (lane == 0) {
-            const uint32_t what = tc::instruction(tc::kNumberE4M3, false, false, kTileRows, kSplitColumns);
-            int stage = 0, turn = 0;
-            uint32_t phase = 0, turn_phase = 0;
-            for (uint32_t b = first_block; b < end_block; ++b) {
+        const uint32_t what = tc::instruction(tc::kNumberE4M3, false, false, kTileRows, kSplitColumns);
+        const bool leader = tc::elected();
+        int stage = 0, turn = 0;
+        uint32_t phase = 0, turn_phase = 0;
+        bool ready = false;
+        for (uint32_t b = first_block; b < end_block; ++b) {
+            if (!ready) {
                 if (!(ok = tc::barrier_poll(full(stage), phase, gave_up))) break;
                 if (!(ok = tc::barrier_poll(taken(turn), turn_phase ^ 1, gave_up))) break;
-                tc::fence_after_sync();
-                const uint32_t at_a = ring_at + stage * stage_bytes, at_b = at_a + stage_a;
+            }
+            tc::fence_after_sync();
+            const uint64_t at_a = tc::operand(ring_at + stage * stage_bytes, 16, 1024), at_b = tc::operand(ring_at + stage * stage_bytes + stage_a, 16, 1024);
+            const uint32_t to = tmem + turn * kSplitColumns, bar = done(stage);
+            if (++stage == stages) { stage = 0; phase ^= 1; }
+            if (++turn == kThinBuffers) { turn = 0; turn_phase ^= 1; }
+            ready = tc::barrier_test(full(stage), phase) & tc::barrier_test(taken(turn), turn_phase ^ 1);        // ahead, as in scaled_kernel
+            if (leader) {
 #pragma unroll
-                for (int k = 0; k < kStepBytes / 32; ++k)
-                    tc::product_e4m3<false>(tmem + turn * kSplitColumns, tc::operand(at_a + k * 32, 16, 1024), tc::operand(at_b + k * 32, 16, 1024), what, k > 0);
-                tc::products_to<false>(done(stage));
-                if (++stage == stages) { stage = 0; phase ^= 1; }
-                if (++turn == kThinBuffers) { turn = 0; turn_phase ^= 1; }
+                for (int k = 0; k < kStepBytes / 32; ++k) tc::product_e4m3<false>(to, at_a + k * 2, at_b + k * 2, what, k > 0);
+                tc::products_to<false>(bar);
             }
-            if (!ok) {
-                tc::products_to<false>(tc::shared_address(&s.drained));
-                const long long t0 = clock64();
-                while (!tc::barrier_try(tc::shared_address(&s.drained), 0) && clock64() - t0 < tc::kWaitDrain) {}
-            }
+            __syncwarp();
+        }
+        if (!ok && leader) {
+            tc::products_to<false>(tc::shared_address(&s.drained));
+            const long long t0 = clock64();
+            while (!tc::barrier_try(tc::shared_address(&s.drained), 0) && clock64() - t0 < tc::kWaitDrain) {}
         }
         __syncwarp();
     } else if (warp >= kFirstResultWarp) {

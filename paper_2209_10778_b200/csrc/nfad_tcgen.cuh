@@ -60,6 +60,15 @@ NFAD_TC bool barrier_try(uint32_t bar, uint32_t parity)
     return ok != 0;
 }
 
+// One lane of the warp, always the same.  The warp goes through an issuing loop together, so that what its instructions take in uniform
+// registers is formed there, and this lane issues.
+NFAD_TC bool elected()
+{
+    uint32_t one;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+    return one != 0;
+}
+
 // whether the phase has completed, at once
 NFAD_TC bool barrier_test(uint32_t bar, uint32_t parity)
 {

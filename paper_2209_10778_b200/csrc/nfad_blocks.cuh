@@ -15,11 +15,15 @@
 // NaN and q 0, so that everything computed from it is NaN.
 #pragma once
 
+#include <type_traits>
+
 #include "nfad_bytes.cuh"
 
 namespace nfad {
 
 constexpr int kBlockSide = 128;
+template <class S> struct IsBF16 { static constexpr bool value = false; };
+template <> struct IsBF16<StoreBF16> { static constexpr bool value = true; };
 constexpr float kLargestE4M3 = 448.0f;
 
 struct BlockArgs {
@@ -32,21 +36,24 @@ struct BlockArgs {
     int vec;
 };
 
-__device__ __forceinline__ float block_factor(float amax, float* scale)
+// The factor that takes a block to its bytes (0: a block of zeros, whatever it holds), and its scale.  kSnap: an estimate of the reciprocal
+// (2^-23) does, see above.
+template <bool kSnap> __device__ __forceinline__ float block_factor(float amax, float* scale)
 {
     const bool finite = amax <= 3.40282347e+38f;                      // false for NaN too
     const bool some = amax >= 7.7037198e-34f;                         // 2^-110
     *scale = finite ? (some ? __fdiv_rn(amax, kLargestE4M3) : 0.0f) : __int_as_float(0x7fffffff);
-    return finite && some ? __fdiv_rn(kLargestE4M3, amax) : 0.0f;
+    return finite && some ? (kSnap ? (kLargestE4M3 * 0.0009765625f) * hw::rcp_approx(amax * 0.0009765625f)      // neither end of the range leaves fp32
+                                    : __fdiv_rn(kLargestE4M3, amax)) : 0.0f;
 }
 
-// four values to four bytes; kSnap: through 18 bits, see above.  A factor of 0 stands for a block of zeros, whatever x.
+// four values to four bytes; kSnap: through 18 bits, see above
 template <bool kSnap> __device__ __forceinline__ uint32_t block_bytes(const float* x, float factor)
 {
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        v[e] = factor == 0.0f ? 0.0f : __fmul_rn(x[e], factor);
+        v[e] = __fmul_rn(x[e], factor);
         if (kSnap) v[e] = __uint_as_float((__float_as_uint(v[e]) + 32u) & ~63u);
     }
     unsigned short lo, hi;
@@ -56,25 +63,48 @@ template <bool kSnap> __device__ __forceinline__ uint32_t block_bytes(const floa
 }
 template <class S> struct Snap { static constexpr bool value = S::kVec == 8; };
 
-// V values from element c of a row on (zeros behind its end)
-template <class S> __device__ __forceinline__ void block_load(const BlockArgs& a, size_t row, uint32_t c, float (&v)[S::kVec])
+// a packet's largest magnitude (NaN if it holds one); 16-bit values two at a time
+template <class S> __device__ __forceinline__ float packet_largest(const uint4& p)
+{
+    if constexpr (S::kVec == 4) {
+        float v[4];
+        S::unpack(p, v);
+        return larger(larger(fabsf(v[0]), fabsf(v[1])), larger(fabsf(v[2]), fabsf(v[3])));
+    } else {
+        using E2 = typename std::conditional<IsBF16<S>::value, __nv_bfloat162, __half2>::type;
+        auto two = [](uint32_t w) { w &= 0x7fff7fffu; return *reinterpret_cast<const E2*>(&w); };
+        const E2 m = __hmax2_nan(__hmax2_nan(two(p.x), two(p.y)), __hmax2_nan(two(p.z), two(p.w)));
+        return larger(S::load1(&m.x), S::load1(&m.y));
+    }
+}
+
+// V values from element c of a row on (zeros behind its end); returns their largest magnitude
+template <class S> __device__ __forceinline__ float block_load(const BlockArgs& a, size_t row, uint32_t c, float (&v)[S::kVec])
 {
     constexpr int V = S::kVec;
     const typename S::elem* x = static_cast<const typename S::elem*>(a.x) + row * a.cols + c;
+    float m = 0.0f;
     if (a.vec) {
-        S::unpack(c < a.cols ? load_packet(reinterpret_cast<const uint4*>(x)) : make_uint4(0, 0, 0, 0), v);
+        const uint4 p = c < a.cols ? load_packet(reinterpret_cast<const uint4*>(x)) : make_uint4(0, 0, 0, 0);
+        S::unpack(p, v);
+        m = packet_largest<S>(p);
     } else {
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = c + e < a.cols ? S::load1(x + e) : 0.0f;
+        for (int e = 0; e < V; ++e) {
+            v[e] = c + e < a.cols ? S::load1(x + e) : 0.0f;
+            m = larger(m, fabsf(v[e]));
+        }
     }
+    return m;
 }
 template <class S> __device__ __forceinline__ void block_store(const BlockArgs& a, size_t row, uint32_t c, const float (&v)[S::kVec], float factor)
 {
     constexpr int V = S::kVec;
     unsigned char* q = a.q + row * a.cols + c;
-    uint32_t w[V / 4];
+    uint32_t w[V / 4] = {};
+    if (factor != 0.0f)
 #pragma unroll
-    for (int i = 0; i < V / 4; ++i) w[i] = block_bytes<Snap<S>::value>(v + i * 4, factor);
+        for (int i = 0; i < V / 4; ++i) w[i] = block_bytes<Snap<S>::value>(v + i * 4, factor);
     if (a.vec) {
         if (c >= a.cols) return;
         if constexpr (V == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
@@ -86,7 +116,53 @@ template <class S> __device__ __forceinline__ void block_store(const BlockArgs& 
     }
 }
 
-// Groups of kBlockSide / V threads, a block of a row each; scale [groups, rows].
+// Rows on 16-byte boundaries: a group of kBlockSide / V threads has one block of each of kGroupRows rows, so that nothing is divided to find its
+// place, and one division makes the scales of all of them, a lane each.
+constexpr int kGroupRows = 4;
+template <class S> __global__ void __launch_bounds__(kBlock) quantize_row_groups_kernel(const __grid_constant__ BlockArgs a)
+{
+    constexpr int V = S::kVec, T = kBlockSide / V, U = kGroupRows;
+    asm volatile("griddepcontrol.wait;" ::: "memory");               // the order: see quantize_groups_kernel
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const uint32_t lane = threadIdx.x % T, group = (blockIdx.x * blockDim.x + threadIdx.x) / T, c = group * kBlockSide + lane * V;
+    const bool on = c < a.cols;                                       // else a thread behind the row's end, there for the shuffles
+    for (size_t row0 = size_t(blockIdx.y) * U; row0 < a.rows; row0 += size_t(gridDim.y) * U) {
+        const uint4* x = reinterpret_cast<const uint4*>(static_cast<const typename S::elem*>(a.x) + row0 * a.cols + c);
+        const size_t pitch = a.cols / V;
+        uint4 raw[U];
+        float m[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = on && row0 + u < a.rows ? load_packet(x + u * pitch) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) m[u] = packet_largest<S>(raw[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int o = T / 2; o > 0; o >>= 1) m[u] = larger(m[u], __shfl_xor_sync(0xffffffffu, m[u], o));
+        float mine = m[0];
+#pragma unroll
+        for (int u = 1; u < U; ++u) mine = lane == u ? m[u] : mine;
+        float scale;
+        const float f = block_factor<Snap<S>::value>(mine, &scale);
+        if (lane < U && group < a.groups && row0 + lane < a.rows) a.scale[size_t(group) * a.rows + row0 + lane] = scale;
+        unsigned char* q = a.q + row0 * a.cols + c;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float factor = __shfl_sync(0xffffffffu, f, u, T);
+            if (!on || row0 + u >= a.rows) continue;
+            float v[V];
+            S::unpack(raw[u], v);
+            uint32_t w[V / 4] = {};
+            if (factor != 0.0f)
+#pragma unroll
+                for (int i = 0; i < V / 4; ++i) w[i] = block_bytes<Snap<S>::value>(v + i * 4, factor);
+            if constexpr (V == 8) *reinterpret_cast<uint2*>(q + size_t(u) * a.cols) = make_uint2(w[0], w[1]);
+            else *reinterpret_cast<uint32_t*>(q + size_t(u) * a.cols) = w[0];
+        }
+    }
+}
+
+// Any rows: groups of kBlockSide / V threads, a block of a row each; scale [groups, rows].
 template <class S> __global__ void __launch_bounds__(kBlock) quantize_groups_kernel(const __grid_constant__ BlockArgs a)
 {
     constexpr int V = S::kVec, T = kBlockSide / V, U = 2;
@@ -107,20 +183,17 @@ template <class S> __global__ void __launch_bounds__(kBlock) quantize_groups_ker
             group[u] = uint32_t(i - row[u] * a.groups);
             c[u] = i < total ? group[u] * kBlockSide + lane * V : a.cols;
             if (i >= total) row[u] = 0;
-            block_load<S>(a, row[u], c[u], v[u]);
+            m[u] = block_load<S>(a, row[u], c[u], v[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            m[u] = 0.0f;
-#pragma unroll
-            for (int e = 0; e < V; ++e) m[u] = larger(m[u], fabsf(v[u][e]));
 #pragma unroll
             for (int o = T / 2; o > 0; o >>= 1) m[u] = larger(m[u], __shfl_xor_sync(0xffffffffu, m[u], o));
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float scale;
-            const float f = block_factor(m[u], &scale);
+            const float f = block_factor<Snap<S>::value>(m[u], &scale);
             if (lane == 0 && c[u] < a.cols) a.scale[size_t(group[u]) * a.rows + row[u]] = scale;
             block_store<S>(a, row[u], c[u], v[u], f);
         }
@@ -142,15 +215,8 @@ template <class S> __global__ void __launch_bounds__(kBlock) quantize_blocks_ker
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
         const uint32_t r = r0 + i * kRows;
-        if (r < a.matrix_rows) block_load<S>(a, matrix * a.matrix_rows + r, c, v[i]);
-        else
-#pragma unroll
-            for (int e = 0; e < V; ++e) v[i][e] = 0.0f;
+        if (r < a.matrix_rows) m = larger(m, block_load<S>(a, matrix * a.matrix_rows + r, c, v[i]));
     }
-#pragma unroll
-    for (int i = 0; i < kTurns; ++i)
-#pragma unroll
-        for (int e = 0; e < V; ++e) m = larger(m, fabsf(v[i][e]));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = larger(m, __shfl_xor_sync(0xffffffffu, m, o));
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
@@ -159,7 +225,7 @@ template <class S> __global__ void __launch_bounds__(kBlock) quantize_blocks_ker
 #pragma unroll
     for (int w = 1; w < kBlock / 32; ++w) m = larger(m, part[w]);
     float scale;
-    const float f = block_factor(m, &scale);
+    const float f = block_factor<Snap<S>::value>(m, &scale);
     if (threadIdx.x == 0) a.scale[blockIdx.x] = scale;
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
@@ -179,10 +245,17 @@ template <class S> BlockArgs block_args(const void* x, unsigned char* q, float* 
 template <class S> cudaError_t launch_quantize_groups(const void* x, unsigned char* q, float* scale, size_t rows, uint32_t cols, cudaStream_t st)
 {
     const BlockArgs a = block_args<S>(x, q, scale, rows, 0, cols);
-    constexpr size_t per = kBlock / (kBlockSide / S::kVec) * 2;
-    const size_t grid = (rows * a.groups + per - 1) / per;
     cudaLaunchConfig_t cfg;
     cudaLaunchAttribute attr[1];
+    if (a.vec) {
+        const uint32_t threads = (a.groups * (kBlockSide / S::kVec) + 31) / 32 * 32, block = threads < kBlock ? threads : kBlock;
+        const size_t runs = (rows + kGroupRows - 1) / kGroupRows;
+        norm_launch_config(&cfg, attr, (threads + block - 1) / block, block, st);
+        cfg.gridDim.y = unsigned(runs < 65535 ? runs : 65535);
+        return cudaLaunchKernelEx(&cfg, quantize_row_groups_kernel<S>, a);
+    }
+    constexpr size_t per = kBlock / (kBlockSide / S::kVec) * 2;
+    const size_t grid = (rows * a.groups + per - 1) / per;
     norm_launch_config(&cfg, attr, grid < 0x7fffffff ? grid : 0x7fffffff, kBlock, st);
     return cudaLaunchKernelEx(&cfg, quantize_groups_kernel<S>, a);
 }

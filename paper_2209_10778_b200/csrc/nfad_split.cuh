@@ -124,6 +124,7 @@ split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtenso
         }
     } else if (warp == 1) {
         const uint32_t what = tc::instruction(Kind::kBytes ? tc::kNumberS8 : IsBF16<S>::value ? tc::kNumberBF16 : tc::kNumberF16, Kind::kTurnA, Kind::kTurnB, kTileRows, n);
+        const bool leader = tc::elected();
         int stage = 0;
         uint32_t phase = 0, landed_phases = 0;
         for (int r = r0; r < r1; r += kStep) {
@@ -135,10 +136,10 @@ split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtenso
                 __syncwarp();
                 if (lane < 2) tc::barrier_arrive(full(stage));
             }
-            if (!(ok = tc::barrier_wait(full(stage), phase, gave_up))) break;
+            if (!(ok = tc::barrier_poll(full(stage), phase, gave_up))) break;
             tc::fence_after_sync();
             const uint32_t at_a = ring_at + stage * kSplitStage, at_b = at_a + kTileRows * kStepBytes;
-            if (lane == 0) {
+            if (leader) {
 #pragma unroll
                 for (int k = 0; k < kStepBytes / 32; ++k) {
                     if (OP == kProdWeight && k * kProductRows >= q.r_end - r) break;
@@ -152,7 +153,7 @@ split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtenso
             if (++stage == kSplitStages) { stage = 0; phase ^= 1; }
         }
         // every product issued is done when this arrives, after a wait that ran out too
-        if (lane == 0) tc::products_to<false>(done);
+        if (leader) tc::products_to<false>(done);
         __syncwarp();
     }
     // every CTA's sums into its own shared memory: the ring is free once its products are done

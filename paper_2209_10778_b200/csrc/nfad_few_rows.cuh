@@ -20,7 +20,7 @@ constexpr int kFewSteps = 4;                        // of 64 bytes of each row: 
 constexpr int kFewMaxRows = 256;
 
 // d += a b of four 8-bit floating-point values each, as two pairs of halves, which hold them exactly.  (The instruction for 8-bit operands itself
-// spills 172 bytes a thread and took 46 us for one token, 4096 -> 2 x 14336, where this takes 32.)
+// spills 172 bytes a thread and took 46 us for one token, 4096 -> 2 x 14336, where this takes 28.)
 __device__ __forceinline__ void few_product_e4m3(float (&f)[4], uint32_t lo, uint32_t hi, uint32_t x)
 {
     asm volatile("{\n .reg .b16 l, h;\n .reg .b32 a0, a1, a2, a3, b0, b1;\n"
@@ -298,7 +298,8 @@ template <int OP, class S, int NT> cudaError_t launch_few_rows_tiles(const ProdA
     constexpr int kOutputs = kFewOutputs / ProdKind<OP>::kPerResult;
     const size_t jobs = (g.outs + kOutputs - 1) / kOutputs * live, fit = size_t(sms) * FewResident<OP, NT>::value;
     // one expert, whose jobs are known: as many for each CTA, rather than a last turn of a few (13.3 -> 12.6 us); else all that fit
-    const size_t turns = g.experts == 1 ? (jobs + fit - 1) / fit : 1, grid = (jobs + turns - 1) / turns;
+    // (beside block scales, whose conversions want every warp that fits, they cost more than the last turn: 28 -> 32 us)
+    const size_t turns = g.experts == 1 && !ProdKind<OP>::kScaled ? (jobs + fit - 1) / fit : 1, grid = (jobs + turns - 1) / turns;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(grid < fit ? grid : fit));
     cfg.blockDim = dim3(kFewWarps * 32);

@@ -110,7 +110,7 @@ template <int OP, class S> cudaError_t launch_scaled_store(const ProdArgs& g, cu
     // a tensor copy needs rows that begin on 16-byte boundaries (and something to copy)
     if (low % 16 || g.in == 0) return launch_scaled_tile<OP, 64, S, true>(g, di.sm_count, st);
     // Up to eight rows, a column each of the small matrix instruction.  Against tiles (us): 8 rows 4096 -> 4096 10.3 (14.3 split over 4), gated
-    // 4096 -> 2 x 14336 36.9 (34.8), 1 row of it 32.4 (36.7); with two such groups 16 rows of it took 57 (34.8).
+    // 4096 -> 2 x 14336 36.9 (34.8), 1 row of it 28.3 (36.7); with two such groups 16 rows of it took 57 (34.8).
     if (few_rows(g) && g.rows <= 8) return launch_few_rows_tiles<OP, S, 1>(g, di.sm_count, g.b_ready, st);
     if (const unsigned ranks = scaled_split_ranks<OP>(g, di.sm_count)) return launch_scaled_split<OP, S>(g, ranks, st);
     switch (product_tile<OP>(g, di.sm_count)) {

@@ -354,3 +354,40 @@ def test_refusals():
                 lambda: nfad.nfad_f8_linear(None, xq.cpu(), xs, wq, ws, None, y)):
         with pytest.raises(TypeError):
             bad()
+
+
+@pytest.mark.parametrize("rows,n_in,n_out,gated", [(300, 1024, 4100, False), (2600, 384, 1036, True), (1500, 256, 2500, False), (520, 640, 1100, True)])
+def test_results_off_the_packets(rows, n_in, n_out, gated):
+    # rows of results that no tensor copy can store, in every tile width
+    xq, xs, wq, ws = _case(rows, n_in, n_out, gated, 21)
+    bias = W.normal(2 * n_out, "bf16", 1, 0.5).view(2, n_out)
+    bias = bias if gated else bias[0].contiguous()
+    _check("gelu_tanh", xq, xs, wq, ws, bias, _run("gelu_tanh", xq, xs, wq, ws, bias, "bf16"))
+
+
+def test_several_calls_at_once():
+    # streams with their own results and scratch side by side, several times over: each call's bits are those of the call alone
+    cases = [(1, 4096, 1000, True), (40, 2064, 520, False), (300, 512, 1032, True), (900, 1024, 1536, False), (50, 300, 130, True)]
+    calls = []
+    for i, (rows, n_in, n_out, gated) in enumerate(cases):
+        x = W.normal(rows * n_in, "bf16", i, 1.0).view(rows, n_in).to(DEV)
+        w = W.normal((2 if gated else 1) * n_out * n_in, "bf16", 50 + i, n_in ** -0.5).view((2, n_out, n_in) if gated else (n_out, n_in)).to(DEV)
+        wq = torch.empty(w.shape, dtype=F8, device=DEV)
+        ws = torch.empty(*w.shape[:-2], _blocks(n_out), _blocks(n_in), device=DEV)
+        nfad.nfad_f8_quantize_blocks(w, wq, ws)
+        call = nfad.nfad_f8_gated_linear_dynamic if gated else nfad.nfad_f8_linear_dynamic
+        y, scratch = torch.empty(rows, n_out, dtype=torch.bfloat16, device=DEV), nfad.nfad_f8_linear_dynamic_scratch(x)
+        calls.append(lambda y=y, call=call, x=x, wq=wq, ws=ws, scratch=scratch: (call("swish", x, wq, ws, None, y, scratch), y)[1])
+    alone = [c().clone() for c in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(5):
+        got = []
+        for c, s in zip(calls, streams):
+            with torch.cuda.stream(s):
+                for _ in range(3):
+                    y = c().fill_(0)
+                got.append(c())
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, want) for y, want in zip(got, alone))
+    assert nfad.nfad_wait_faults() == 0

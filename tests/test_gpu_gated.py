@@ -358,3 +358,36 @@ def test_refusals():
     scratch = nfad.nfad_expert_act_backward_scratch(big_both.flatten(1))
     assert status(lambda: nfad.nfad_expert_gated_backward(big, big_both, off, big_both, gb, scratch[:16])) == 7
     assert status(lambda: nfad.nfad_expert_gated_backward(big, big_both, off, big_both, gb, None)) == 3
+
+
+@pytest.mark.parametrize("way", [0, 3, 5, 7, 9, 11])
+def test_the_same_bits_every_time(way):
+    counts, lead, tail, n_in, n_out = WAYS[way]
+    x, w, b, off, o = _case(WAYS[way], "bf16", 400 + way)
+    first = _forward("mish", x, w, b, off)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    dx, dw, db, doff = x.to(DEV), w.to(DEV), b.to(DEV), off.to(DEV)
+    torch.cuda.synchronize()
+    results = []
+    for s in streams:                                                 # three calls at once
+        with torch.cuda.stream(s):
+            y, both = _nan(x.shape[0], n_out, dtype=x.dtype), _nan(x.shape[0], 2, n_out, dtype=x.dtype)
+            nfad.nfad_expert_gated_linear("mish", dx, dw, db, doff, y, both)
+            results.append((y, both))
+    torch.cuda.synchronize()
+    for r in results:
+        assert torch.equal(r[0], first[0]) and torch.equal(r[1], first[1])
+    assert nfad.nfad_wait_faults() == 0
+
+
+def test_non_finite_values_take_their_way():
+    # an infinity in a row of x makes both projections infinite or NaN there, and nothing elsewhere; a value with the same sign on both sides
+    # keeps y = f(a) u what the formula gives
+    x, w, b, off, o = _case(([40], 0, 0, 64, 72), "bf16", 7)
+    x[3, 5], x[7, 9] = float("inf"), float("nan")
+    y, both = (t.cpu() for t in _forward("swish", x, w, b, off))
+    assert not torch.isfinite(both[3, 1][w[0, 0, :, 5] > 0]).any() and torch.isnan(y[7]).all() and torch.isnan(both[7]).all()
+    keep = [r for r in range(40) if r not in (3, 7)]
+    assert torch.isfinite(y[keep]).all()
+    gate_up = (w[0, 0, :, 5] > 0) & (w[0, 1, :, 5] > 0)
+    assert (y[3][gate_up] == float("inf")).all()

@@ -225,12 +225,12 @@ __global__ void __launch_bounds__(kFewWarps * 32, FewResident<OP, NT>::value) fe
 #pragma unroll
                         for (int e = 0; e < 4; ++e) acc[n][e] = __float_as_uint(fmaf(__uint_as_float(part[e]), scale[e], __uint_as_float(acc[n][e])));
                     }
-                    continue;
-                }
+                } else {
 #pragma unroll
-                for (int i = 0; i < kFewSteps; ++i) {
-                    few_product<kNumber>(acc[n], lo[i].x, hi[i].x, lo[i].y, hi[i].y, v[i].x, v[i].y);
-                    few_product<kNumber>(acc[n], lo[i].z, hi[i].z, lo[i].w, hi[i].w, v[i].z, v[i].w);
+                    for (int i = 0; i < kFewSteps; ++i) {
+                        few_product<kNumber>(acc[n], lo[i].x, hi[i].x, lo[i].y, hi[i].y, v[i].x, v[i].y);
+                        few_product<kNumber>(acc[n], lo[i].z, hi[i].z, lo[i].w, hi[i].w, v[i].z, v[i].w);
+                    }
                 }
             }
             if (b + kFewWarps < blocks) request(job, b + kFewWarps);

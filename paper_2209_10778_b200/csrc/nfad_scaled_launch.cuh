@@ -88,9 +88,9 @@ template <int OP, class S> cudaError_t launch_scaled_split(const ProdArgs& g, un
 }
 
 // Over how many CTAs a tile's reduction is split (0: not at all; tiles of another size, which CTAs walk over): as many as one to an SM allows,
-// with eight blocks left for each.  Measured (us, against tiles that are walked over): 100 rows 4096 -> 2048 over 4: 14.3 (22.5), over 8: 20.6;
-// 400 rows 4096 -> 1024 over 2: 17.2 (22.5); 40 rows 8192 -> 4096 over 2: 22.5 (33.7); gated 200 rows 4096 -> 2 x 1024 over 2: 18.4 (20.4).
-// One CTA to a tile of this size was never the fastest (40 rows 4096 -> 28672: 45, by tiles of 128 34.8).
+// with eight blocks left for each.  Measured (us, against tiles that are walked over): 100 rows 4096 -> 1024 over 4: 14.3 (17.5), over 8: 18.4;
+// 400 rows 4096 -> 1024 over 2: 17.2 (19.4), over 4: 19.4; 40 rows 8192 -> 2048 over 4: 18.4 (26.6); gated 100 rows 8192 -> 2 x 2048 over 2:
+// 25.5 (27.6).  One CTA to a tile of this size was never the fastest (40 rows 4096 -> 28672: 43, by tiles of 128 33.8).
 template <int OP> unsigned scaled_split_ranks(const ProdArgs& g, int sms)
 {
     if (g.outs % 8 || (reinterpret_cast<uintptr_t>(g.out) | reinterpret_cast<uintptr_t>(g.bias)) % 16) return 0;      // its results go by packets
@@ -109,8 +109,8 @@ template <int OP, class S> cudaError_t launch_scaled_store(const ProdArgs& g, cu
     const uintptr_t low = reinterpret_cast<uintptr_t>(g.a) | reinterpret_cast<uintptr_t>(g.b) | uintptr_t(g.in);
     // a tensor copy needs rows that begin on 16-byte boundaries (and something to copy)
     if (low % 16 || g.in == 0) return launch_scaled_tile<OP, 64, S, true>(g, di.sm_count, st);
-    // Up to eight rows, a column each of the small matrix instruction.  Against tiles (us): 8 rows 4096 -> 4096 10.3 (14.3 split over 4), gated
-    // 4096 -> 2 x 14336 36.9 (34.8), 1 row of it 28.3 (36.7); with two such groups 16 rows of it took 57 (34.8).
+    // Up to eight rows, a column each of the small matrix instruction.  Against tiles (us): 8 rows 4096 -> 4096 11.1 (14.3 split over 4), gated
+    // 4096 -> 2 x 14336 32.9 (35.8), 1 row of it 31.7 (37.7); with two such groups 16 rows of it took 57 when tiles took 34.8.
     if (few_rows(g) && g.rows <= 8) return launch_few_rows_tiles<OP, S, 1>(g, di.sm_count, g.b_ready, st);
     if (const unsigned ranks = scaled_split_ranks<OP>(g, di.sm_count)) return launch_scaled_split<OP, S>(g, ranks, st);
     switch (product_tile<OP>(g, di.sm_count)) {

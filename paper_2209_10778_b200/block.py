@@ -168,11 +168,12 @@ class Dropout:
     """A mask: ``nfad_dropout_mask`` with the tensor it points to.
 
     p in [0, 1] (held to a multiple of 2^-16); seed and offset: 64-bit integers; step: None, or an int64 CUDA tensor of one value that is
-    added to offset when a call runs.  The same numbers give the same mask; layers and steps differ in offset (or step).
+    added to offset when a call runs.  The same numbers give the same mask; layers and steps differ in offset (or step).  None of the four
+    can be set on a mask that exists: its backward pass draws by the same object, or by its numbers.  Another mask is another object.
     """
 
     def __init__(self, p: float, seed: int, offset: int = 0, step: Optional[torch.Tensor] = None):
-        self.p, self.seed, self.offset, self.step = float(p), int(seed), int(offset), step
+        self._p, self._seed, self._offset, self._step = float(p), int(seed), int(offset), step
         if not 0.0 <= self.p <= 1.0:
             raise ValueError("p must be in [0, 1]")
         if not (0 <= self.seed < 2 ** 64 and 0 <= self.offset < 2 ** 64):
@@ -184,6 +185,11 @@ class Dropout:
                 raise ValueError("step must hold one value")
         self.desc = DropoutMask(self.p, self.seed, self.offset, None if step is None else step.data_ptr())
         self.ref = ctypes.byref(self.desc)
+
+    p = property(lambda self: self._p)
+    seed = property(lambda self: self._seed)
+    offset = property(lambda self: self._offset)
+    step = property(lambda self: self._step)
 
 
 def _mask(drop: Dropout, x: torch.Tensor):

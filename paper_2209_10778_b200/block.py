@@ -183,7 +183,7 @@ class Dropout:
                 raise TypeError("step must be an int64 CUDA tensor")
             if step.numel() != 1:
                 raise ValueError("step must hold one value")
-        self.desc = DropoutMask(self.p, self.seed, self.offset, None if step is None else step.data_ptr())
+        self.desc = DropoutMask(self.p, self.seed, self.offset, None)      # the step's address is filled in by each call
         self.ref = ctypes.byref(self.desc)
 
     p = property(lambda self: self._p)
@@ -195,8 +195,10 @@ class Dropout:
 def _mask(drop: Dropout, x: torch.Tensor):
     if not isinstance(drop, Dropout):
         raise TypeError("drop must be a Dropout")
-    if drop.step is not None and drop.step.get_device() != x.get_device():
-        raise ValueError("the mask's step must be on the tensors' device")
+    if drop.step is not None:
+        if drop.step.get_device() != x.get_device():
+            raise ValueError("the mask's step must be on the tensors' device")
+        drop.desc.step = drop.step.data_ptr()            # where it is now: a tensor's storage can be exchanged
     return drop.ref
 
 

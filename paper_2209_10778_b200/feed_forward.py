@@ -89,7 +89,7 @@ class ServingBlock:
         self.norm = ops.BlockNorm(post="rms", pre="rms", residual_scale=block.residual_scale,
                                   **{k: getattr(block, k).detach().clone() for k in ("post_gain", "gate", "pre_gain")})
         self.kind, self.dtype = block.kind, block.w1.dtype
-        self._rows = 0
+        self._rows = -1                                               # none seen, not even none
 
     def _quantized(self, w):
         q, s = torch.empty(w.shape[1:], dtype=torch.int8, device=w.device), torch.empty(w.shape[1], device=w.device)

@@ -78,8 +78,8 @@ class GatedFeedForwardBlock(FeedForwardBlock):
 
 class ServingBlock:
     """A one-expert block's value-only pass with its weights in 8-bit integers: a scale for each output channel, formed here once,
-    and for each token, formed on the way.  Everything is a copy: training the block on changes nothing here.  Keeps its buffers for
-    the largest number of rows seen."""
+    and for each token, formed on the way.  Everything is a copy: training the block on changes nothing here.  Keeps buffers for the
+    largest number of rows seen, for each CUDA stream that it is called on."""
 
     def __init__(self, block: FeedForwardBlock):
         if block.w1.shape[0] != 1:
@@ -89,7 +89,7 @@ class ServingBlock:
         self.norm = ops.BlockNorm(post="rms", pre="rms", residual_scale=block.residual_scale,
                                   **{k: getattr(block, k).detach().clone() for k in ("post_gain", "gate", "pre_gain")})
         self.kind, self.dtype = block.kind, block.w1.dtype
-        self._rows = -1                                               # none seen, not even none
+        self._kept = {}                                               # stream -> (rows, tensors)
 
     def _quantized(self, w):
         q, s = torch.empty(w.shape[1:], dtype=torch.int8, device=w.device), torch.empty(w.shape[1], device=w.device)
@@ -99,22 +99,36 @@ class ServingBlock:
     def _scratch_bytes(self, rows: int, n: int) -> int:
         return ops.nfad_i8_linear_dynamic_scratch_bytes(rows, n)
 
-    def _products(self, h, y1, u):
-        ops.nfad_i8_linear_dynamic(self.kind, h, self.q1, self.s1, self.b1, y1, self._scratch)
-        ops.nfad_i8_linear_dynamic(None, y1, self.q2, self.s2, self.b2, u, self._scratch)
+    def _products(self, h, y1, u, scratch):
+        ops.nfad_i8_linear_dynamic(self.kind, h, self.q1, self.s1, self.b1, y1, scratch)
+        ops.nfad_i8_linear_dynamic(None, y1, self.q2, self.s2, self.b2, u, scratch)
+
+    def _make(self, rows: int):
+        dev, width, hidden = self.q1.device, *self.q2.shape
+        size = max(self._scratch_bytes(rows, n) for n in (width, hidden))
+        return (*(torch.empty(rows, n, dtype=self.dtype, device=dev) for n in (hidden, width, width)),
+                torch.empty(max(size, 16), dtype=torch.uint8, device=dev))
 
     def _buffers(self, rows: int):
-        if rows > self._rows:
-            dev, width, hidden = self.q1.device, *self.q2.shape
-            self._y1, self._u, self._h = (torch.empty(rows, n, dtype=self.dtype, device=dev) for n in (hidden, width, width))
-            size = max(self._scratch_bytes(rows, n) for n in (width, hidden))
-            self._scratch, self._rows = torch.empty(max(size, 16), dtype=torch.uint8, device=dev), rows
-        return self._y1[:rows], self._u[:rows], self._h[:rows]
+        """y1, u, h and scratch: what the current stream keeps, which no other stream writes and which is given back in its order.  A captured
+        call has its own, in the memory of its graph: a replay may come at any time later."""
+        dev = self.q1.device
+        if dev.index is not None and dev.index != torch.cuda.current_device():
+            with torch.cuda.device(dev):
+                return self._buffers(rows)
+        if torch.cuda.is_current_stream_capturing():
+            return self._make(rows)
+        at = torch.cuda.current_stream().cuda_stream
+        most, kept = self._kept.get(at, (-1, None))
+        if rows > most:
+            kept = self._make(rows)
+            self._kept[at] = rows, kept
+        return (*(t[:rows] for t in kept[:3]), kept[3])
 
     def __call__(self, stream: torch.Tensor, h: torch.Tensor) -> torch.Tensor:
-        """Adds the block to `stream` in place and returns the next block's input (valid until the next call)."""
-        y1, u, out = self._buffers(h.shape[0])
-        self._products(h, y1, u)
+        """Adds the block to `stream` in place and returns the next block's input (valid until the next call on this CUDA stream)."""
+        y1, u, out, scratch = self._buffers(h.shape[0])
+        self._products(h, y1, u, scratch)
         ops.nfad_block_norm_forward(self.norm, u, stream, stream, out)
         return out
 
@@ -134,9 +148,9 @@ class GatedServingBlock(ServingBlock):
     def _scratch_bytes(self, rows: int, n: int) -> int:
         return ops.nfad_f8_linear_dynamic_scratch_bytes(rows, n)
 
-    def _products(self, h, y1, u):
-        ops.nfad_f8_gated_linear_dynamic(self.kind, h, self.q1, self.s1, self.b1, y1, self._scratch)
-        ops.nfad_f8_linear_dynamic(None, y1, self.q2, self.s2, self.b2, u, self._scratch)
+    def _products(self, h, y1, u, scratch):
+        ops.nfad_f8_gated_linear_dynamic(self.kind, h, self.q1, self.s1, self.b1, y1, scratch)
+        ops.nfad_f8_linear_dynamic(None, y1, self.q2, self.s2, self.b2, u, scratch)
 
 
 def main() -> None:

@@ -1,4 +1,5 @@
-"""The serving blocks called as a program may call them: with no rows, for one."""
+"""The serving blocks called as a program may call them: captured calls beside larger ones, two streams at once, no rows; and the copy
+that they are of the block."""
 import pytest
 import torch
 
@@ -24,6 +25,52 @@ def _serve(serve, x):
     stream = x.clone()
     h = serve(stream, x)
     return stream, h.clone()
+
+
+@pytest.mark.parametrize("make", BLOCKS)
+def test_captured_calls_outlive_larger_ones(make):
+    serve = _block(make).serving()
+    xs = [_rows(8, 1), _rows(8, 2)]
+    want = [_serve(serve, x) for x in xs]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for x in xs:
+        stream = torch.empty_like(x)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            stream.copy_(x)
+            outs.append((stream, serve(stream, x)))
+        graphs.append(g)
+    large = _serve(serve, _rows(300, 3))                              # keeps larger buffers from now on
+    noise = [torch.full((1 << 16,), float("nan"), device=DEV) for _ in range(64)]      # whatever was given back has another owner now
+    torch.cuda.synchronize()
+    for _ in range(2):
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for out, w in zip(outs, want):
+            assert all(torch.equal(a, b) for a, b in zip(out, w))
+    assert all(torch.isnan(t).all() for t in noise)
+    assert all(torch.equal(a, b) for a, b in zip(_serve(serve, _rows(300, 3)), large))
+
+
+@pytest.mark.parametrize("make", BLOCKS)
+def test_two_streams_at_once(make):
+    serve = _block(make).serving()
+    xs = [_rows(200, 1), _rows(70, 2)]
+    want = [_serve(serve, x) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    for _ in range(5):
+        got = []
+        for x, s in zip(xs, streams):
+            with torch.cuda.stream(s):
+                for _ in range(3):
+                    out = _serve(serve, x)
+                got.append(out)
+        torch.cuda.synchronize()
+        for out, w in zip(got, want):
+            assert all(torch.equal(a, b) for a, b in zip(out, w))
 
 
 @pytest.mark.parametrize("make", BLOCKS)

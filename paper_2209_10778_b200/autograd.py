@@ -235,15 +235,36 @@ def expert_feed_forward(x, w1, b1, w2, b2, offsets, kind="gelu_erf"):
     return ExpertFeedForward.apply(x, w1, b1, w2, b2, offsets, kind)
 
 
+def _differentiated(*tensors):
+    """Whether a gradient can be asked for: else nothing is kept, and the derivatives are neither formed nor stored."""
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+def _contiguous(t):
+    return None if t is None else t.contiguous()
+
+
+def _gated_layer(x, w, bias, offsets, kind, train):
+    """f(a) u and, in a pass that will be differentiated, its two derivatives; contiguous tensors."""
+    y = torch.empty(x.shape[0], w.shape[2], dtype=x.dtype, device=x.device)
+    both = torch.empty(x.shape[0], 2, w.shape[2], dtype=x.dtype, device=x.device) if train else None
+    block.nfad_expert_gated_linear(kind, x, w, bias, offsets, y, both)
+    return y, both
+
+
+def _second_layer(y1, w, bias, offsets):
+    y = torch.empty(y1.shape[0], w.shape[1], dtype=y1.dtype, device=y1.device)
+    block.nfad_expert_linear(None, y1, w, bias, offsets, y)
+    return y
+
+
 class ExpertGatedLinear(torch.autograd.Function):
     """y = f(a) u, a and u the products with the two weights, for rows grouped by expert; saved: x, w and y's two derivatives (no a, no u)."""
 
     @staticmethod
     def forward(ctx, x, w, bias, offsets, kind):
-        xc, wc, bc = x.contiguous(), w.contiguous(), None if bias is None else bias.contiguous()
-        y = torch.empty(xc.shape[0], wc.shape[2], dtype=xc.dtype, device=xc.device)
-        both = torch.empty(xc.shape[0], 2, wc.shape[2], dtype=xc.dtype, device=xc.device)
-        block.nfad_expert_gated_linear(kind, xc, wc, bc, offsets, y, both)
+        xc, wc = x.contiguous(), w.contiguous()
+        y, both = _gated_layer(xc, wc, _contiguous(bias), offsets, kind, True)
         ctx.save_for_backward(xc, wc, offsets, both)
         ctx.bias_dtype = None if bias is None else bias.dtype
         return y
@@ -275,6 +296,8 @@ def _gated_products(gz, x, w, offsets, need):
 
 def expert_gated_linear(x, w, bias, offsets, kind="swish"):
     """x [rows, in] sorted by expert, w [experts, 2, out, in] (the gate's first), bias [experts, 2, out] or None, offsets int32 [experts + 1]."""
+    if not _differentiated(x, w, bias):
+        return _gated_layer(x.contiguous(), w.contiguous(), _contiguous(bias), offsets, kind, False)[0]
     return ExpertGatedLinear.apply(x, w, bias, offsets, kind)
 
 
@@ -285,12 +308,8 @@ class ExpertGatedFeedForward(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w1, b1, w2, b2, offsets, kind):
         xc, w1c, w2c = x.contiguous(), w1.contiguous(), w2.contiguous()
-        rows, hidden = xc.shape[0], w1c.shape[2]
-        y1 = torch.empty(rows, hidden, dtype=xc.dtype, device=xc.device)
-        both = torch.empty(rows, 2, hidden, dtype=xc.dtype, device=xc.device)
-        block.nfad_expert_gated_linear(kind, xc, w1c, None if b1 is None else b1.contiguous(), offsets, y1, both)
-        y2 = torch.empty(rows, w2c.shape[1], dtype=xc.dtype, device=xc.device)
-        block.nfad_expert_linear(None, y1, w2c, None if b2 is None else b2.contiguous(), offsets, y2)
+        y1, both = _gated_layer(xc, w1c, _contiguous(b1), offsets, kind, True)
+        y2 = _second_layer(y1, w2c, _contiguous(b2), offsets)
         ctx.save_for_backward(xc, y1, both, w1c, w2c, offsets)
         ctx.bias_dtypes = [None if b is None else b.dtype for b in (b1, b2)]
         return y2
@@ -317,6 +336,9 @@ class ExpertGatedFeedForward(torch.autograd.Function):
 
 def expert_gated_feed_forward(x, w1, b1, w2, b2, offsets, kind="swish"):
     """A gated layer and a linear one: w1 [experts, 2, hidden, in] (the gate's first), w2 [experts, out, hidden]."""
+    if not _differentiated(x, w1, b1, w2, b2):
+        y1, _ = _gated_layer(x.contiguous(), w1.contiguous(), _contiguous(b1), offsets, kind, False)
+        return _second_layer(y1, w2.contiguous(), _contiguous(b2), offsets)
     return ExpertGatedFeedForward.apply(x, w1, b1, w2, b2, offsets, kind)
 
 

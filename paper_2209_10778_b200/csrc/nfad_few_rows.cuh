@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, FewResident<OP, NT>::value) fe
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         if (!kGated && e) sw[h][e] = sw[h][0];
-                        else sw[h][e] = b * 2 + h < in_blocks ? __ldg(g.b_scale + (size_t(e ? (g.outs + 127) / 128 : 0) + o0 / 128) * in_blocks + b * 2 + h) : 0.0f;
+                        else sw[h][e] = b * 2 + h < in_blocks ? g.b_scale[(size_t(e ? (g.outs + 127) / 128 : 0) + o0 / 128) * in_blocks + b * 2 + h] : 0.0f;
                     }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, FewResident<OP, NT>::value) fe
                 int t = 0;
 #pragma unroll
                 for (int k = 0; k < kFewWarps; ++k) t += int(sums[k][i % kOutputs][token]);
-                z = float(t) * (g.a_scale[row] * __ldg(g.b_scale + o));
+                z = float(t) * (g.a_scale[row] * g.b_scale[o]);
             } else {
                 z = 0.0f;
 #pragma unroll

@@ -182,7 +182,8 @@ __device__ __forceinline__ void clear_runs(unsigned char* at, int runs, int keep
 // Not turned: 128 rows of the operand's own dimension, 128 bytes of the reduction.  Turned: two boxes of 64 reduction steps (128
 // for bytes there are none) by 128 bytes along the own dimension.  Elements outside read as zeros.  A packet that starts
 // anywhere comes from the two aligned ones that hold it, shifted; at the ends of a row and of the whole operand ([begin, end))
-// it comes element by element.
+// it comes element by element.  (By ordinary loads, not the read-only path: a kernel in front that has not ended yet when this one begins may
+// write either operand.)
 struct GatherSource {
     const unsigned char *begin, *end, *at;
     uint32_t pitch;
@@ -214,8 +215,8 @@ template <int ES, bool kTurn, bool kHalves = false, int kRows = kTileRows> struc
             lo[j] = hi[j] = make_uint4(0, 0, 0, 0);
             if (n >= PER && q >= src.begin && q + (p == q ? 16 : 32) <= src.end) {
                 whole |= 1u << j;
-                lo[j] = __ldg(reinterpret_cast<const uint4*>(q));
-                if (p != q) hi[j] = __ldg(reinterpret_cast<const uint4*>(q) + 1);
+                lo[j] = *reinterpret_cast<const uint4*>(q);
+                if (p != q) hi[j] = reinterpret_cast<const uint4*>(q)[1];
             }
         }
     }
@@ -245,8 +246,8 @@ template <int ES, bool kTurn, bool kHalves = false, int kRows = kTileRows> struc
 #pragma unroll
                 for (int e = 0; e < PER; ++e)
                     if (e < n) {
-                        if (ES == 2) w[e >> 1] |= uint32_t(__ldg(reinterpret_cast<const unsigned short*>(p) + e)) << (16 * (e & 1));
-                        else w[e >> 2] |= uint32_t(__ldg(p + e)) << (8 * (e & 3));
+                        if (ES == 2) w[e >> 1] |= uint32_t(reinterpret_cast<const unsigned short*>(p)[e]) << (16 * (e & 1));
+                        else w[e >> 2] |= uint32_t(p[e]) << (8 * (e & 3));
                     }
                 v = make_uint4(w[0], w[1], w[2], w[3]);
             }
@@ -688,7 +689,7 @@ product_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUten
                     const typename S::elem* own = static_cast<const typename S::elem*>(g.bias) + size_t(q.expert) * width * Kind::kPerResult + col;
                     bias[j] = g.bias && inside ? S::load1(own) : 0.0f;
                     if (Kind::kGated) scales[j] = g.bias && inside ? S::load1(own + width) : 0.0f;
-                    else scales[j] = Kind::kBytes && inside ? __ldg(g.b_scale + col) : 0.0f;
+                    else scales[j] = Kind::kBytes && inside ? g.b_scale[col] : 0.0f;
                 }
 #pragma unroll
                 for (int j = 0; j < kOwnChunks; ++j) {

@@ -81,10 +81,12 @@ __device__ __forceinline__ uint32_t fresh(uint32_t v)
 }
 
 // A load that stays where it stands: left to itself it sinks to its use, a step later, and every step waits for it (500 of 1000 cycles).
+// (An ordinary one, like all loads of what a kernel in front may write: these kernels begin before that one has ended, and the read-only
+// path asks for data that nothing writes while the kernel lives.)
 __device__ __forceinline__ float load_now(const float* p)
 {
     float v;
-    asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v) : "l"(p));
+    asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
     return v;
 }
 

@@ -239,7 +239,7 @@ split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtenso
             if (Kind::kBytes) {
                 const float scale = g.a_scale[q.a0 + row];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) z[e] = float(t[e]) * (scale * __ldg(g.b_scale + col + e));
+                for (int e = 0; e < 8; ++e) z[e] = float(t[e]) * (scale * g.b_scale[col + e]);
             }
             float f[8];
             if (Kind::kForward && g.bias) {

@@ -79,3 +79,21 @@ def test_no_rows_first(make):
     for n in (0, 3, 0):
         stream, h = _serve(serve, _rows(n, 1))
         assert stream.shape == h.shape == (n, 128)
+
+
+@pytest.mark.parametrize("make", BLOCKS)
+def test_the_copy_does_not_follow_the_block(make):
+    block = _block(make)
+    with torch.no_grad():
+        for b in (block.b1, block.b2):
+            b.normal_()
+    serve, x = block.serving(), _rows(9, 1)
+    everything = torch.tensor([0, 9], dtype=torch.int32, device=DEV)
+    with torch.no_grad():
+        want, own = _serve(serve, x), block(x, x, everything)
+        for p in block.parameters():
+            before = p.clone()
+            p.mul_(-0.5).add_(0.25)
+            assert not torch.equal(p, before)
+            assert all(torch.equal(a, b) for a, b in zip(_serve(serve, x), want))
+        assert not any(torch.equal(a, b) for a, b in zip(block(x, x, everything), own))

@@ -78,13 +78,13 @@ template <class S> __device__ __forceinline__ float packet_largest(const uint4& 
     }
 }
 
-// V values from element c of a row on (zeros behind its end); returns their largest magnitude
-template <class S> __device__ __forceinline__ float block_load(const BlockArgs& a, size_t row, uint32_t c, float (&v)[S::kVec])
+// V values from element c of a row on (zeros behind its end); returns their largest magnitude.  vec: rows begin on 16-byte boundaries
+template <class S> __device__ __forceinline__ float block_load(const BlockArgs& a, bool vec, size_t row, uint32_t c, float (&v)[S::kVec])
 {
     constexpr int V = S::kVec;
     const typename S::elem* x = static_cast<const typename S::elem*>(a.x) + row * a.cols + c;
     float m = 0.0f;
-    if (a.vec) {
+    if (vec) {
         const uint4 p = c < a.cols ? load_packet(reinterpret_cast<const uint4*>(x)) : make_uint4(0, 0, 0, 0);
         S::unpack(p, v);
         m = packet_largest<S>(p);
@@ -97,7 +97,7 @@ template <class S> __device__ __forceinline__ float block_load(const BlockArgs& 
     }
     return m;
 }
-template <class S> __device__ __forceinline__ void block_store(const BlockArgs& a, size_t row, uint32_t c, const float (&v)[S::kVec], float factor)
+template <class S> __device__ __forceinline__ void block_store(const BlockArgs& a, bool vec, size_t row, uint32_t c, const float (&v)[S::kVec], float factor)
 {
     constexpr int V = S::kVec;
     unsigned char* q = a.q + row * a.cols + c;
@@ -105,7 +105,7 @@ template <class S> __device__ __forceinline__ void block_store(const BlockArgs& 
     if (factor != 0.0f)
 #pragma unroll
         for (int i = 0; i < V / 4; ++i) w[i] = block_bytes<Snap<S>::value>(v + i * 4, factor);
-    if (a.vec) {
+    if (vec) {
         if (c >= a.cols) return;
         if constexpr (V == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
         else *reinterpret_cast<uint32_t*>(q) = w[0];
@@ -162,7 +162,7 @@ template <class S> __global__ void __launch_bounds__(kBlock) quantize_row_groups
     }
 }
 
-// Any rows: groups of kBlockSide / V threads, a block of a row each; scale [groups, rows].
+// Rows off the 16-byte boundaries: groups of kBlockSide / V threads, a block of a row each, element by element; scale [groups, rows].
 template <class S> __global__ void __launch_bounds__(kBlock) quantize_groups_kernel(const __grid_constant__ BlockArgs a)
 {
     constexpr int V = S::kVec, T = kBlockSide / V, U = 2;
@@ -183,7 +183,7 @@ template <class S> __global__ void __launch_bounds__(kBlock) quantize_groups_ker
             group[u] = uint32_t(i - row[u] * a.groups);
             c[u] = i < total ? group[u] * kBlockSide + lane * V : a.cols;
             if (i >= total) row[u] = 0;
-            m[u] = block_load<S>(a, row[u], c[u], v[u]);
+            m[u] = block_load<S>(a, false, row[u], c[u], v[u]);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -195,7 +195,7 @@ template <class S> __global__ void __launch_bounds__(kBlock) quantize_groups_ker
             float scale;
             const float f = block_factor<Snap<S>::value>(m[u], &scale);
             if (lane == 0 && c[u] < a.cols) a.scale[size_t(group[u]) * a.rows + row[u]] = scale;
-            block_store<S>(a, row[u], c[u], v[u], f);
+            block_store<S>(a, false, row[u], c[u], v[u], f);
         }
     }
 }
@@ -215,7 +215,7 @@ template <class S> __global__ void __launch_bounds__(kBlock) quantize_blocks_ker
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
         const uint32_t r = r0 + i * kRows;
-        if (r < a.matrix_rows) m = larger(m, block_load<S>(a, matrix * a.matrix_rows + r, c, v[i]));
+        if (r < a.matrix_rows) m = larger(m, block_load<S>(a, a.vec, matrix * a.matrix_rows + r, c, v[i]));
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = larger(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -230,7 +230,7 @@ template <class S> __global__ void __launch_bounds__(kBlock) quantize_blocks_ker
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
         const uint32_t r = r0 + i * kRows;
-        if (r < a.matrix_rows) block_store<S>(a, matrix * a.matrix_rows + r, c, v[i], f);
+        if (r < a.matrix_rows) block_store<S>(a, a.vec, matrix * a.matrix_rows + r, c, v[i], f);
     }
 }
 

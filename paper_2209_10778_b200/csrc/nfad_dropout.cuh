@@ -41,16 +41,16 @@ __device__ __forceinline__ Draw philox(uint64_t index, uint64_t at, uint64_t see
 // whether element j of the draw is kept; `dropped` is T 2^16 (T = 65536, where nothing is, never gets here)
 __device__ __forceinline__ bool kept(const DropoutArgs& a, uint32_t w, int j) { return (j & 1 ? w : w << 16) >= a.dropped; }
 
-// V results from element 8 draw + first on; K void: no activation
+// V results, whose bits are the first V halves of the draw; K void: no activation
 template <class S, class K, class P> struct DropoutBody {
     static constexpr int V = S::kVec;
     // x, then bias or residual (null: none); out and slope
-    static __device__ __forceinline__ void packet(const DropoutArgs& a, const Draw& draw, int first, const float (&x)[V], const float* other, float (&y)[V], float (&d)[V])
+    static __device__ __forceinline__ void packet(const DropoutArgs& a, const Draw& draw, const float (&x)[V], const float* other, float (&y)[V], float (&d)[V])
     {
         if constexpr (IsVoid<K>::value) {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const bool keep = kept(a, draw.w[(first + e) >> 1], e);
+                const bool keep = kept(a, draw.w[e >> 1], e);
                 const float r = other ? other[e] : 0.0f;
                 y[e] = keep ? fmaf(x[e], a.scale, r) : r;
             }
@@ -60,7 +60,7 @@ template <class S, class K, class P> struct DropoutBody {
             float z[V], factor[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const bool keep = kept(a, draw.w[(first + e) >> 1], e);
+                const bool keep = kept(a, draw.w[e >> 1], e);
                 z[e] = keep ? (other ? bias_sum(x[e], other[e]) : x[e]) : 0.0f;
                 factor[e] = keep ? a.scale : 0.0f;
             }
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kBlock, 4) dropout_kernel(const __grid_constan
                     if (++c == a.cols) c = 0;
                 }
             }
-            DropoutBody<S, K, P>::packet(a, mine, 0, x, kWhere == kOtherNone ? nullptr : r, y, d);
+            DropoutBody<S, K, P>::packet(a, mine, x, kWhere == kOtherNone ? nullptr : r, y, d);
             store_packet<true>(static_cast<uint4*>(a.y) + pk, S::pack(y));
             if (kAct) store_packet<false>(static_cast<uint4*>(a.slope) + pk, S::pack(d));
         }
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(kBiasMaxBlock, 4) dropout_rows_kernel(const __
             if (V == 4 && (pk & 1)) { draw.w[0] = draw.w[2]; draw.w[1] = draw.w[3]; }
             float x[V], y[V], d[V];
             S::unpack(raw[u], x);
-            DropoutBody<S, K, P>::packet(a, draw, 0, x, bias, y, d);
+            DropoutBody<S, K, P>::packet(a, draw, x, bias, y, d);
             store_packet<true>(static_cast<uint4*>(a.y) + pk, S::pack(y));
             store_packet<false>(static_cast<uint4*>(a.slope) + pk, S::pack(d));
         }

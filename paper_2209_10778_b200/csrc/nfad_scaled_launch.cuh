@@ -70,9 +70,8 @@ template <int OP, class S> cudaError_t launch_scaled_split(const ProdArgs& g, un
     if (e != cudaSuccess) return e;
     constexpr size_t kResults = kSplitColumns / Kind::kPerResult;
     const size_t tiles = ((g.rows + kTileRows - 1) / kTileRows) * ((g.outs + kResults - 1) / kResults);
-    if (tiles * ranks >= (size_t(1) << 31)) return cudaErrorInvalidValue;     // beyond what any device's memory holds
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(tiles * ranks));
+    cfg.gridDim = dim3(unsigned(tiles * ranks));     // no more than SMs
     cfg.blockDim = dim3(kSplitThreads);
     cfg.dynamicSmemBytes = kThinSmem;
     cfg.stream = st;

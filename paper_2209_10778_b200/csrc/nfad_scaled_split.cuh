@@ -177,7 +177,7 @@ scaled_split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ 
             *reinterpret_cast<float4*>(ring + place(row, c * 8 + p)) = make_float4(acc[2 * p].x, acc[2 * p].y, acc[2 * p + 1].x, acc[2 * p + 1].y);
     }
     __syncthreads();
-    if (ranks > 1) tc::pair_sync();                  // of the whole cluster
+    tc::pair_sync();                                 // of the whole cluster
     {
         // packets of eight results, shared out over the cluster
         const int live_rows = int(min(uint32_t(kTileRows), rows - a0));
@@ -219,7 +219,7 @@ scaled_split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ 
         }
     }
     __syncthreads();
-    if (ranks > 1) tc::pair_sync();                  // no CTA reads this one's sums any more
+    tc::pair_sync();                                 // no CTA reads this one's sums any more
     tc::fence_after_sync();
     if (warp == 2) tc::tmem_free<false>(tmem, kThinBuffers * kSplitColumns);
     if (threadIdx.x == 0 && s.gave_up) atomicAdd(&g_product_faults, 1u);

@@ -87,9 +87,10 @@ template <int OP, class S> cudaError_t launch_scaled_split(const ProdArgs& g, un
 }
 
 // Over how many CTAs a tile's reduction is split (0: not at all; tiles of another size, which CTAs walk over): as many as one to an SM allows,
-// with eight blocks left for each.  Measured (us, against tiles that are walked over): 100 rows 4096 -> 1024 over 4: 14.3 (17.5), over 8: 18.4;
-// 400 rows 4096 -> 1024 over 2: 17.2 (19.4), over 4: 19.4; 40 rows 8192 -> 2048 over 4: 18.4 (26.6); gated 100 rows 8192 -> 2 x 2048 over 2:
-// 25.5 (27.6).  One CTA to a tile of this size was never the fastest (40 rows 4096 -> 28672: 43, by tiles of 128 33.8).
+// with eight blocks left for each.  Measured (us a call with its quantiser, captured calls on inputs in turn that the caches do not hold; in
+// brackets by tiles that are walked over): 100 rows 4096 -> 1024 over 4: 11.1 (17.4), over 8: 19.2; 400 rows 4096 -> 1024 over 2: 15.5 (18.6),
+// over 4: 22.5; 40 rows 8192 -> 2048 over 4: 15.4 (29.5); gated 100 rows 8192 -> 2 x 2048 over 2: 22.3 (29.4).  One CTA to a tile of this size
+// was never the fastest (40 rows 4096 -> 28672: 57, by tiles of 256 26.9).
 template <int OP> unsigned scaled_split_ranks(const ProdArgs& g, int sms)
 {
     if (g.outs % 8 || (reinterpret_cast<uintptr_t>(g.out) | reinterpret_cast<uintptr_t>(g.bias)) % 16) return 0;      // its results go by packets

@@ -1,11 +1,12 @@
 // nfad_scaled_split.cuh -- the products in 8-bit floating point with block scales when there are few rows or few tiles.
 //
-// A tile of 128 rows x 64 columns, two CTAs to an SM; with fewer tiles than that takes, a cluster of CTAs splits each tile's reduction
-// and adds up through its shared memory, as nfad_split.cuh does.  A step is a block of 128 of the reduction, its products in one of four
-// buffers of 64 columns, times its scale into 32 sums a thread.
+// Tiles of 128 rows x 64 columns, at most half as many as SMs: a cluster of two, four or eight CTAs splits each tile's reduction and adds up
+// through its shared memory, as nfad_split.cuh does; one CTA to an SM (see scaled_split_ranks).  A step is a block of 128 of the reduction, its
+// products in one of four buffers of 64 columns, times its scale into 32 sums a thread.  (Registers for a second CTA that never comes, 80 a
+// thread of the 94 wanted: 100 rows 4096 -> 1024 in calls one behind another 11.4 us, now 10.5; 40 rows 8192 -> 2048 15.4, now 14.3.)
 //
 // For few rows the weights' bytes are what takes the time, and the ring is laid out for them: a stage holds as many rows of x as there are, to
-// the next 32, beside the weights' 8 KB, so that up to eight stages (64 KB of weights, 128 KB an SM) are on their way.  (The products read
+// the next 32, beside the weights' 8 KB, so that up to eight stages (64 KB of weights) are on their way.  (The products read
 // 128 rows whatever the stage holds: what lies behind its rows of x are weights or another stage's bytes, in rows of the sums that nobody
 // reads.)
 #pragma once
@@ -26,7 +27,7 @@ struct ThinShared {
 constexpr int kThinSmem = 1024 + kThinRing + int(sizeof(ThinShared));
 
 template <int OP, class S>
-__global__ void __launch_bounds__(kSplitThreads, 2)
+__global__ void __launch_bounds__(kSplitThreads, 1)
 scaled_split_kernel(const __grid_constant__ ProdArgs g, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, uint32_t ranks)
 {
     using Kind = ProdKind<OP>;

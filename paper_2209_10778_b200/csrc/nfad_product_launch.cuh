@@ -174,7 +174,8 @@ template <int OP> int product_tile(const ProdArgs& g, int sms)
     };
     int best = 256;
     size_t least = turns(128, 256, sms) * 384;
-    for (int columns = 128; columns >= (Kind::kGated ? 128 : 64); columns /= 2)       // a gated tile has results for two warps of each lane quarter
+    // 64: a gated tile has results for two warps of each lane quarter, and one with block scales is no narrower than a block
+    for (int columns = 128; columns >= (Kind::kGated || Kind::kScaled ? 128 : 64); columns /= 2)
         if (const size_t cost = turns(128, columns, sms) * (128 + columns); cost < least) {
             least = cost;
             best = columns;

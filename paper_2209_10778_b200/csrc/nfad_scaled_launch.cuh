@@ -113,6 +113,9 @@ template <int OP, class S> cudaError_t launch_scaled_store(const ProdArgs& g, cu
     // 4096 -> 2 x 14336 32.9 (35.8), 1 row of it 31.7 (37.7); with two such groups 16 rows of it took 57 when tiles took 34.8.
     if (few_rows(g) && g.rows <= 8) return launch_few_rows_tiles<OP, S, 1>(g, di.sm_count, g.b_ready, st);
     if (const unsigned ranks = scaled_split_ranks<OP>(g, di.sm_count)) return launch_scaled_split<OP, S>(g, ranks, st);
+    // The rule of the other products, by turns of all SMs, holds for these too.  Alone, in turn as above (us, by 128 / 256 columns / pairs): 128 rows
+    // 4096 -> 8192 19.6 / 21.0 / 21.4; 40 rows 4096 -> 28672 31.8 / 25.1 / 37.4, gated 4096 -> 2 x 14336 32.6 / 26.7 / 40.3; 300 rows 2048 -> 8192
+    // 17.0 / 13.4 / 14.0; 1024 rows 4096 -> 4096 31.2 / 22.6 / 23.4; 4096 rows 88.8 / 71.9 / 70.4, gated 185 / 137 / 122.
     switch (product_tile<OP>(g, di.sm_count)) {
     case kPairTile: return launch_scaled_tile<OP, 256, S, false, true>(g, di.sm_count, st);
     case 256: return launch_scaled_tile<OP, 256, S, false>(g, di.sm_count, st);

@@ -183,8 +183,8 @@ class Dropout:
                 raise TypeError("step must be an int64 CUDA tensor")
             if step.numel() != 1:
                 raise ValueError("step must hold one value")
-        self.desc = DropoutMask(self.p, self.seed, self.offset, None)      # the step's address is filled in by each call
-        self.ref = ctypes.byref(self.desc)
+        self.desc = DropoutMask(self.p, self.seed, self.offset, None)      # the step's address is filled in by the calls
+        self.ref, self._at = ctypes.byref(self.desc), None
 
     p = property(lambda self: self._p)
     seed = property(lambda self: self._seed)
@@ -195,10 +195,13 @@ class Dropout:
 def _mask(drop: Dropout, x: torch.Tensor):
     if not isinstance(drop, Dropout):
         raise TypeError("drop must be a Dropout")
-    if drop.step is not None:
-        if drop.step.get_device() != x.get_device():
+    step = drop._step
+    if step is not None:
+        if step.get_device() != x.get_device():
             raise ValueError("the mask's step must be on the tensors' device")
-        drop.desc.step = drop.step.data_ptr()            # where it is now: a tensor's storage can be exchanged
+        at = step.data_ptr()                             # where it is now: a tensor's storage can be exchanged
+        if at != drop._at:
+            drop._at = drop.desc.step = at
     return drop.ref
 
 

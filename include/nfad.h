@@ -463,13 +463,16 @@ NFAD_API int nfad_expert_linear_backward_weight(int dtype, const void* grad_z, c
  *   a function of two variables, and nested forward differentiation gives both its derivatives with it:
  *   partials [rows, 2, out] or NULL: dy/da = f'(a) u, then dy/du = f(a), each rounded once: all that the layer's backward keeps.
  * Backward: grad_z = [grad_y dy/da, grad_y dy/du], [rows, 2, out], the gradient of both projections at once.  From there on the layer
- *   is a linear one with 2 out outputs: nfad_expert_linear_backward_input and _weight with grad_z, w and out doubled.
+ *   is a linear one with 2 out outputs: nfad_expert_linear_backward_input and _weight with grad_z, w and out doubled.  grad_z is a tensor of
+ *   dtype, which is what the tensor cores take: its rounding (2^-8 of each value in bf16, 2^-11 in fp16, at most) is as large as the results'
+ *   own, and the gradients of x and w are off by about 1.4 times what results of a grad_z in fp32 would be.
  * nfad_expert_gated_backward: grad_out [rows, out] is the gradient of y.  grad_bias [experts, 2, out] or NULL: the column sums of the
  *   unrounded products (fp32, fixed order).  grad_z may equal partials.  scratch as for nfad_expert_act_backward with 2 out columns; needed for
  *   grad_bias only.
  * nfad_expert_linear_backward_gated: the same where the layer behind is a linear one, w [experts, out, in] and grad_z [rows, out] the
  *   gradient of its result: its input's gradient g = grad_z w_e stays in the kernel, and grad [rows, 2, in] = [g dy/da, g dy/du],
- *   rounded once.  grad may equal partials [rows, 2, in].
+ *   rounded once.  grad may equal partials [rows, 2, in].  Bias sums of it (nfad_expert_act_backward without dfdx) are sums of those rounded
+ *   values; through nfad_expert_linear_backward_input and nfad_expert_gated_backward they are sums of unrounded products of a rounded g.
  */
 NFAD_API int nfad_expert_gated_linear(int kind, int dtype, const void* x, const void* w, const void* bias, const int* offsets, void* y, void* partials,
                                       size_t rows, size_t in, size_t out, size_t experts, nfad_stream_t stream);
@@ -509,7 +512,8 @@ NFAD_API size_t nfad_i8_linear_dynamic_scratch_bytes(size_t rows, size_t in);
  *   2^-110 get scale 0 and q 0; blocks that hold an infinity or a NaN get scale NaN and q 0.  The last block of a row may be shorter.
  * nfad_f8_quantize_blocks: the same of `matrices` matrices [rows, cols] by blocks of 128 x 128; scale [matrices, ceil(rows / 128), ceil(cols / 128)].
  * nfad_f8_linear: z[r, o] = sum_b x_scale[b, r] w_scale[o / 128, b] sum_{k in block b} xq[r, k] wq[o, k] + bias[o], y = f(z): products exact, sums
- *   fp32, rounded once to dtype (NFAD_BF16 or NFAD_F16).  wq [out, in], w_scale [ceil(out / 128), B]; bias [out] of dtype, or NULL; kind
+ *   fp32, rounded once to dtype (NFAD_BF16 or NFAD_F16); a block's two scales are multiplied first, in fp32: terms whose x_scale w_scale
+ *   leaves its normal range (2^-126 to 2^128) lose bits, are 0 or are not finite.  wq [out, in], w_scale [ceil(out / 128), B]; bias [out] of dtype, or NULL; kind
  *   NFAD_NO_ACT: no activation; value only.  The two byte values that stand for NaN give NaN.
  * nfad_f8_gated_linear: the gated layer y = f(a) u with a and u such sums of two weights: wq [2, out, in], w_scale [2, ceil(out / 128), B],
  *   bias [2, out] or NULL; the gate's first.

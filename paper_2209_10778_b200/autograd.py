@@ -303,7 +303,8 @@ def expert_gated_linear(x, w, bias, offsets, kind="swish"):
 
 class ExpertGatedFeedForward(torch.autograd.Function):
     """w2 (f(a) u) + b2, a and u the products of x with w1's two weights.  Saved: x, y1 = f(a) u, its two derivatives and the weights; on the way
-    back the second layer's input gradient leaves its product already multiplied by both."""
+    back the second layer's input gradient leaves its product already multiplied by both, rounded once: b1's gradient sums those rounded values
+    (expert_gated_linear's sums unrounded products of a gradient that was rounded before: other last bits)."""
 
     @staticmethod
     def forward(ctx, x, w1, b1, w2, b2, offsets, kind):

@@ -2,12 +2,13 @@
 //
 // Then the weights' bytes are what takes the time, and each weight is used a handful of times: what matters is that every SM
 // has plenty of long contiguous reads of them in flight.  A CTA takes 16 outputs; its eight warps split the reduction, each
-// reading 512 contiguous bytes of each of the 16 weight rows at once, straight into registers.  There they are the A
+// reading 256 contiguous bytes of each of the 16 weight rows at once, straight into registers.  There they are the A
 // operand of a small matrix instruction (16 outputs x 8 tokens), whose reduction slots are permuted so that a lane's 16 bytes
 // are its own fragments: no shared memory and no shuffles between memory and the products.  The tokens' fragments are
 // read the same way (they come from L1 or L2).  The warps' sums meet in shared memory, and bias, scales and activation follow.
 // Bound by HBM: 24 rows over 64 experts, 2048 -> 1408, bf16 (about 20 experts' weights, 115 MB) 24 us, 0.75 of the copy rate with
-// the launch in it.  Four 64-byte steps in flight per warp and four CTAs to an SM; eight steps and two CTAs took 34 us.
+// the launch in it.  Four 64-byte steps in flight per warp and four CTAs to an SM, three beside block scales or for 16 tokens at once; eight
+// steps and two CTAs took 34 us.
 #pragma once
 
 #include "nfad_product.cuh"

@@ -109,8 +109,8 @@ template <int OP, class S> cudaError_t launch_scaled_store(const ProdArgs& g, cu
     const uintptr_t low = reinterpret_cast<uintptr_t>(g.a) | reinterpret_cast<uintptr_t>(g.b) | uintptr_t(g.in);
     // a tensor copy needs rows that begin on 16-byte boundaries (and something to copy)
     if (low % 16 || g.in == 0) return launch_scaled_tile<OP, 64, S, true>(g, di.sm_count, st);
-    // Up to eight rows, a column each of the small matrix instruction.  Against tiles (us): 8 rows 4096 -> 4096 11.1 (14.3 split over 4), gated
-    // 4096 -> 2 x 14336 32.9 (35.8), 1 row of it 31.7 (37.7); with two such groups 16 rows of it took 57 when tiles took 34.8.
+    // Up to eight rows, a column each of the small matrix instruction.  Against tiles (us, measured as above): 8 rows 4096 -> 4096 8.2 (11.1 split
+    // over 4, 15.1 walked over), gated 4096 -> 2 x 14336 30.4 (31.5), 1 row of it 28.0 (32.9); with two such groups 16 rows of it take 93 (30.8).
     if (few_rows(g) && g.rows <= 8) return launch_few_rows_tiles<OP, S, 1>(g, di.sm_count, g.b_ready, st);
     if (const unsigned ranks = scaled_split_ranks<OP>(g, di.sm_count)) return launch_scaled_split<OP, S>(g, ranks, st);
     // The rule of the other products, by turns of all SMs, holds for these too.  Alone, in turn as above (us, by 128 / 256 columns / pairs): 128 rows
